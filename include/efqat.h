@@ -11,6 +11,9 @@
  *   efqat_linear_bwd       Eq. 5 restricted as in Alg. 1, plus S_x / Z_x / S_w gradients
  *   efqat_conv_bwd         the same two contractions with Eq. 8's shapes
  *
+ * and what a language model needs between its quantized layers: layer norm, the activation of
+ * a feed-forward block with its inputs kept in 8 bits, and the loss over the vocabulary.
+ *
  * Conventions common to every call
  *   - Every tensor pointer is a DEVICE pointer owned by the caller; the library
  *     allocates nothing and keeps no state between calls (the benchmark timing hooks
@@ -379,6 +382,90 @@ size_t efqat_linear_fwd_workspace_bytes(int64_t T, int64_t c_in, int64_t c_out);
 int efqat_linear_fwd(const uint8_t* x_codes, const float* s_x, const float* z_x, const int8_t* w_codes,
                      const float* s_w, int64_t T, int64_t c_in, int64_t c_out, void* y, int y_dtype,
                      void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------ 8-bit checkpoints
+ * What the backward pass of a layer norm or an activation needs of the forward's inputs, in 8 bits: a
+ * row in groups of 128 columns, each with a scale, in fp32
+ *   scale = max(max|x| * fl(1/127), 2^-126),   code = rne(x * fl(1/scale)),   kept value = scale * code
+ * (at most half a step of max|x| / 127 off; a group that holds an infinity or a NaN reads back as NaN).
+ *   codes   int8 [rows][efqat_ckpt8_pitch(cols)], the columns rounded up to 16; 16-byte aligned.  Codes
+ *           behind the columns are zero
+ *   scales  float [rows][ceil(cols / 128)]
+ * Rows of x (here and in the calls below) may lie apart: ld* is the number of elements from one row to
+ * the next, >= cols; any element alignment. */
+#define EFQAT_CKPT8_GROUP 128
+int64_t efqat_ckpt8_pitch(int64_t cols);
+int efqat_ckpt8_save(const void* x, int64_t ldx, int dtype, int64_t rows, int64_t cols, int8_t* codes, float* scales,
+                     void* stream);
+int efqat_ckpt8_load(const int8_t* codes, const float* scales, int64_t rows, int64_t cols, void* x, int64_t ldx,
+                     int dtype, void* stream);
+
+/* ------------------------------------------------------------------ activation of a feed-forward block
+ *   y = f(x)  or, with up,  y = f(x) * up;   f: GELU x Phi(x), or SiLU x / (1 + exp(-x))
+ * computed in fp32 and rounded once.  The backward pass reads the checkpoints of x and up:
+ *   dx = dy f'(x) [* up],   dup = dy f(x)
+ *   x, up, y, dy, dx, dup  [rows][cols], dtype F32 or BF16 (one for all); up NULL: not gated
+ *   x_codes, x_scales, up_codes, up_scales   see efqat_ckpt8_save.  Forward: out, in the pass that reads
+ *           x and up; NULL: not kept (evaluation)
+ *   dup     NULL iff the forward was not gated */
+#define EFQAT_ACT_GELU 0
+#define EFQAT_ACT_SILU 1
+int efqat_act_fwd(const void* x, int64_t ldx, const void* up, int64_t ldup, int dtype, int64_t rows, int64_t cols, int kind,
+                  void* y, int64_t ldy, int8_t* x_codes, float* x_scales, int8_t* up_codes, float* up_scales,
+                  void* stream);
+int efqat_act_bwd(const void* dy, int64_t lddy, int dtype, int64_t rows, int64_t cols, int kind, const int8_t* x_codes,
+                  const float* x_scales, const int8_t* up_codes, const float* up_scales, void* dx, int64_t lddx, void* dup,
+                  int64_t lddup, void* stream);
+
+/* ------------------------------------------------------------------ layer norm
+ * Over the columns of each row; parameters and statistics are fp32, as are all sums:
+ *   xhat = (x - mean) rstd,  rstd = 1 / sqrt(var + eps),  y = xhat weight + bias
+ *   g = dy weight,  dx = rstd (g - mean_j g - xhat mean_j (g xhat))
+ *   dweight = sum over the rows of dy xhat,  dbias = sum over the rows of dy   (never frozen: Sec. 3.4)
+ *   x, y, dy, dx    [rows][cols], dtype F32 or BF16
+ *   weight, bias    float[cols]; NULL: 1, 0
+ *   mean, rstd      float[rows]; forward: out, nullable (evaluation)
+ *   x_codes, x_scales   8-bit checkpoint of x.  Forward: out, nullable.  Backward: read where x is NULL
+ *   dweight, dbias  out float[cols], nullable; summed in a fixed order (bit-reproducible) */
+int efqat_layer_norm_fwd(const void* x, int64_t ldx, int dtype, int64_t rows, int64_t cols, const float* weight,
+                         const float* bias, float eps, void* y, int64_t ldy, float* mean, float* rstd, int8_t* x_codes,
+                         float* x_scales, void* stream);
+size_t efqat_layer_norm_bwd_workspace_bytes(int64_t rows, int64_t cols);
+int efqat_layer_norm_bwd(const void* dy, int64_t lddy, int dtype, const void* x, int64_t ldx, const int8_t* x_codes,
+                         const float* x_scales, const float* mean, const float* rstd, const float* weight, int64_t rows,
+                         int64_t cols, void* dx, int64_t lddx, float* dweight, float* dbias, void* ws, size_t ws_bytes,
+                         void* stream);
+
+/* ------------------------------------------------------------------ softmax cross entropy over a vocabulary
+ * Of the logits z = h w^T, which are not kept:
+ *   lse[t] = log sum_v exp(z[t][v]),   loss of token t = lse[t] - z[t][targets[t]]
+ *   G = (exp(z - lse) - [v = targets[t]]) * (upstream gradient of token t's loss),  dh = G w,  dw = G^T h
+ *   h        in  [T][D], w in [V][D], dtype F32 or BF16 (both); BF16 with D a multiple of 64: w 16-byte
+ *                aligned and ldw a multiple of 8
+ *   targets  in  int64[T].  A token whose target is ignore_index, or outside [0, V), has no class: it takes no
+ *                part, whatever its row of h holds; its loss, lse and row of dh are 0
+ *   reduction    loss is float[T] (NONE), or float[1]: the mean or the sum over the tokens with a class (0
+ *                if there is none)
+ *   n_valid  out, nullable  int32[1]: tokens with a class
+ *   dloss    in, nullable (all ones)  float[T] (NONE) or float[1]: gradient of what the forward returned
+ *   lse      in  (backward) as the forward left it
+ *   dh [T][D], dw [V][D]  out, dtype; either may be NULL.  With BF16, G is rounded to bf16 for the matrix cores; with
+ *                F32 the products are formed from three bf16 parts of every operand, which keep 24 bits (infinite
+ *                elements of h and w count as +-3.39e38).
+ * Sums are fp32, in a fixed order (bit-reproducible).  Both calls count and gather the tokens on the device; nothing
+ * waits for the host.  At most 2^30 tokens and classes, D <= 2^20. */
+#define EFQAT_XENT_NONE 0
+#define EFQAT_XENT_MEAN 1
+#define EFQAT_XENT_SUM 2
+size_t efqat_linear_xent_fwd_workspace_bytes(int64_t T, int64_t D, int64_t V, int dtype);
+int efqat_linear_xent_fwd(const void* h, int64_t ldh, const void* w, int64_t ldw, int dtype, int64_t T, int64_t D, int64_t V,
+                          const int64_t* targets, int64_t ignore_index, int reduction, float* loss, float* lse,
+                          int32_t* n_valid, void* ws, size_t ws_bytes, void* stream);
+size_t efqat_linear_xent_bwd_workspace_bytes(int64_t T, int64_t D, int64_t V, int dtype);
+int efqat_linear_xent_bwd(const void* h, int64_t ldh, const void* w, int64_t ldw, int dtype, int64_t T, int64_t D, int64_t V,
+                          const int64_t* targets, int64_t ignore_index, int reduction, const float* lse,
+                          const float* dloss, void* dh, int64_t lddh, void* dw, int64_t lddw, void* ws, size_t ws_bytes,
+                          void* stream);
 
 /* ------------------------------------------------------------------ kernel timing (benchmarks)
  * To report each kernel class against its roofline a benchmark can have the library bracket its

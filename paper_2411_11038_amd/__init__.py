@@ -12,4 +12,6 @@ from .binding import (  # noqa: F401
     W_PER_ROW_SYM, DY_TOKEN_MAJOR, DY_CHANNEL_MAJOR, EXPORTS, OptStep, profile_enable, profile_read, DX_KERNEL_AUTO,
     DX_KERNEL_BF16, DX_KERNEL_INT8, DX_KERNEL_BF16_PINNED, PROF_DX, PROF_DW, PROF_FWD, PROF_PREP, PROF_FINISH,
     PROF_QUANT_ACT, PROF_QUANT_W, PROF_IMPORTANCE, PROF_TOPK, PROF_BIAS, PROF_CLASSES,
+    ckpt8_save, ckpt8_load, act_fwd, act_bwd, layer_norm_fwd, layer_norm_bwd, linear_xent_fwd, linear_xent_bwd, CKPT8_GROUP, ACT_GELU,
+    ACT_SILU, XENT_NONE, XENT_MEAN, XENT_SUM,
 )

@@ -30,6 +30,10 @@ EXPORTS = [
     "efqat_linear_fwd_workspace_bytes", "efqat_linear_fwd",
     "efqat_profile_enable", "efqat_profile_read", "efqat_linear_bwd_plan", "efqat_conv_bwd_plan",
     "efqat_linear_bwd_dx_tile", "efqat_linear_fwd_plan",
+    "efqat_ckpt8_pitch", "efqat_ckpt8_save", "efqat_ckpt8_load", "efqat_act_fwd", "efqat_act_bwd",
+    "efqat_layer_norm_fwd", "efqat_layer_norm_bwd_workspace_bytes", "efqat_layer_norm_bwd",
+    "efqat_linear_xent_fwd_workspace_bytes", "efqat_linear_xent_fwd",
+    "efqat_linear_xent_bwd_workspace_bytes", "efqat_linear_xent_bwd",
 ]
 
 
@@ -132,6 +136,30 @@ def lib():
     L.efqat_linear_fwd_plan.argtypes = [i64] * 3 + [C.POINTER(C.c_int32)]
     L.efqat_conv_bwd_plan.restype = ci
     L.efqat_conv_bwd_plan.argtypes = [i64] * 10 + [ci, ci, ci, C.POINTER(C.c_int32)]
+    L.efqat_ckpt8_pitch.restype = i64
+    L.efqat_ckpt8_pitch.argtypes = [i64]
+    L.efqat_ckpt8_save.restype = ci
+    L.efqat_ckpt8_save.argtypes = [vp, i64, ci, i64, i64, vp, vp, vp]
+    L.efqat_ckpt8_load.restype = ci
+    L.efqat_ckpt8_load.argtypes = [vp, vp, i64, i64, vp, i64, ci, vp]
+    L.efqat_act_fwd.restype = ci
+    L.efqat_act_fwd.argtypes = [vp, i64, vp, i64, ci, i64, i64, ci, vp, i64, vp, vp, vp, vp, vp]
+    L.efqat_act_bwd.restype = ci
+    L.efqat_act_bwd.argtypes = [vp, i64, ci, i64, i64, ci, vp, vp, vp, vp, vp, i64, vp, i64, vp]
+    L.efqat_layer_norm_fwd.restype = ci
+    L.efqat_layer_norm_fwd.argtypes = [vp, i64, ci, i64, i64, vp, vp, C.c_float, vp, i64, vp, vp, vp, vp, vp]
+    L.efqat_layer_norm_bwd_workspace_bytes.restype = sz
+    L.efqat_layer_norm_bwd_workspace_bytes.argtypes = [i64, i64]
+    L.efqat_layer_norm_bwd.restype = ci
+    L.efqat_layer_norm_bwd.argtypes = [vp, i64, ci, vp, i64, vp, vp, vp, vp, vp, i64, i64, vp, i64, vp, vp, vp, sz, vp]
+    L.efqat_linear_xent_fwd_workspace_bytes.restype = sz
+    L.efqat_linear_xent_fwd_workspace_bytes.argtypes = [i64, i64, i64, ci]
+    L.efqat_linear_xent_fwd.restype = ci
+    L.efqat_linear_xent_fwd.argtypes = [vp, i64, vp, i64, ci, i64, i64, i64, vp, i64, ci, vp, vp, vp, vp, sz, vp]
+    L.efqat_linear_xent_bwd_workspace_bytes.restype = sz
+    L.efqat_linear_xent_bwd_workspace_bytes.argtypes = [i64, i64, i64, ci]
+    L.efqat_linear_xent_bwd.restype = ci
+    L.efqat_linear_xent_bwd.argtypes = [vp, i64, vp, i64, ci, i64, i64, i64, vp, i64, ci, vp, vp, vp, i64, vp, i64, vp, sz, vp]
     _LIB = L
     return L
 
@@ -493,3 +521,230 @@ def conv_bwd(dy, x_codes, x_clip, x, s_x, z_x, w_codes, w_clip, w, s_w, idx, str
                                side_stream.cuda_stream if side_stream else None)
     _check(rc, "efqat_conv_bwd")
     return dict(dx=dx, dw=dw, ds_w=ds_w, ds_x=ds_x, dz_x=dz_x)
+
+
+# ------------------------------------------------------------------ 8-bit checkpoints, activation, layer norm
+CKPT8_GROUP = 128
+ACT_GELU, ACT_SILU = 0, 1
+
+
+def _kept(rows, cols, device, out=None, prefix="x"):
+    """(codes, scales) of a checkpoint: those of `out`, or new ones."""
+    codes, scales = (out.get(prefix + "_codes"), out.get(prefix + "_scales")) if out else (None, None)
+    if codes is None:
+        codes = torch.empty((rows, -(-cols // 16) * 16), dtype=torch.int8, device=device)
+    if scales is None:
+        scales = torch.empty((rows, -(-cols // CKPT8_GROUP)), dtype=torch.float32, device=device)
+    _kept_shape(codes, scales, rows, cols)
+    return codes, scales
+
+
+def _like(t, shape, dtype, what):
+    """Checks a tensor that the kernels take by its address: they know no other size than the call's."""
+    if t.dtype != dtype:
+        raise TypeError(f"{what}: {dtype} expected, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what}: shape {tuple(shape)} expected, got {tuple(t.shape)}")
+
+
+def _kept_shape(codes, scales, rows, cols, what="x"):
+    _like(codes, (rows, -(-cols // 16) * 16), torch.int8, what + "_codes")
+    _like(scales, (rows, -(-cols // CKPT8_GROUP)), torch.float32, what + "_scales")
+
+
+def _rows_cols(x):
+    if x.dim() != 2:
+        raise ValueError("tensor must be two-dimensional with contiguous rows")
+    return x.shape
+
+
+def _ld(t):
+    """Elements from one row to the next."""
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def ckpt8_save(x, out=None):
+    """8-bit checkpoint of x [rows, cols] (rows may lie apart).  Returns (codes, scales); `out` may carry them as
+    x_codes, x_scales."""
+    rows, cols = _rows_cols(x)
+    codes, scales = _kept(rows, cols, x.device, out)
+    _check(_native().ckpt8_save(x, _ld(x), _dt(x), rows, cols, codes, scales, _STREAM), "efqat_ckpt8_save")
+    return codes, scales
+
+
+def ckpt8_load(codes, scales, cols, dtype=torch.bfloat16, out=None):
+    """The values that a checkpoint of rows of `cols` columns holds, [rows, cols]."""
+    rows = codes.shape[0]
+    _kept_shape(codes, scales, rows, cols)
+    x = torch.empty((rows, cols), dtype=dtype, device=codes.device) if out is None else out
+    _like(x, (rows, cols), x.dtype, "out")
+    _check(_native().ckpt8_load(codes, scales, rows, cols, x, _ld(x), _dt(x), _STREAM), "efqat_ckpt8_load")
+    return x
+
+
+def act_fwd(x, kind, up=None, checkpoint=False, out=None):
+    """y = f(x), or f(x) * up, for x, up [rows, cols] (rows may lie apart); checkpoint: their 8-bit checkpoints too.  Returns
+    dict(y, x_codes, x_scales, up_codes, up_scales); `out` may carry preallocated ones."""
+    rows, cols = _rows_cols(x)
+    out = out or {}
+    y = out.get("y")
+    if y is None:
+        y = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+    else:
+        _like(y, (rows, cols), x.dtype, "y")
+    if up is not None:
+        _like(up, (rows, cols), x.dtype, "up")
+    xc, xs = _kept(rows, cols, x.device, out) if checkpoint else (None, None)
+    uc, us = _kept(rows, cols, x.device, out, "up") if checkpoint and up is not None else (None, None)
+    _check(_native().act_fwd(x, _ld(x), up, 0 if up is None else _ld(up), _dt(x), rows, cols, kind, y, _ld(y), xc, xs, uc,
+                             us, _STREAM), "efqat_act_fwd")
+    return dict(y=y, x_codes=xc, x_scales=xs, up_codes=uc, up_scales=us)
+
+
+def act_bwd(dy, kind, x_codes, x_scales, up_codes=None, up_scales=None, out=None):
+    """Backward of act_fwd from the checkpoints that it left.  Returns dict(dx, dup); `out` may carry them (rows may lie
+    apart)."""
+    rows, cols = _rows_cols(dy)
+    _kept_shape(x_codes, x_scales, rows, cols)
+    gated = up_codes is not None or up_scales is not None
+    if gated:
+        if up_codes is None or up_scales is None:
+            raise ValueError("up_codes and up_scales belong together")
+        _kept_shape(up_codes, up_scales, rows, cols, "up")
+    out = out or {}
+    dx, dup = out.get("dx"), out.get("dup") if gated else None
+    if dx is None:
+        dx = torch.empty((rows, cols), dtype=dy.dtype, device=dy.device)
+    if gated and dup is None:
+        dup = torch.empty((rows, cols), dtype=dy.dtype, device=dy.device)
+    _like(dx, (rows, cols), dy.dtype, "dx")
+    if gated:
+        _like(dup, (rows, cols), dy.dtype, "dup")
+    _check(_native().act_bwd(dy, _ld(dy), _dt(dy), rows, cols, kind, x_codes, x_scales, up_codes, up_scales, dx, _ld(dx),
+                             dup, _ld(dup) if gated else 0, _STREAM), "efqat_act_bwd")
+    return dict(dx=dx, dup=dup)
+
+
+def layer_norm_fwd(x, weight=None, bias=None, eps=1e-5, checkpoint=False, out=None):
+    """Layer norm of x [rows, cols] (rows may lie apart); weight, bias fp32 [cols] or None; checkpoint: the 8-bit checkpoint of
+    x too.  Returns dict(y, mean, rstd, x_codes, x_scales); `out` may carry preallocated ones."""
+    rows, cols = _rows_cols(x)
+    out = out or {}
+    dev = x.device
+    y, mean, rstd = out.get("y"), out.get("mean"), out.get("rstd")
+    if y is None:
+        y = torch.empty((rows, cols), dtype=x.dtype, device=dev)
+    if mean is None:
+        mean = torch.empty(rows, dtype=torch.float32, device=dev)
+    if rstd is None:
+        rstd = torch.empty(rows, dtype=torch.float32, device=dev)
+    _like(y, (rows, cols), x.dtype, "y")
+    _like(mean, (rows,), torch.float32, "mean")
+    _like(rstd, (rows,), torch.float32, "rstd")
+    for t, what in ((weight, "weight"), (bias, "bias")):
+        if t is not None:
+            _like(t, (cols,), torch.float32, what)
+    xc, xs = _kept(rows, cols, dev, out) if checkpoint else (None, None)
+    _check(_native().layer_norm_fwd(x, _ld(x), _dt(x), rows, cols, weight, bias, eps, y, _ld(y), mean, rstd, xc, xs, _STREAM),
+           "efqat_layer_norm_fwd")
+    return dict(y=y, mean=mean, rstd=rstd, x_codes=xc, x_scales=xs)
+
+
+def layer_norm_bwd(dy, weight, mean, rstd, x=None, x_codes=None, x_scales=None, ws=None, out=None):
+    """Backward of layer_norm_fwd from x, or from the checkpoint that it left.  Returns dict(dx, dweight, dbias); `out` may
+    carry preallocated ones."""
+    rows, cols = _rows_cols(dy)
+    if x is None:
+        if x_codes is None or x_scales is None:
+            raise ValueError("x, or x_codes and x_scales, expected")
+        _kept_shape(x_codes, x_scales, rows, cols)
+    else:
+        _like(x, (rows, cols), dy.dtype, "x")
+    if weight is not None:
+        _like(weight, (cols,), torch.float32, "weight")
+    _like(mean, (rows,), torch.float32, "mean")
+    _like(rstd, (rows,), torch.float32, "rstd")
+    out = out or {}
+    dev = dy.device
+    dx, dweight, dbias = out.get("dx"), out.get("dweight"), out.get("dbias")
+    if dx is None:
+        dx = torch.empty((rows, cols), dtype=dy.dtype, device=dev)
+    if dweight is None:
+        dweight = torch.empty(cols, dtype=torch.float32, device=dev)
+    if dbias is None:
+        dbias = torch.empty(cols, dtype=torch.float32, device=dev)
+    _like(dx, (rows, cols), dy.dtype, "dx")
+    _like(dweight, (cols,), torch.float32, "dweight")
+    _like(dbias, (cols,), torch.float32, "dbias")
+    if ws is None:
+        ws = _ws(lib().efqat_layer_norm_bwd_workspace_bytes(rows, cols), dy)
+    _check(_native().layer_norm_bwd(dy, _ld(dy), _dt(dy), x, 0 if x is None else _ld(x), None if x is not None else x_codes,
+                                    None if x is not None else x_scales, mean, rstd, weight, rows, cols, dx, _ld(dx), dweight,
+                                    dbias, ws, ws.numel(), _STREAM), "efqat_layer_norm_bwd")
+    return dict(dx=dx, dweight=dweight, dbias=dbias)
+
+
+# ------------------------------------------------------------------ softmax cross entropy over a vocabulary
+XENT_NONE, XENT_MEAN, XENT_SUM = 0, 1, 2
+
+
+def _xent_shapes(h, w, targets):
+    T, D = _rows_cols(h)
+    if w.dim() != 2 or w.shape[1] != D:
+        raise ValueError(f"w: [classes, {D}] expected, got {tuple(w.shape)}")
+    if w.dtype != h.dtype:
+        raise TypeError(f"w: {h.dtype} expected, got {w.dtype}")
+    _like(targets, (T,), torch.int64, "targets")
+    return T, D, w.shape[0]
+
+
+def linear_xent_fwd(h, w, targets, ignore_index=-100, reduction=XENT_MEAN, ws=None, out=None):
+    """Loss of the logits h w^T (never kept) against one class a token: h [T, D], w [V, D] (rows may lie apart), targets
+    int64 [T].  Returns dict(loss, lse, n_valid); `out` may carry them."""
+    T, D, V = _xent_shapes(h, w, targets)
+    out = out or {}
+    dev = h.device
+    n_loss = T if reduction == XENT_NONE else 1
+    loss, lse, n_valid = out.get("loss"), out.get("lse"), out.get("n_valid")
+    if loss is None:
+        loss = torch.empty(n_loss, dtype=torch.float32, device=dev)
+    if lse is None:
+        lse = torch.empty(T, dtype=torch.float32, device=dev)
+    if n_valid is None:
+        n_valid = torch.empty(1, dtype=torch.int32, device=dev)
+    _like(loss, (n_loss,), torch.float32, "loss")
+    _like(lse, (T,), torch.float32, "lse")
+    _like(n_valid, (1,), torch.int32, "n_valid")
+    if ws is None:
+        ws = _ws(lib().efqat_linear_xent_fwd_workspace_bytes(T, D, V, _dt(h)), h)
+    _check(_native().linear_xent_fwd(h, _ld(h), w, _ld(w), _dt(h), T, D, V, targets, ignore_index, reduction, loss, lse, n_valid,
+                                     ws, ws.numel(), _STREAM), "efqat_linear_xent_fwd")
+    return dict(loss=loss, lse=lse, n_valid=n_valid)
+
+
+def linear_xent_bwd(h, w, targets, lse, dloss=None, ignore_index=-100, reduction=XENT_MEAN, want_dh=True, want_dw=True, ws=None,
+                    out=None):
+    """Gradients of linear_xent_fwd from its lse; dloss: gradient of the loss it returned (None: ones).  Returns dict(dh, dw)
+    (None where not wanted); `out` may carry them (rows may lie apart)."""
+    T, D, V = _xent_shapes(h, w, targets)
+    _like(lse, (T,), torch.float32, "lse")
+    if dloss is not None:
+        _like(dloss, (T if reduction == XENT_NONE else 1,), torch.float32, "dloss")
+    out = out or {}
+    dh, dw = out.get("dh"), out.get("dw")
+    if want_dh:
+        dh = torch.empty((T, D), dtype=h.dtype, device=h.device) if dh is None else dh
+        _like(dh, (T, D), h.dtype, "dh")
+    else:
+        dh = None
+    if want_dw:
+        dw = torch.empty((V, D), dtype=w.dtype, device=w.device) if dw is None else dw
+        _like(dw, (V, D), w.dtype, "dw")
+    else:
+        dw = None
+    if ws is None:
+        ws = _ws(lib().efqat_linear_xent_bwd_workspace_bytes(T, D, V, _dt(h)), h)
+    _check(_native().linear_xent_bwd(h, _ld(h), w, _ld(w), _dt(h), T, D, V, targets, ignore_index, reduction, lse, dloss, dh,
+                                     _ld(dh) if want_dh else 0, dw, _ld(dw) if want_dw else 0, ws, ws.numel(), _STREAM),
+           "efqat_linear_xent_bwd")
+    return dict(dh=dh, dw=dw)

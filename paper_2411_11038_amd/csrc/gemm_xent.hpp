@@ -1,0 +1,539 @@
+// The three products of the loss over a vocabulary, on bf16 operands with fp32 sums:
+//
+//   out[n][m] = sum_k A[m][k] B[n][k]
+//
+//   logits (XG_LSE, XG_GRAD)  A = class weights W [m = class][k = feature], B = features H [n = token][k]
+//   dH     (XG_OUT)           A = W read as [k = class][m = feature], B = G [n = token][k = class]
+//   dW     (XG_OUT)           A = H read as [k = token][m = feature], B = G read as [k = token][n = class]
+//
+// An operand whose contraction index is its row (TR) is copied into LDS as it lies and transposed by the LDS reads
+// (ds_read_b64_tr_b16), so that no transposed copy of W, H or G exists.  With classes along m and tokens along n the accumulators
+// of a lane are classes of one token: the softmax statistics of a token are sums over registers and one exchange between the two
+// halves of a wavefront, instead of a reduction over 32 lanes for every row.
+//
+// Square tiles: 256 by eight wavefronts of 128 x 64 (the accumulators are half of a lane's registers, two wavefronts a SIMD),
+// 128 and 64 by four.  K stages of 64 in two LDS buffers; a stage's copies go out in the last sub-step of the stage before the
+// previous one's end and in the first of the previous, so that they have two sub-steps to land; fragment reads run a sub-step ahead
+// of the matrix instructions.  The order is pinned, one group per matrix instruction.
+//
+// fp32 operands are three bf16 parts each (x = x0 + x1 + x2 with 24 bits), side by side in a row; the product of two is the six
+// largest of the nine products of parts, smallest first: `segments` walks them, each a contraction of its own over the same rows.
+// What is left out is below 2^-24 of the product of the magnitudes.
+#pragma once
+#include "rows.hpp"
+
+#include <type_traits>
+
+#include "gemm_epilogue.hpp"
+#include "lds_copy.hpp"
+
+namespace efqat {
+
+enum XentMode { XG_LSE = 0, XG_GRAD = 1, XG_OUT = 2 };
+
+struct XentGemmArgs {
+  const bf16_t *A, *B;
+  int64_t lda, ldb;               // elements between rows
+  int a_cols, b_cols;             // TR: columns that exist (multiples of 64), else unused
+  int a_part, b_part;             // columns between the parts of an operand (segments == 6)
+  int segments;                   // 1, or 6 products of parts
+  int M, N, K;                    // N, K: as many as exist at most, see `count`
+  int count_n, count_k;           // 1: N / K is the number of tokens that have a class, on the device
+  const int32_t* n_valid;
+  int a_rows;                     // TR A whose last stage passes the rows that exist: K rows; 0: K is whole stages
+  int tiles_m, tiles_n;           // of the grid (the most there can be)
+  int split_blocks, split_stages; // XG_OUT: K is cut so that about that many blocks work (xent_split, by the K of a whole piece)
+  // XG_LSE / XG_GRAD: classes m of [class0, class0 + M), per token slot n
+  int class0;
+  const int32_t* target;          // [slots] class, -1 behind the last token
+  float2* part;                   // XG_LSE: [tile of classes][slots] (largest logit, sum of exp(logit - largest))
+  float* target_logit;            // XG_LSE: [slots]
+  int slots;
+  const float *lse, *scale;       // XG_GRAD: [slots]
+  bf16_t* grad;                   // XG_GRAD: G [slots][parts][grad_pitch]
+  int grad_pitch;
+  // XG_OUT: fp32 partial results [slice][n][m] (pitch M), or the output itself
+  float* acc;
+  int acc_add;                    // 1: added to what acc holds
+  int acc_write;                  // 1: the result goes to acc, 0: to out
+  void* out;
+  int out_dtype;
+  int64_t ldo;
+  const int32_t* rows;            // rows of out, by n; NULL: n
+};
+
+// Slices of K of an XG_OUT product of so many tiles: about `blocks` blocks, none with fewer than 8 stages
+__host__ __device__ inline int xent_split(int tiles, int stages, int blocks) {
+  const int by_blocks = tiles > 0 ? blocks / tiles : 1, by_stages = stages / 8;
+  const int s = by_blocks < by_stages ? by_blocks : by_stages;
+  return s < 1 ? 1 : s;
+}
+
+// One wave-wide global -> LDS copy (see dma16) from a uniform base and 32-bit offsets
+__device__ __forceinline__ void dma16_at(const char* base, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0" ::"s"(lds) : "m0");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base));
+}
+
+typedef int intx4_xg_t __attribute__((ext_vector_type(4)));
+
+// One operand of a tile: BW rows (or columns, TR) of the tile, WW of them a wavefront's
+template <int BW, int WW, int NW, bool TR>
+struct XentOperand {
+  static constexpr int T = WW / 32;                   // fragments of a wavefront and sub-step
+  static constexpr int G = BW / 8 / NW;               // 1-KiB copies of a wavefront and stage
+  static constexpr int RB = 2 * BW;                   // TR: bytes of an LDS row
+  static constexpr int CPR = RB / 16, RPC = 1024 / RB; // TR: chunks of a row, rows of a copy
+  static constexpr int READS = TR ? 2 * T : T;
+  static constexpr int ADDR = TR ? T : 4;
+  uint32_t voff[G];
+  int addr[ADDR];
+  struct Frag { intx4_xg_t v; };
+
+  // physical 16-byte chunk of an LDS row: reads of half a wavefront touch all banks once
+  __device__ static __forceinline__ int swz(int c, int k) { return c ^ (4 * (BW == 64 ? (k >> 1) & 1 : k & 3)); }
+
+  // limit: rows (columns, TR) of the tile that exist; the others repeat one that does, their results are dropped
+  __device__ __forceinline__ void setup(int64_t ld, int limit, int wave, int wpos, int lane, int lds0) {
+    const uint32_t ld2 = (uint32_t)(ld * 2);
+#pragma unroll
+    for (int j = 0; j < G; ++j) {
+      const int u = wave + NW * j;
+      if constexpr (TR) {
+        const int k = u * RPC + lane / CPR;
+        int col = swz(lane % CPR, k) * 8;
+        col = col < limit ? col : 0;
+        voff[j] = (uint32_t)k * ld2 + (uint32_t)col * 2;
+      } else {
+        const int r = u * 8 + (lane >> 3);
+        const int c = (lane & 7) ^ ((r >> 1) & 7);
+        voff[j] = (uint32_t)(r < limit ? r : limit - 1) * ld2 + (uint32_t)c * 16;
+      }
+    }
+    if constexpr (TR) {
+      const int s = lane & 15, q = lane >> 4, mb = 16 * (q & 1), h = q >> 1, k = 8 * h + (s >> 2);
+#pragma unroll
+      for (int i = 0; i < T; ++i) {
+        const int c = (wpos * WW + 32 * i + mb + 4 * (s & 3)) >> 3;
+        addr[i] = lds0 + k * RB + (swz(c, k) << 4) + 8 * (s & 1);
+      }
+    } else {
+      const int fr = lane & 31, fh = lane >> 5;
+#pragma unroll
+      for (int sub = 0; sub < 4; ++sub)
+        addr[sub] = lds0 + (wpos * WW + fr) * 128 + (((2 * sub + fh) ^ ((fr >> 1) & 7)) << 4);
+    }
+  }
+  // copy j of a stage; last: rows k >= left of a TR operand do not exist, the last one is repeated (the other operand's are zero)
+  __device__ __forceinline__ void copy(const char* base, uint32_t lds, int wave, int j) const {
+    dma16_at(base, voff[j], lds + (wave + NW * j) * 1024);
+  }
+  __device__ __forceinline__ void copy_last(const char* base, uint32_t lds, int wave, int lane, int j, int64_t ld, int left) const {
+    uint32_t off = voff[j];
+    if constexpr (TR) {
+      const int k = (wave + NW * j) * RPC + lane / CPR;
+      if (k >= left) off -= (uint32_t)(k - left + 1) * (uint32_t)(ld * 2);
+    }
+    dma16_at(base, off, lds + (wave + NW * j) * 1024);
+  }
+  // read number r of sub-step sub
+  __device__ __forceinline__ void read(const char* smem, int sub, int r, Frag (&f)[T]) const {
+    if constexpr (TR) {
+      const int i = r >> 1, hh = r & 1;
+      const shortx4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (__attribute__((address_space(3))) shortx4_t*)(smem + addr[i] + sub * 16 * RB + hh * 4 * RB));
+      const intx2_t w = __builtin_bit_cast(intx2_t, v);
+      f[i].v[2 * hh] = w[0];
+      f[i].v[2 * hh + 1] = w[1];
+    } else {
+      f[r].v = *reinterpret_cast<const intx4_xg_t*>(smem + addr[sub] + r * 4096);
+    }
+  }
+  __device__ __forceinline__ void other_buffer(int stage_bytes) {
+#pragma unroll
+    for (int i = 0; i < ADDR; ++i) addr[i] ^= stage_bytes;
+  }
+};
+
+template <int BT>
+struct XentCfg {
+  static constexpr int NW = BT == 256 ? 8 : 4, WGM = 2, WGN = NW / 2;
+  static constexpr int WM = BT / WGM, WN = BT / WGN, TM = WM / 32, TN = WN / 32;
+  static constexpr int STAGE = BT * 256;              // bytes of both operands' stage, a power of two
+  static constexpr int OUT_PITCH = WM * 2 + 16;       // bytes of a row of a wavefront's bf16 results in LDS
+  static constexpr int LDS = 2 * STAGE > NW * WN * OUT_PITCH ? 2 * STAGE : NW * WN * OUT_PITCH;
+};
+
+// bf16 parts of x: x0 + x1 + x2 = x up to 2^-24.  A NaN is its first part.  What bf16 has no finite value for, infinities among it,
+// is the largest one it has: an infinite first part times another operand's zero part would be a NaN in every product.
+__device__ __forceinline__ void split3(float x, float (&p)[3]) {
+  constexpr float kMost = 0x1.FEp127f;
+  x = fabsf(x) > kMost ? copysignf(kMost, x) : x;
+  p[0] = __uint_as_float(pack_bf16x2(x, x) << 16);
+  const float r1 = p[0] == p[0] ? x - p[0] : 0.0f;
+  p[1] = __uint_as_float(pack_bf16x2(r1, r1) << 16);
+  p[2] = r1 - p[1];
+}
+
+template <int BT, bool ATR, bool BTR, int MODE>
+__global__ __launch_bounds__(XentCfg<BT>::NW * 64) void k_xent_gemm(const XentGemmArgs g) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  using C = XentCfg<BT>;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave / C::WGN, wn = wave % C::WGN;
+
+  const int valid = g.n_valid[0];
+  const int N = g.count_n ? valid : g.N, K = g.count_k ? valid : g.K;
+  const int tiles_n = (N + BT - 1) / BT, tiles = g.tiles_m * tiles_n;
+  const int nks = (K + 63) / 64;                      // stages of a segment
+  // slices of K (XG_OUT), tiles of a slice; neighbours run on one XCD, in groups of 4 rows of tiles
+  int nslice = 1;
+  if constexpr (MODE == XG_OUT) nslice = g.split_blocks > 0 ? xent_split(tiles, g.count_k ? nks : g.split_stages, g.split_blocks) : 1;
+  const int total = tiles * nslice;
+  if ((int)blockIdx.x >= total) return;
+  const int logical = xcd_contiguous_index(blockIdx.x, total);
+  const int slice = logical / tiles, pid = logical - slice * tiles;
+  constexpr int GM = 4;
+  const int per_group = GM * tiles_n, group = pid / per_group, first_m = group * GM;
+  const int gsize = g.tiles_m - first_m < GM ? g.tiles_m - first_m : GM;
+  const int tm = first_m + (pid % per_group) % gsize, tn = (pid % per_group) / gsize;
+  const int m0 = tm * BT, n0 = tn * BT;
+  const int k_first = (int)((int64_t)nks * slice / nslice), k_end = (int)((int64_t)nks * (slice + 1) / nslice);
+  const int per_seg = k_end - k_first, nstage = per_seg * g.segments;
+
+  XentOperand<BT, C::WM, C::NW, ATR> A;
+  XentOperand<BT, C::WN, C::NW, BTR> B;
+  A.setup(g.lda, ATR ? g.a_cols - m0 : g.M - m0, wave, wm, lane, 0);
+  B.setup(g.ldb, BTR ? g.b_cols - n0 : N - n0, wave, wn, lane, BT * 128);
+  const int64_t a_step = ATR ? g.lda * 128 : 128, b_step = BTR ? g.ldb * 128 : 128;
+  const char* a_base = (const char*)g.A + (ATR ? (int64_t)m0 * 2 : (int64_t)m0 * g.lda * 2) + k_first * a_step;
+  const char* b_base = (const char*)g.B + (BTR ? (int64_t)n0 * 2 : (int64_t)n0 * g.ldb * 2) + k_first * b_step;
+  // the copy stream: stage, its place in its segment, its sources
+  int c_seg = 0, c_kt = 0;
+  auto seg_a = [&](int s) { return (int)((0x001102u >> (4 * (g.segments == 6 ? s : 5))) & 15u); };
+  auto seg_b = [&](int s) { return (int)((0x010120u >> (4 * (g.segments == 6 ? s : 5))) & 15u); };
+  const char* a_src = a_base + (int64_t)seg_a(0) * g.a_part * 2;
+  const char* b_src = b_base + (int64_t)seg_b(0) * g.b_part * 2;
+  auto next_stage = [&]() {
+    if (++c_kt == per_seg) {
+      c_kt = 0;
+      ++c_seg;
+      a_src = a_base + (int64_t)seg_a(c_seg) * g.a_part * 2;
+      b_src = b_base + (int64_t)seg_b(c_seg) * g.b_part * 2;
+    } else {
+      a_src += a_step;
+      b_src += b_step;
+    }
+  };
+  constexpr int AG = decltype(A)::G, BG = decltype(B)::G, LPS = AG + BG, H0 = (LPS + 1) / 2;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)smem;
+  auto issue = [&](auto lastc, int buf, int t0, int t1) {
+    const uint32_t l = lds0 + buf * C::STAGE;
+#pragma unroll
+    for (int t = t0; t < t1; ++t) {
+      if (t < AG) {
+        if constexpr (decltype(lastc)::value) A.copy_last(a_src, l, wave, lane, t, g.lda, g.a_rows - (k_end - 1) * 64);
+        else A.copy(a_src, l, wave, t);
+      } else {
+        B.copy(b_src, l + BT * 128, wave, t - AG);
+      }
+    }
+  };
+  using Last = std::integral_constant<bool, true>;
+  using Whole = std::integral_constant<bool, false>;
+  // the last stage of a TR A whose rows end inside it is copied apart
+  const int nfull = ATR && g.a_rows && k_end == nks && (g.a_rows & 63) ? nstage - 1 : nstage;
+
+  floatx16_t acc[C::TM][C::TN];
+#pragma unroll
+  for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+    for (int j = 0; j < C::TN; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+
+  typename decltype(A)::Frag af[2][C::TM];
+  typename decltype(B)::Frag bf[2][C::TN];
+  constexpr int RA = decltype(A)::READS, RBR = decltype(B)::READS, NRD = RA + RBR, MF = C::TM * C::TN;
+  auto read_one = [&](int sub, int rb, int r) {
+    if (r < RBR) B.read(smem, sub, r, bf[rb]);
+    else A.read(smem, sub, r - RBR, af[rb]);
+  };
+  auto read_all = [&](int sub, int rb) {
+#pragma unroll
+    for (int r = 0; r < NRD; ++r) read_one(sub, rb, r);
+  };
+  auto mfma_one = [&](int rb, int i, int j) {
+    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, af[rb][i].v),
+                                                        __builtin_bit_cast(bf16x8_t, bf[rb][j].v), acc[i][j], 0, 0, 0);
+  };
+  auto mfma_all = [&](int rb) {
+#pragma unroll
+    for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+      for (int j = 0; j < C::TN; ++j) mfma_one(rb, i, j);
+  };
+  // the copies of the next stage have landed, every wavefront has read all of this one's
+  auto stage_sync = [&]() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    A.other_buffer(C::STAGE);
+    B.other_buffer(C::STAGE);
+  };
+  // matrix instructions of fragment set rb; the reads of sub-step sub_next into the other set; copies t0 .. t1 - 1 into buf
+  constexpr int RG = (2 * MF + 2) / 3;
+  auto substep = [&](int sub_next, int rb, int buf, int t0, int t1) {
+#pragma unroll
+    for (int q = 0; q < MF; ++q) {
+      mfma_one(rb, q / C::TN, q % C::TN);
+      if (q < RG) {
+#pragma unroll
+        for (int r = (q * NRD) / RG; r < ((q + 1) * NRD) / RG; ++r) read_one(sub_next, rb ^ 1, r);
+      }
+      issue(Whole{}, buf, t0 + (t1 - t0) * q / MF, t0 + (t1 - t0) * (q + 1) / MF);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  // On entry to stage s the first H0 copies of stage s + 1 are under way if and only if s + 1 < nfull.
+  if (nstage > 0) {
+    if (nfull > 0) issue(Whole{}, 0, 0, LPS);
+    else issue(Last{}, 0, 0, LPS);
+    next_stage();
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (1 < nfull) issue(Whole{}, 1, 0, H0);
+    read_all(0, 0);
+    int s = 0, buf = 0;
+    for (; s + 2 < nfull; ++s, buf ^= 1) {
+      __builtin_amdgcn_sched_barrier(0);
+      substep(1, 0, buf ^ 1, H0, LPS);
+      next_stage();
+      substep(2, 1, 0, 0, 0);
+      substep(3, 0, 0, 0, 0);
+      stage_sync();
+      substep(0, 1, buf, 0, H0);
+    }
+    for (; s < nstage; ++s, buf ^= 1) {
+      if (s + 1 < nfull) {
+        issue(Whole{}, buf ^ 1, H0, LPS);
+        next_stage();
+      } else if (s + 1 < nstage) {
+        issue(Last{}, buf ^ 1, 0, LPS);
+        next_stage();
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      read_all(1, 1);
+      mfma_all(0);
+      __builtin_amdgcn_sched_barrier(0);
+      read_all(2, 0);
+      mfma_all(1);
+      __builtin_amdgcn_sched_barrier(0);
+      read_all(3, 1);
+      mfma_all(0);
+      stage_sync();
+      if (s + 1 < nstage) read_all(0, 0);
+      if (s + 2 < nfull) issue(Whole{}, buf, 0, H0);
+      mfma_all(1);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  __syncthreads();
+
+  // ---- accumulators: column n = lane & 31, rows m = 8 (r / 4) + 4 (lane / 32) + r % 4 of their 32 x 32
+  const int fr = lane & 31, fh = lane >> 5;
+  const int mw = m0 + wm * C::WM + 4 * fh, nw = n0 + wn * C::WN + fr;
+  auto m_of = [&](int i, int r) { return mw + 32 * i + 8 * (r >> 2) + (r & 3); };
+
+  if constexpr (MODE == XG_LSE) {
+    // largest logit and sum of exponentials of the tile's classes, for every token; the tile's wavefronts join theirs in LDS
+    float2* red = reinterpret_cast<float2*>(smem);    // [WGM][BT]
+    const bool edge = m0 + BT > g.M;
+#pragma unroll
+    for (int j = 0; j < C::TN; ++j) {
+      const int n = nw + 32 * j;
+      float top = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          if (edge && m_of(i, r) >= g.M) acc[i][j][r] = -INFINITY;
+          top = fmaxf(top, acc[i][j][r]);
+        }
+      top = fmaxf(top, __shfl_xor(top, 32));
+      // a token whose logits are all -inf has sum 0; a NaN makes the sum NaN
+      const float base = top == -INFINITY ? 0.0f : top;
+      float sum = 0.0f;
+#pragma unroll
+      for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f((acc[i][j][r] - base) * 1.4426950408889634f);
+      sum += __shfl_xor(sum, 32);
+      if (fh == 0) red[wm * BT + wn * C::WN + 32 * j + fr] = make_float2(top, sum);
+      const int rel = n < N ? g.target[n] - g.class0 - m0 - wm * C::WM : -1;   // row of the wavefront's tile that is the class
+      if (__any(rel >= 0 && rel < C::WM)) {
+        const int mine = rel - 4 * fh;
+#pragma unroll
+        for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (mine == 32 * i + 8 * (r >> 2) + (r & 3)) g.target_logit[n] = acc[i][j][r];
+      }
+    }
+    __syncthreads();
+    if (tid < BT && n0 + tid < N) {
+      float2 a = red[tid];
+      const float2 b = red[BT + tid];
+      const float top = fmaxf(a.x, b.x), base = top == -INFINITY ? 0.0f : top;
+      a.y = a.y * __builtin_amdgcn_exp2f((a.x - base) * 1.4426950408889634f) + b.y * __builtin_amdgcn_exp2f((b.x - base) * 1.4426950408889634f);
+      a.x = top;
+      g.part[(int64_t)(g.class0 / BT + tm) * g.slots + n0 + tid] = a;
+    }
+  } else {
+    // a wavefront's results as rows of WM values in LDS, from where they leave 16 bytes a lane
+    char* tile = smem + wave * (C::WN * C::OUT_PITCH);
+    constexpr int CPR = C::WM * 2 / 16, RPI = 64 / CPR;            // chunks of a row, rows of an access
+    auto put = [&](int i, int j, int q, float a, float b, float c, float d) {
+      *reinterpret_cast<uint2*>(tile + (32 * j + fr) * C::OUT_PITCH + (32 * i + 8 * q + 4 * fh) * 2) =
+          make_uint2(pack_bf16x2(a, b), pack_bf16x2(c, d));
+    };
+    if constexpr (MODE == XG_GRAD) {
+      // G = (softmax - [class of the token]) scale; zero outside the classes and behind the last token
+#pragma unroll
+      for (int j = 0; j < C::TN; ++j) {
+        const int n = nw + 32 * j;
+        const bool in = n < N;
+        const float lse = in ? g.lse[n] : 0.0f, scale = in ? g.scale[n] : 0.0f;
+        const int rel = in ? g.target[n] - g.class0 : -1;
+#pragma unroll
+        for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int m = m_of(i, r);
+            float p = __builtin_amdgcn_exp2f((acc[i][j][r] - lse) * 1.4426950408889634f);
+            p = (m == rel ? p - 1.0f : p) * scale;
+            acc[i][j][r] = in && m < g.M ? p : 0.0f;
+          }
+      }
+      const int parts = g.segments == 6 ? 3 : 1;
+      for (int part = 0; part < parts; ++part) {
+#pragma unroll
+        for (int j = 0; j < C::TN; ++j)
+#pragma unroll
+          for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              float p[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                p[e] = acc[i][j][4 * q + e];
+                const float head = __uint_as_float(pack_bf16x2(p[e], p[e]) << 16);
+                if (part + 1 < parts) acc[i][j][4 * q + e] = fabsf(head) < INFINITY ? p[e] - head : 0.0f;
+              }
+              put(i, j, q, p[0], p[1], p[2], p[3]);
+            }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int r0 = 0; r0 < C::WN; r0 += RPI) {
+          const int r = r0 + lane / CPR, c = lane % CPR;
+          const uint4 v = *reinterpret_cast<const uint4*>(tile + r * C::OUT_PITCH + c * 16);
+          bf16_t* to = g.grad + ((int64_t)(n0 + wn * C::WN + r) * parts + part) * g.grad_pitch + m0 + wm * C::WM + c * 8;
+          *reinterpret_cast<uint4*>(to) = v;
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      }
+    } else {
+      float* part = g.acc + (int64_t)slice * N * g.M;
+      const bool to_acc = g.acc_write || nslice > 1;
+      if (g.acc_add || to_acc || g.out_dtype == EFQAT_F32) {
+#pragma unroll
+        for (int j = 0; j < C::TN; ++j) {
+          const int n = nw + 32 * j;
+          if (n >= N) continue;
+          const int64_t row = to_acc ? n : g.rows ? g.rows[n] : n;
+#pragma unroll
+          for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const int m = m_of(i, 4 * q), left = g.M - m;
+              if (left <= 0) continue;
+              float v[4];
+              typedef float vec __attribute__((ext_vector_type(4), aligned(4)));
+#pragma unroll
+              for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * q + e];
+              if (g.acc_add) {
+                const float* from = part + (int64_t)n * g.M + m;
+                if (left >= 4) {
+                  const vec o = *reinterpret_cast<const vec*>(from);
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) v[e] += o[e];
+                } else {
+#pragma unroll
+                  for (int e = 0; e < 3; ++e)
+                    if (e < left) v[e] += from[e];
+                }
+              }
+              if (to_acc || g.out_dtype == EFQAT_F32) {
+                float* to = to_acc ? part + row * g.M + m : (float*)g.out + row * g.ldo + m;
+                if (left >= 4) {
+                  vec o;
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) o[e] = v[e];
+                  *reinterpret_cast<vec*>(to) = o;
+                } else {
+#pragma unroll
+                  for (int e = 0; e < 3; ++e)
+                    if (e < left) to[e] = v[e];
+                }
+              } else {
+                bf16_t* to = (bf16_t*)g.out + row * g.ldo + m;
+                typedef uint32_t pair __attribute__((ext_vector_type(2), aligned(2)));
+                if (left >= 4) {
+                  *reinterpret_cast<pair*>(to) = pair{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+                } else {
+#pragma unroll
+                  for (int e = 0; e < 3; ++e)
+                    if (e < left) to[e] = from_f32<bf16_t>(v[e]);
+                }
+              }
+            }
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < C::TN; ++j)
+#pragma unroll
+          for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) put(i, j, q, acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int r0 = 0; r0 < C::WN; r0 += RPI) {
+          const int r = r0 + lane / CPR, c = lane % CPR;
+          const int n = n0 + wn * C::WN + r, m = m0 + wm * C::WM + c * 8;
+          const uint4 v = *reinterpret_cast<const uint4*>(tile + r * C::OUT_PITCH + c * 16);
+          const int left = n < N ? g.M - m : 0;
+          if (left > 0) {
+            bf16_t* to = (bf16_t*)g.out + (int64_t)(g.rows ? g.rows[n] : n) * g.ldo + m;
+            if (left >= 8) {
+              Raw8<bf16_t> o;
+              o.a[0] = v.x; o.a[1] = v.y; o.a[2] = v.z; o.a[3] = v.w;
+              o.store(to);
+            } else {
+              const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+              for (int e = 0; e < 7; ++e)
+                if (e < left) to[e] = (bf16_t)(w[e >> 1] >> (16 * (e & 1)));
+            }
+          }
+        }
+      }
+    }
+  }
+#endif
+}
+
+}  // namespace efqat

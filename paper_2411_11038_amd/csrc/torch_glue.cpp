@@ -48,8 +48,25 @@ void* tensor_address(PyObject* o) {
   return t.data_ptr();
 }
 
-// STREAM: the parameter is a stream (every entry ends in `void* stream` or `void* stream, void* side_stream`)
-template <class T, bool STREAM>
+// rows that may lie apart: the elements of a row are neighbours (its row stride is an argument of its own)
+void* rows_address(PyObject* o) {
+  if (o == Py_None) return nullptr;
+  if (!THPVariable_Check(o)) refuse(PyExc_TypeError, "tensor", o);
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!t.is_cuda()) {
+    PyErr_SetString(PyExc_ValueError, "tensor must live on the GPU");
+    throw BadArgument();
+  }
+  if (t.dim() != 2 || (t.size(1) > 1 && t.stride(1) != 1)) {
+    PyErr_SetString(PyExc_ValueError, "tensor must be two-dimensional with contiguous rows");
+    throw BadArgument();
+  }
+  return t.data_ptr();
+}
+
+// STREAM: the parameter is a stream (every entry ends in `void* stream` or `void* stream, void* side_stream`).
+// ROWS: the pointer is followed by the stride of its rows
+template <class T, bool STREAM, bool ROWS>
 T from_python(PyObject* o) {
   if constexpr (STREAM) {
     if (o == Py_None) return nullptr;
@@ -58,7 +75,11 @@ T from_python(PyObject* o) {
   } else if constexpr (std::is_same_v<T, const efqat_opt_step*>) {
     return o == Py_None ? nullptr : (T)(uintptr_t)integer(o, "address of an efqat_opt_step");
   } else if constexpr (std::is_pointer_v<T>) {
-    return (T)tensor_address(o);
+    return (T)(ROWS ? rows_address(o) : tensor_address(o));
+  } else if constexpr (std::is_floating_point_v<T>) {
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) throw BadArgument();
+    return (T)v;
   } else {
     return (T)integer(o, "integer");
   }
@@ -72,10 +93,18 @@ constexpr bool is_stream(size_t i) {
   return i == n - 1 || (i == n - 2 && is_void[i]);
 }
 
-template <class... A, size_t... I>
+// row-strided tensors: an untyped pointer whose next parameter is a 64-bit stride, in entries that have such (APART)
+template <bool APART, class... A>
+constexpr bool is_rows(size_t i) {
+  constexpr bool is_void[] = {std::is_same_v<A, void*> || std::is_same_v<A, const void*>...};
+  constexpr bool is_long[] = {std::is_same_v<A, int64_t>...};
+  return APART && is_void[i] && i + 1 < sizeof...(A) && is_long[i + 1];
+}
+
+template <bool APART, class... A, size_t... I>
 PyObject* call(int (*fn)(A...), PyObject* const* args, std::index_sequence<I...>) {
   try {
-    std::tuple<A...> a{from_python<A, is_stream<A...>(I)>(args[I])...};     // braces: in order, so that the first bad argument is reported
+    std::tuple<A...> a{from_python<A, is_stream<A...>(I), is_rows<APART, A...>(I)>(args[I])...};     // braces: in order, so that the first bad argument is reported
     int rc;
     Py_BEGIN_ALLOW_THREADS
     rc = std::apply(fn, a);
@@ -89,24 +118,28 @@ PyObject* call(int (*fn)(A...), PyObject* const* args, std::index_sequence<I...>
   }
 }
 
-template <class... A>
+template <bool APART, class... A>
 PyObject* call_n(int (*fn)(A...), PyObject* const* args, Py_ssize_t n) {
   if (n != (Py_ssize_t)sizeof...(A)) {
     PyErr_Format(PyExc_TypeError, "%zd arguments, %zd expected", n, (Py_ssize_t)sizeof...(A));
     return nullptr;
   }
-  return call(fn, args, std::index_sequence_for<A...>{});
+  return call<APART>(fn, args, std::index_sequence_for<A...>{});
 }
 
-template <auto FN>
-PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) { return call_n(FN, args, n); }
+template <auto FN, bool APART>
+PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) { return call_n<APART>(FN, args, n); }
 
-#define EFQAT_ENTRY(name) {#name, (PyCFunction)(void (*)(void))entry<efqat_##name>, METH_FASTCALL, nullptr}
+#define EFQAT_ENTRY(name) {#name, (PyCFunction)(void (*)(void))entry<efqat_##name, false>, METH_FASTCALL, nullptr}
+#define EFQAT_ENTRY_ROWS(name) {#name, (PyCFunction)(void (*)(void))entry<efqat_##name, true>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     EFQAT_ENTRY(fakequant_fwd),  EFQAT_ENTRY(channel_select), EFQAT_ENTRY(channel_select_static),
     EFQAT_ENTRY(weight_quant_select), EFQAT_ENTRY(network_select), EFQAT_ENTRY(layer_select),
     EFQAT_ENTRY(bias_grad),      EFQAT_ENTRY(linear_bwd_ex),  EFQAT_ENTRY(linear_bwd_weight_operand),
-    EFQAT_ENTRY(conv_bwd_ex),    EFQAT_ENTRY(linear_fwd),     {nullptr, nullptr, 0, nullptr}};
+    EFQAT_ENTRY(conv_bwd_ex),    EFQAT_ENTRY(linear_fwd),
+    EFQAT_ENTRY_ROWS(ckpt8_save), EFQAT_ENTRY_ROWS(ckpt8_load), EFQAT_ENTRY_ROWS(act_fwd), EFQAT_ENTRY_ROWS(act_bwd),
+    EFQAT_ENTRY_ROWS(layer_norm_fwd), EFQAT_ENTRY_ROWS(layer_norm_bwd), EFQAT_ENTRY_ROWS(linear_xent_fwd),
+    EFQAT_ENTRY_ROWS(linear_xent_bwd), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_efqat_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

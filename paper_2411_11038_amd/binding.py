@@ -526,25 +526,36 @@ def conv_bwd(dy, x_codes, x_clip, x, s_x, z_x, w_codes, w_clip, w, s_w, idx, str
 # ------------------------------------------------------------------ 8-bit checkpoints, activation, layer norm
 CKPT8_GROUP = 128
 ACT_GELU, ACT_SILU = 0, 1
-
-
-def _kept(rows, cols, device, out=None, prefix="x"):
-    """(codes, scales) of a checkpoint: those of `out`, or new ones."""
-    codes, scales = (out.get(prefix + "_codes"), out.get(prefix + "_scales")) if out else (None, None)
-    if codes is None:
-        codes = torch.empty((rows, -(-cols // 16) * 16), dtype=torch.int8, device=device)
-    if scales is None:
-        scales = torch.empty((rows, -(-cols // CKPT8_GROUP)), dtype=torch.float32, device=device)
-    _kept_shape(codes, scales, rows, cols)
-    return codes, scales
+_LIKE, _F32, _I8, _I32, _U8 = range(5)                 # types of _native().empty
+_TORCH = {_F32: torch.float32, _I8: torch.int8, _I32: torch.int32}
 
 
 def _like(t, shape, dtype, what):
     """Checks a tensor that the kernels take by its address: they know no other size than the call's."""
     if t.dtype != dtype:
         raise TypeError(f"{what}: {dtype} expected, got {t.dtype}")
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{what}: shape {tuple(shape)} expected, got {tuple(t.shape)}")
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{what}: shape {shape} expected, got {tuple(t.shape)}")
+
+
+def _outputs(like, out, names, spec):
+    """The tensors `names` of `out`, new ones for those that it does not have.  spec: (type, rows, columns or -1) each, flat."""
+    if not out:
+        return _native().empty(like, *spec)
+    res = []
+    for i, name in enumerate(names):
+        kind, rows, cols = spec[3 * i: 3 * i + 3]
+        t = out.get(name)
+        if t is None:
+            t, = _native().empty(like, kind, rows, cols)
+        else:
+            _like(t, (rows,) if cols < 0 else (rows, cols), like.dtype if kind == _LIKE else _TORCH[kind], name)
+        res.append(t)
+    return res
+
+
+def _kept_spec(rows, cols):
+    return (_I8, rows, -(-cols // 16) * 16, _F32, rows, -(-cols // CKPT8_GROUP))
 
 
 def _kept_shape(codes, scales, rows, cols, what="x"):
@@ -560,14 +571,15 @@ def _rows_cols(x):
 
 def _ld(t):
     """Elements from one row to the next."""
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    rows, cols = t.shape
+    return t.stride(0) if rows > 1 else cols
 
 
 def ckpt8_save(x, out=None):
     """8-bit checkpoint of x [rows, cols] (rows may lie apart).  Returns (codes, scales); `out` may carry them as
     x_codes, x_scales."""
     rows, cols = _rows_cols(x)
-    codes, scales = _kept(rows, cols, x.device, out)
+    codes, scales = _outputs(x, out, ("x_codes", "x_scales"), _kept_spec(rows, cols))
     _check(_native().ckpt8_save(x, _ld(x), _dt(x), rows, cols, codes, scales, _STREAM), "efqat_ckpt8_save")
     return codes, scales
 
@@ -576,28 +588,31 @@ def ckpt8_load(codes, scales, cols, dtype=torch.bfloat16, out=None):
     """The values that a checkpoint of rows of `cols` columns holds, [rows, cols]."""
     rows = codes.shape[0]
     _kept_shape(codes, scales, rows, cols)
-    x = torch.empty((rows, cols), dtype=dtype, device=codes.device) if out is None else out
-    _like(x, (rows, cols), x.dtype, "out")
-    _check(_native().ckpt8_load(codes, scales, rows, cols, x, _ld(x), _dt(x), _STREAM), "efqat_ckpt8_load")
-    return x
+    if out is None:
+        out = torch.empty((rows, cols), dtype=dtype, device=codes.device)
+    else:
+        _like(out, (rows, cols), out.dtype, "out")
+    _check(_native().ckpt8_load(codes, scales, rows, cols, out, _ld(out), _dt(out), _STREAM), "efqat_ckpt8_load")
+    return out
 
 
 def act_fwd(x, kind, up=None, checkpoint=False, out=None):
     """y = f(x), or f(x) * up, for x, up [rows, cols] (rows may lie apart); checkpoint: their 8-bit checkpoints too.  Returns
     dict(y, x_codes, x_scales, up_codes, up_scales); `out` may carry preallocated ones."""
     rows, cols = _rows_cols(x)
-    out = out or {}
-    y = out.get("y")
-    if y is None:
-        y = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
-    else:
-        _like(y, (rows, cols), x.dtype, "y")
+    ldx, ldu = _ld(x), 0
     if up is not None:
         _like(up, (rows, cols), x.dtype, "up")
-    xc, xs = _kept(rows, cols, x.device, out) if checkpoint else (None, None)
-    uc, us = _kept(rows, cols, x.device, out, "up") if checkpoint and up is not None else (None, None)
-    _check(_native().act_fwd(x, _ld(x), up, 0 if up is None else _ld(up), _dt(x), rows, cols, kind, y, _ld(y), xc, xs, uc,
-                             us, _STREAM), "efqat_act_fwd")
+        ldu = _ld(up)
+    xc = xs = uc = us = None
+    if not checkpoint:
+        y, = _outputs(x, out, ("y",), (_LIKE, rows, cols))
+    elif up is None:
+        y, xc, xs = _outputs(x, out, ("y", "x_codes", "x_scales"), (_LIKE, rows, cols) + _kept_spec(rows, cols))
+    else:
+        y, xc, xs, uc, us = _outputs(x, out, ("y", "x_codes", "x_scales", "up_codes", "up_scales"),
+                                     (_LIKE, rows, cols) + 2 * _kept_spec(rows, cols))
+    _check(_native().act_fwd(x, ldx, up, ldu, _dt(x), rows, cols, kind, y, _ld(y), xc, xs, uc, us, _STREAM), "efqat_act_fwd")
     return dict(y=y, x_codes=xc, x_scales=xs, up_codes=uc, up_scales=us)
 
 
@@ -606,22 +621,17 @@ def act_bwd(dy, kind, x_codes, x_scales, up_codes=None, up_scales=None, out=None
     apart)."""
     rows, cols = _rows_cols(dy)
     _kept_shape(x_codes, x_scales, rows, cols)
-    gated = up_codes is not None or up_scales is not None
-    if gated:
+    if up_codes is None and up_scales is None:
+        dx, = _outputs(dy, out, ("dx",), (_LIKE, rows, cols))
+        dup, lddup = None, 0
+    else:
         if up_codes is None or up_scales is None:
             raise ValueError("up_codes and up_scales belong together")
         _kept_shape(up_codes, up_scales, rows, cols, "up")
-    out = out or {}
-    dx, dup = out.get("dx"), out.get("dup") if gated else None
-    if dx is None:
-        dx = torch.empty((rows, cols), dtype=dy.dtype, device=dy.device)
-    if gated and dup is None:
-        dup = torch.empty((rows, cols), dtype=dy.dtype, device=dy.device)
-    _like(dx, (rows, cols), dy.dtype, "dx")
-    if gated:
-        _like(dup, (rows, cols), dy.dtype, "dup")
-    _check(_native().act_bwd(dy, _ld(dy), _dt(dy), rows, cols, kind, x_codes, x_scales, up_codes, up_scales, dx, _ld(dx),
-                             dup, _ld(dup) if gated else 0, _STREAM), "efqat_act_bwd")
+        dx, dup = _outputs(dy, out, ("dx", "dup"), (_LIKE, rows, cols, _LIKE, rows, cols))
+        lddup = _ld(dup)
+    _check(_native().act_bwd(dy, _ld(dy), _dt(dy), rows, cols, kind, x_codes, x_scales, up_codes, up_scales, dx, _ld(dx), dup,
+                             lddup, _STREAM), "efqat_act_bwd")
     return dict(dx=dx, dup=dup)
 
 
@@ -629,22 +639,16 @@ def layer_norm_fwd(x, weight=None, bias=None, eps=1e-5, checkpoint=False, out=No
     """Layer norm of x [rows, cols] (rows may lie apart); weight, bias fp32 [cols] or None; checkpoint: the 8-bit checkpoint of
     x too.  Returns dict(y, mean, rstd, x_codes, x_scales); `out` may carry preallocated ones."""
     rows, cols = _rows_cols(x)
-    out = out or {}
-    dev = x.device
-    y, mean, rstd = out.get("y"), out.get("mean"), out.get("rstd")
-    if y is None:
-        y = torch.empty((rows, cols), dtype=x.dtype, device=dev)
-    if mean is None:
-        mean = torch.empty(rows, dtype=torch.float32, device=dev)
-    if rstd is None:
-        rstd = torch.empty(rows, dtype=torch.float32, device=dev)
-    _like(y, (rows, cols), x.dtype, "y")
-    _like(mean, (rows,), torch.float32, "mean")
-    _like(rstd, (rows,), torch.float32, "rstd")
-    for t, what in ((weight, "weight"), (bias, "bias")):
-        if t is not None:
-            _like(t, (cols,), torch.float32, what)
-    xc, xs = _kept(rows, cols, dev, out) if checkpoint else (None, None)
+    if weight is not None:
+        _like(weight, (cols,), torch.float32, "weight")
+    if bias is not None:
+        _like(bias, (cols,), torch.float32, "bias")
+    xc = xs = None
+    spec = (_LIKE, rows, cols, _F32, rows, -1, _F32, rows, -1)
+    if checkpoint:
+        y, mean, rstd, xc, xs = _outputs(x, out, ("y", "mean", "rstd", "x_codes", "x_scales"), spec + _kept_spec(rows, cols))
+    else:
+        y, mean, rstd = _outputs(x, out, ("y", "mean", "rstd"), spec)
     _check(_native().layer_norm_fwd(x, _ld(x), _dt(x), rows, cols, weight, bias, eps, y, _ld(y), mean, rstd, xc, xs, _STREAM),
            "efqat_layer_norm_fwd")
     return dict(y=y, mean=mean, rstd=rstd, x_codes=xc, x_scales=xs)
@@ -654,33 +658,25 @@ def layer_norm_bwd(dy, weight, mean, rstd, x=None, x_codes=None, x_scales=None, 
     """Backward of layer_norm_fwd from x, or from the checkpoint that it left.  Returns dict(dx, dweight, dbias); `out` may
     carry preallocated ones."""
     rows, cols = _rows_cols(dy)
-    if x is None:
-        if x_codes is None or x_scales is None:
-            raise ValueError("x, or x_codes and x_scales, expected")
-        _kept_shape(x_codes, x_scales, rows, cols)
-    else:
+    ldx = 0
+    if x is not None:
         _like(x, (rows, cols), dy.dtype, "x")
+        ldx = _ld(x)
+        x_codes = x_scales = None
+    elif x_codes is None or x_scales is None:
+        raise ValueError("x, or x_codes and x_scales, expected")
+    else:
+        _kept_shape(x_codes, x_scales, rows, cols)
     if weight is not None:
         _like(weight, (cols,), torch.float32, "weight")
     _like(mean, (rows,), torch.float32, "mean")
     _like(rstd, (rows,), torch.float32, "rstd")
-    out = out or {}
-    dev = dy.device
-    dx, dweight, dbias = out.get("dx"), out.get("dweight"), out.get("dbias")
-    if dx is None:
-        dx = torch.empty((rows, cols), dtype=dy.dtype, device=dev)
-    if dweight is None:
-        dweight = torch.empty(cols, dtype=torch.float32, device=dev)
-    if dbias is None:
-        dbias = torch.empty(cols, dtype=torch.float32, device=dev)
-    _like(dx, (rows, cols), dy.dtype, "dx")
-    _like(dweight, (cols,), torch.float32, "dweight")
-    _like(dbias, (cols,), torch.float32, "dbias")
+    native = _native()
+    dx, dweight, dbias = _outputs(dy, out, ("dx", "dweight", "dbias"), (_LIKE, rows, cols, _F32, cols, -1, _F32, cols, -1))
     if ws is None:
-        ws = _ws(lib().efqat_layer_norm_bwd_workspace_bytes(rows, cols), dy)
-    _check(_native().layer_norm_bwd(dy, _ld(dy), _dt(dy), x, 0 if x is None else _ld(x), None if x is not None else x_codes,
-                                    None if x is not None else x_scales, mean, rstd, weight, rows, cols, dx, _ld(dx), dweight,
-                                    dbias, ws, ws.numel(), _STREAM), "efqat_layer_norm_bwd")
+        ws, = native.empty(dy, _U8, native.layer_norm_bwd_workspace_bytes(rows, cols), -1)
+    _check(native.layer_norm_bwd(dy, _ld(dy), _dt(dy), x, ldx, x_codes, x_scales, mean, rstd, weight, rows, cols, dx, _ld(dx), dweight,
+                                 dbias, ws, ws.numel(), _STREAM), "efqat_layer_norm_bwd")
     return dict(dx=dx, dweight=dweight, dbias=dbias)
 
 
@@ -702,23 +698,13 @@ def linear_xent_fwd(h, w, targets, ignore_index=-100, reduction=XENT_MEAN, ws=No
     """Loss of the logits h w^T (never kept) against one class a token: h [T, D], w [V, D] (rows may lie apart), targets
     int64 [T].  Returns dict(loss, lse, n_valid); `out` may carry them."""
     T, D, V = _xent_shapes(h, w, targets)
-    out = out or {}
-    dev = h.device
-    n_loss = T if reduction == XENT_NONE else 1
-    loss, lse, n_valid = out.get("loss"), out.get("lse"), out.get("n_valid")
-    if loss is None:
-        loss = torch.empty(n_loss, dtype=torch.float32, device=dev)
-    if lse is None:
-        lse = torch.empty(T, dtype=torch.float32, device=dev)
-    if n_valid is None:
-        n_valid = torch.empty(1, dtype=torch.int32, device=dev)
-    _like(loss, (n_loss,), torch.float32, "loss")
-    _like(lse, (T,), torch.float32, "lse")
-    _like(n_valid, (1,), torch.int32, "n_valid")
+    native, dt = _native(), _dt(h)
+    loss, lse, n_valid = _outputs(h, out, ("loss", "lse", "n_valid"),
+                                  (_F32, T if reduction == XENT_NONE else 1, -1, _F32, T, -1, _I32, 1, -1))
     if ws is None:
-        ws = _ws(lib().efqat_linear_xent_fwd_workspace_bytes(T, D, V, _dt(h)), h)
-    _check(_native().linear_xent_fwd(h, _ld(h), w, _ld(w), _dt(h), T, D, V, targets, ignore_index, reduction, loss, lse, n_valid,
-                                     ws, ws.numel(), _STREAM), "efqat_linear_xent_fwd")
+        ws, = native.empty(h, _U8, native.linear_xent_fwd_workspace_bytes(T, D, V, dt), -1)
+    _check(native.linear_xent_fwd(h, _ld(h), w, _ld(w), dt, T, D, V, targets, ignore_index, reduction, loss, lse, n_valid, ws,
+                                  ws.numel(), _STREAM), "efqat_linear_xent_fwd")
     return dict(loss=loss, lse=lse, n_valid=n_valid)
 
 
@@ -730,21 +716,17 @@ def linear_xent_bwd(h, w, targets, lse, dloss=None, ignore_index=-100, reduction
     _like(lse, (T,), torch.float32, "lse")
     if dloss is not None:
         _like(dloss, (T if reduction == XENT_NONE else 1,), torch.float32, "dloss")
-    out = out or {}
-    dh, dw = out.get("dh"), out.get("dw")
+    native, dt = _native(), _dt(h)
+    dh = dw = None
+    lddh = lddw = 0
     if want_dh:
-        dh = torch.empty((T, D), dtype=h.dtype, device=h.device) if dh is None else dh
-        _like(dh, (T, D), h.dtype, "dh")
-    else:
-        dh = None
+        dh, = _outputs(h, out, ("dh",), (_LIKE, T, D))
+        lddh = _ld(dh)
     if want_dw:
-        dw = torch.empty((V, D), dtype=w.dtype, device=w.device) if dw is None else dw
-        _like(dw, (V, D), w.dtype, "dw")
-    else:
-        dw = None
+        dw, = _outputs(w, out, ("dw",), (_LIKE, V, D))
+        lddw = _ld(dw)
     if ws is None:
-        ws = _ws(lib().efqat_linear_xent_bwd_workspace_bytes(T, D, V, _dt(h)), h)
-    _check(_native().linear_xent_bwd(h, _ld(h), w, _ld(w), _dt(h), T, D, V, targets, ignore_index, reduction, lse, dloss, dh,
-                                     _ld(dh) if want_dh else 0, dw, _ld(dw) if want_dw else 0, ws, ws.numel(), _STREAM),
-           "efqat_linear_xent_bwd")
+        ws, = native.empty(h, _U8, native.linear_xent_bwd_workspace_bytes(T, D, V, dt), -1)
+    _check(native.linear_xent_bwd(h, _ld(h), w, _ld(w), dt, T, D, V, targets, ignore_index, reduction, lse, dloss, dh, lddh, dw, lddw,
+                                  ws, ws.numel(), _STREAM), "efqat_linear_xent_bwd")
     return dict(dh=dh, dw=dw)

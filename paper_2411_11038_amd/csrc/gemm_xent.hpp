@@ -3,8 +3,8 @@
 //   out[n][m] = sum_k A[m][k] B[n][k]
 //
 //   logits (XG_LSE, XG_GRAD)  A = class weights W [m = class][k = feature], B = features H [n = token][k]
-//   dH     (XG_OUT)           A = W read as [k = class][m = feature], B = G [n = token][k = class]
-//   dW     (XG_OUT)           A = H read as [k = token][m = feature], B = G read as [k = token][n = class]
+//   dH     (XG_DH)            A = W read as [k = class][m = feature], B = G [n = token][k = class]
+//   dW     (XG_DW)            A = H read as [k = token][m = feature], B = G read as [k = token][n = class]
 //
 // An operand whose contraction index is its row (TR) is copied into LDS as it lies and transposed by the LDS reads
 // (ds_read_b64_tr_b16), so that no transposed copy of W, H or G exists.  With classes along m and tokens along n the accumulators
@@ -29,45 +29,84 @@
 
 namespace efqat {
 
-enum XentMode { XG_LSE = 0, XG_GRAD = 1, XG_OUT = 2 };
+enum XentMode { XG_LSE = 0, XG_GRAD = 1, XG_DH = 2, XG_DW = 3 };
+
+// The classes are taken in pieces, whose size follows from the number of tokens that have a class: a piece's G has about `elems`
+// elements (of all its parts), and its classes, where they are laid out anew, are `cap` at most.  The host knows the number of tokens
+// only as a limit and launches the pieces that the limit needs; the last of them may find nothing left.
+struct XentPieces {
+  int V, cap;
+  uint32_t elems;                 // 0: no limit but cap
+  int parts;
+  __host__ __device__ int size(int tokens) const {
+    const uint32_t slots = tokens < 1 ? 256u : ((uint32_t)tokens + 255u) / 256u * 256u;
+    uint32_t most = (uint32_t)cap;
+    if (elems) {
+      const uint32_t fit = elems / (slots * (uint32_t)parts) / 256u * 256u;       // slots * parts < 2^32: check_xent
+      most = fit < 1024u ? 1024u : fit;
+      most = most < (uint32_t)cap ? most : (uint32_t)cap;
+    }
+    const uint32_t n = ((uint32_t)V + most - 1u) / most, even = ((uint32_t)V + n - 1u) / n;
+    return (int)((even + 255u) / 256u * 256u);
+  }
+};
 
 struct XentGemmArgs {
-  const bf16_t *A, *B;
-  int64_t lda, ldb;               // elements between rows
-  int a_cols, b_cols;             // TR: columns that exist (multiples of 64), else unused
-  int a_part, b_part;             // columns between the parts of an operand (segments == 6)
+  const bf16_t *W, *H;            // operands in whole stages: [class][parts][Dp] (W: of all classes, or of the piece alone), [slot][parts][Dp]
+  bf16_t* G;                      // [slot][parts][piece]
+  int w_piece;                    // 1: W holds the piece alone, zeros behind its last class
+  int64_t ldw, Dp;                // elements between the rows of W; features in whole stages
+  int64_t D;
   int segments;                   // 1, or 6 products of parts
-  int M, N, K;                    // N, K: as many as exist at most, see `count`
-  int count_n, count_k;           // 1: N / K is the number of tokens that have a class, on the device
+  XentPieces pieces;
+  int piece;                      // number of the piece
   const int32_t* n_valid;
-  int a_rows;                     // TR A whose last stage passes the rows that exist: K rows; 0: K is whole stages
-  int tiles_m, tiles_n;           // of the grid (the most there can be)
-  int split_blocks, split_stages; // XG_OUT: K is cut so that about that many blocks work (xent_split, by the K of a whole piece)
-  // XG_LSE / XG_GRAD: classes m of [class0, class0 + M), per token slot n
-  int class0;
-  const int32_t* target;          // [slots] class, -1 behind the last token
+  int split_blocks;               // products of G: K is cut so that about that many blocks work (xent_split)
+  // logits, per token slot
+  const int32_t* target;
   float2* part;                   // XG_LSE: [tile of classes][slots] (largest logit, sum of exp(logit - largest))
-  float* target_logit;            // XG_LSE: [slots]
-  int slots;
-  const float *lse, *scale;       // XG_GRAD: [slots]
-  bf16_t* grad;                   // XG_GRAD: G [slots][parts][grad_pitch]
-  int grad_pitch;
-  // XG_OUT: fp32 partial results [slice][n][m] (pitch M), or the output itself
+  float* target_logit;            // XG_LSE
+  int64_t slots;
+  const float *lse, *scale;       // XG_GRAD; mean: scale is divided by the number of tokens
+  int mean;
+  // products of G: fp32 partial results [slice][n][D], and the output
   float* acc;
-  int acc_add;                    // 1: added to what acc holds
-  int acc_write;                  // 1: the result goes to acc, 0: to out
   void* out;
   int out_dtype;
   int64_t ldo;
-  const int32_t* rows;            // rows of out, by n; NULL: n
+  const int32_t* rows;            // XG_DH: rows of the output, by slot
 };
 
-// Slices of K of an XG_OUT product of so many tiles: about `blocks` blocks, none with fewer than 8 stages
-__host__ __device__ inline int xent_split(int tiles, int stages, int blocks) {
-  const int by_blocks = tiles > 0 ? blocks / tiles : 1, by_stages = stages / 8;
+// Slices of K of a product of G of so many tiles: about `blocks` blocks, none with fewer than 8 stages
+__host__ __device__ inline int xent_split(int64_t tiles, int stages, int segments, int blocks) {
+  const int by_blocks = tiles > blocks || tiles < 1 ? 1 : blocks / (int)tiles;
+  const int by_stages = segments >= 8 ? stages : (int)((int64_t)stages * segments >> 3);
   const int s = by_blocks < by_stages ? by_blocks : by_stages;
   return s < 1 ? 1 : s;
 }
+
+// Sizes of a product, from the number of tokens
+struct XentShape {
+  int64_t class0;
+  int classes, piece;             // of this piece (0: nothing left), of a whole one
+  int M, N, K, nks;               // nks: stages of a segment
+  int split_stages, split_n;
+  __device__ __forceinline__ int split_tiles(int bt) const { return ((M + bt - 1) / bt) * ((split_n + bt - 1) / bt); }
+  __device__ __forceinline__ XentShape(const XentGemmArgs& g, XentMode mode, int valid) {
+    piece = __builtin_amdgcn_readfirstlane(g.pieces.size(valid));
+    class0 = (int64_t)piece * g.piece;
+    const int64_t left = g.pieces.V - class0;
+    classes = (int)(left < 0 ? 0 : left < piece ? left : piece);
+    M = mode == XG_LSE || mode == XG_GRAD ? classes : (int)g.D;
+    N = mode == XG_DW ? classes : valid;
+    K = mode == XG_DW ? valid : mode == XG_DH ? classes : (int)g.Dp;
+    nks = (K + 63) / 64;
+    // slices by a whole piece: dH adds those of the last, shorter one to the same partial results
+    const int whole = piece < g.pieces.V ? piece : g.pieces.V;
+    split_stages = mode == XG_DH ? (whole + 63) / 64 : nks;
+    split_n = mode == XG_DW ? whole : N;
+  }
+};
 
 // One wave-wide global -> LDS copy (see dma16) from a uniform base and 32-bit offsets
 __device__ __forceinline__ void dma16_at(const char* base, uint32_t off, uint32_t lds) {
@@ -160,8 +199,9 @@ struct XentCfg {
   static constexpr int NW = BT == 256 ? 8 : 4, WGM = 2, WGN = NW / 2;
   static constexpr int WM = BT / WGM, WN = BT / WGN, TM = WM / 32, TN = WN / 32;
   static constexpr int STAGE = BT * 256;              // bytes of both operands' stage, a power of two
+  static constexpr int NST = BT == 64 ? 4 : 2;        // LDS stages
   static constexpr int OUT_PITCH = WM * 2 + 16;       // bytes of a row of a wavefront's bf16 results in LDS
-  static constexpr int LDS = 2 * STAGE > NW * WN * OUT_PITCH ? 2 * STAGE : NW * WN * OUT_PITCH;
+  static constexpr int LDS = NST * STAGE > NW * WN * OUT_PITCH ? NST * STAGE : NW * WN * OUT_PITCH;
 };
 
 // bf16 parts of x: x0 + x1 + x2 = x up to 2^-24.  A NaN is its first part.  What bf16 has no finite value for, infinities among it,
@@ -175,53 +215,67 @@ __device__ __forceinline__ void split3(float x, float (&p)[3]) {
   p[2] = r1 - p[1];
 }
 
-template <int BT, bool ATR, bool BTR, int MODE>
+template <int BT, XentMode MODE>
 __global__ __launch_bounds__(XentCfg<BT>::NW * 64) void k_xent_gemm(const XentGemmArgs g) {
 #if defined(__HIP_DEVICE_COMPILE__)
   using C = XentCfg<BT>;
+  constexpr bool LOGITS = MODE == XG_LSE || MODE == XG_GRAD;
+  constexpr bool ATR = !LOGITS, BTR = MODE == XG_DW;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / C::WGN, wn = wave % C::WGN;
 
   const int valid = g.n_valid[0];
-  const int N = g.count_n ? valid : g.N, K = g.count_k ? valid : g.K;
-  const int tiles_n = (N + BT - 1) / BT, tiles = g.tiles_m * tiles_n;
-  const int nks = (K + 63) / 64;                      // stages of a segment
-  // slices of K (XG_OUT), tiles of a slice; neighbours run on one XCD, in groups of 4 rows of tiles
-  int nslice = 1;
-  if constexpr (MODE == XG_OUT) nslice = g.split_blocks > 0 ? xent_split(tiles, g.count_k ? nks : g.split_stages, g.split_blocks) : 1;
+  const XentShape z(g, MODE, valid);
+  if (z.classes == 0) return;
+  const int M = z.M, N = z.N, nks = z.nks;
+  const int tiles_m = (M + BT - 1) / BT, tiles_n = (N + BT - 1) / BT, tiles = tiles_m * tiles_n;
+  // slices of K (dW: by the tiles of a whole piece), tiles of a slice; neighbours run on one XCD, in groups of 4 rows of tiles
+  const int nslice = LOGITS ? 1 : __builtin_amdgcn_readfirstlane(xent_split(z.split_tiles(BT), z.split_stages, g.segments, g.split_blocks));
   const int total = tiles * nslice;
   if ((int)blockIdx.x >= total) return;
   const int logical = xcd_contiguous_index(blockIdx.x, total);
   const int slice = logical / tiles, pid = logical - slice * tiles;
   constexpr int GM = 4;
   const int per_group = GM * tiles_n, group = pid / per_group, first_m = group * GM;
-  const int gsize = g.tiles_m - first_m < GM ? g.tiles_m - first_m : GM;
-  const int tm = first_m + (pid % per_group) % gsize, tn = (pid % per_group) / gsize;
+  const int gsize = tiles_m - first_m < GM ? tiles_m - first_m : GM;
+  const int tm = __builtin_amdgcn_readfirstlane(first_m + (pid % per_group) % gsize);
+  const int tn = __builtin_amdgcn_readfirstlane((pid % per_group) / gsize);
   const int m0 = tm * BT, n0 = tn * BT;
-  const int k_first = (int)((int64_t)nks * slice / nslice), k_end = (int)((int64_t)nks * (slice + 1) / nslice);
+  const int k_first = __builtin_amdgcn_readfirstlane((int)((int64_t)nks * slice / nslice));
+  const int k_end = __builtin_amdgcn_readfirstlane((int)((int64_t)nks * (slice + 1) / nslice));
   const int per_seg = k_end - k_first, nstage = per_seg * g.segments;
+
+  const int parts = g.segments == 6 ? 3 : 1;
+  const int64_t ldh = parts * g.Dp, ldg = (int64_t)parts * z.piece;
+  const bf16_t* W = g.W + (g.w_piece ? 0 : z.class0 * g.ldw);
+  const bf16_t* opA = MODE == XG_DW ? g.H : W;
+  const bf16_t* opB = LOGITS ? g.H : g.G;
+  const int64_t lda = MODE == XG_DW ? ldh : g.ldw, ldb = LOGITS ? ldh : ldg;
+  const int64_t a_part = g.Dp, b_part = LOGITS ? g.Dp : z.piece;
+  // the rows of W end inside the last stage of dH
+  const int a_rows = MODE == XG_DH && !g.w_piece ? z.K : 0;
 
   XentOperand<BT, C::WM, C::NW, ATR> A;
   XentOperand<BT, C::WN, C::NW, BTR> B;
-  A.setup(g.lda, ATR ? g.a_cols - m0 : g.M - m0, wave, wm, lane, 0);
-  B.setup(g.ldb, BTR ? g.b_cols - n0 : N - n0, wave, wn, lane, BT * 128);
-  const int64_t a_step = ATR ? g.lda * 128 : 128, b_step = BTR ? g.ldb * 128 : 128;
-  const char* a_base = (const char*)g.A + (ATR ? (int64_t)m0 * 2 : (int64_t)m0 * g.lda * 2) + k_first * a_step;
-  const char* b_base = (const char*)g.B + (BTR ? (int64_t)n0 * 2 : (int64_t)n0 * g.ldb * 2) + k_first * b_step;
+  A.setup(lda, ATR ? (int)g.Dp - m0 : M - m0, wave, wm, lane, 0);
+  B.setup(ldb, BTR ? z.piece - n0 : N - n0, wave, wn, lane, BT * 128);
+  const int64_t a_step = ATR ? lda * 128 : 128, b_step = BTR ? ldb * 128 : 128;
+  const char* a_base = (const char*)opA + (ATR ? (int64_t)m0 * 2 : (int64_t)m0 * lda * 2) + k_first * a_step;
+  const char* b_base = (const char*)opB + (BTR ? (int64_t)n0 * 2 : (int64_t)n0 * ldb * 2) + k_first * b_step;
   // the copy stream: stage, its place in its segment, its sources
   int c_seg = 0, c_kt = 0;
   auto seg_a = [&](int s) { return (int)((0x001102u >> (4 * (g.segments == 6 ? s : 5))) & 15u); };
   auto seg_b = [&](int s) { return (int)((0x010120u >> (4 * (g.segments == 6 ? s : 5))) & 15u); };
-  const char* a_src = a_base + (int64_t)seg_a(0) * g.a_part * 2;
-  const char* b_src = b_base + (int64_t)seg_b(0) * g.b_part * 2;
+  const char* a_src = a_base + (int64_t)seg_a(0) * a_part * 2;
+  const char* b_src = b_base + (int64_t)seg_b(0) * b_part * 2;
   auto next_stage = [&]() {
     if (++c_kt == per_seg) {
       c_kt = 0;
       ++c_seg;
-      a_src = a_base + (int64_t)seg_a(c_seg) * g.a_part * 2;
-      b_src = b_base + (int64_t)seg_b(c_seg) * g.b_part * 2;
+      a_src = a_base + (int64_t)seg_a(c_seg) * a_part * 2;
+      b_src = b_base + (int64_t)seg_b(c_seg) * b_part * 2;
     } else {
       a_src += a_step;
       b_src += b_step;
@@ -234,7 +288,7 @@ __global__ __launch_bounds__(XentCfg<BT>::NW * 64) void k_xent_gemm(const XentGe
 #pragma unroll
     for (int t = t0; t < t1; ++t) {
       if (t < AG) {
-        if constexpr (decltype(lastc)::value) A.copy_last(a_src, l, wave, lane, t, g.lda, g.a_rows - (k_end - 1) * 64);
+        if constexpr (decltype(lastc)::value) A.copy_last(a_src, l, wave, lane, t, lda, a_rows - (k_end - 1) * 64);
         else A.copy(a_src, l, wave, t);
       } else {
         B.copy(b_src, l + BT * 128, wave, t - AG);
@@ -244,7 +298,7 @@ __global__ __launch_bounds__(XentCfg<BT>::NW * 64) void k_xent_gemm(const XentGe
   using Last = std::integral_constant<bool, true>;
   using Whole = std::integral_constant<bool, false>;
   // the last stage of a TR A whose rows end inside it is copied apart
-  const int nfull = ATR && g.a_rows && k_end == nks && (g.a_rows & 63) ? nstage - 1 : nstage;
+  const int nfull = a_rows && k_end == nks && (a_rows & 63) ? nstage - 1 : nstage;
 
   floatx16_t acc[C::TM][C::TN];
 #pragma unroll
@@ -299,6 +353,36 @@ __global__ __launch_bounds__(XentCfg<BT>::NW * 64) void k_xent_gemm(const XentGe
     }
   };
 
+  if constexpr (C::NST > 2) {
+    // Few matrix instructions a stage: the copies of two stages and more stay in flight across a stage's barrier, behind which those of
+    // the stage NST - 1 further on go into the buffer that everybody has read.
+    auto issue_stage = [&](int s, int buf) {
+      if (s < nfull) issue(Whole{}, buf, 0, LPS);
+      else issue(Last{}, buf, 0, LPS);
+      next_stage();
+    };
+#pragma unroll
+    for (int s = 0; s < C::NST - 1; ++s)
+      if (s < nstage) issue_stage(s, s);
+    for (int s = 0; s < nstage; ++s) {
+      if (s + C::NST - 2 < nstage) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((C::NST - 2) * LPS) : "memory");
+      else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      __builtin_amdgcn_sched_barrier(0);
+      if (s + C::NST - 1 < nstage) issue_stage(s + C::NST - 1, (s + C::NST - 1) % C::NST);
+      const char* at = smem + (s % C::NST) * C::STAGE;
+#pragma unroll
+      for (int sub = 0; sub < 4; ++sub) {
+#pragma unroll
+        for (int r = 0; r < RBR; ++r) B.read(at, sub, r, bf[sub & 1]);
+#pragma unroll
+        for (int r = 0; r < RA; ++r) A.read(at, sub, r, af[sub & 1]);
+        mfma_all(sub & 1);
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  } else
   // On entry to stage s the first H0 copies of stage s + 1 are under way if and only if s + 1 < nfull.
   if (nstage > 0) {
     if (nfull > 0) issue(Whole{}, 0, 0, LPS);
@@ -352,7 +436,7 @@ __global__ __launch_bounds__(XentCfg<BT>::NW * 64) void k_xent_gemm(const XentGe
   if constexpr (MODE == XG_LSE) {
     // largest logit and sum of exponentials of the tile's classes, for every token; the tile's wavefronts join theirs in LDS
     float2* red = reinterpret_cast<float2*>(smem);    // [WGM][BT]
-    const bool edge = m0 + BT > g.M;
+    const bool edge = m0 + BT > M;
 #pragma unroll
     for (int j = 0; j < C::TN; ++j) {
       const int n = nw + 32 * j;
@@ -361,7 +445,7 @@ __global__ __launch_bounds__(XentCfg<BT>::NW * 64) void k_xent_gemm(const XentGe
       for (int i = 0; i < C::TM; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          if (edge && m_of(i, r) >= g.M) acc[i][j][r] = -INFINITY;
+          if (edge && m_of(i, r) >= M) acc[i][j][r] = -INFINITY;
           top = fmaxf(top, acc[i][j][r]);
         }
       top = fmaxf(top, __shfl_xor(top, 32));
@@ -374,7 +458,7 @@ __global__ __launch_bounds__(XentCfg<BT>::NW * 64) void k_xent_gemm(const XentGe
         for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f((acc[i][j][r] - base) * 1.4426950408889634f);
       sum += __shfl_xor(sum, 32);
       if (fh == 0) red[wm * BT + wn * C::WN + 32 * j + fr] = make_float2(top, sum);
-      const int rel = n < N ? g.target[n] - g.class0 - m0 - wm * C::WM : -1;   // row of the wavefront's tile that is the class
+      const int rel = n < N ? g.target[n] - (int)z.class0 - m0 - wm * C::WM : -1;   // row of the wavefront's tile that is the class
       if (__any(rel >= 0 && rel < C::WM)) {
         const int mine = rel - 4 * fh;
 #pragma unroll
@@ -391,7 +475,7 @@ __global__ __launch_bounds__(XentCfg<BT>::NW * 64) void k_xent_gemm(const XentGe
       const float top = fmaxf(a.x, b.x), base = top == -INFINITY ? 0.0f : top;
       a.y = a.y * __builtin_amdgcn_exp2f((a.x - base) * 1.4426950408889634f) + b.y * __builtin_amdgcn_exp2f((b.x - base) * 1.4426950408889634f);
       a.x = top;
-      g.part[(int64_t)(g.class0 / BT + tm) * g.slots + n0 + tid] = a;
+      g.part[(z.class0 / BT + tm) * g.slots + n0 + tid] = a;
     }
   } else {
     // a wavefront's results as rows of WM values in LDS, from where they leave 16 bytes a lane
@@ -403,12 +487,13 @@ __global__ __launch_bounds__(XentCfg<BT>::NW * 64) void k_xent_gemm(const XentGe
     };
     if constexpr (MODE == XG_GRAD) {
       // G = (softmax - [class of the token]) scale; zero outside the classes and behind the last token
+      const float count = g.mean ? (float)valid : 1.0f;
 #pragma unroll
       for (int j = 0; j < C::TN; ++j) {
         const int n = nw + 32 * j;
         const bool in = n < N;
-        const float lse = in ? g.lse[n] : 0.0f, scale = in ? g.scale[n] : 0.0f;
-        const int rel = in ? g.target[n] - g.class0 : -1;
+        const float lse = in ? g.lse[n] : 0.0f, scale = in ? g.scale[n] / count : 0.0f;
+        const int rel = in ? g.target[n] - (int)z.class0 : -1;
 #pragma unroll
         for (int i = 0; i < C::TM; ++i)
 #pragma unroll
@@ -416,10 +501,9 @@ __global__ __launch_bounds__(XentCfg<BT>::NW * 64) void k_xent_gemm(const XentGe
             const int m = m_of(i, r);
             float p = __builtin_amdgcn_exp2f((acc[i][j][r] - lse) * 1.4426950408889634f);
             p = (m == rel ? p - 1.0f : p) * scale;
-            acc[i][j][r] = in && m < g.M ? p : 0.0f;
+            acc[i][j][r] = in && m < M ? p : 0.0f;
           }
       }
-      const int parts = g.segments == 6 ? 3 : 1;
       for (int part = 0; part < parts; ++part) {
 #pragma unroll
         for (int j = 0; j < C::TN; ++j)
@@ -441,32 +525,36 @@ __global__ __launch_bounds__(XentCfg<BT>::NW * 64) void k_xent_gemm(const XentGe
         for (int r0 = 0; r0 < C::WN; r0 += RPI) {
           const int r = r0 + lane / CPR, c = lane % CPR;
           const uint4 v = *reinterpret_cast<const uint4*>(tile + r * C::OUT_PITCH + c * 16);
-          bf16_t* to = g.grad + ((int64_t)(n0 + wn * C::WN + r) * parts + part) * g.grad_pitch + m0 + wm * C::WM + c * 8;
+          bf16_t* to = g.G + (n0 + wn * C::WN + r) * ldg + (int64_t)part * z.piece + m0 + wm * C::WM + c * 8;
           *reinterpret_cast<uint4*>(to) = v;
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       }
     } else {
-      float* part = g.acc + (int64_t)slice * N * g.M;
-      const bool to_acc = g.acc_write || nslice > 1;
-      if (g.acc_add || to_acc || g.out_dtype == EFQAT_F32) {
+      // dH: the pieces are added up in acc, the last one leaves for the output.  Slices leave for acc in any case, and are joined later.
+      float* part = g.acc + (int64_t)slice * N * M;
+      const bool add = MODE == XG_DH && g.piece > 0;
+      const bool to_acc = nslice > 1 || (MODE == XG_DH && z.class0 + z.piece < g.pieces.V);
+      char* const out = (char*)g.out + (MODE == XG_DW ? z.class0 * g.ldo * (g.out_dtype == EFQAT_F32 ? 4 : 2) : 0);
+      auto row_of = [&](int n) -> int64_t { return MODE == XG_DH ? g.rows[n] : n; };
+      if (add || to_acc || g.out_dtype == EFQAT_F32) {
 #pragma unroll
         for (int j = 0; j < C::TN; ++j) {
           const int n = nw + 32 * j;
           if (n >= N) continue;
-          const int64_t row = to_acc ? n : g.rows ? g.rows[n] : n;
+          const int64_t row = to_acc ? n : row_of(n);
 #pragma unroll
           for (int i = 0; i < C::TM; ++i)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-              const int m = m_of(i, 4 * q), left = g.M - m;
+              const int m = m_of(i, 4 * q), left = M - m;
               if (left <= 0) continue;
               float v[4];
               typedef float vec __attribute__((ext_vector_type(4), aligned(4)));
 #pragma unroll
               for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * q + e];
-              if (g.acc_add) {
-                const float* from = part + (int64_t)n * g.M + m;
+              if (add) {
+                const float* from = part + (int64_t)n * M + m;
                 if (left >= 4) {
                   const vec o = *reinterpret_cast<const vec*>(from);
 #pragma unroll
@@ -478,7 +566,7 @@ __global__ __launch_bounds__(XentCfg<BT>::NW * 64) void k_xent_gemm(const XentGe
                 }
               }
               if (to_acc || g.out_dtype == EFQAT_F32) {
-                float* to = to_acc ? part + row * g.M + m : (float*)g.out + row * g.ldo + m;
+                float* to = to_acc ? part + row * M + m : (float*)out + row * g.ldo + m;
                 if (left >= 4) {
                   vec o;
 #pragma unroll
@@ -490,7 +578,7 @@ __global__ __launch_bounds__(XentCfg<BT>::NW * 64) void k_xent_gemm(const XentGe
                     if (e < left) to[e] = v[e];
                 }
               } else {
-                bf16_t* to = (bf16_t*)g.out + row * g.ldo + m;
+                bf16_t* to = (bf16_t*)out + row * g.ldo + m;
                 typedef uint32_t pair __attribute__((ext_vector_type(2), aligned(2)));
                 if (left >= 4) {
                   *reinterpret_cast<pair*>(to) = pair{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
@@ -515,9 +603,9 @@ __global__ __launch_bounds__(XentCfg<BT>::NW * 64) void k_xent_gemm(const XentGe
           const int r = r0 + lane / CPR, c = lane % CPR;
           const int n = n0 + wn * C::WN + r, m = m0 + wm * C::WM + c * 8;
           const uint4 v = *reinterpret_cast<const uint4*>(tile + r * C::OUT_PITCH + c * 16);
-          const int left = n < N ? g.M - m : 0;
+          const int left = n < N ? M - m : 0;
           if (left > 0) {
-            bf16_t* to = (bf16_t*)g.out + (int64_t)(g.rows ? g.rows[n] : n) * g.ldo + m;
+            bf16_t* to = (bf16_t*)out + row_of(n) * g.ldo + m;
             if (left >= 8) {
               Raw8<bf16_t> o;
               o.a[0] = v.x; o.a[1] = v.y; o.a[2] = v.z; o.a[3] = v.w;

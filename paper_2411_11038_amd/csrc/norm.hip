@@ -7,7 +7,7 @@
 // variance from the differences to the mean, so that an offset of the row costs no digits - and its outputs leave from there.
 // A block keeps its columns' parameters and, backward, their sums over all its rows in registers; the rows that come next are
 // requested before the present ones are worked on.  The sums of the blocks are added in a second pass, in a fixed order.
-// Rows longer than the registers hold (kNormMaxCols, kNormBwdMaxCols) are read again for every step.
+// Rows longer than the registers hold (kNormMaxCols, kNormBwdMaxCols), and shorter than a chunk, are read again for every step.
 #include "rows.hpp"
 
 #include <algorithm>
@@ -29,9 +29,10 @@ struct RowSum {
   static constexpr int WPR = TPR / 64, WAVES = THREADS / 64;
   float2 (*buf)[WAVES];
   int turn = 0;
+  __device__ __forceinline__ float operator()(float a) { return (*this)(a, 0.0f).x; }
   __device__ __forceinline__ float2 operator()(float a, float b) {
-    a = wave_sum(a);
-    b = wave_sum(b);
+    a = wave_total(a);
+    b = wave_total(b);
     if constexpr (WPR == 1) return make_float2(a, b);
     const int wave = threadIdx.x >> 6;
     if ((threadIdx.x & 63) == 0) buf[turn][wave] = make_float2(a, b);
@@ -48,6 +49,14 @@ struct RowSum {
     return s;
   }
 };
+
+// From the sums of d = x - mean and of d^2: what the mean has lost to rounding is put back (the sum of d is not quite zero), and what
+// that adds to the squares taken off.
+__device__ __forceinline__ float norm_rstd(float2 sums, float inv_cols, float eps, float* mean) {
+  const float more = sums.x * inv_cols;
+  *mean += more;
+  return 1.0f / sqrtf(fmaxf(fmaf(sums.y, inv_cols, -more * more), 0.0f) + eps);
+}
 
 struct NormFwdArgs {
   const void* x;
@@ -69,54 +78,62 @@ __device__ __forceinline__ void load_param(const float* p, float dflt, int64_t c
   }
 }
 
+// the same for rows that are read without a branch
+__device__ __forceinline__ void load_param(const float* p, float dflt, const ChunkPlace& at, float (&v)[8]) {
+  if (p) {
+    Raw8<float> r;
+    r.load(p + at.at);
+    get_chunk(r, at, v);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = dflt;
+  }
+}
+
 template <typename T, int THREADS, int TPR, int NIT, bool KEEP>
 __global__ __launch_bounds__(THREADS) void k_norm_fwd(const NormFwdArgs g) {
   constexpr int RPB = THREADS / TPR;
   __shared__ float2 sums[2][THREADS / 64];
   RowSum<THREADS, TPR> row_sum{sums};
   const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
-  int n[NIT];
-  int64_t col[NIT];
+  ChunkPlace at[NIT];
   float w[NIT][8], b[NIT][8];
 #pragma unroll
-  for (int i = 0; i < NIT; ++i) {
-    col[i] = (int64_t)(i * TPR + t) * 8;
-    n[i] = chunk_len(g.cols, col[i]);
-  }
+  for (int i = 0; i < NIT; ++i) at[i] = ChunkPlace(g.cols, (i * TPR + t) * 8);
   const int64_t step = (int64_t)gridDim.x * RPB;
   int64_t row = (int64_t)blockIdx.x * RPB + sub;
   const float inv_cols = 1.0f / (float)g.cols;
   Raw8<T> next[NIT];
   auto request = [&](int64_t r) {
 #pragma unroll
-    for (int i = 0; i < NIT; ++i) next[i] = load_chunk((const T*)g.x + r * g.ldx + col[i], r < g.rows ? n[i] : 0);
+    for (int i = 0; i < NIT; ++i) next[i].load((const T*)g.x + (r < g.rows ? r : g.rows - 1) * g.ldx + at[i].at);
   };
   request(row);
 #pragma unroll
   for (int i = 0; i < NIT; ++i) {
-    load_param(g.w, 1.0f, col[i], n[i], w[i]);
-    load_param(g.b, 0.0f, col[i], n[i], b[i]);
+    load_param(g.w, 1.0f, at[i], w[i]);
+    load_param(g.b, 0.0f, at[i], b[i]);
   }
   for (int64_t base = (int64_t)blockIdx.x * RPB; base < g.rows; base += step, row += step) {
     float v[NIT][8];
 #pragma unroll
-    for (int i = 0; i < NIT; ++i) next[i].get(v[i]);
+    for (int i = 0; i < NIT; ++i) get_chunk(next[i], at[i], v[i]);
     request(row + step);
     float s = 0.0f;
 #pragma unroll
     for (int i = 0; i < NIT; ++i)
 #pragma unroll
       for (int j = 0; j < 8; ++j) s += v[i][j];
-    const float mean = row_sum(s, 0.0f).x * inv_cols;
-    float q = 0.0f;
+    float mean = row_sum(s) * inv_cols, q = 0.0f, rest = 0.0f;
 #pragma unroll
     for (int i = 0; i < NIT; ++i)
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float d = j < n[i] ? v[i][j] - mean : 0.0f;
+        const float d = j < at[i].n ? v[i][j] - mean : 0.0f;
+        rest += d;
         q = fmaf(d, d, q);
       }
-    const float rstd = 1.0f / sqrtf(fmaf(row_sum(q, 0.0f).x, inv_cols, g.eps));
+    const float rstd = norm_rstd(row_sum(rest, q), inv_cols, g.eps, &mean);
     if (row >= g.rows) continue;                      // the whole wavefront: its lanes are of one row
     if (t == 0) {
       if (g.mean) g.mean[row] = mean;
@@ -127,12 +144,13 @@ __global__ __launch_bounds__(THREADS) void k_norm_fwd(const NormFwdArgs g) {
       float o[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) o[j] = fmaf((v[i][j] - mean) * rstd, w[i][j], b[i][j]);
-      store_chunk((T*)g.y + row * g.ldy + col[i], n[i], o);
+      const int col = (i * TPR + t) * 8;
+      store_chunk((T*)g.y + row * g.ldy + col, at[i].n, o);
       if constexpr (KEEP) {
         float scale;
         const uint2 c = ckpt_encode(v[i], &scale);
-        if (col[i] < ckpt_pitch(g.cols)) *reinterpret_cast<uint2*>(g.codes + row * ckpt_pitch(g.cols) + col[i]) = c;
-        if ((t & (kGroupLanes - 1)) == 0 && col[i] < g.cols) g.scales[row * ckpt_groups(g.cols) + col[i] / kCkptGroup] = scale;
+        if (col < ckpt_pitch(g.cols)) *reinterpret_cast<uint2*>(g.codes + row * ckpt_pitch(g.cols) + col) = c;
+        if ((t & (kGroupLanes - 1)) == 0 && col < g.cols) g.scales[row * ckpt_groups(g.cols) + col / kCkptGroup] = scale;
       }
     }
   }
@@ -154,7 +172,7 @@ __global__ __launch_bounds__(1024) void k_norm_fwd_long(const NormFwdArgs g) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) s += v[j];
     }
-    const float mean = row_sum(s, 0.0f).x * inv_cols;
+    float mean = row_sum(s) * inv_cols, rest = 0.0f;
     for (int64_t c = threadIdx.x * 8; c < g.cols; c += 8192) {
       const int n = chunk_len(g.cols, c);
       float v[8];
@@ -162,10 +180,11 @@ __global__ __launch_bounds__(1024) void k_norm_fwd_long(const NormFwdArgs g) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float d = j < n ? v[j] - mean : 0.0f;
+        rest += d;
         q = fmaf(d, d, q);
       }
     }
-    const float rstd = 1.0f / sqrtf(fmaf(row_sum(q, 0.0f).x, inv_cols, g.eps));
+    const float rstd = norm_rstd(row_sum(rest, q), inv_cols, g.eps, &mean);
     if (threadIdx.x == 0) {
       if (g.mean) g.mean[row] = mean;
       if (g.rstd) g.rstd[row] = rstd;
@@ -223,22 +242,34 @@ struct InputChunk {
     if constexpr (CKPT) ckpt_decode(q, scale, v);
     else raw.get(v);
   }
+  // without a branch, in rows of 8 columns and more (codes behind the columns are zeros)
+  __device__ __forceinline__ void request(const NormBwdArgs& g, int64_t row, int64_t col, const ChunkPlace& at) {
+    if constexpr (CKPT) {
+      const int64_t pitch = ckpt_pitch(g.cols), groups = ckpt_groups(g.cols);
+      q = *reinterpret_cast<const uint2*>(g.codes + row * pitch + (col < pitch ? col : pitch - 8));
+      scale = g.scales[row * groups + (col < g.cols ? col / kCkptGroup : groups - 1)];
+    } else {
+      raw.load((const T*)g.x + row * g.ldx + at.at);
+    }
+  }
+  __device__ __forceinline__ void get(const ChunkPlace& at, float (&v)[8]) const {
+    if constexpr (CKPT) ckpt_decode(q, scale, v);
+    else get_chunk(raw, at, v);
+  }
 };
 
 template <typename T, bool CKPT, int THREADS, int TPR, int NIT>
-__global__ __launch_bounds__(THREADS) void k_norm_bwd(const NormBwdArgs g) {
+__global__ __launch_bounds__(THREADS, 4) void k_norm_bwd(const NormBwdArgs g) {
   constexpr int RPB = THREADS / TPR;
   __shared__ float2 sums[2][THREADS / 64];
   __shared__ float red[RPB > 1 ? THREADS * 16 : 1];
   RowSum<THREADS, TPR> row_sum{sums};
   const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
-  int n[NIT];
-  int64_t col[NIT];
+  ChunkPlace at[NIT];
   float w[NIT][8], aw[NIT][8], ab[NIT][8];
 #pragma unroll
   for (int i = 0; i < NIT; ++i) {
-    col[i] = (int64_t)(i * TPR + t) * 8;
-    n[i] = chunk_len(g.cols, col[i]);
+    at[i] = ChunkPlace(g.cols, (i * TPR + t) * 8);
 #pragma unroll
     for (int j = 0; j < 8; ++j) aw[i][j] = ab[i][j] = 0.0f;
   }
@@ -249,27 +280,34 @@ __global__ __launch_bounds__(THREADS) void k_norm_bwd(const NormBwdArgs g) {
   InputChunk<T, CKPT> next_x[NIT];
   float next_mean = 0.0f, next_rstd = 0.0f;
   auto request = [&](int64_t r) {
-    const bool in = r < g.rows;
+    r = r < g.rows ? r : g.rows - 1;
 #pragma unroll
     for (int i = 0; i < NIT; ++i) {
-      next_dy[i] = load_chunk((const T*)g.dy + r * g.lddy + col[i], in ? n[i] : 0);
-      next_x[i].request(g, r, col[i], in ? n[i] : 0);
+      next_dy[i].load((const T*)g.dy + r * g.lddy + at[i].at);
+      next_x[i].request(g, r, (i * TPR + t) * 8, at[i]);
     }
-    next_mean = in ? g.mean[r] : 0.0f;
-    next_rstd = in ? g.rstd[r] : 0.0f;
+    next_mean = g.mean[r];
+    next_rstd = g.rstd[r];
   };
   request(row);
 #pragma unroll
-  for (int i = 0; i < NIT; ++i) load_param(g.w, 1.0f, col[i], n[i], w[i]);
+  for (int i = 0; i < NIT; ++i) load_param(g.w, 1.0f, at[i], w[i]);
   for (int64_t base = (int64_t)blockIdx.x * RPB; base < g.rows; base += step, row += step) {
     float d[NIT][8], xh[NIT][8];
-    const float mean = next_mean, rstd = next_rstd;
+    const bool in = row < g.rows;
+    const float mean = in ? next_mean : 0.0f, rstd = in ? next_rstd : 0.0f;
 #pragma unroll
     for (int i = 0; i < NIT; ++i) {
-      next_dy[i].get(d[i]);
-      next_x[i].get(xh[i]);
+      get_chunk(next_dy[i], at[i], d[i]);
+      next_x[i].get(at[i], xh[i]);
     }
     request(row + step);
+    if (!in) {                                        // nothing of a row that does not exist is summed
+#pragma unroll
+      for (int i = 0; i < NIT; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) d[i][j] = xh[i][j] = 0.0f;
+    }
     float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
     for (int i = 0; i < NIT; ++i)
@@ -284,12 +322,12 @@ __global__ __launch_bounds__(THREADS) void k_norm_bwd(const NormBwdArgs g) {
       }
     const float2 s = row_sum(s1, s2);
     const float m1 = s.x * inv_cols, m2 = s.y * inv_cols;
-    if (row >= g.rows) continue;                      // the whole wavefront: its lanes are of one row
+    if (!in) continue;                                // the whole wavefront: its lanes are of one row
 #pragma unroll
     for (int i = 0; i < NIT; ++i) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) d[i][j] = (d[i][j] - m1 - xh[i][j] * m2) * rstd;
-      store_chunk((T*)g.dx + row * g.lddx + col[i], n[i], d[i]);
+      store_chunk((T*)g.dx + row * g.lddx + (i * TPR + t) * 8, at[i].n, d[i]);
     }
   }
   if (!g.dw && !g.db) return;
@@ -322,8 +360,8 @@ __global__ __launch_bounds__(THREADS) void k_norm_bwd(const NormBwdArgs g) {
       }
     }
     if (sub == 0) {
-      if (ow) store_chunk(ow + col[i], n[i], aw[i]);
-      if (ob) store_chunk(ob + col[i], n[i], ab[i]);
+      if (ow) store_chunk(ow + (i * TPR + t) * 8, at[i].n, aw[i]);
+      if (ob) store_chunk(ob + (i * TPR + t) * 8, at[i].n, ab[i]);
     }
   }
 }
@@ -366,22 +404,37 @@ __global__ __launch_bounds__(256) void k_norm_bwd_long_cols(const NormBwdArgs g)
   load_param(g.w, 1.0f, c, n, w);
 #pragma unroll
   for (int j = 0; j < 8; ++j) aw[j] = ab[j] = 0.0f;
-  for (int64_t row = blockIdx.y; row < g.rows; row += gridDim.y) {
-    const float mean = g.mean[row], rstd = g.rstd[row];
-    const float2 m = g.row_sums[row];
-    InputChunk<T, CKPT> in;
-    float d[8], x[8];
-    in.request(g, row, c, n);
-    load_chunk((const T*)g.dy + row * g.lddy + c, n).get(d);
-    in.get(x);
+  constexpr int NR = 4;                               // rows whose loads are in flight together
+  for (int64_t r0 = blockIdx.y; r0 < g.rows; r0 += NR * (int64_t)gridDim.y) {
+    InputChunk<T, CKPT> in[NR];
+    Raw8<T> dy[NR];
+    float mean[NR], rstd[NR];
+    float2 m[NR];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float xh = (x[j] - mean) * rstd;
-      aw[j] = fmaf(d[j], xh, aw[j]);
-      ab[j] += d[j];
-      d[j] = (d[j] * w[j] - m.x - xh * m.y) * rstd;
+    for (int u = 0; u < NR; ++u) {
+      const int64_t next = r0 + u * (int64_t)gridDim.y, row = next < g.rows ? next : r0;
+      in[u].request(g, row, c, n);
+      dy[u] = load_chunk((const T*)g.dy + row * g.lddy + c, n);
+      mean[u] = g.mean[row];
+      rstd[u] = g.rstd[row];
+      m[u] = g.row_sums[row];
     }
-    store_chunk((T*)g.dx + row * g.lddx + c, n, d);
+#pragma unroll
+    for (int u = 0; u < NR; ++u) {
+      const int64_t row = r0 + u * (int64_t)gridDim.y;
+      if (row >= g.rows) break;
+      float d[8], x[8];
+      dy[u].get(d);
+      in[u].get(x);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float xh = (x[j] - mean[u]) * rstd[u];
+        aw[j] = fmaf(d[j], xh, aw[j]);
+        ab[j] += d[j];
+        d[j] = (d[j] * w[j] - m[u].x - xh * m[u].y) * rstd[u];
+      }
+      store_chunk((T*)g.dx + row * g.lddx + c, n, d);
+    }
   }
   if (!g.dw && !g.db) return;
   float* ow = gridDim.y == 1 ? g.dw : g.part + (int64_t)blockIdx.y * 2 * g.cols;
@@ -390,78 +443,86 @@ __global__ __launch_bounds__(256) void k_norm_bwd_long_cols(const NormBwdArgs g)
   if (ob) store_chunk(ob + c, n, ab);
 }
 
-// The blocks' sums, 64 columns a block (of the 2 cols that dw and db have together), dealt to 16 groups of lanes whose sums
-// are added in double precision in a fixed order.
+// The blocks' sums, 32 columns a block (of the 2 cols that dw and db have together), dealt to 32 groups of lanes whose sums are added in
+// double precision in a fixed order.
 __global__ __launch_bounds__(1024) void k_norm_finish(const float* __restrict__ part, int nblk, int64_t cols, float* __restrict__ dw,
                                                       float* __restrict__ db) {
-  __shared__ double red[16][64];
-  const int lane = threadIdx.x & 63, grp = threadIdx.x >> 6;
-  const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+  __shared__ double red[32][33];
+  const int lane = threadIdx.x & 31, grp = threadIdx.x >> 5;
+  const int64_t c = (int64_t)blockIdx.x * 32 + lane;
   double s = 0.0;
   if (c < 2 * cols) {
-    int i = grp;
-    for (; i + 112 < nblk; i += 128) {                // eight independent loads in flight
-      float v[8];
+    for (int i = grp; i < nblk; i += 512) {           // sixteen independent loads in flight
+      float v[16];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) v[u] = part[(int64_t)(i + 16 * u) * 2 * cols + c];
+      for (int u = 0; u < 16; ++u) v[u] = part[(int64_t)(i + 32 * u < nblk ? i + 32 * u : nblk - 1) * 2 * cols + c];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) s += (double)v[u];
+      for (int u = 0; u < 16; ++u) s += i + 32 * u < nblk ? (double)v[u] : 0.0;
     }
-    for (; i < nblk; i += 16) s += (double)part[(int64_t)i * 2 * cols + c];
   }
   red[grp][lane] = s;
   __syncthreads();
-  if (grp == 0 && c < 2 * cols) {
+  // 32 lanes take a column each: the groups of a column pairwise, by the lanes of half a wavefront
+  double t = red[lane][grp];                          // column grp, group lane
 #pragma unroll
-    for (int i = 1; i < 16; ++i) s += red[i][lane];
-    float* out = c < cols ? dw : db;
-    if (out) out[c < cols ? c : c - cols] = (float)s;
+  for (int o = 16; o > 0; o >>= 1) t += __shfl_xor(t, o, 32);
+  const int64_t k = (int64_t)blockIdx.x * 32 + grp;
+  if (lane == 0 && k < 2 * cols) {
+    float* out = k < cols ? dw : db;
+    if (out) out[k < cols ? k : k - cols] = (float)t;
   }
 }
 
-// Blocks of the backward pass: two a CU (rows are walked by a block, whose sums over them are one partial result), fewer where
-// there are fewer rows than that.
-static int64_t norm_rows_per_block(int64_t cols) { return cols <= 1024 ? 8 : cols <= 2048 ? 4 : cols <= 4096 ? 2 : 1; }
-static int64_t norm_bwd_blocks(int64_t rows, int64_t cols) {
-  if (cols > kNormBwdMaxCols) return std::min<int64_t>(rows, std::max<int64_t>(1, 1024 / ceil_div(cols, kNormLongCols)));
-  return std::min<int64_t>(ceil_div(rows, norm_rows_per_block(cols)), 512);
+// most blocks: `most`; every block walks as many rows as the others, or one step fewer
+static unsigned even_blocks(int64_t rows, int64_t rows_per_block, int64_t most) {
+  const int64_t steps = ceil_div(ceil_div(rows, rows_per_block), most);
+  return (unsigned)ceil_div(rows, rows_per_block * steps);
 }
 
+// Blocks of the backward pass: as many as the chip holds (two of 512 threads a CU, one of 1024; a block walks rows, and its sums over
+// them are one partial result), fewer where there are fewer rows than that.
+static int64_t norm_rows_per_block(int64_t cols) { return cols <= 512 ? 8 : cols <= 1024 ? 4 : cols <= 2048 ? 2 : 1; }
+static bool norm_bwd_long(int64_t cols) { return cols < 8 || cols > kNormBwdMaxCols; }
+static int64_t norm_bwd_blocks(int64_t rows, int64_t cols) {
+  // long rows: blocks of 2048 columns, 1024 in all; eight rows a block at least, whose sums cost a quarter of what the rows do
+  if (norm_bwd_long(cols)) return std::min<int64_t>(ceil_div(rows, 8), std::max<int64_t>(1, 1024 / ceil_div(cols, kNormLongCols)));
+  return even_blocks(rows, norm_rows_per_block(cols), cols <= 4096 ? 512 : 256);
+}
+
+// A row by TPR lanes of one chunk (NIT = 1) or two.  One chunk a lane is the shorter way of one row, two keep more bytes in flight and
+// need half of the wavefronts to talk to each other: one where the chip holds all rows' blocks at once (2048 threads a CU), else two in
+// blocks that walk the rows, all as many.  One against two, us: 16 x 768 bf16 3.22 / 3.63, 2049 x 777 4.59 / 4.92, 12288 x 768 11.7 /
+// 10.9, 8192 x 4096 23.0 / 22.1, 2048 x 8192 16.0 / 13.1 (buffers that the last-level cache holds).
 template <typename T, bool KEEP>
 static int launch_norm_fwd(const NormFwdArgs& g, hipStream_t st) {
   const int64_t cols = g.cols;
-  // blocks that the chip holds at once walk the rows
-#define EFQAT_NORM(THREADS, TPR, NIT)                                                                                             \
-  EFQAT_TRY(launch((k_norm_fwd<T, THREADS, TPR, NIT, KEEP>),                                                                    \
-                     dim3((unsigned)std::min<int64_t>(ceil_div(g.rows, (THREADS) / (TPR)), 256 * 2048 / (THREADS))), dim3(THREADS), \
-                     0, st, g))
+  if (cols < 8 || cols > kNormMaxCols) return launch((k_norm_fwd_long<T, KEEP>), dim3((unsigned)std::min<int64_t>(g.rows, 512)), dim3(1024), 0, st, g);
+#define EFQAT_NORM(THREADS, TPR, NIT) \
+  return launch((k_norm_fwd<T, THREADS, TPR, NIT, KEEP>), dim3(even_blocks(g.rows, (THREADS) / (TPR), 256 * (NIT == 1 ? 2048 : 1024) / (THREADS))), dim3(THREADS), 0, st, g)
+  auto at_once = [&](int threads, int tpr) { return ceil_div(g.rows, threads / tpr) <= 256 * 2048 / threads; };
   if (cols <= 512) EFQAT_NORM(256, 64, 1);
-  else if (cols <= 1024) EFQAT_NORM(256, 64, 2);
-  else if (cols <= 2048) EFQAT_NORM(256, 128, 2);
-  else if (cols <= 4096) EFQAT_NORM(256, 256, 2);
-  else if (cols <= 8192) EFQAT_NORM(512, 512, 2);
-  else if (cols <= kNormMaxCols) EFQAT_NORM(1024, 1024, 2);
-  else EFQAT_TRY(launch((k_norm_fwd_long<T, KEEP>), dim3((unsigned)std::min<int64_t>(g.rows, 512)), dim3(1024), 0, st, g));
+  if (cols <= 1024) { if (at_once(256, 128)) EFQAT_NORM(256, 128, 1); EFQAT_NORM(256, 64, 2); }
+  if (cols <= 2048) { if (at_once(256, 256)) EFQAT_NORM(256, 256, 1); EFQAT_NORM(256, 128, 2); }
+  if (cols <= 4096) { if (at_once(512, 512)) EFQAT_NORM(512, 512, 1); EFQAT_NORM(256, 256, 2); }
+  if (cols <= 8192) { if (at_once(1024, 1024)) EFQAT_NORM(1024, 1024, 1); EFQAT_NORM(512, 512, 2); }
+  EFQAT_NORM(1024, 1024, 2);
 #undef EFQAT_NORM
-  return EFQAT_OK;
 }
 
 template <typename T, bool CKPT>
 static int launch_norm_bwd(const NormBwdArgs& g, int64_t blocks, hipStream_t st) {
   const int64_t cols = g.cols;
-#define EFQAT_NORM(TPR, NIT) \
-  EFQAT_TRY(launch((k_norm_bwd<T, CKPT, 512, TPR, NIT>), dim3((unsigned)blocks), dim3(512), 0, st, g))
-  if (cols <= 512) EFQAT_NORM(64, 1);
-  else if (cols <= 1024) EFQAT_NORM(64, 2);
-  else if (cols <= 2048) EFQAT_NORM(128, 2);
-  else if (cols <= 4096) EFQAT_NORM(256, 2);
-  else if (cols <= kNormBwdMaxCols) EFQAT_NORM(512, 2);
-  else {
+  if (norm_bwd_long(cols)) {
     EFQAT_TRY(launch((k_norm_bwd_long_rows<T, CKPT>), dim3((unsigned)std::min<int64_t>(g.rows, 512)), dim3(1024), 0, st, g));
-    EFQAT_TRY(launch((k_norm_bwd_long_cols<T, CKPT>), dim3((unsigned)ceil_div(cols, kNormLongCols), (unsigned)blocks), dim3(256), 0, st, g));
+    return launch((k_norm_bwd_long_cols<T, CKPT>), dim3((unsigned)ceil_div(cols, kNormLongCols), (unsigned)blocks), dim3(256), 0, st, g);
   }
+#define EFQAT_NORM(THREADS, TPR) return launch((k_norm_bwd<T, CKPT, THREADS, TPR, 1>), dim3((unsigned)blocks), dim3(THREADS), 0, st, g)
+  if (cols <= 512) EFQAT_NORM(512, 64);
+  if (cols <= 1024) EFQAT_NORM(512, 128);
+  if (cols <= 2048) EFQAT_NORM(512, 256);
+  if (cols <= 4096) EFQAT_NORM(512, 512);
+  EFQAT_NORM(1024, 1024);
 #undef EFQAT_NORM
-  return EFQAT_OK;
 }
 
 }  // namespace efqat
@@ -489,7 +550,7 @@ extern "C" size_t efqat_layer_norm_bwd_workspace_bytes(int64_t rows, int64_t col
   if (rows <= 0 || cols <= 0 || cols > INT32_MAX) return 256;
   const int64_t blocks = norm_bwd_blocks(rows, cols);
   size_t need = blocks > 1 ? (size_t)round_up(blocks * 2 * cols * (int64_t)sizeof(float), 256) : 0;
-  if (cols > kNormBwdMaxCols) need += (size_t)round_up(rows * (int64_t)sizeof(float2), 256);
+  if (norm_bwd_long(cols)) need += (size_t)round_up(rows * (int64_t)sizeof(float2), 256);
   return std::max<size_t>(need, 256);
 }
 
@@ -508,13 +569,13 @@ extern "C" int efqat_layer_norm_bwd(const void* dy, int64_t lddy, int dtype, con
   const int64_t blocks = norm_bwd_blocks(rows, cols);
   WsCarver carve(ws);
   float* part = blocks > 1 ? (float*)carve.take((size_t)(blocks * 2 * cols) * sizeof(float)) : nullptr;
-  float2* row_sums = cols > kNormBwdMaxCols ? (float2*)carve.take((size_t)rows * sizeof(float2)) : nullptr;
+  float2* row_sums = norm_bwd_long(cols) ? (float2*)carve.take((size_t)rows * sizeof(float2)) : nullptr;
   const NormBwdArgs g = {dy, x, x_codes, x_scales, mean, rstd, weight, dx, part, dweight, dbias, row_sums, rows, cols, lddy, ldx, lddx};
   hipStream_t st = (hipStream_t)stream;
   EFQAT_TRY(dtype == EFQAT_F32 ? (ckpt ? launch_norm_bwd<float, true>(g, blocks, st) : launch_norm_bwd<float, false>(g, blocks, st))
                               : (ckpt ? launch_norm_bwd<bf16_t, true>(g, blocks, st) : launch_norm_bwd<bf16_t, false>(g, blocks, st)));
   if (blocks > 1 && (dweight || dbias)) {
-    EFQAT_TRY(launch(k_norm_finish, dim3((unsigned)ceil_div(2 * cols, 64)), dim3(1024), 0, st, part, (int)blocks, cols, dweight, dbias));
+    EFQAT_TRY(launch(k_norm_finish, dim3((unsigned)ceil_div(2 * cols, 32)), dim3(1024), 0, st, part, (int)blocks, cols, dweight, dbias));
   }
   return EFQAT_OK;
 }

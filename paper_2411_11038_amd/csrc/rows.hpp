@@ -89,6 +89,33 @@ __device__ __forceinline__ void store_chunk(T* p, int n, const float (&v)[8]) {
   }
 }
 
+// Place of a chunk in rows of cols >= 8 elements that are read without a branch: a chunk that passes the end is the row's last 8
+// elements, moved down by `shift` with zeros behind them; one that begins behind the end (shift 8) is zeros.
+struct ChunkPlace {
+  int at, shift, n;               // first element that is read; elements to move; elements that exist
+  __device__ __forceinline__ ChunkPlace() {}
+  __device__ __forceinline__ ChunkPlace(int64_t cols, int64_t col) {
+    const int64_t over = col + 8 - cols;
+    at = (int)(over > 0 ? cols - 8 : col);
+    shift = (int)(over < 0 ? 0 : over > 8 ? 8 : over);
+    n = 8 - shift;
+  }
+};
+// element j + shift in the place of element j
+__device__ __forceinline__ void move_down(float (&v)[8], int shift) {
+#pragma unroll
+  for (int s = 4; s > 0; s >>= 1)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = shift & s ? (j + s < 8 ? v[j + s < 8 ? j + s : 7] : 0.0f) : v[j];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = shift >= 8 ? 0.0f : v[j];
+}
+template <typename T>
+__device__ __forceinline__ void get_chunk(const Raw8<T>& r, const ChunkPlace& c, float (&v)[8]) {
+  r.get(v);
+  if (c.shift) move_down(v, c.shift);
+}
+
 // ---- the 8-bit checkpoint: bytes a row of codes takes, scales a row has
 __host__ __device__ inline int64_t ckpt_pitch(int64_t cols) { return round_up(cols, 16); }
 __host__ __device__ inline int64_t ckpt_groups(int64_t cols) { return ceil_div(cols, kCkptGroup); }
@@ -101,6 +128,18 @@ __device__ __forceinline__ uint32_t group_max(uint32_t v) {
   step(__builtin_amdgcn_update_dpp(0, v, 0x141, 0xF, 0xF, true));     // row_half_mirror: lane -> 7 - lane
   step(__builtin_amdgcn_update_dpp(0, v, 0x140, 0xF, 0xF, true));     // row_mirror: lane -> 15 - lane
   return v;
+}
+
+// the sum of a wavefront, in all its lanes: rows of 16 by DPP, the four rows through scalar registers, in a fixed order (a butterfly
+// over __shfl_xor goes through LDS six times)
+__device__ __forceinline__ float wave_total(float v) {
+  auto add = [&](int o) { v += __builtin_bit_cast(float, o); };
+  add(__builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0xB1, 0xF, 0xF, true));
+  add(__builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x4E, 0xF, 0xF, true));
+  add(__builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x141, 0xF, 0xF, true));
+  add(__builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x140, 0xF, 0xF, true));
+  auto row = [&](int lane) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane)); };
+  return (row(0) + row(16)) + (row(32) + row(48));
 }
 
 // Codes of a chunk and the scale of its group; all 16 lanes of the group take part (chunks without columns hold zeros).

@@ -27,62 +27,96 @@ struct XentRowsArgs {
   int reduction;
   float *slot_lse, *slot_scale;
 };
+// One block walks the tokens, 16 x 1024 a round.  A wavefront's 64 neighbouring tokens are counted by one ballot; the 256 counts of a
+// round are scanned by one wavefront, so that slots are in the order of the tokens and every access is of neighbours.
+constexpr int kXentHeld = 16;
 __global__ __launch_bounds__(1024) void k_xent_rows(const XentRowsArgs g) {
-  __shared__ int wave_count[16];
+  __shared__ int before[kXentHeld * 16];
+  __shared__ int round_total;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t per = (g.T + 1023) / 1024;
-  const int64_t t0 = threadIdx.x * per, t1 = t0 + per < g.T ? t0 + per : g.T;
-  auto has_class = [&](int64_t c) { return c >= 0 && c < g.V && c != g.ignore; };
-  int mine = 0;
-  for (int64_t t = t0; t < t1; ++t) mine += has_class(g.targets[t]) ? 1 : 0;
-  int before = mine;                                  // inclusive scan of the wavefront
+  int total = 0;
+  const float up = g.slot_scale && g.reduction != EFQAT_XENT_NONE && g.dloss ? g.dloss[0] : 1.0f;
+  const float* ups = g.reduction == EFQAT_XENT_NONE ? g.dloss : nullptr;
+  for (int64_t t0 = 0; t0 < g.T; t0 += kXentHeld * 1024) {
+    const int64_t t = t0 + threadIdx.x;
+    int64_t c[kXentHeld];
+    float lse[kXentHeld], scale[kXentHeld];
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int v = __shfl_up(before, o);
-    before += lane >= o ? v : 0;
-  }
-  if (lane == 63) wave_count[wave] = before;
-  __syncthreads();
-  int slot = before - mine, total = 0;
+    for (int i = 0; i < kXentHeld; ++i) c[i] = t + i * 1024 < g.T ? g.targets[t + i * 1024] : -1;
+    if (g.slot_scale) {
 #pragma unroll
-  for (int w = 0; w < 16; ++w) {
-    if (w < wave) slot += wave_count[w];
-    total += wave_count[w];
+      for (int i = 0; i < kXentHeld; ++i) {
+        const bool in = t + i * 1024 < g.T;
+        lse[i] = in ? g.lse_in[t + i * 1024] : 0.0f;
+        scale[i] = in && ups ? ups[t + i * 1024] : up;
+      }
+    }
+    uint64_t who[kXentHeld];
+#pragma unroll
+    for (int i = 0; i < kXentHeld; ++i) {
+      who[i] = __ballot(c[i] >= 0 && c[i] < g.V && c[i] != g.ignore);
+      if (lane == 0) before[i * 16 + wave] = __popcll(who[i]);
+    }
+    __syncthreads();
+    if (wave == 0) {
+      int n[4], mine = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        n[j] = before[4 * lane + j];
+        mine += n[j];
+      }
+      int sum = mine;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int v = __shfl_up(sum, o);
+        sum += lane >= o ? v : 0;
+      }
+      int at = sum - mine;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        before[4 * lane + j] = at;
+        at += n[j];
+      }
+      if (lane == 63) round_total = sum;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kXentHeld; ++i) {
+      const int64_t ti = t + i * 1024;
+      if (ti >= g.T) break;
+      if (who[i] >> lane & 1) {
+        const int slot = total + before[i * 16 + wave] + __popcll(who[i] & ((UINT64_C(1) << lane) - 1));
+        g.rows[slot] = (int32_t)ti;
+        g.target[slot] = (int32_t)c[i];
+        if (g.slot_scale) {
+          g.slot_lse[slot] = lse[i];
+          g.slot_scale[slot] = scale[i];
+        }
+      } else {
+        if (g.loss) g.loss[ti] = 0.0f;
+        if (g.lse) g.lse[ti] = 0.0f;
+      }
+    }
+    total += round_total;
+    __syncthreads();
   }
   if (threadIdx.x == 0) {
     g.n_valid[0] = total;
     if (g.n_out) g.n_out[0] = total;
   }
-  float scale = 1.0f;
-  if (g.slot_scale && g.reduction != EFQAT_XENT_NONE) {
-    scale = g.dloss ? g.dloss[0] : 1.0f;
-    if (g.reduction == EFQAT_XENT_MEAN) scale /= (float)total;
-  }
-  for (int64_t t = t0; t < t1; ++t) {
-    const int64_t c = g.targets[t];
-    if (has_class(c)) {
-      g.rows[slot] = (int32_t)t;
-      g.target[slot] = (int32_t)c;
-      if (g.slot_scale) {
-        g.slot_lse[slot] = g.lse_in[t];
-        g.slot_scale[slot] = g.reduction == EFQAT_XENT_NONE && g.dloss ? g.dloss[t] : scale;
-      }
-      ++slot;
-    } else {
-      if (g.loss) g.loss[t] = 0.0f;
-      if (g.lse) g.lse[t] = 0.0f;
-    }
-  }
 }
 
-// ---- operands in bf16, in rows of whole K stages: src rows (by rows[], those of the slots that exist) -> dst [row][PARTS][pitch],
-// zeros behind the columns and the rows.  Backward: rows of dh without a class are cleared on the way.
+// ---- operands in bf16, in rows of whole K stages -> dst [row][PARTS][pitch], zeros behind the columns and the rows.  Tokens: the rows
+// rows[] of the slots that exist, zeros in the others; backward, rows of dh without a class are cleared on the way.  Classes: those of
+// a piece, zeros up to whole stages.
 struct XentStageArgs {
   const void* src;
   int64_t ld;
   int64_t cols, pitch;                                // pitch: cols rounded up to 64
-  const int32_t *rows, *n_valid;                      // NULL: rows as they lie, n_rows of them
-  int64_t n_rows, dst_rows;
+  const int32_t *rows, *n_valid;                      // rows NULL: classes
+  XentPieces pieces;
+  int piece;
+  int64_t dst_rows;                                   // most rows of dst
   bf16_t* dst;
   const int64_t* targets;                             // with clear
   int64_t T, V, ignore;
@@ -91,15 +125,23 @@ struct XentStageArgs {
 };
 template <typename T, int PARTS>
 __global__ __launch_bounds__(256) void k_xent_stage(const XentStageArgs g) {
-  const int64_t n = g.n_valid ? g.n_valid[0] : g.n_rows;
+  const int valid = g.n_valid[0];
+  int64_t n = valid, first = 0, dst_rows = g.dst_rows;
+  if (!g.rows) {
+    const int64_t p = g.pieces.size(valid);
+    first = p * g.piece;
+    n = g.pieces.V - first < p ? g.pieces.V - first : p;
+    if (n <= 0) return;
+    dst_rows = (n + 63) / 64 * 64;
+  }
   // lanes of a row: as many as its chunks of 8 columns, up to a block
   const int chunks = (int)(g.pitch / 8);
   const int lanes = chunks >= 256 ? 256 : chunks > 64 ? 128 : chunks > 32 ? 64 : chunks > 16 ? 32 : chunks > 8 ? 16 : 8;
   const int64_t r = (int64_t)blockIdx.x * (256 / lanes) + threadIdx.x / lanes;
   const int lane = threadIdx.x % lanes;
-  if (r < g.dst_rows) {
+  if (r < dst_rows) {
     const bool in = r < n;
-    const T* src = (const T*)g.src + (in ? (g.rows ? (int64_t)g.rows[r] : r) : 0) * g.ld;
+    const T* src = (const T*)g.src + (in ? (g.rows ? (int64_t)g.rows[r] : first + r) : 0) * g.ld;
     bf16_t* dst = g.dst + r * PARTS * g.pitch;
     for (int c = lane; c < chunks; c += lanes) {
       const int64_t left = in ? g.cols - 8 * (int64_t)c : 0;
@@ -187,48 +229,70 @@ __global__ __launch_bounds__(1024) void k_xent_reduce_loss(const float* __restri
   }
 }
 
-// slices of K of an XG_OUT product added in their order; nothing where there is one (the product wrote its output itself)
-template <typename T>
+// slices of K of a product of G added in their order; nothing where there is one (the product wrote its output itself).  dH: after the
+// last piece.
+template <typename T, XentMode MODE>
 __global__ __launch_bounds__(256) void k_xent_join_slices(const XentGemmArgs g, int bt) {
-  const int valid = g.n_valid[0];
-  const int N = g.count_n ? valid : g.N, K = g.count_k ? valid : g.K;
-  const int nslice = xent_split(g.tiles_m * ((N + bt - 1) / bt), g.count_k ? (K + 63) / 64 : g.split_stages, g.split_blocks);
+  const XentShape z(g, MODE, g.n_valid[0]);
+  if (MODE == XG_DW && z.classes == 0) return;
+  const int nslice = xent_split(z.split_tiles(bt), z.split_stages, g.segments, g.split_blocks);
   if (nslice <= 1) return;
-  const int64_t all = (int64_t)N * g.M, chunks = (all + 7) / 8;
+  const int64_t all = (int64_t)z.N * z.M, chunks = (all + 7) / 8;
+  T* const out = (T*)g.out + (MODE == XG_DW ? z.class0 * g.ldo : 0);
+  auto row_of = [&](int64_t n) -> int64_t { return MODE == XG_DH ? g.rows[n] : n; };
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < chunks; i += (int64_t)gridDim.x * 256) {
     const int64_t at = i * 8;
     const int n8 = (int)std::min<int64_t>(8, all - at);
     float s[8] = {};
-    for (int k = 0; k < nslice; ++k) {
+    int k = 0;
+    for (; k + 4 <= nslice; k += 4) {                 // four loads in flight
+      Raw8<float> r[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) r[u] = load_chunk(g.acc + (k + u) * all + at, n8);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        float v[8];
+        r[u].get(v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[j] += v[j];
+      }
+    }
+    for (; k < nslice; ++k) {
       float v[8];
       load_chunk(g.acc + k * all + at, n8).get(v);
 #pragma unroll
       for (int j = 0; j < 8; ++j) s[j] += v[j];
     }
-    const int64_t n = at / g.M, m = at - n * g.M;
-    if (m + 8 <= g.M) {
-      store_chunk((T*)g.out + (g.rows ? (int64_t)g.rows[n] : n) * g.ldo + m, n8, s);
+    const int64_t n = at / z.M, m = at - n * z.M;
+    if (m + 8 <= z.M) {
+      store_chunk(out + row_of(n) * g.ldo + m, n8, s);
     } else {                                          // the chunk passes the end of a row
       for (int j = 0; j < n8; ++j) {
-        const int64_t nj = (at + j) / g.M, mj = at + j - nj * g.M;
-        ((T*)g.out)[(g.rows ? (int64_t)g.rows[nj] : nj) * g.ldo + mj] = from_f32<T>(s[j]);
+        const int64_t nj = (at + j) / z.M, mj = at + j - nj * z.M;
+        out[row_of(nj) * g.ldo + mj] = from_f32<T>(s[j]);
       }
     }
   }
 }
 
 // ---- plans
-constexpr int64_t kXentGradElems = INT64_C(1) << 26;  // most elements of G at a time: 128 MiB of bf16, which the last-level cache holds
+// Elements of G at a time: half of what all classes need, 128 MiB of bf16 at least and 512 MiB at most.  A piece costs five launches and
+// a pass over the sums of dh: pieces of 128 / 256 / 512 MiB took 505 / 482 / 476 us for 12288 tokens, one in seven with a class, of
+// width 768 against 30522 classes, and 6.77 / 6.73 / 6.66 ms for 8192 of width 4096 against 32000.
+constexpr int64_t kXentGradLeast = INT64_C(1) << 26, kXentGradMost = INT64_C(1) << 28;
 constexpr int64_t kXentStageElems = INT64_C(1) << 26; // most elements of a staged piece of W
 
 struct XentPlan {
-  int parts;                      // bf16 parts of an operand
-  int64_t Dp, slots;              // features in whole stages, token slots in whole tiles
+  int parts, segments;            // bf16 parts of an operand, products of parts
+  int64_t Dp, slots;              // features in whole stages, most token slots in whole tiles
   bool stage_w;
-  int64_t piece;                  // classes of a piece, a multiple of 256 (one piece: all of them, rounded up)
-  int64_t pieces;
-  int bt;                         // tile of the logits
-  int bt_dh, bt_dw, blocks_dh, blocks_dw;
+  XentPieces pieces;
+  int n_pieces;                   // most there can be
+  int64_t grad_elems, stage_rows; // of G, of a staged piece
+  int bt, bt_dh, bt_dw;           // tiles of the logits and of the two products
+  int blocks_dh, blocks_dw;
+  int64_t grid, grid_dh, grid_dw; // blocks
+  bool join_dh, join_dw;          // K may be cut
   int64_t acc_dh, acc_dw;         // fp32 partial results
 };
 
@@ -237,7 +301,7 @@ static int logits_tile(int64_t T, int64_t V) {
   if (T > 64 && ceil_div(V, 128) * ceil_div(T, 128) >= 128) return 128;
   return 64;
 }
-// tile and blocks of an XG_OUT product [N][M] over so many stages
+// tile and blocks of a product of G [N][M] over so many stages
 static int out_tile(int64_t M, int64_t N, int64_t stages, int* blocks) {
   const int64_t t256 = ceil_div(M, 256) * ceil_div(N, 256), t128 = ceil_div(M, 128) * ceil_div(N, 128);
   if (t256 * std::max<int64_t>(1, stages / 8) >= 192 && N > 128) { *blocks = 256; return 256; }
@@ -245,37 +309,44 @@ static int out_tile(int64_t M, int64_t N, int64_t stages, int* blocks) {
   *blocks = 1024;
   return 64;
 }
-// most fp32 partial results of such a product: slices times rows, for every number of rows up to N
-static int64_t out_acc_elems(int64_t M, int64_t N, int64_t stages, int bt, int blocks, bool pieces) {
-  const int64_t tm = ceil_div(M, bt);
-  const int64_t most = std::max<int64_t>(1, stages / 8);
+// most fp32 partial results of such a product: slices times rows, for every number of rows from `fewest` to N
+static int64_t out_acc_elems(int64_t M, int64_t fewest, int64_t N, int64_t stages, int segments, int bt, int blocks, bool pieces, bool* join) {
+  const int64_t tm = ceil_div(M, bt), most = xent_split(tm * ceil_div(fewest, bt), (int)stages, segments, blocks);
+  *join = most > 1;
+  if (most <= 1 && !pieces) return 0;
   // slices <= blocks / tiles, so that slices * rows <= blocks * bt / tm; a single slice has all rows
-  int64_t rows = std::min<int64_t>(most * N, std::max<int64_t>(blocks * (int64_t)bt / tm, N));
-  if (xent_split((int)std::min<int64_t>(tm, INT32_MAX), (int)std::min<int64_t>(stages, INT32_MAX), blocks) <= 1 && !pieces) rows = 0;
-  return rows * M;
+  return std::max(N, std::min(most * N, blocks * (int64_t)bt / tm)) * M;
 }
 
 static XentPlan xent_plan(int64_t T, int64_t D, int64_t V, int dtype, bool backward) {
   XentPlan p = {};
   p.parts = dtype == EFQAT_F32 ? 3 : 1;
+  p.segments = dtype == EFQAT_F32 ? 6 : 1;
   p.Dp = round_up(D, 64);
   p.slots = round_up(T, 256);
   p.stage_w = p.parts == 3 || D % 64 != 0;
-  int64_t most = INT64_C(1) << 31;                     // more than there are classes
-  if (p.stage_w) most = kXentStageElems / (p.Dp * p.parts);
-  if (backward) most = std::min(most, kXentGradElems / (p.slots * p.parts));
-  most = std::max<int64_t>(most / 256 * 256, 1024);
-  p.pieces = ceil_div(V, most);
-  p.piece = round_up(ceil_div(V, p.pieces), 256);
-  p.pieces = ceil_div(V, p.piece);
-  p.bt = logits_tile(T, std::min(V, p.piece));
-  if (backward) {
-    const int64_t kv = std::min(V, p.piece);
-    p.bt_dh = out_tile(D, T, p.parts == 3 ? kv / 64 * 6 : kv / 64, &p.blocks_dh);
-    p.bt_dw = out_tile(D, kv, p.parts == 3 ? T / 64 * 6 : T / 64, &p.blocks_dw);
-    p.acc_dh = out_acc_elems(D, T, ceil_div(kv, 64), p.bt_dh, p.blocks_dh, p.pieces > 1);
-    p.acc_dw = out_acc_elems(D, kv, ceil_div(T, 64), p.bt_dw, p.blocks_dw, false);
+  p.pieces.V = (int)V;
+  p.pieces.parts = p.parts;
+  p.pieces.elems = backward ? (uint32_t)std::min(std::max(p.slots * p.parts * round_up(ceil_div(V, 2), 256), kXentGradLeast), kXentGradMost) : 0;
+  p.pieces.cap = (int)round_up(V, 256);
+  if (p.stage_w) p.pieces.cap = (int)std::min<int64_t>(p.pieces.cap, std::max<int64_t>(kXentStageElems / (p.Dp * p.parts) / 256 * 256, 1024));
+  const int64_t piece = p.pieces.size((int)T), widest = p.pieces.size(0);  // of the most and the fewest tokens
+  p.n_pieces = (int)ceil_div(V, piece);
+  p.stage_rows = p.stage_w ? widest : 0;
+  p.bt = logits_tile(T, std::min(V, piece));
+  if (!backward) {
+    p.grid = ceil_div(piece, p.bt) * ceil_div(T, p.bt);
+    return p;
   }
+  // a piece of G: `elems`, or 1024 classes of many tokens, or all classes
+  p.grad_elems = std::min(p.slots * p.parts * round_up(V, 256), std::max<int64_t>(p.pieces.elems, p.slots * p.parts * 1024));
+  p.grid = std::min(ceil_div(V, p.bt) * ceil_div(T, p.bt), p.grad_elems / p.parts / (p.bt * p.bt) + 1);
+  p.bt_dh = out_tile(D, T, ceil_div(piece, 64) * p.segments, &p.blocks_dh);
+  p.bt_dw = out_tile(D, std::min(V, piece), ceil_div(T, 64) * p.segments, &p.blocks_dw);
+  p.grid_dh = std::max<int64_t>(ceil_div(D, p.bt_dh) * ceil_div(T, p.bt_dh), p.blocks_dh);
+  p.grid_dw = std::max<int64_t>(ceil_div(D, p.bt_dw) * ceil_div(std::min(V, widest), p.bt_dw), p.blocks_dw);
+  p.acc_dh = out_acc_elems(D, 1, T, ceil_div(V, 64), p.segments, p.bt_dh, p.blocks_dh, p.n_pieces > 1, &p.join_dh);
+  p.acc_dw = out_acc_elems(D, std::min(V, piece), std::min(V, widest), ceil_div(T, 64), p.segments, p.bt_dw, p.blocks_dw, false, &p.join_dw);
   return p;
 }
 
@@ -293,11 +364,11 @@ static XentWs xent_ws(void* ws, const XentPlan& p, int64_t T, int64_t V, bool ba
   w.rows = (int32_t*)c.take((size_t)T * sizeof(int32_t));
   w.target = (int32_t*)c.take((size_t)T * sizeof(int32_t));
   w.h = (bf16_t*)c.take((size_t)(p.slots * p.parts * p.Dp) * 2);
-  if (p.stage_w) w.w = (bf16_t*)c.take((size_t)(p.piece * p.parts * p.Dp) * 2);
+  if (p.stage_w) w.w = (bf16_t*)c.take((size_t)(p.stage_rows * p.parts * p.Dp) * 2);
   if (backward) {
     w.slot_lse = (float*)c.take((size_t)T * sizeof(float));
     w.slot_scale = (float*)c.take((size_t)T * sizeof(float));
-    w.grad = (bf16_t*)c.take((size_t)(p.slots * p.parts * p.piece) * 2);
+    w.grad = (bf16_t*)c.take((size_t)p.grad_elems * 2);
     w.acc_dh = (float*)c.take((size_t)p.acc_dh * sizeof(float));
     w.acc_dw = (float*)c.take((size_t)p.acc_dw * sizeof(float));
   } else {
@@ -309,25 +380,24 @@ static XentWs xent_ws(void* ws, const XentPlan& p, int64_t T, int64_t V, bool ba
   return w;
 }
 
-template <int BT, bool ATR, bool BTR, int MODE>
+template <int BT, XentMode MODE>
 static int launch_xent_gemm(const XentGemmArgs& g, int64_t blocks, hipStream_t st) {
   using C = XentCfg<BT>;
-  static const hipError_t attr = hipFuncSetAttribute((const void*)k_xent_gemm<BT, ATR, BTR, MODE>, hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS);
+  static const hipError_t attr = hipFuncSetAttribute((const void*)k_xent_gemm<BT, MODE>, hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS);
   if (attr != hipSuccess) return EFQAT_ERR_HIP;
-  EFQAT_TRY(launch((k_xent_gemm<BT, ATR, BTR, MODE>), dim3((unsigned)blocks), dim3(C::NW * 64), C::LDS, st, g));
-  return EFQAT_OK;
+  return launch((k_xent_gemm<BT, MODE>), dim3((unsigned)blocks), dim3(C::NW * 64), C::LDS, st, g);
 }
-template <bool ATR, bool BTR, int MODE>
-static int launch_xent_tile(int bt, const XentGemmArgs& a, hipStream_t st) {
-  XentGemmArgs g = a;
-  g.tiles_m = (int)ceil_div(g.M, bt);
-  g.tiles_n = (int)ceil_div(g.N, bt);
-  int64_t blocks = (int64_t)g.tiles_m * g.tiles_n;
-  if (MODE == XG_OUT && g.split_blocks > 0) blocks = std::max<int64_t>(blocks, g.split_blocks);
+template <XentMode MODE>
+static int launch_xent_tile(int bt, const XentGemmArgs& g, int64_t blocks, hipStream_t st) {
   if (blocks > INT32_MAX) return EFQAT_ERR_BAD_SHAPE;
-  if (bt == 256) return launch_xent_gemm<256, ATR, BTR, MODE>(g, blocks, st);
-  if (bt == 128) return launch_xent_gemm<128, ATR, BTR, MODE>(g, blocks, st);
-  return launch_xent_gemm<64, ATR, BTR, MODE>(g, blocks, st);
+  if (bt == 256) return launch_xent_gemm<256, MODE>(g, blocks, st);
+  if (bt == 128) return launch_xent_gemm<128, MODE>(g, blocks, st);
+  return launch_xent_gemm<64, MODE>(g, blocks, st);
+}
+template <XentMode MODE>
+static int launch_xent_join(int bt, const XentGemmArgs& g, hipStream_t st) {
+  if (g.out_dtype == EFQAT_F32) return launch(k_xent_join_slices<float, MODE>, dim3(1024), dim3(256), 0, st, g, bt);
+  return launch(k_xent_join_slices<bf16_t, MODE>, dim3(1024), dim3(256), 0, st, g, bt);
 }
 
 static int stage_blocks(int64_t rows, int64_t pitch, unsigned* blocks) {
@@ -346,12 +416,36 @@ static int launch_stage(const XentStageArgs& g, int dtype, hipStream_t st) {
   return EFQAT_OK;
 }
 
+static XentGemmArgs xent_gemm_args(const XentPlan& p, const XentWs& k, const void* w, int64_t ldw, int64_t D) {
+  XentGemmArgs g = {};
+  g.W = p.stage_w ? k.w : (const bf16_t*)w;
+  g.w_piece = p.stage_w ? 1 : 0;
+  g.ldw = p.stage_w ? p.parts * p.Dp : ldw;
+  g.H = k.h;
+  g.G = k.grad;
+  g.Dp = p.Dp;
+  g.D = D;
+  g.segments = p.segments;
+  g.pieces = p.pieces;
+  g.n_valid = k.n_valid;
+  g.target = k.target;
+  g.slots = p.slots;
+  return g;
+}
+static int stage_piece(const XentPlan& p, const XentWs& k, const void* w, int64_t ldw, int dtype, int64_t D, int piece, hipStream_t st) {
+  XentStageArgs s = {};
+  s.src = w; s.ld = ldw; s.cols = D; s.pitch = p.Dp; s.n_valid = k.n_valid; s.pieces = p.pieces; s.piece = piece;
+  s.dst_rows = p.stage_rows; s.dst = k.w;
+  return launch_stage(s, dtype, st);
+}
+
+static bool xent_sizes_ok(int64_t T, int64_t D, int64_t V) {
+  return T > 0 && D > 0 && V > 0 && T <= INT64_C(1) << 30 && V <= INT64_C(1) << 30 && D <= INT64_C(1) << 20;
+}
 static int check_xent(const void* h, int64_t ldh, const void* w, int64_t ldw, int dtype, int64_t T, int64_t D, int64_t V,
                       const int64_t* targets, int reduction, const void* ws) {
   // token slots and classes are 32-bit numbers, offsets inside a tile of 256 rows too
-  if (T <= 0 || D <= 0 || V <= 0 || T > INT64_C(1) << 30 || V > INT64_C(1) << 30 || D > INT64_C(1) << 20 || ldh < D || ldw < D ||
-      ldw > INT64_C(1) << 22)
-    return EFQAT_ERR_BAD_SHAPE;
+  if (!xent_sizes_ok(T, D, V) || ldh < D || ldw < D || ldw > INT64_C(1) << 22) return EFQAT_ERR_BAD_SHAPE;
   if (!known_dtype(dtype)) return EFQAT_ERR_BAD_DTYPE;
   if (reduction != EFQAT_XENT_NONE && reduction != EFQAT_XENT_MEAN && reduction != EFQAT_XENT_SUM) return EFQAT_ERR_BAD_LAYOUT;
   if (!h || !w || !targets || !ws) return EFQAT_ERR_NULL_PTR;
@@ -367,11 +461,11 @@ static int check_xent(const void* h, int64_t ldh, const void* w, int64_t ldw, in
 using namespace efqat;
 
 extern "C" size_t efqat_linear_xent_fwd_workspace_bytes(int64_t T, int64_t D, int64_t V, int dtype) {
-  if (T <= 0 || D <= 0 || V <= 0 || !known_dtype(dtype)) return 256;
+  if (!xent_sizes_ok(T, D, V) || !known_dtype(dtype)) return 256;
   return xent_ws(nullptr, xent_plan(T, D, V, dtype, false), T, V, false).bytes;
 }
 extern "C" size_t efqat_linear_xent_bwd_workspace_bytes(int64_t T, int64_t D, int64_t V, int dtype) {
-  if (T <= 0 || D <= 0 || V <= 0 || !known_dtype(dtype)) return 256;
+  if (!xent_sizes_ok(T, D, V) || !known_dtype(dtype)) return 256;
   return xent_ws(nullptr, xent_plan(T, D, V, dtype, true), T, V, true).bytes;
 }
 
@@ -397,25 +491,12 @@ extern "C" int efqat_linear_xent_fwd(const void* h, int64_t ldh, const void* w, 
   sh.src = h; sh.ld = ldh; sh.cols = D; sh.pitch = p.Dp; sh.rows = k.rows; sh.n_valid = k.n_valid; sh.dst_rows = p.slots; sh.dst = k.h;
   EFQAT_TRY(launch_stage(sh, dtype, st));
 
-  for (int64_t v0 = 0; v0 < V; v0 += p.piece) {
-    const int64_t n = std::min(p.piece, V - v0);
-    XentGemmArgs g = {};
-    g.segments = p.parts == 3 ? 6 : 1;
-    if (p.stage_w) {
-      XentStageArgs sw = {};
-      sw.src = (const char*)w + v0 * ldw * (dtype == EFQAT_F32 ? 4 : 2);
-      sw.ld = ldw; sw.cols = D; sw.pitch = p.Dp; sw.n_rows = n; sw.dst_rows = n; sw.dst = k.w;
-      EFQAT_TRY(launch_stage(sw, dtype, st));
-      g.A = k.w; g.lda = p.parts * p.Dp;
-    } else {
-      g.A = (const bf16_t*)w + v0 * ldw; g.lda = ldw;
-    }
-    g.B = k.h; g.ldb = p.parts * p.Dp;
-    g.a_part = g.b_part = (int)p.Dp;
-    g.M = (int)n; g.N = (int)T; g.K = (int)p.Dp;
-    g.count_n = 1; g.n_valid = k.n_valid;
-    g.class0 = (int)v0; g.target = k.target; g.part = k.part; g.target_logit = k.target_logit; g.slots = (int)p.slots;
-    EFQAT_TRY(launch_xent_tile<false, false, XG_LSE>(p.bt, g, st));
+  XentGemmArgs g = xent_gemm_args(p, k, w, ldw, D);
+  g.part = k.part;
+  g.target_logit = k.target_logit;
+  for (g.piece = 0; g.piece < p.n_pieces; ++g.piece) {
+    if (p.stage_w) EFQAT_TRY(stage_piece(p, k, w, ldw, dtype, D, g.piece, st));
+    EFQAT_TRY(launch_xent_tile<XG_LSE>(p.bt, g, p.grid, st));
   }
 
   // tiles of a piece are whole but for the last piece's: pieces are multiples of 256 classes
@@ -438,7 +519,6 @@ extern "C" int efqat_linear_xent_bwd(const void* h, int64_t ldh, const void* w, 
   const XentWs k = xent_ws(ws, p, T, V, true);
   if (ws_bytes < k.bytes) return EFQAT_ERR_WORKSPACE;
   hipStream_t st = (hipStream_t)stream;
-  const int64_t elem = dtype == EFQAT_F32 ? 4 : 2;
 
   XentRowsArgs r = {};
   r.targets = targets; r.T = T; r.V = V; r.ignore = ignore_index;
@@ -451,58 +531,25 @@ extern "C" int efqat_linear_xent_bwd(const void* h, int64_t ldh, const void* w, 
   sh.targets = targets; sh.T = T; sh.V = V; sh.ignore = ignore_index; sh.clear = dh; sh.ld_clear = lddh;
   EFQAT_TRY(launch_stage(sh, dtype, st));
 
-  for (int64_t v0 = 0; v0 < V; v0 += p.piece) {
-    const int64_t n = std::min(p.piece, V - v0);
-    const bool first = v0 == 0, last = v0 + p.piece >= V;
-    XentGemmArgs g = {};
-    g.segments = p.parts == 3 ? 6 : 1;
-    g.n_valid = k.n_valid;
-    const bf16_t* W = (const bf16_t*)w + v0 * ldw;
-    int64_t ldW = ldw;
-    if (p.stage_w) {
-      XentStageArgs sw = {};
-      sw.src = (const char*)w + v0 * ldw * elem;
-      sw.ld = ldw; sw.cols = D; sw.pitch = p.Dp; sw.n_rows = n; sw.dst_rows = round_up(n, 64); sw.dst = k.w;
-      EFQAT_TRY(launch_stage(sw, dtype, st));
-      W = k.w; ldW = p.parts * p.Dp;
-    }
-    const int64_t ldG = p.parts * p.piece;
-    {
-      XentGemmArgs q = g;
-      q.A = W; q.lda = ldW; q.a_part = (int)p.Dp;
-      q.B = k.h; q.ldb = p.parts * p.Dp; q.b_part = (int)p.Dp;
-      q.M = (int)n; q.N = (int)T; q.K = (int)p.Dp; q.count_n = 1;
-      q.class0 = (int)v0; q.target = k.target; q.lse = k.slot_lse; q.scale = k.slot_scale; q.grad = k.grad; q.grad_pitch = (int)p.piece;
-      EFQAT_TRY(launch_xent_tile<false, false, XG_GRAD>(p.bt, q, st));
-    }
+  XentGemmArgs g = xent_gemm_args(p, k, w, ldw, D);
+  g.lse = k.slot_lse;
+  g.scale = k.slot_scale;
+  g.mean = reduction == EFQAT_XENT_MEAN ? 1 : 0;
+  g.out_dtype = dtype;
+  for (g.piece = 0; g.piece < p.n_pieces; ++g.piece) {
+    if (p.stage_w) EFQAT_TRY(stage_piece(p, k, w, ldw, dtype, D, g.piece, st));
+    EFQAT_TRY(launch_xent_tile<XG_GRAD>(p.bt, g, p.grid, st));
     if (dw) {
       XentGemmArgs q = g;
-      q.A = k.h; q.lda = p.parts * p.Dp; q.a_part = (int)p.Dp; q.a_cols = (int)p.Dp;
-      q.B = k.grad; q.ldb = ldG; q.b_part = (int)p.piece; q.b_cols = (int)p.piece;
-      q.M = (int)D; q.N = (int)n; q.K = (int)T; q.count_k = 1;
-      q.split_blocks = p.blocks_dw; q.acc = k.acc_dw;
-      q.out = (char*)dw + v0 * lddw * elem; q.out_dtype = dtype; q.ldo = lddw;
-      EFQAT_TRY(launch_xent_tile<true, true, XG_OUT>(p.bt_dw, q, st));
-      q.tiles_m = (int)ceil_div(D, p.bt_dw);
-      if (xent_split((int)(q.tiles_m * ceil_div(n, p.bt_dw)), (int)ceil_div(T, 64), p.blocks_dw) > 1) {   // for enough tokens
-        if (dtype == EFQAT_F32) EFQAT_TRY(launch(k_xent_join_slices<float>, dim3(1024), dim3(256), 0, st, q, p.bt_dw));
-        else EFQAT_TRY(launch(k_xent_join_slices<bf16_t>, dim3(1024), dim3(256), 0, st, q, p.bt_dw));
-      }
+      q.split_blocks = p.blocks_dw; q.acc = k.acc_dw; q.out = dw; q.ldo = lddw;
+      EFQAT_TRY(launch_xent_tile<XG_DW>(p.bt_dw, q, p.grid_dw, st));
+      if (p.join_dw) EFQAT_TRY(launch_xent_join<XG_DW>(p.bt_dw, q, st));
     }
     if (dh) {
       XentGemmArgs q = g;
-      q.A = W; q.lda = ldW; q.a_part = (int)p.Dp; q.a_cols = (int)p.Dp; q.a_rows = p.stage_w ? 0 : (int)n;
-      q.B = k.grad; q.ldb = ldG; q.b_part = (int)p.piece;
-      q.M = (int)D; q.N = (int)T; q.K = (int)n; q.count_n = 1;
-      q.split_blocks = p.blocks_dh; q.split_stages = (int)ceil_div(std::min(p.piece, V), 64);
-      q.acc = k.acc_dh; q.acc_add = first ? 0 : 1; q.acc_write = last ? 0 : 1;
-      q.out = dh; q.out_dtype = dtype; q.ldo = lddh; q.rows = k.rows;
-      EFQAT_TRY(launch_xent_tile<true, false, XG_OUT>(p.bt_dh, q, st));
-      q.tiles_m = (int)ceil_div(D, p.bt_dh);
-      if (last && xent_split(q.tiles_m, q.split_stages, q.split_blocks) > 1) {   // for few enough tokens
-        if (dtype == EFQAT_F32) EFQAT_TRY(launch(k_xent_join_slices<float>, dim3(1024), dim3(256), 0, st, q, p.bt_dh));
-        else EFQAT_TRY(launch(k_xent_join_slices<bf16_t>, dim3(1024), dim3(256), 0, st, q, p.bt_dh));
-      }
+      q.split_blocks = p.blocks_dh; q.acc = k.acc_dh; q.out = dh; q.ldo = lddh; q.rows = k.rows;
+      EFQAT_TRY(launch_xent_tile<XG_DH>(p.bt_dh, q, p.grid_dh, st));
+      if (p.join_dh && g.piece == p.n_pieces - 1) EFQAT_TRY(launch_xent_join<XG_DH>(p.bt_dh, q, st));
     }
   }
   return EFQAT_OK;

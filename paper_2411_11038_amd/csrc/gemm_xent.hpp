@@ -77,10 +77,10 @@ struct XentGemmArgs {
   const int32_t* rows;            // XG_DH: rows of the output, by slot
 };
 
-// Slices of K of a product of G of so many tiles: about `blocks` blocks, none with fewer than 8 stages
+// Slices of K of a product of G of so many tiles: about `blocks` blocks, none with fewer than 12 stages
 __host__ __device__ inline int xent_split(int64_t tiles, int stages, int segments, int blocks) {
   const int by_blocks = tiles > blocks || tiles < 1 ? 1 : blocks / (int)tiles;
-  const int by_stages = segments >= 8 ? stages : (int)((int64_t)stages * segments >> 3);
+  const int by_stages = (int)((int64_t)stages * segments / 12);
   const int s = by_blocks < by_stages ? by_blocks : by_stages;
   return s < 1 ? 1 : s;
 }
@@ -196,12 +196,15 @@ struct XentOperand {
 
 template <int BT>
 struct XentCfg {
-  static constexpr int NW = BT == 256 ? 8 : 4, WGM = 2, WGN = NW / 2;
+  static constexpr int NW = BT == 256 ? 8 : 4, WGM = 2, WGN = NW / 2;       // wavefronts of a tile
+  static constexpr int KG = BT == 64 ? 2 : 1;         // groups of them that take the K stages in turn
+  static constexpr int THREADS = NW * KG * 64;
+  static constexpr int CHIP = BT == 128 ? 512 : 256;  // blocks that the chip holds at once
   static constexpr int WM = BT / WGM, WN = BT / WGN, TM = WM / 32, TN = WN / 32;
   static constexpr int STAGE = BT * 256;              // bytes of both operands' stage, a power of two
-  static constexpr int NST = BT == 64 ? 4 : 2;        // LDS stages
+  static constexpr int NST = BT == 64 ? 4 : 2;        // LDS stages of a group
   static constexpr int OUT_PITCH = WM * 2 + 16;       // bytes of a row of a wavefront's bf16 results in LDS
-  static constexpr int LDS = NST * STAGE > NW * WN * OUT_PITCH ? NST * STAGE : NW * WN * OUT_PITCH;
+  static constexpr int LDS = KG * NST * STAGE > NW * WN * OUT_PITCH ? KG * NST * STAGE : NW * WN * OUT_PITCH;
 };
 
 // bf16 parts of x: x0 + x1 + x2 = x up to 2^-24.  A NaN is its first part.  What bf16 has no finite value for, infinities among it,
@@ -215,27 +218,34 @@ __device__ __forceinline__ void split3(float x, float (&p)[3]) {
   p[2] = r1 - p[1];
 }
 
+// Tiles of a product (times its slices of K)
+struct XentTiles {
+  int m, n, slices;
+  __device__ __forceinline__ XentTiles(const XentGemmArgs& g, const XentShape& z, XentMode mode, int bt) {
+    m = (z.M + bt - 1) / bt;
+    n = (z.N + bt - 1) / bt;
+    const bool cut = mode == XG_DH || mode == XG_DW;
+    slices = cut ? __builtin_amdgcn_readfirstlane(xent_split(z.split_tiles(bt), z.split_stages, g.segments, g.split_blocks)) : 1;
+  }
+  __device__ __forceinline__ int total() const { return m * n * slices; }
+};
+
+// one tile (and slice) of a product: number `bid` of them in the order of the launch
 template <int BT, XentMode MODE>
-__global__ __launch_bounds__(XentCfg<BT>::NW * 64) void k_xent_gemm(const XentGemmArgs g) {
+__device__ __forceinline__ void xent_gemm_block(const XentGemmArgs& g, const XentShape& z, const XentTiles& tiles_of, int valid, int bid, char* smem) {
 #if defined(__HIP_DEVICE_COMPILE__)
   using C = XentCfg<BT>;
   constexpr bool LOGITS = MODE == XG_LSE || MODE == XG_GRAD;
   constexpr bool ATR = !LOGITS, BTR = MODE == XG_DW;
-  extern __shared__ __attribute__((aligned(16))) char smem[];
   const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int all_wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int kg = all_wave / C::NW, wave = all_wave % C::NW;         // group along K, wavefront of the tile
   const int wm = wave / C::WGN, wn = wave % C::WGN;
 
-  const int valid = g.n_valid[0];
-  const XentShape z(g, MODE, valid);
-  if (z.classes == 0) return;
   const int M = z.M, N = z.N, nks = z.nks;
-  const int tiles_m = (M + BT - 1) / BT, tiles_n = (N + BT - 1) / BT, tiles = tiles_m * tiles_n;
-  // slices of K (dW: by the tiles of a whole piece), tiles of a slice; neighbours run on one XCD, in groups of 4 rows of tiles
-  const int nslice = LOGITS ? 1 : __builtin_amdgcn_readfirstlane(xent_split(z.split_tiles(BT), z.split_stages, g.segments, g.split_blocks));
-  const int total = tiles * nslice;
-  if ((int)blockIdx.x >= total) return;
-  const int logical = xcd_contiguous_index(blockIdx.x, total);
+  const int tiles_m = tiles_of.m, tiles_n = tiles_of.n, nslice = tiles_of.slices, tiles = tiles_m * tiles_n, total = tiles * nslice;
+  // neighbours run on one XCD, in groups of 4 rows of tiles
+  const int logical = xcd_contiguous_index(bid, total);
   const int slice = logical / tiles, pid = logical - slice * tiles;
   constexpr int GM = 4;
   const int per_group = GM * tiles_n, group = pid / per_group, first_m = group * GM;
@@ -256,6 +266,22 @@ __global__ __launch_bounds__(XentCfg<BT>::NW * 64) void k_xent_gemm(const XentGe
   const int64_t a_part = g.Dp, b_part = LOGITS ? g.Dp : z.piece;
   // the rows of W end inside the last stage of dH
   const int a_rows = MODE == XG_DH && !g.w_piece ? z.K : 0;
+
+  // what the epilogue needs of the tokens: on its way while the product runs
+  const int n_lane = n0 + wn * C::WN + (lane & 31);
+  int tok_class[LOGITS ? C::TN : 1];
+  float tok_lse[MODE == XG_GRAD ? C::TN : 1], tok_scale[MODE == XG_GRAD ? C::TN : 1];
+  if constexpr (LOGITS) {
+#pragma unroll
+    for (int j = 0; j < C::TN; ++j) {
+      const int n = n_lane + 32 * j;
+      tok_class[j] = n < N ? g.target[n] : -1;
+      if constexpr (MODE == XG_GRAD) {
+        tok_lse[j] = n < N ? g.lse[n] : 0.0f;
+        tok_scale[j] = n < N ? g.scale[n] : 0.0f;
+      }
+    }
+  }
 
   XentOperand<BT, C::WM, C::NW, ATR> A;
   XentOperand<BT, C::WN, C::NW, BTR> B;
@@ -354,33 +380,85 @@ __global__ __launch_bounds__(XentCfg<BT>::NW * 64) void k_xent_gemm(const XentGe
   };
 
   if constexpr (C::NST > 2) {
-    // Few matrix instructions a stage: the copies of two stages and more stay in flight across a stage's barrier, behind which those of
-    // the stage NST - 1 further on go into the buffer that everybody has read.
-    auto issue_stage = [&](int s, int buf) {
+    // Few matrix instructions a stage: what a stage costs is the way from its barrier over the LDS reads to the last of them.  Two groups
+    // of wavefronts take every other stage, each into a ring of its own; the copies of two stages and more stay in flight across a
+    // barrier, behind which those of the group's stage NST - 1 further on go into the buffer that it has read.
+    const int mine = (nstage - kg + C::KG - 1) / C::KG, rounds = (nstage + C::KG - 1) / C::KG;     // stages of this group, of the first
+    const int ring = kg * C::NST;
+    floatx16_t odd[C::TM][C::TN];                     // every other sub-step: two chains of dependent instructions
+#pragma unroll
+    for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+      for (int j = 0; j < C::TN; ++j) odd[i][j] = acc[i][j];
+    for (int k = 0; k < kg && k < nstage; ++k) next_stage();
+    auto issue_stage = [&](int r) {
+      const int s = r * C::KG + kg, buf = ring + r % C::NST;
       if (s < nfull) issue(Whole{}, buf, 0, LPS);
       else issue(Last{}, buf, 0, LPS);
-      next_stage();
+#pragma unroll
+      for (int k = 0; k < C::KG; ++k) next_stage();
     };
 #pragma unroll
-    for (int s = 0; s < C::NST - 1; ++s)
-      if (s < nstage) issue_stage(s, s);
-    for (int s = 0; s < nstage; ++s) {
-      if (s + C::NST - 2 < nstage) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((C::NST - 2) * LPS) : "memory");
+    for (int r = 0; r < C::NST - 1; ++r)
+      if (r < mine) issue_stage(r);
+    for (int r = 0; r < rounds; ++r) {
+      if (r + C::NST - 2 < mine) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((C::NST - 2) * LPS) : "memory");
       else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       __builtin_amdgcn_s_barrier();
       __builtin_amdgcn_sched_barrier(0);
-      if (s + C::NST - 1 < nstage) issue_stage(s + C::NST - 1, (s + C::NST - 1) % C::NST);
-      const char* at = smem + (s % C::NST) * C::STAGE;
+      if (r + C::NST - 1 < mine) issue_stage(r + C::NST - 1);
+      if (r < mine) {
+        const char* at = smem + (ring + r % C::NST) * C::STAGE;
+        typename decltype(A)::Frag a4[4][C::TM];
+        typename decltype(B)::Frag b4[4][C::TN];
 #pragma unroll
-      for (int sub = 0; sub < 4; ++sub) {
+        for (int sub = 0; sub < 4; ++sub) {
 #pragma unroll
-        for (int r = 0; r < RBR; ++r) B.read(at, sub, r, bf[sub & 1]);
+          for (int q = 0; q < RBR; ++q) B.read(at, sub, q, b4[sub]);
 #pragma unroll
-        for (int r = 0; r < RA; ++r) A.read(at, sub, r, af[sub & 1]);
-        mfma_all(sub & 1);
+          for (int q = 0; q < RA; ++q) A.read(at, sub, q, a4[sub]);
+        }
+#pragma unroll
+        for (int sub = 0; sub < 4; ++sub)
+#pragma unroll
+          for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+            for (int j = 0; j < C::TN; ++j) {
+              floatx16_t& d = sub & 1 ? odd[i][j] : acc[i][j];
+              d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a4[sub][i].v),
+                                                          __builtin_bit_cast(bf16x8_t, b4[sub][j].v), d, 0, 0, 0);
+            }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
       }
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      __builtin_amdgcn_sched_barrier(0);
+    }
+    // the sums of the groups, in the first one
+#pragma unroll
+    for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+      for (int j = 0; j < C::TN; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[i][j][r] += odd[i][j][r];
+    __syncthreads();
+    float* sum = reinterpret_cast<float*>(smem);
+    if (kg > 0) {
+#pragma unroll
+      for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+        for (int j = 0; j < C::TN; ++j)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) sum[(((kg - 1) * C::NW + wave) * C::TM * C::TN + i * C::TN + j) * 1024 + r * 64 + lane] = acc[i][j][r];
+    }
+    __syncthreads();
+    if (kg == 0) {
+#pragma unroll
+      for (int k = 1; k < C::KG; ++k)
+#pragma unroll
+        for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+          for (int j = 0; j < C::TN; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] += sum[(((k - 1) * C::NW + wave) * C::TM * C::TN + i * C::TN + j) * 1024 + r * 64 + lane];
     }
   } else
   // On entry to stage s the first H0 copies of stage s + 1 are under way if and only if s + 1 < nfull.
@@ -439,6 +517,7 @@ __global__ __launch_bounds__(XentCfg<BT>::NW * 64) void k_xent_gemm(const XentGe
     const bool edge = m0 + BT > M;
 #pragma unroll
     for (int j = 0; j < C::TN; ++j) {
+      if (kg > 0) break;
       const int n = nw + 32 * j;
       float top = -INFINITY;
 #pragma unroll
@@ -458,7 +537,7 @@ __global__ __launch_bounds__(XentCfg<BT>::NW * 64) void k_xent_gemm(const XentGe
         for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f((acc[i][j][r] - base) * 1.4426950408889634f);
       sum += __shfl_xor(sum, 32);
       if (fh == 0) red[wm * BT + wn * C::WN + 32 * j + fr] = make_float2(top, sum);
-      const int rel = n < N ? g.target[n] - (int)z.class0 - m0 - wm * C::WM : -1;   // row of the wavefront's tile that is the class
+      const int rel = n < N ? tok_class[j] - (int)z.class0 - m0 - wm * C::WM : -1;   // row of the wavefront's tile that is the class
       if (__any(rel >= 0 && rel < C::WM)) {
         const int mine = rel - 4 * fh;
 #pragma unroll
@@ -477,7 +556,7 @@ __global__ __launch_bounds__(XentCfg<BT>::NW * 64) void k_xent_gemm(const XentGe
       a.x = top;
       g.part[(z.class0 / BT + tm) * g.slots + n0 + tid] = a;
     }
-  } else {
+  } else if (kg == 0) {
     // a wavefront's results as rows of WM values in LDS, from where they leave 16 bytes a lane
     char* tile = smem + wave * (C::WN * C::OUT_PITCH);
     constexpr int CPR = C::WM * 2 / 16, RPI = 64 / CPR;            // chunks of a row, rows of an access
@@ -488,21 +567,41 @@ __global__ __launch_bounds__(XentCfg<BT>::NW * 64) void k_xent_gemm(const XentGe
     if constexpr (MODE == XG_GRAD) {
       // G = (softmax - [class of the token]) scale; zero outside the classes and behind the last token
       const float count = g.mean ? (float)valid : 1.0f;
+      const bool edge = m0 + BT > M;
 #pragma unroll
       for (int j = 0; j < C::TN; ++j) {
         const int n = nw + 32 * j;
         const bool in = n < N;
-        const float lse = in ? g.lse[n] : 0.0f, scale = in ? g.scale[n] / count : 0.0f;
-        const int rel = in ? g.target[n] - (int)z.class0 : -1;
+        const float lse = tok_lse[j], scale = tok_scale[j] / count;
+        const int rel = in ? tok_class[j] - (int)z.class0 - m0 - wm * C::WM : -1;   // row of the wavefront's tile that is the class
 #pragma unroll
         for (int i = 0; i < C::TM; ++i)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int m = m_of(i, r);
-            float p = __builtin_amdgcn_exp2f((acc[i][j][r] - lse) * 1.4426950408889634f);
-            p = (m == rel ? p - 1.0f : p) * scale;
-            acc[i][j][r] = in && m < M ? p : 0.0f;
-          }
+          for (int r = 0; r < 16; ++r) acc[i][j][r] = __builtin_amdgcn_exp2f((acc[i][j][r] - lse) * 1.4426950408889634f);
+        if (__any(rel >= 0 && rel < C::WM)) {
+          const int mine = rel - 4 * fh;
+#pragma unroll
+          for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+              if (mine == 32 * i + 8 * (r >> 2) + (r & 3)) acc[i][j][r] -= 1.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[i][j][r] *= scale;
+        if (edge) {                                   // a repeated class may be anything
+#pragma unroll
+          for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = m_of(i, r) < M ? acc[i][j][r] : 0.0f;
+        }
+        if (!in) {                                    // a repeated token too
+#pragma unroll
+          for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+        }
       }
       for (int part = 0; part < parts; ++part) {
 #pragma unroll
@@ -620,6 +719,46 @@ __global__ __launch_bounds__(XentCfg<BT>::NW * 64) void k_xent_gemm(const XentGe
         }
       }
     }
+  }
+#endif
+}
+
+// A launch has at most as many blocks as the chip holds; they walk the tiles that there are (an empty block is not free: it waits for
+// a CU's LDS like the others).
+template <int BT, XentMode MODE>
+__global__ __launch_bounds__(XentCfg<BT>::THREADS) void k_xent_gemm(const XentGemmArgs g) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int valid = g.n_valid[0];
+  const XentShape z(g, MODE, valid);
+  if (z.classes == 0) return;
+  const XentTiles t(g, z, MODE, BT);
+  const int total = t.total();
+  for (int bid = blockIdx.x; bid < total; bid += gridDim.x) {
+    xent_gemm_block<BT, MODE>(g, z, t, valid, bid, smem);
+    __syncthreads();
+  }
+#endif
+}
+
+// both products of G in one grid, the longer contraction first: neither has to wait for the other's last, partly filled round
+template <int BT>
+__global__ __launch_bounds__(XentCfg<BT>::THREADS) void k_xent_gemm_pair(const XentGemmArgs h, const XentGemmArgs w) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int valid = h.n_valid[0];
+  const XentShape zh(h, XG_DH, valid), zw(w, XG_DW, valid);
+  if (zh.classes == 0) return;
+  const XentTiles th(h, zh, XG_DH, BT), tw(w, zw, XG_DW, BT);
+  const int first = th.total(), total = first + tw.total();
+  int bid = blockIdx.x;
+  for (; bid < first; bid += gridDim.x) {
+    xent_gemm_block<BT, XG_DH>(h, zh, th, valid, bid, smem);
+    __syncthreads();
+  }
+  for (; bid < total; bid += gridDim.x) {
+    xent_gemm_block<BT, XG_DW>(w, zw, tw, valid, bid - first, smem);
+    __syncthreads();
   }
 #endif
 }

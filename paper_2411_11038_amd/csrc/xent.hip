@@ -123,8 +123,12 @@ struct XentStageArgs {
   void* clear;
   int64_t ld_clear;
 };
+// tokens (blocks 0 .. first - 1) and classes (the others) in one launch
 template <typename T, int PARTS>
-__global__ __launch_bounds__(256) void k_xent_stage(const XentStageArgs g) {
+__global__ __launch_bounds__(256) void k_xent_stage(const XentStageArgs tokens, int first_blocks, const XentStageArgs classes) {
+  const bool second = (int)blockIdx.x >= first_blocks;
+  const XentStageArgs& g = second ? classes : tokens;
+  const int64_t block = second ? (int64_t)blockIdx.x - first_blocks : blockIdx.x;
   const int valid = g.n_valid[0];
   int64_t n = valid, first = 0, dst_rows = g.dst_rows;
   if (!g.rows) {
@@ -137,7 +141,7 @@ __global__ __launch_bounds__(256) void k_xent_stage(const XentStageArgs g) {
   // lanes of a row: as many as its chunks of 8 columns, up to a block
   const int chunks = (int)(g.pitch / 8);
   const int lanes = chunks >= 256 ? 256 : chunks > 64 ? 128 : chunks > 32 ? 64 : chunks > 16 ? 32 : chunks > 8 ? 16 : 8;
-  const int64_t r = (int64_t)blockIdx.x * (256 / lanes) + threadIdx.x / lanes;
+  const int64_t r = block * (256 / lanes) + threadIdx.x / lanes;
   const int lane = threadIdx.x % lanes;
   if (r < dst_rows) {
     const bool in = r < n;
@@ -174,13 +178,19 @@ __global__ __launch_bounds__(256) void k_xent_stage(const XentStageArgs g) {
 }
 
 // ---- forward: the tiles of classes joined, 64 tokens a block, four groups of tiles
-__global__ __launch_bounds__(256) void k_xent_join(const float2* __restrict__ part, int tiles, int slots, const int32_t* __restrict__ n_valid,
-                                                   const int32_t* __restrict__ rows, const float* __restrict__ target_logit,
-                                                   float* __restrict__ lse, float* __restrict__ loss, float* __restrict__ slot_loss) {
+struct XentJoinArgs {
+  const float2* part;
+  int tiles;
+  int64_t slots;
+  const int32_t *n_valid, *rows;
+  const float* target_logit;
+  float *lse, *loss, *slot_loss;                      // loss of the tokens by row, or (NULL) by slot
+};
+__global__ __launch_bounds__(256) void k_xent_join(const XentJoinArgs g) {
   __shared__ float2 red[4][64];
   const int lane = threadIdx.x & 63, grp = threadIdx.x >> 6;
   const int n = blockIdx.x * 64 + lane;
-  const int valid = n_valid[0];
+  const int valid = g.n_valid[0];
   if ((int)blockIdx.x * 64 >= valid) return;
   float top = -INFINITY, sum = 0.0f;
   auto join = [&](float2 o) {
@@ -190,25 +200,25 @@ __global__ __launch_bounds__(256) void k_xent_join(const float2* __restrict__ pa
   };
   if (n < valid) {
     int i = grp;
-    for (; i + 28 < tiles; i += 32) {
+    for (; i + 28 < g.tiles; i += 32) {
       float2 v[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) v[u] = part[(int64_t)(i + 4 * u) * slots + n];
+      for (int u = 0; u < 8; ++u) v[u] = g.part[(i + 4 * u) * g.slots + n];
 #pragma unroll
       for (int u = 0; u < 8; ++u) join(v[u]);
     }
-    for (; i < tiles; i += 4) join(part[(int64_t)i * slots + n]);
+    for (; i < g.tiles; i += 4) join(g.part[i * g.slots + n]);
   }
   red[grp][lane] = make_float2(top, sum);
   __syncthreads();
   if (grp != 0 || n >= valid) return;
 #pragma unroll
   for (int i = 1; i < 4; ++i) join(red[i][lane]);
-  const float l = top + logf(sum), d = l - target_logit[n];
-  const int row = rows[n];
-  lse[row] = l;
-  if (loss) loss[row] = d;
-  else slot_loss[n] = d;
+  const float l = top + logf(sum), d = l - g.target_logit[n];
+  const int row = g.rows[n];
+  g.lse[row] = l;
+  if (g.loss) g.loss[row] = d;
+  else g.slot_loss[n] = d;
 }
 
 // mean or sum over the tokens, in double precision
@@ -217,7 +227,13 @@ __global__ __launch_bounds__(1024) void k_xent_reduce_loss(const float* __restri
   __shared__ double red[16];
   const int n = n_valid[0];
   double s = 0.0;
-  for (int i = threadIdx.x; i < n; i += 1024) s += (double)slot_loss[i];
+  for (int i = threadIdx.x; i < n; i += 4096) {       // four loads in flight
+    float v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u] = slot_loss[i + 1024 * u < n ? i + 1024 * u : i];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) s += i + 1024 * u < n ? (double)v[u] : 0.0;
+  }
   s = wave_sum(s);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
   __syncthreads();
@@ -232,8 +248,9 @@ __global__ __launch_bounds__(1024) void k_xent_reduce_loss(const float* __restri
 // slices of K of a product of G added in their order; nothing where there is one (the product wrote its output itself).  dH: after the
 // last piece.
 template <typename T, XentMode MODE>
-__global__ __launch_bounds__(256) void k_xent_join_slices(const XentGemmArgs g, int bt) {
-  const XentShape z(g, MODE, g.n_valid[0]);
+__device__ __forceinline__ void xent_join_slices(const XentGemmArgs& g, int bt) {
+  const int valid = g.n_valid[0];
+  const XentShape z(g, MODE, valid);
   if (MODE == XG_DW && z.classes == 0) return;
   const int nslice = xent_split(z.split_tiles(bt), z.split_stages, g.segments, g.split_blocks);
   if (nslice <= 1) return;
@@ -275,6 +292,13 @@ __global__ __launch_bounds__(256) void k_xent_join_slices(const XentGemmArgs g, 
   }
 }
 
+// dH (blocks of y = 0) and dW (y = 1), those that are asked for
+template <typename T>
+__global__ __launch_bounds__(256) void k_xent_join_slices(const XentGemmArgs h, int bt_h, const XentGemmArgs w, int bt_w) {
+  if (blockIdx.y == 0 && h.out) xent_join_slices<T, XG_DH>(h, bt_h);
+  if (blockIdx.y == 1 && w.out) xent_join_slices<T, XG_DW>(w, bt_w);
+}
+
 // ---- plans
 // Elements of G at a time: half of what all classes need, 128 MiB of bf16 at least and 512 MiB at most.  A piece costs five launches and
 // a pass over the sums of dh: pieces of 128 / 256 / 512 MiB took 505 / 482 / 476 us for 12288 tokens, one in seven with a class, of
@@ -291,7 +315,7 @@ struct XentPlan {
   int64_t grad_elems, stage_rows; // of G, of a staged piece
   int bt, bt_dh, bt_dw;           // tiles of the logits and of the two products
   int blocks_dh, blocks_dw;
-  int64_t grid, grid_dh, grid_dw; // blocks
+  int64_t grid, grid_dh, grid_dw; // tiles and slices, at most
   bool join_dh, join_dw;          // K may be cut
   int64_t acc_dh, acc_dw;         // fp32 partial results
 };
@@ -304,9 +328,9 @@ static int logits_tile(int64_t T, int64_t V) {
 // tile and blocks of a product of G [N][M] over so many stages
 static int out_tile(int64_t M, int64_t N, int64_t stages, int* blocks) {
   const int64_t t256 = ceil_div(M, 256) * ceil_div(N, 256), t128 = ceil_div(M, 128) * ceil_div(N, 128);
-  if (t256 * std::max<int64_t>(1, stages / 8) >= 192 && N > 128) { *blocks = 256; return 256; }
-  if (t128 * std::max<int64_t>(1, stages / 8) >= 128 && N > 64) { *blocks = 512; return 128; }
-  *blocks = 1024;
+  if (t256 * std::max<int64_t>(1, stages / 12) >= 192 && N > 128) { *blocks = 256; return 256; }
+  if (t128 * std::max<int64_t>(1, stages / 12) >= 128 && N > 64) { *blocks = 512; return 128; }
+  *blocks = 256;
   return 64;
 }
 // most fp32 partial results of such a product: slices times rows, for every number of rows from `fewest` to N
@@ -385,19 +409,20 @@ static int launch_xent_gemm(const XentGemmArgs& g, int64_t blocks, hipStream_t s
   using C = XentCfg<BT>;
   static const hipError_t attr = hipFuncSetAttribute((const void*)k_xent_gemm<BT, MODE>, hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS);
   if (attr != hipSuccess) return EFQAT_ERR_HIP;
-  return launch((k_xent_gemm<BT, MODE>), dim3((unsigned)blocks), dim3(C::NW * 64), C::LDS, st, g);
+  return launch((k_xent_gemm<BT, MODE>), dim3((unsigned)std::min<int64_t>(blocks, C::CHIP)), dim3(C::THREADS), C::LDS, st, g);
 }
 template <XentMode MODE>
 static int launch_xent_tile(int bt, const XentGemmArgs& g, int64_t blocks, hipStream_t st) {
-  if (blocks > INT32_MAX) return EFQAT_ERR_BAD_SHAPE;
   if (bt == 256) return launch_xent_gemm<256, MODE>(g, blocks, st);
   if (bt == 128) return launch_xent_gemm<128, MODE>(g, blocks, st);
   return launch_xent_gemm<64, MODE>(g, blocks, st);
 }
-template <XentMode MODE>
-static int launch_xent_join(int bt, const XentGemmArgs& g, hipStream_t st) {
-  if (g.out_dtype == EFQAT_F32) return launch(k_xent_join_slices<float, MODE>, dim3(1024), dim3(256), 0, st, g, bt);
-  return launch(k_xent_join_slices<bf16_t, MODE>, dim3(1024), dim3(256), 0, st, g, bt);
+template <int BT>
+static int launch_xent_pair(const XentGemmArgs& h, const XentGemmArgs& w, int64_t blocks, hipStream_t st) {
+  using C = XentCfg<BT>;
+  static const hipError_t attr = hipFuncSetAttribute((const void*)k_xent_gemm_pair<BT>, hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS);
+  if (attr != hipSuccess) return EFQAT_ERR_HIP;
+  return launch(k_xent_gemm_pair<BT>, dim3((unsigned)std::min<int64_t>(blocks, C::CHIP)), dim3(C::THREADS), C::LDS, st, h, w);
 }
 
 static int stage_blocks(int64_t rows, int64_t pitch, unsigned* blocks) {
@@ -408,12 +433,17 @@ static int stage_blocks(int64_t rows, int64_t pitch, unsigned* blocks) {
   *blocks = (unsigned)n;
   return EFQAT_OK;
 }
-static int launch_stage(const XentStageArgs& g, int dtype, hipStream_t st) {
-  unsigned blocks;
-  if (const int rc = stage_blocks(std::max(g.dst_rows, g.clear ? g.T : 0), g.pitch, &blocks)) return rc;
-  if (dtype == EFQAT_F32) EFQAT_TRY(launch((k_xent_stage<float, 3>), dim3(blocks), dim3(256), 0, st, g));
-  else EFQAT_TRY(launch((k_xent_stage<bf16_t, 1>), dim3(blocks), dim3(256), 0, st, g));
-  return EFQAT_OK;
+// tokens and / or classes (NULL: none)
+static int launch_stage(const XentStageArgs* tokens, const XentStageArgs* classes, int dtype, hipStream_t st) {
+  const XentStageArgs none = {};
+  unsigned n_tokens = 0, n_classes = 0;
+  if (tokens) EFQAT_TRY(stage_blocks(std::max(tokens->dst_rows, tokens->clear ? tokens->T : 0), tokens->pitch, &n_tokens));
+  if (classes) EFQAT_TRY(stage_blocks(classes->dst_rows, classes->pitch, &n_classes));
+  if ((int64_t)n_tokens + n_classes > INT32_MAX) return EFQAT_ERR_BAD_SHAPE;
+  const dim3 grid(n_tokens + n_classes);
+  const XentStageArgs &t = tokens ? *tokens : none, &c = classes ? *classes : none;
+  if (dtype == EFQAT_F32) return launch((k_xent_stage<float, 3>), grid, dim3(256), 0, st, t, (int)n_tokens, c);
+  return launch((k_xent_stage<bf16_t, 1>), grid, dim3(256), 0, st, t, (int)n_tokens, c);
 }
 
 static XentGemmArgs xent_gemm_args(const XentPlan& p, const XentWs& k, const void* w, int64_t ldw, int64_t D) {
@@ -432,11 +462,15 @@ static XentGemmArgs xent_gemm_args(const XentPlan& p, const XentWs& k, const voi
   g.slots = p.slots;
   return g;
 }
-static int stage_piece(const XentPlan& p, const XentWs& k, const void* w, int64_t ldw, int dtype, int64_t D, int piece, hipStream_t st) {
+static XentStageArgs xent_stage_tokens(const XentPlan& p, const XentWs& k, const void* h, int64_t ldh, int64_t D) {
   XentStageArgs s = {};
-  s.src = w; s.ld = ldw; s.cols = D; s.pitch = p.Dp; s.n_valid = k.n_valid; s.pieces = p.pieces; s.piece = piece;
-  s.dst_rows = p.stage_rows; s.dst = k.w;
-  return launch_stage(s, dtype, st);
+  s.src = h; s.ld = ldh; s.cols = D; s.pitch = p.Dp; s.rows = k.rows; s.n_valid = k.n_valid; s.dst_rows = p.slots; s.dst = k.h;
+  return s;
+}
+static XentStageArgs xent_stage_classes(const XentPlan& p, const XentWs& k, const void* w, int64_t ldw, int64_t D) {
+  XentStageArgs s = {};
+  s.src = w; s.ld = ldw; s.cols = D; s.pitch = p.Dp; s.n_valid = k.n_valid; s.pieces = p.pieces; s.dst_rows = p.stage_rows; s.dst = k.w;
+  return s;
 }
 
 static bool xent_sizes_ok(int64_t T, int64_t D, int64_t V) {
@@ -478,6 +512,7 @@ extern "C" int efqat_linear_xent_fwd(const void* h, int64_t ldh, const void* w, 
   const XentPlan p = xent_plan(T, D, V, dtype, false);
   const XentWs k = xent_ws(ws, p, T, V, false);
   if (ws_bytes < k.bytes) return EFQAT_ERR_WORKSPACE;
+  if (std::max({p.grid, p.grid_dh, p.grid_dw}) > INT32_MAX / 2) return EFQAT_ERR_BAD_SHAPE;
   hipStream_t st = (hipStream_t)stream;
   const bool none = reduction == EFQAT_XENT_NONE;
 
@@ -487,25 +522,24 @@ extern "C" int efqat_linear_xent_fwd(const void* h, int64_t ldh, const void* w, 
   r.loss = none ? loss : nullptr; r.lse = lse;
   EFQAT_TRY(launch(k_xent_rows, dim3(1), dim3(1024), 0, st, r));
 
-  XentStageArgs sh = {};
-  sh.src = h; sh.ld = ldh; sh.cols = D; sh.pitch = p.Dp; sh.rows = k.rows; sh.n_valid = k.n_valid; sh.dst_rows = p.slots; sh.dst = k.h;
-  EFQAT_TRY(launch_stage(sh, dtype, st));
-
+  const XentStageArgs tokens = xent_stage_tokens(p, k, h, ldh, D);
+  XentStageArgs classes = xent_stage_classes(p, k, w, ldw, D);
   XentGemmArgs g = xent_gemm_args(p, k, w, ldw, D);
   g.part = k.part;
   g.target_logit = k.target_logit;
   for (g.piece = 0; g.piece < p.n_pieces; ++g.piece) {
-    if (p.stage_w) EFQAT_TRY(stage_piece(p, k, w, ldw, dtype, D, g.piece, st));
+    classes.piece = g.piece;
+    if (p.stage_w || g.piece == 0) EFQAT_TRY(launch_stage(g.piece == 0 ? &tokens : nullptr, p.stage_w ? &classes : nullptr, dtype, st));
     EFQAT_TRY(launch_xent_tile<XG_LSE>(p.bt, g, p.grid, st));
   }
 
   // tiles of a piece are whole but for the last piece's: pieces are multiples of 256 classes
-  EFQAT_TRY(launch(k_xent_join, dim3((unsigned)ceil_div(T, 64)), dim3(256), 0, st, k.part, (int)ceil_div(V, p.bt), (int)p.slots, k.n_valid,
-                     k.rows, k.target_logit, lse, none ? loss : (float*)nullptr, k.slot_loss));
-  if (!none) {
-    EFQAT_TRY(launch(k_xent_reduce_loss, dim3(1), dim3(1024), 0, st, k.slot_loss, k.n_valid, reduction == EFQAT_XENT_MEAN ? 1 : 0, loss));
-  }
-  return EFQAT_OK;
+  XentJoinArgs j = {};
+  j.part = k.part; j.tiles = (int)ceil_div(V, p.bt); j.slots = p.slots; j.n_valid = k.n_valid; j.rows = k.rows;
+  j.target_logit = k.target_logit; j.lse = lse; j.loss = none ? loss : nullptr; j.slot_loss = k.slot_loss;
+  EFQAT_TRY(launch(k_xent_join, dim3((unsigned)ceil_div(T, 64)), dim3(256), 0, st, j));
+  if (none) return EFQAT_OK;
+  return launch(k_xent_reduce_loss, dim3(1), dim3(1024), 0, st, k.slot_loss, k.n_valid, reduction == EFQAT_XENT_MEAN ? 1 : 0, loss);
 }
 
 extern "C" int efqat_linear_xent_bwd(const void* h, int64_t ldh, const void* w, int64_t ldw, int dtype, int64_t T, int64_t D, int64_t V,
@@ -518,6 +552,7 @@ extern "C" int efqat_linear_xent_bwd(const void* h, int64_t ldh, const void* w, 
   const XentPlan p = xent_plan(T, D, V, dtype, true);
   const XentWs k = xent_ws(ws, p, T, V, true);
   if (ws_bytes < k.bytes) return EFQAT_ERR_WORKSPACE;
+  if (std::max({p.grid, p.grid_dh, p.grid_dw}) > INT32_MAX / 2) return EFQAT_ERR_BAD_SHAPE;
   hipStream_t st = (hipStream_t)stream;
 
   XentRowsArgs r = {};
@@ -526,30 +561,35 @@ extern "C" int efqat_linear_xent_bwd(const void* h, int64_t ldh, const void* w, 
   r.lse_in = lse; r.dloss = dloss; r.reduction = reduction; r.slot_lse = k.slot_lse; r.slot_scale = k.slot_scale;
   EFQAT_TRY(launch(k_xent_rows, dim3(1), dim3(1024), 0, st, r));
 
-  XentStageArgs sh = {};
-  sh.src = h; sh.ld = ldh; sh.cols = D; sh.pitch = p.Dp; sh.rows = k.rows; sh.n_valid = k.n_valid; sh.dst_rows = p.slots; sh.dst = k.h;
-  sh.targets = targets; sh.T = T; sh.V = V; sh.ignore = ignore_index; sh.clear = dh; sh.ld_clear = lddh;
-  EFQAT_TRY(launch_stage(sh, dtype, st));
-
+  XentStageArgs tokens = xent_stage_tokens(p, k, h, ldh, D), classes = xent_stage_classes(p, k, w, ldw, D);
+  tokens.targets = targets; tokens.T = T; tokens.V = V; tokens.ignore = ignore_index; tokens.clear = dh; tokens.ld_clear = lddh;
   XentGemmArgs g = xent_gemm_args(p, k, w, ldw, D);
   g.lse = k.slot_lse;
   g.scale = k.slot_scale;
   g.mean = reduction == EFQAT_XENT_MEAN ? 1 : 0;
   g.out_dtype = dtype;
   for (g.piece = 0; g.piece < p.n_pieces; ++g.piece) {
-    if (p.stage_w) EFQAT_TRY(stage_piece(p, k, w, ldw, dtype, D, g.piece, st));
+    classes.piece = g.piece;
+    if (p.stage_w || g.piece == 0) EFQAT_TRY(launch_stage(g.piece == 0 ? &tokens : nullptr, p.stage_w ? &classes : nullptr, dtype, st));
     EFQAT_TRY(launch_xent_tile<XG_GRAD>(p.bt, g, p.grid, st));
-    if (dw) {
-      XentGemmArgs q = g;
-      q.split_blocks = p.blocks_dw; q.acc = k.acc_dw; q.out = dw; q.ldo = lddw;
-      EFQAT_TRY(launch_xent_tile<XG_DW>(p.bt_dw, q, p.grid_dw, st));
-      if (p.join_dw) EFQAT_TRY(launch_xent_join<XG_DW>(p.bt_dw, q, st));
+    XentGemmArgs gh = g, gw = g;
+    gh.split_blocks = p.blocks_dh; gh.acc = k.acc_dh; gh.out = dh; gh.ldo = lddh; gh.rows = k.rows;
+    gw.split_blocks = p.blocks_dw; gw.acc = k.acc_dw; gw.out = dw; gw.ldo = lddw;
+    if (dh && dw && p.bt_dh == p.bt_dw) {
+      const int64_t blocks = p.grid_dh + p.grid_dw;
+      EFQAT_TRY(p.bt_dh == 256   ? launch_xent_pair<256>(gh, gw, blocks, st)
+                : p.bt_dh == 128 ? launch_xent_pair<128>(gh, gw, blocks, st)
+                                 : launch_xent_pair<64>(gh, gw, blocks, st));
+    } else {
+      if (dh) EFQAT_TRY(launch_xent_tile<XG_DH>(p.bt_dh, gh, p.grid_dh, st));
+      if (dw) EFQAT_TRY(launch_xent_tile<XG_DW>(p.bt_dw, gw, p.grid_dw, st));
     }
-    if (dh) {
-      XentGemmArgs q = g;
-      q.split_blocks = p.blocks_dh; q.acc = k.acc_dh; q.out = dh; q.ldo = lddh; q.rows = k.rows;
-      EFQAT_TRY(launch_xent_tile<XG_DH>(p.bt_dh, q, p.grid_dh, st));
-      if (p.join_dh && g.piece == p.n_pieces - 1) EFQAT_TRY(launch_xent_join<XG_DH>(p.bt_dh, q, st));
+    if (!p.join_dh || g.piece < p.n_pieces - 1) gh.out = nullptr;
+    if (!p.join_dw) gw.out = nullptr;
+    if (gh.out || gw.out) {
+      const dim3 grid(1024, gw.out ? 2 : 1);
+      EFQAT_TRY(dtype == EFQAT_F32 ? launch(k_xent_join_slices<float>, grid, dim3(256), 0, st, gh, p.bt_dh, gw, p.bt_dw)
+                                   : launch(k_xent_join_slices<bf16_t>, grid, dim3(256), 0, st, gh, p.bt_dh, gw, p.bt_dw));
     }
   }
   return EFQAT_OK;

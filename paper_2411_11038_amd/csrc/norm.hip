@@ -95,7 +95,8 @@ __global__ __launch_bounds__(THREADS) void k_norm_fwd(const NormFwdArgs g) {
   constexpr int RPB = THREADS / TPR;
   __shared__ float2 sums[2][THREADS / 64];
   RowSum<THREADS, TPR> row_sum{sums};
-  const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+  const int t = threadIdx.x % TPR;
+  const int sub = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);             // rows are whole wavefronts': their addresses are scalar
   ChunkPlace at[NIT];
   float w[NIT][8], b[NIT][8];
 #pragma unroll
@@ -126,13 +127,23 @@ __global__ __launch_bounds__(THREADS) void k_norm_fwd(const NormFwdArgs g) {
       for (int j = 0; j < 8; ++j) s += v[i][j];
     float mean = row_sum(s) * inv_cols, q = 0.0f, rest = 0.0f;
 #pragma unroll
-    for (int i = 0; i < NIT; ++i)
+    for (int i = 0; i < NIT; ++i) {
+      if (at[i].n == 8) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float d = j < at[i].n ? v[i][j] - mean : 0.0f;
-        rest += d;
-        q = fmaf(d, d, q);
+        for (int j = 0; j < 8; ++j) {
+          const float d = v[i][j] - mean;
+          rest += d;
+          q = fmaf(d, d, q);
+        }
+      } else if (at[i].n > 0) {
+#pragma unroll
+        for (int j = 0; j < 7; ++j) {
+          const float d = j < at[i].n ? v[i][j] - mean : 0.0f;
+          rest += d;
+          q = fmaf(d, d, q);
+        }
       }
+    }
     const float rstd = norm_rstd(row_sum(rest, q), inv_cols, g.eps, &mean);
     if (row >= g.rows) continue;                      // the whole wavefront: its lanes are of one row
     if (t == 0) {
@@ -264,7 +275,8 @@ __global__ __launch_bounds__(THREADS, 4) void k_norm_bwd(const NormBwdArgs g) {
   __shared__ float2 sums[2][THREADS / 64];
   __shared__ float red[RPB > 1 ? THREADS * 16 : 1];
   RowSum<THREADS, TPR> row_sum{sums};
-  const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+  const int t = threadIdx.x % TPR;
+  const int sub = __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);             // rows are whole wavefronts': their addresses are scalar
   ChunkPlace at[NIT];
   float w[NIT][8], aw[NIT][8], ab[NIT][8];
 #pragma unroll

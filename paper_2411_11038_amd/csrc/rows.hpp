@@ -101,19 +101,22 @@ struct ChunkPlace {
     n = 8 - shift;
   }
 };
-// element j + shift in the place of element j
+// element j + shift in the place of element j, shift < 8
 __device__ __forceinline__ void move_down(float (&v)[8], int shift) {
 #pragma unroll
   for (int s = 4; s > 0; s >>= 1)
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = shift & s ? (j + s < 8 ? v[j + s < 8 ? j + s : 7] : 0.0f) : v[j];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] = shift >= 8 ? 0.0f : v[j];
 }
 template <typename T>
 __device__ __forceinline__ void get_chunk(const Raw8<T>& r, const ChunkPlace& c, float (&v)[8]) {
   r.get(v);
-  if (c.shift) move_down(v, c.shift);
+  if (c.shift >= 8) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+  } else if (c.shift > 0) {
+    move_down(v, c.shift);
+  }
 }
 
 // ---- the 8-bit checkpoint: bytes a row of codes takes, scales a row has
@@ -158,18 +161,22 @@ __device__ __forceinline__ uint2 ckpt_encode(const float (&v)[8], float* scale) 
   s = s < 0x1p-126f ? 0x1p-126f : s;
   *scale = s;
   const float inv = 1.0f / s;
-  uint32_t w[2] = {0, 0};
+  // the product is rounded first, then to an integer by the addition: the lowest byte of 1.5 2^23 + q is q in two's complement
+  uint32_t t[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const int q = (int)rintf(__builtin_amdgcn_fmed3f(v[j] * inv, -127.0f, 127.0f));
-    w[j >> 2] |= (uint32_t)(q & 0xFF) << (8 * (j & 3));
-  }
-  return make_uint2(w[0], w[1]);
+  for (int j = 0; j < 8; ++j) t[j] = __float_as_uint(__fadd_rn(__fmul_rn(v[j], inv), 12582912.0f));
+  auto four = [&](int j) {                            // the lowest bytes of four words
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(t[j + 3], t[j + 2], 0x0C0C0400u), __builtin_amdgcn_perm(t[j + 1], t[j], 0x0C0C0400u),
+                                 0x05040100u);
+  };
+  return make_uint2(four(0), four(4));
 }
+// code * scale, rounded once: with the sign bit turned a byte is code + 128, and 128 * scale is exact
 __device__ __forceinline__ void ckpt_decode(uint2 codes, float scale, float (&v)[8]) {
+  const float base = -128.0f * scale;
+  const uint32_t w[2] = {codes.x ^ 0x80808080u, codes.y ^ 0x80808080u};
 #pragma unroll
-  for (int j = 0; j < 8; ++j)
-    v[j] = (float)(int8_t)((j < 4 ? codes.x : codes.y) >> (8 * (j & 3))) * scale;
+  for (int j = 0; j < 8; ++j) v[j] = fmaf((float)((w[j >> 2] >> (8 * (j & 3))) & 0xFFu), scale, base);
 }
 
 // Launches a kernel and says whether that went well by what the launch itself returns: the last error of the thread may be one

@@ -524,10 +524,74 @@ def conv_bwd(dy, x_codes, x_clip, x, s_x, z_x, w_codes, w_clip, w, s_w, idx, str
 
 
 # ------------------------------------------------------------------ 8-bit checkpoints, activation, layer norm
+# Sizes, row strides and types of these calls are read, and their arguments checked, by the marshalling module, which also makes the
+# tensors that `out` does not have.
 CKPT8_GROUP = 128
 ACT_GELU, ACT_SILU = 0, 1
-_LIKE, _F32, _I8, _I32, _U8 = range(5)                 # types of _native().empty
-_TORCH = {_F32: torch.float32, _I8: torch.int8, _I32: torch.int32}
+
+
+def _results(r, where):
+    if type(r) is int:
+        raise EfqatError(r, where)
+    return r
+
+
+def ckpt8_save(x, out=None):
+    """8-bit checkpoint of x [rows, cols] (rows may lie apart).  Returns (codes, scales); `out` may carry them as
+    x_codes, x_scales."""
+    more = (out.get("x_codes"), out.get("x_scales")) if out else ()
+    return _results((_NATIVE or _native()).ckpt8_save(x, *more), "efqat_ckpt8_save")
+
+
+def ckpt8_load(codes, scales, cols, dtype=torch.bfloat16, out=None):
+    """The values that a checkpoint of rows of `cols` columns holds, [rows, cols] (`out`: there, its rows may lie apart)."""
+    if out is None:
+        if dtype not in _DTYPES:
+            raise TypeError(f"unsupported dtype {dtype}")
+        r = (_NATIVE or _native()).ckpt8_load(codes, scales, cols, dtype is torch.bfloat16)
+    else:
+        r = (_NATIVE or _native()).ckpt8_load(codes, scales, cols, False, out)
+    return _results(r, "efqat_ckpt8_load")[0]
+
+
+def act_fwd(x, kind, up=None, checkpoint=False, out=None):
+    """y = f(x), or f(x) * up, for x, up [rows, cols] (rows may lie apart); checkpoint: their 8-bit checkpoints too.  Returns
+    dict(y, x_codes, x_scales, up_codes, up_scales); `out` may carry preallocated ones."""
+    g = out.get if out else None
+    more = (g("y"), g("x_codes"), g("x_scales"), g("up_codes"), g("up_scales")) if out else ()
+    y, xc, xs, uc, us = _results((_NATIVE or _native()).act_fwd(x, kind, up, checkpoint, *more), "efqat_act_fwd")
+    return {"y": y, "x_codes": xc, "x_scales": xs, "up_codes": uc, "up_scales": us}
+
+
+def act_bwd(dy, kind, x_codes, x_scales, up_codes=None, up_scales=None, out=None):
+    """Backward of act_fwd from the checkpoints that it left.  Returns dict(dx, dup); `out` may carry them (rows may lie
+    apart)."""
+    more = (out.get("dx"), out.get("dup")) if out else ()
+    dx, dup = _results((_NATIVE or _native()).act_bwd(dy, kind, x_codes, x_scales, up_codes, up_scales, *more), "efqat_act_bwd")
+    return {"dx": dx, "dup": dup}
+
+
+def layer_norm_fwd(x, weight=None, bias=None, eps=1e-5, checkpoint=False, out=None):
+    """Layer norm of x [rows, cols] (rows may lie apart); weight, bias fp32 [cols] or None; checkpoint: the 8-bit checkpoint of
+    x too.  Returns dict(y, mean, rstd, x_codes, x_scales); `out` may carry preallocated ones."""
+    g = out.get if out else None
+    more = (g("y"), g("mean"), g("rstd"), g("x_codes"), g("x_scales")) if out else ()
+    y, mean, rstd, xc, xs = _results((_NATIVE or _native()).layer_norm_fwd(x, weight, bias, eps, checkpoint, *more), "efqat_layer_norm_fwd")
+    return {"y": y, "mean": mean, "rstd": rstd, "x_codes": xc, "x_scales": xs}
+
+
+def layer_norm_bwd(dy, weight, mean, rstd, x=None, x_codes=None, x_scales=None, ws=None, out=None):
+    """Backward of layer_norm_fwd from x, or from the checkpoint that it left.  Returns dict(dx, dweight, dbias); `out` may
+    carry preallocated ones."""
+    more = (out.get("dx"), out.get("dweight"), out.get("dbias")) if out else ()
+    dx, dw, db = _results((_NATIVE or _native()).layer_norm_bwd(dy, weight, mean, rstd, x, x_codes, x_scales, ws, *more), "efqat_layer_norm_bwd")
+    return {"dx": dx, "dweight": dw, "dbias": db}
+
+
+# ------------------------------------------------------------------ softmax cross entropy over a vocabulary
+XENT_NONE, XENT_MEAN, XENT_SUM = 0, 1, 2
+_LIKE, _F32, _I32, _U8 = 0, 1, 3, 4                    # types of _native().empty
+_TORCH = {_F32: torch.float32, _I32: torch.int32}
 
 
 def _like(t, shape, dtype, what):
@@ -554,15 +618,6 @@ def _outputs(like, out, names, spec):
     return res
 
 
-def _kept_spec(rows, cols):
-    return (_I8, rows, -(-cols // 16) * 16, _F32, rows, -(-cols // CKPT8_GROUP))
-
-
-def _kept_shape(codes, scales, rows, cols, what="x"):
-    _like(codes, (rows, -(-cols // 16) * 16), torch.int8, what + "_codes")
-    _like(scales, (rows, -(-cols // CKPT8_GROUP)), torch.float32, what + "_scales")
-
-
 def _rows_cols(x):
     if x.dim() != 2:
         raise ValueError("tensor must be two-dimensional with contiguous rows")
@@ -573,115 +628,6 @@ def _ld(t):
     """Elements from one row to the next."""
     rows, cols = t.shape
     return t.stride(0) if rows > 1 else cols
-
-
-def ckpt8_save(x, out=None):
-    """8-bit checkpoint of x [rows, cols] (rows may lie apart).  Returns (codes, scales); `out` may carry them as
-    x_codes, x_scales."""
-    rows, cols = _rows_cols(x)
-    codes, scales = _outputs(x, out, ("x_codes", "x_scales"), _kept_spec(rows, cols))
-    _check(_native().ckpt8_save(x, _ld(x), _dt(x), rows, cols, codes, scales, _STREAM), "efqat_ckpt8_save")
-    return codes, scales
-
-
-def ckpt8_load(codes, scales, cols, dtype=torch.bfloat16, out=None):
-    """The values that a checkpoint of rows of `cols` columns holds, [rows, cols]."""
-    rows = codes.shape[0]
-    _kept_shape(codes, scales, rows, cols)
-    if out is None:
-        out = torch.empty((rows, cols), dtype=dtype, device=codes.device)
-    else:
-        _like(out, (rows, cols), out.dtype, "out")
-    _check(_native().ckpt8_load(codes, scales, rows, cols, out, _ld(out), _dt(out), _STREAM), "efqat_ckpt8_load")
-    return out
-
-
-def act_fwd(x, kind, up=None, checkpoint=False, out=None):
-    """y = f(x), or f(x) * up, for x, up [rows, cols] (rows may lie apart); checkpoint: their 8-bit checkpoints too.  Returns
-    dict(y, x_codes, x_scales, up_codes, up_scales); `out` may carry preallocated ones."""
-    rows, cols = _rows_cols(x)
-    ldx, ldu = _ld(x), 0
-    if up is not None:
-        _like(up, (rows, cols), x.dtype, "up")
-        ldu = _ld(up)
-    xc = xs = uc = us = None
-    if not checkpoint:
-        y, = _outputs(x, out, ("y",), (_LIKE, rows, cols))
-    elif up is None:
-        y, xc, xs = _outputs(x, out, ("y", "x_codes", "x_scales"), (_LIKE, rows, cols) + _kept_spec(rows, cols))
-    else:
-        y, xc, xs, uc, us = _outputs(x, out, ("y", "x_codes", "x_scales", "up_codes", "up_scales"),
-                                     (_LIKE, rows, cols) + 2 * _kept_spec(rows, cols))
-    _check(_native().act_fwd(x, ldx, up, ldu, _dt(x), rows, cols, kind, y, _ld(y), xc, xs, uc, us, _STREAM), "efqat_act_fwd")
-    return dict(y=y, x_codes=xc, x_scales=xs, up_codes=uc, up_scales=us)
-
-
-def act_bwd(dy, kind, x_codes, x_scales, up_codes=None, up_scales=None, out=None):
-    """Backward of act_fwd from the checkpoints that it left.  Returns dict(dx, dup); `out` may carry them (rows may lie
-    apart)."""
-    rows, cols = _rows_cols(dy)
-    _kept_shape(x_codes, x_scales, rows, cols)
-    if up_codes is None and up_scales is None:
-        dx, = _outputs(dy, out, ("dx",), (_LIKE, rows, cols))
-        dup, lddup = None, 0
-    else:
-        if up_codes is None or up_scales is None:
-            raise ValueError("up_codes and up_scales belong together")
-        _kept_shape(up_codes, up_scales, rows, cols, "up")
-        dx, dup = _outputs(dy, out, ("dx", "dup"), (_LIKE, rows, cols, _LIKE, rows, cols))
-        lddup = _ld(dup)
-    _check(_native().act_bwd(dy, _ld(dy), _dt(dy), rows, cols, kind, x_codes, x_scales, up_codes, up_scales, dx, _ld(dx), dup,
-                             lddup, _STREAM), "efqat_act_bwd")
-    return dict(dx=dx, dup=dup)
-
-
-def layer_norm_fwd(x, weight=None, bias=None, eps=1e-5, checkpoint=False, out=None):
-    """Layer norm of x [rows, cols] (rows may lie apart); weight, bias fp32 [cols] or None; checkpoint: the 8-bit checkpoint of
-    x too.  Returns dict(y, mean, rstd, x_codes, x_scales); `out` may carry preallocated ones."""
-    rows, cols = _rows_cols(x)
-    if weight is not None:
-        _like(weight, (cols,), torch.float32, "weight")
-    if bias is not None:
-        _like(bias, (cols,), torch.float32, "bias")
-    xc = xs = None
-    spec = (_LIKE, rows, cols, _F32, rows, -1, _F32, rows, -1)
-    if checkpoint:
-        y, mean, rstd, xc, xs = _outputs(x, out, ("y", "mean", "rstd", "x_codes", "x_scales"), spec + _kept_spec(rows, cols))
-    else:
-        y, mean, rstd = _outputs(x, out, ("y", "mean", "rstd"), spec)
-    _check(_native().layer_norm_fwd(x, _ld(x), _dt(x), rows, cols, weight, bias, eps, y, _ld(y), mean, rstd, xc, xs, _STREAM),
-           "efqat_layer_norm_fwd")
-    return dict(y=y, mean=mean, rstd=rstd, x_codes=xc, x_scales=xs)
-
-
-def layer_norm_bwd(dy, weight, mean, rstd, x=None, x_codes=None, x_scales=None, ws=None, out=None):
-    """Backward of layer_norm_fwd from x, or from the checkpoint that it left.  Returns dict(dx, dweight, dbias); `out` may
-    carry preallocated ones."""
-    rows, cols = _rows_cols(dy)
-    ldx = 0
-    if x is not None:
-        _like(x, (rows, cols), dy.dtype, "x")
-        ldx = _ld(x)
-        x_codes = x_scales = None
-    elif x_codes is None or x_scales is None:
-        raise ValueError("x, or x_codes and x_scales, expected")
-    else:
-        _kept_shape(x_codes, x_scales, rows, cols)
-    if weight is not None:
-        _like(weight, (cols,), torch.float32, "weight")
-    _like(mean, (rows,), torch.float32, "mean")
-    _like(rstd, (rows,), torch.float32, "rstd")
-    native = _native()
-    dx, dweight, dbias = _outputs(dy, out, ("dx", "dweight", "dbias"), (_LIKE, rows, cols, _F32, cols, -1, _F32, cols, -1))
-    if ws is None:
-        ws, = native.empty(dy, _U8, native.layer_norm_bwd_workspace_bytes(rows, cols), -1)
-    _check(native.layer_norm_bwd(dy, _ld(dy), _dt(dy), x, ldx, x_codes, x_scales, mean, rstd, weight, rows, cols, dx, _ld(dx), dweight,
-                                 dbias, ws, ws.numel(), _STREAM), "efqat_layer_norm_bwd")
-    return dict(dx=dx, dweight=dweight, dbias=dbias)
-
-
-# ------------------------------------------------------------------ softmax cross entropy over a vocabulary
-XENT_NONE, XENT_MEAN, XENT_SUM = 0, 1, 2
 
 
 def _xent_shapes(h, w, targets):

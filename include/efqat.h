@@ -453,7 +453,8 @@ int efqat_layer_norm_bwd(const void* dy, int64_t lddy, int dtype, const void* x,
  *                F32 the products are formed from three bf16 parts of every operand, which keep 24 bits (infinite
  *                elements of h and w count as +-3.39e38).
  * Sums are fp32, in a fixed order (bit-reproducible).  Both calls count and gather the tokens on the device; nothing
- * waits for the host.  At most 2^30 tokens and classes, D <= 2^20. */
+ * waits for the host.  At most 2^30 tokens and classes (and 2^30 tiles of 64 x 64 to 256 x 256 logits), D <= 2^20,
+ * ldw <= 2^22. */
 #define EFQAT_XENT_NONE 0
 #define EFQAT_XENT_MEAN 1
 #define EFQAT_XENT_SUM 2

@@ -16,7 +16,7 @@
 
 namespace efqat {
 
-// ---- tokens that have a class: their rows, classes and scales by slot
+// ---- tokens that have a class: their rows, classes and scales by slot (few tokens: see xent_few_rows)
 struct XentRowsArgs {
   const int64_t* targets;
   int64_t T, V, ignore;
@@ -27,88 +27,70 @@ struct XentRowsArgs {
   int reduction;
   float *slot_lse, *slot_scale;
 };
-// One block walks the tokens, 16 x 1024 a round.  A wavefront's 64 neighbouring tokens are counted by one ballot; the 256 counts of a
-// round are scanned by one wavefront, so that slots are in the order of the tokens and every access is of neighbours.
-constexpr int kXentHeld = 16;
+// A block places 2048 tokens: it counts those with a class among all tokens before its own (eight reads in flight a lane), then ranks its
+// own by ballots, so that slots are in the order of the tokens and every access is of neighbours.  One block for all took 9 us for 12288
+// tokens.
+constexpr int kXentOwn = 2;                           // tokens of a thread
 __global__ __launch_bounds__(1024) void k_xent_rows(const XentRowsArgs g) {
-  __shared__ int before[kXentHeld * 16];
-  __shared__ int round_total;
+  __shared__ int earlier[16], count[kXentOwn * 16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int total = 0;
-  const float up = g.slot_scale && g.reduction != EFQAT_XENT_NONE && g.dloss ? g.dloss[0] : 1.0f;
-  const float* ups = g.reduction == EFQAT_XENT_NONE ? g.dloss : nullptr;
-  for (int64_t t0 = 0; t0 < g.T; t0 += kXentHeld * 1024) {
-    const int64_t t = t0 + threadIdx.x;
-    int64_t c[kXentHeld];
-    float lse[kXentHeld], scale[kXentHeld];
+  const int64_t t0 = (int64_t)blockIdx.x * kXentOwn * 1024, t = t0 + threadIdx.x;
+  auto has_class = [&](int64_t c) { return c >= 0 && c < g.V && c != g.ignore; };
+  int64_t c[kXentOwn];
 #pragma unroll
-    for (int i = 0; i < kXentHeld; ++i) c[i] = t + i * 1024 < g.T ? g.targets[t + i * 1024] : -1;
-    if (g.slot_scale) {
+  for (int i = 0; i < kXentOwn; ++i) c[i] = t + i * 1024 < g.T ? g.targets[t + i * 1024] : -1;
+  int before = 0;
+  for (int64_t u0 = 0; u0 < t0; u0 += 8 * 1024) {
+    int64_t v[8];
 #pragma unroll
-      for (int i = 0; i < kXentHeld; ++i) {
-        const bool in = t + i * 1024 < g.T;
-        lse[i] = in ? g.lse_in[t + i * 1024] : 0.0f;
-        scale[i] = in && ups ? ups[t + i * 1024] : up;
-      }
+    for (int i = 0; i < 8; ++i) {
+      const int64_t u = u0 + i * 1024 + threadIdx.x;
+      v[i] = g.targets[u < t0 ? u : threadIdx.x];
     }
-    uint64_t who[kXentHeld];
 #pragma unroll
-    for (int i = 0; i < kXentHeld; ++i) {
-      who[i] = __ballot(c[i] >= 0 && c[i] < g.V && c[i] != g.ignore);
-      if (lane == 0) before[i * 16 + wave] = __popcll(who[i]);
-    }
-    __syncthreads();
-    if (wave == 0) {
-      int n[4], mine = 0;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        n[j] = before[4 * lane + j];
-        mine += n[j];
-      }
-      int sum = mine;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const int v = __shfl_up(sum, o);
-        sum += lane >= o ? v : 0;
-      }
-      int at = sum - mine;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        before[4 * lane + j] = at;
-        at += n[j];
-      }
-      if (lane == 63) round_total = sum;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kXentHeld; ++i) {
-      const int64_t ti = t + i * 1024;
-      if (ti >= g.T) break;
-      if (who[i] >> lane & 1) {
-        const int slot = total + before[i * 16 + wave] + __popcll(who[i] & ((UINT64_C(1) << lane) - 1));
-        g.rows[slot] = (int32_t)ti;
-        g.target[slot] = (int32_t)c[i];
-        if (g.slot_scale) {
-          g.slot_lse[slot] = lse[i];
-          g.slot_scale[slot] = scale[i];
-        }
-      } else {
-        if (g.loss) g.loss[ti] = 0.0f;
-        if (g.lse) g.lse[ti] = 0.0f;
-      }
-    }
-    total += round_total;
-    __syncthreads();
+    for (int i = 0; i < 8; ++i) before += __popcll(__ballot(u0 + i * 1024 < t0 && has_class(v[i])));
   }
-  if (threadIdx.x == 0) {
+  uint64_t who[kXentOwn];
+#pragma unroll
+  for (int i = 0; i < kXentOwn; ++i) {
+    who[i] = __ballot(has_class(c[i]));
+    if (lane == 0) count[i * 16 + wave] = __popcll(who[i]);
+  }
+  if (lane == 0) earlier[wave] = before;
+  __syncthreads();
+  int total = 0;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) total += earlier[w];
+  const float up = g.slot_scale && g.reduction != EFQAT_XENT_NONE && g.dloss ? g.dloss[0] : 1.0f;
+#pragma unroll
+  for (int i = 0; i < kXentOwn; ++i) {
+    int slot = total + __popcll(who[i] & ((UINT64_C(1) << lane) - 1));
+#pragma unroll
+    for (int w = 0; w < 16; ++w) {
+      slot += w < wave ? count[i * 16 + w] : 0;
+      total += count[i * 16 + w];
+    }
+    const int64_t ti = t + i * 1024;
+    if (who[i] >> lane & 1) {
+      g.rows[slot] = (int32_t)ti;
+      g.target[slot] = (int32_t)c[i];
+      if (g.slot_scale) {
+        g.slot_lse[slot] = g.lse_in[ti];
+        g.slot_scale[slot] = g.reduction == EFQAT_XENT_NONE && g.dloss ? g.dloss[ti] : up;
+      }
+    } else if (ti < g.T) {
+      if (g.loss) g.loss[ti] = 0.0f;
+      if (g.lse) g.lse[ti] = 0.0f;
+    }
+  }
+  if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) {
     g.n_valid[0] = total;
     if (g.n_out) g.n_out[0] = total;
   }
 }
 
 // ---- operands in bf16, in rows of whole K stages -> dst [row][PARTS][pitch], zeros behind the columns and the rows.  Tokens: the rows
-// rows[] of the slots that exist, zeros in the others; backward, rows of dh without a class are cleared on the way.  Classes: those of
-// a piece, zeros up to whole stages.
+// rows[] of the slots that exist; backward, rows of dh without a class are cleared on the way.  Classes: those of a piece.
 struct XentStageArgs {
   const void* src;
   int64_t ld;
@@ -123,14 +105,70 @@ struct XentStageArgs {
   void* clear;
   int64_t ld_clear;
 };
-// tokens (blocks 0 .. first - 1) and classes (the others) in one launch
-template <typename T, int PARTS>
-__global__ __launch_bounds__(256) void k_xent_stage(const XentStageArgs tokens, int first_blocks, const XentStageArgs classes) {
+// What k_xent_rows does, by every block of 256 threads for itself, for up to kXentFew tokens: the rows by slot, and their number.  The
+// block that writes leaves all of it in memory for the kernels that follow.
+constexpr int kXentFew = 1024;
+__device__ __forceinline__ int xent_few_rows(const XentRowsArgs& g, bool writes, int* row_of_slot) {
+  __shared__ int count[16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int64_t c[4];
+  uint64_t who[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int t = i * 256 + threadIdx.x;
+    c[i] = t < g.T ? g.targets[t] : -1;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    who[i] = __ballot(c[i] >= 0 && c[i] < g.V && c[i] != g.ignore);
+    if (lane == 0) count[i * 4 + wave] = __popcll(who[i]);
+  }
+  __syncthreads();
+  int total = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int t = i * 256 + threadIdx.x;
+    int slot = __popcll(who[i] & ((UINT64_C(1) << lane) - 1)) + total;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      slot += w < wave ? count[i * 4 + w] : 0;
+      total += count[i * 4 + w];
+    }
+    if (who[i] >> lane & 1) {
+      row_of_slot[slot] = t;
+      if (writes) {
+        g.rows[slot] = t;
+        g.target[slot] = (int32_t)c[i];
+        if (g.slot_scale) {
+          g.slot_lse[slot] = g.lse_in[t];
+          g.slot_scale[slot] = g.dloss ? g.dloss[g.reduction == EFQAT_XENT_NONE ? t : 0] : 1.0f;
+        }
+      }
+    } else if (writes && t < g.T) {
+      if (g.loss) g.loss[t] = 0.0f;
+      if (g.lse) g.lse[t] = 0.0f;
+    }
+  }
+  if (writes && threadIdx.x == 0) {
+    g.n_valid[0] = total;
+    if (g.n_out) g.n_out[0] = total;
+  }
+  __syncthreads();
+  return total;
+}
+
+// tokens (blocks 0 .. first - 1) and classes (the others) in one launch; FEW: it finds the tokens that have a class itself
+template <typename T, int PARTS, bool FEW>
+__global__ __launch_bounds__(256) void k_xent_stage(const XentStageArgs tokens, int first_blocks, const XentStageArgs classes, const XentRowsArgs few) {
+  __shared__ int row_of_slot[FEW ? kXentFew : 1];
   const bool second = (int)blockIdx.x >= first_blocks;
   const XentStageArgs& g = second ? classes : tokens;
   const int64_t block = second ? (int64_t)blockIdx.x - first_blocks : blockIdx.x;
-  const int valid = g.n_valid[0];
-  int64_t n = valid, first = 0, dst_rows = g.dst_rows;
+  int valid;
+  if constexpr (FEW) valid = xent_few_rows(few, blockIdx.x == 0, row_of_slot);
+  else valid = g.n_valid[0];
+  // rows behind the last one: zeros up to whole stages, which dW's contraction (tokens) and dH's (classes) read
+  int64_t n = valid, first = 0, dst_rows = (n + 63) / 64 * 64;
   if (!g.rows) {
     const int64_t p = g.pieces.size(valid);
     first = p * g.piece;
@@ -145,7 +183,7 @@ __global__ __launch_bounds__(256) void k_xent_stage(const XentStageArgs tokens, 
   const int lane = threadIdx.x % lanes;
   if (r < dst_rows) {
     const bool in = r < n;
-    const T* src = (const T*)g.src + (in ? (g.rows ? (int64_t)g.rows[r] : first + r) : 0) * g.ld;
+    const T* src = (const T*)g.src + (in ? (!g.rows ? first + r : FEW ? (int64_t)row_of_slot[r] : (int64_t)g.rows[r]) : 0) * g.ld;
     bf16_t* dst = g.dst + r * PARTS * g.pitch;
     for (int c = lane; c < chunks; c += lanes) {
       const int64_t left = in ? g.cols - 8 * (int64_t)c : 0;
@@ -433,8 +471,8 @@ static int stage_blocks(int64_t rows, int64_t pitch, unsigned* blocks) {
   *blocks = (unsigned)n;
   return EFQAT_OK;
 }
-// tokens and / or classes (NULL: none)
-static int launch_stage(const XentStageArgs* tokens, const XentStageArgs* classes, int dtype, hipStream_t st) {
+// tokens and / or classes (NULL: none).  rows: with up to kXentFew tokens, what would have been k_xent_rows' arguments
+static int launch_stage(const XentStageArgs* tokens, const XentStageArgs* classes, const XentRowsArgs* rows, int dtype, hipStream_t st) {
   const XentStageArgs none = {};
   unsigned n_tokens = 0, n_classes = 0;
   if (tokens) EFQAT_TRY(stage_blocks(std::max(tokens->dst_rows, tokens->clear ? tokens->T : 0), tokens->pitch, &n_tokens));
@@ -442,8 +480,12 @@ static int launch_stage(const XentStageArgs* tokens, const XentStageArgs* classe
   if ((int64_t)n_tokens + n_classes > INT32_MAX) return EFQAT_ERR_BAD_SHAPE;
   const dim3 grid(n_tokens + n_classes);
   const XentStageArgs &t = tokens ? *tokens : none, &c = classes ? *classes : none;
-  if (dtype == EFQAT_F32) return launch((k_xent_stage<float, 3>), grid, dim3(256), 0, st, t, (int)n_tokens, c);
-  return launch((k_xent_stage<bf16_t, 1>), grid, dim3(256), 0, st, t, (int)n_tokens, c);
+  const XentRowsArgs no_rows = {}, &r = rows ? *rows : no_rows;
+#define EFQAT_STAGE(E, PARTS, FEW) return launch((k_xent_stage<E, PARTS, FEW>), grid, dim3(256), 0, st, t, (int)n_tokens, c, r)
+  if (dtype == EFQAT_F32) { if (rows) EFQAT_STAGE(float, 3, true); EFQAT_STAGE(float, 3, false); }
+  if (rows) EFQAT_STAGE(bf16_t, 1, true);
+  EFQAT_STAGE(bf16_t, 1, false);
+#undef EFQAT_STAGE
 }
 
 static XentGemmArgs xent_gemm_args(const XentPlan& p, const XentWs& k, const void* w, int64_t ldw, int64_t D) {
@@ -520,7 +562,8 @@ extern "C" int efqat_linear_xent_fwd(const void* h, int64_t ldh, const void* w, 
   r.targets = targets; r.T = T; r.V = V; r.ignore = ignore_index;
   r.rows = k.rows; r.target = k.target; r.n_valid = k.n_valid; r.n_out = n_valid;
   r.loss = none ? loss : nullptr; r.lse = lse;
-  EFQAT_TRY(launch(k_xent_rows, dim3(1), dim3(1024), 0, st, r));
+  const bool few = T <= kXentFew;
+  if (!few) EFQAT_TRY(launch(k_xent_rows, dim3((unsigned)ceil_div(T, kXentOwn * 1024)), dim3(1024), 0, st, r));
 
   const XentStageArgs tokens = xent_stage_tokens(p, k, h, ldh, D);
   XentStageArgs classes = xent_stage_classes(p, k, w, ldw, D);
@@ -529,7 +572,7 @@ extern "C" int efqat_linear_xent_fwd(const void* h, int64_t ldh, const void* w, 
   g.target_logit = k.target_logit;
   for (g.piece = 0; g.piece < p.n_pieces; ++g.piece) {
     classes.piece = g.piece;
-    if (p.stage_w || g.piece == 0) EFQAT_TRY(launch_stage(g.piece == 0 ? &tokens : nullptr, p.stage_w ? &classes : nullptr, dtype, st));
+    if (p.stage_w || g.piece == 0) EFQAT_TRY(launch_stage(g.piece == 0 ? &tokens : nullptr, p.stage_w ? &classes : nullptr, few && g.piece == 0 ? &r : nullptr, dtype, st));
     EFQAT_TRY(launch_xent_tile<XG_LSE>(p.bt, g, p.grid, st));
   }
 
@@ -559,7 +602,8 @@ extern "C" int efqat_linear_xent_bwd(const void* h, int64_t ldh, const void* w, 
   r.targets = targets; r.T = T; r.V = V; r.ignore = ignore_index;
   r.rows = k.rows; r.target = k.target; r.n_valid = k.n_valid;
   r.lse_in = lse; r.dloss = dloss; r.reduction = reduction; r.slot_lse = k.slot_lse; r.slot_scale = k.slot_scale;
-  EFQAT_TRY(launch(k_xent_rows, dim3(1), dim3(1024), 0, st, r));
+  const bool few = T <= kXentFew;
+  if (!few) EFQAT_TRY(launch(k_xent_rows, dim3((unsigned)ceil_div(T, kXentOwn * 1024)), dim3(1024), 0, st, r));
 
   XentStageArgs tokens = xent_stage_tokens(p, k, h, ldh, D), classes = xent_stage_classes(p, k, w, ldw, D);
   tokens.targets = targets; tokens.T = T; tokens.V = V; tokens.ignore = ignore_index; tokens.clear = dh; tokens.ld_clear = lddh;
@@ -570,7 +614,7 @@ extern "C" int efqat_linear_xent_bwd(const void* h, int64_t ldh, const void* w, 
   g.out_dtype = dtype;
   for (g.piece = 0; g.piece < p.n_pieces; ++g.piece) {
     classes.piece = g.piece;
-    if (p.stage_w || g.piece == 0) EFQAT_TRY(launch_stage(g.piece == 0 ? &tokens : nullptr, p.stage_w ? &classes : nullptr, dtype, st));
+    if (p.stage_w || g.piece == 0) EFQAT_TRY(launch_stage(g.piece == 0 ? &tokens : nullptr, p.stage_w ? &classes : nullptr, few && g.piece == 0 ? &r : nullptr, dtype, st));
     EFQAT_TRY(launch_xent_tile<XG_GRAD>(p.bt, g, p.grid, st));
     XentGemmArgs gh = g, gw = g;
     gh.split_blocks = p.blocks_dh; gh.acc = k.acc_dh; gh.out = dh; gh.ldo = lddh; gh.rows = k.rows;

@@ -252,3 +252,12 @@ def test_bindings_refuse():
         ef.linear_xent_fwd(hd, wd.new_empty(16 * 64 + 1)[1:].view(16, 64), td)     # whole stages, not aligned to 16 bytes
     with pytest.raises(ef.EfqatError):
         ef.linear_xent_fwd(hd, wd, td, ws=torch.empty(256, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("T", [1024, 1025, 2048, 2049, 4096 + 77, 20000])
+def test_the_count_of_tokens(T):
+    """tokens counted by one block, by several, by every block for itself"""
+    h, w, t, hd, wd, td = make(T, 64, 40, "bf16", T, ignored=0.4)
+    t[[0, T - 1]] = [-100, 3]
+    r = check_all(h, w, t, hd, wd, torch.from_numpy(t).cuda(), "bf16")
+    assert (r["dh"][0] == 0).all() and (r["dh"][T - 1] != 0).any()

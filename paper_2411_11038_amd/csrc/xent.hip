@@ -22,10 +22,9 @@ struct XentRowsArgs {
   int64_t T, V, ignore;
   int32_t *rows, *target, *n_valid, *n_out;           // n_out: the caller's count, nullable
   float *loss, *lse;                                  // forward: zero for the other tokens (loss: nullable)
-  // backward: what the loss of a token is multiplied by
+  // backward: log-sum-exp of the tokens and, where every loss has a gradient of its own, that
   const float *lse_in, *dloss;
-  int reduction;
-  float *slot_lse, *slot_scale;
+  float *slot_lse, *slot_scale;                       // slot_scale: nullable
 };
 // A block places 2048 tokens: it counts those with a class among all tokens before its own (eight reads in flight a lane), then ranks its
 // own by ballots, so that slots are in the order of the tokens and every access is of neighbours.  One block for all took 9 us for 12288
@@ -61,7 +60,6 @@ __global__ __launch_bounds__(1024) void k_xent_rows(const XentRowsArgs g) {
   int total = 0;
 #pragma unroll
   for (int w = 0; w < 16; ++w) total += earlier[w];
-  const float up = g.slot_scale && g.reduction != EFQAT_XENT_NONE && g.dloss ? g.dloss[0] : 1.0f;
 #pragma unroll
   for (int i = 0; i < kXentOwn; ++i) {
     int slot = total + __popcll(who[i] & ((UINT64_C(1) << lane) - 1));
@@ -74,10 +72,8 @@ __global__ __launch_bounds__(1024) void k_xent_rows(const XentRowsArgs g) {
     if (who[i] >> lane & 1) {
       g.rows[slot] = (int32_t)ti;
       g.target[slot] = (int32_t)c[i];
-      if (g.slot_scale) {
-        g.slot_lse[slot] = g.lse_in[ti];
-        g.slot_scale[slot] = g.reduction == EFQAT_XENT_NONE && g.dloss ? g.dloss[ti] : up;
-      }
+      if (g.slot_lse) g.slot_lse[slot] = g.lse_in[ti];
+      if (g.slot_scale) g.slot_scale[slot] = g.dloss[ti];
     } else if (ti < g.T) {
       if (g.loss) g.loss[ti] = 0.0f;
       if (g.lse) g.lse[ti] = 0.0f;
@@ -139,10 +135,8 @@ __device__ __forceinline__ int xent_few_rows(const XentRowsArgs& g, bool writes,
       if (writes) {
         g.rows[slot] = t;
         g.target[slot] = (int32_t)c[i];
-        if (g.slot_scale) {
-          g.slot_lse[slot] = g.lse_in[t];
-          g.slot_scale[slot] = g.dloss ? g.dloss[g.reduction == EFQAT_XENT_NONE ? t : 0] : 1.0f;
-        }
+        if (g.slot_lse) g.slot_lse[slot] = g.lse_in[t];
+        if (g.slot_scale) g.slot_scale[slot] = g.dloss[t];
       }
     } else if (writes && t < g.T) {
       if (g.loss) g.loss[t] = 0.0f;
@@ -601,7 +595,9 @@ extern "C" int efqat_linear_xent_bwd(const void* h, int64_t ldh, const void* w, 
   XentRowsArgs r = {};
   r.targets = targets; r.T = T; r.V = V; r.ignore = ignore_index;
   r.rows = k.rows; r.target = k.target; r.n_valid = k.n_valid;
-  r.lse_in = lse; r.dloss = dloss; r.reduction = reduction; r.slot_lse = k.slot_lse; r.slot_scale = k.slot_scale;
+  const bool own = reduction == EFQAT_XENT_NONE && dloss;          // gradients of the tokens' losses
+  r.lse_in = lse; r.slot_lse = k.slot_lse;
+  r.dloss = own ? dloss : nullptr; r.slot_scale = own ? k.slot_scale : nullptr;
   const bool few = T <= kXentFew;
   if (!few) EFQAT_TRY(launch(k_xent_rows, dim3((unsigned)ceil_div(T, kXentOwn * 1024)), dim3(1024), 0, st, r));
 
@@ -609,7 +605,8 @@ extern "C" int efqat_linear_xent_bwd(const void* h, int64_t ldh, const void* w, 
   tokens.targets = targets; tokens.T = T; tokens.V = V; tokens.ignore = ignore_index; tokens.clear = dh; tokens.ld_clear = lddh;
   XentGemmArgs g = xent_gemm_args(p, k, w, ldw, D);
   g.lse = k.slot_lse;
-  g.scale = k.slot_scale;
+  g.scale = own ? k.slot_scale : nullptr;
+  g.factor = own ? nullptr : dloss;
   g.mean = reduction == EFQAT_XENT_MEAN ? 1 : 0;
   g.out_dtype = dtype;
   for (g.piece = 0; g.piece < p.n_pieces; ++g.piece) {

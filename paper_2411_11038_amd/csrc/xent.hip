@@ -25,21 +25,48 @@ struct XentRowsArgs {
   // backward: log-sum-exp of the tokens and, where every loss has a gradient of its own, that
   const float *lse_in, *dloss;
   float *slot_lse, *slot_scale;                       // slot_scale: nullable
+  const int32_t* counts;                              // NULL, or of every 2048 tokens, those with a class
 };
+constexpr int kXentOwn = 2;                           // tokens of a thread of k_xent_rows
+constexpr int kXentBlock = kXentOwn * 1024;
+// tokens with a class among a block's
+__global__ __launch_bounds__(1024) void k_xent_count(const int64_t* __restrict__ targets, int64_t T, int64_t V, int64_t ignore,
+                                                     int32_t* __restrict__ counts) {
+  __shared__ int count[16];
+  const int64_t t = (int64_t)blockIdx.x * kXentBlock + threadIdx.x;
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < kXentOwn; ++i) {
+    const int64_t c = t + i * 1024 < T ? targets[t + i * 1024] : -1;
+    n += __popcll(__ballot(c >= 0 && c < V && c != ignore));
+  }
+  if ((threadIdx.x & 63) == 0) count[threadIdx.x >> 6] = n;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    n = 0;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) n += count[w];
+    counts[blockIdx.x] = n;
+  }
+}
 // A block places 2048 tokens: it counts those with a class among all tokens before its own (eight reads in flight a lane), then ranks its
 // own by ballots, so that slots are in the order of the tokens and every access is of neighbours.  One block for all took 9 us for 12288
-// tokens.
-constexpr int kXentOwn = 2;                           // tokens of a thread
+// tokens.  What is read grows with the square of the tokens: from kXentMany on, the blocks' counts are taken first.
 __global__ __launch_bounds__(1024) void k_xent_rows(const XentRowsArgs g) {
   __shared__ int earlier[16], count[kXentOwn * 16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t t0 = (int64_t)blockIdx.x * kXentOwn * 1024, t = t0 + threadIdx.x;
+  const int64_t t0 = (int64_t)blockIdx.x * kXentBlock, t = t0 + threadIdx.x;
   auto has_class = [&](int64_t c) { return c >= 0 && c < g.V && c != g.ignore; };
   int64_t c[kXentOwn];
 #pragma unroll
   for (int i = 0; i < kXentOwn; ++i) c[i] = t + i * 1024 < g.T ? g.targets[t + i * 1024] : -1;
   int before = 0;
-  for (int64_t u0 = 0; u0 < t0; u0 += 8 * 1024) {
+  if (g.counts) {
+    for (int64_t u = threadIdx.x; u < (int64_t)blockIdx.x; u += 1024) before += g.counts[u];
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) before += __shfl_xor(before, off);
+  }
+  for (int64_t u0 = 0; u0 < t0 && !g.counts; u0 += 8 * 1024) {
     int64_t v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -332,6 +359,9 @@ __global__ __launch_bounds__(256) void k_xent_join_slices(const XentGemmArgs h, 
 }
 
 // ---- plans
+// Tokens from which on the blocks' counts are taken first: a launch more, 2.5 us of it at work and 3.9 for the places, against 5.8 / 7.8 /
+// 12.7 / 199 us in one launch of 12288 / 32768 / 65536 / 1048576 tokens.
+constexpr int64_t kXentMany = INT64_C(1) << 15;
 // Elements of G at a time: half of what all classes need, 128 MiB of bf16 at least and 512 MiB at most.  A piece costs five launches and
 // a pass over the sums of dh: pieces of 128 / 256 / 512 MiB took 505 / 482 / 476 us for 12288 tokens, one in seven with a class, of
 // width 768 against 30522 classes, and 6.77 / 6.73 / 6.66 ms for 8192 of width 4096 against 32000.
@@ -407,7 +437,7 @@ static XentPlan xent_plan(int64_t T, int64_t D, int64_t V, int dtype, bool backw
 }
 
 struct XentWs {
-  int32_t *n_valid, *rows, *target;
+  int32_t *n_valid, *rows, *target, *counts;
   bf16_t *h, *w, *grad;
   float2* part;
   float *target_logit, *slot_loss, *slot_lse, *slot_scale, *acc_dh, *acc_dw;
@@ -419,6 +449,7 @@ static XentWs xent_ws(void* ws, const XentPlan& p, int64_t T, int64_t V, bool ba
   w.n_valid = (int32_t*)c.take(sizeof(int32_t));
   w.rows = (int32_t*)c.take((size_t)T * sizeof(int32_t));
   w.target = (int32_t*)c.take((size_t)T * sizeof(int32_t));
+  if (T >= kXentMany) w.counts = (int32_t*)c.take((size_t)ceil_div(T, kXentBlock) * sizeof(int32_t));
   w.h = (bf16_t*)c.take((size_t)(p.slots * p.parts * p.Dp) * 2);
   if (p.stage_w) w.w = (bf16_t*)c.take((size_t)(p.stage_rows * p.parts * p.Dp) * 2);
   if (backward) {
@@ -455,6 +486,13 @@ static int launch_xent_pair(const XentGemmArgs& h, const XentGemmArgs& w, int64_
   static const hipError_t attr = hipFuncSetAttribute((const void*)k_xent_gemm_pair<BT>, hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS);
   if (attr != hipSuccess) return EFQAT_ERR_HIP;
   return launch(k_xent_gemm_pair<BT>, dim3((unsigned)std::min<int64_t>(blocks, C::CHIP)), dim3(C::THREADS), C::LDS, st, h, w);
+}
+
+static int launch_rows(XentRowsArgs r, int32_t* counts, hipStream_t st) {
+  const dim3 grid((unsigned)ceil_div(r.T, kXentBlock));
+  if (counts) EFQAT_TRY(launch(k_xent_count, grid, dim3(1024), 0, st, r.targets, r.T, r.V, r.ignore, counts));
+  r.counts = counts;
+  return launch(k_xent_rows, grid, dim3(1024), 0, st, r);
 }
 
 static int stage_blocks(int64_t rows, int64_t pitch, unsigned* blocks) {
@@ -557,7 +595,7 @@ extern "C" int efqat_linear_xent_fwd(const void* h, int64_t ldh, const void* w, 
   r.rows = k.rows; r.target = k.target; r.n_valid = k.n_valid; r.n_out = n_valid;
   r.loss = none ? loss : nullptr; r.lse = lse;
   const bool few = T <= kXentFew;
-  if (!few) EFQAT_TRY(launch(k_xent_rows, dim3((unsigned)ceil_div(T, kXentOwn * 1024)), dim3(1024), 0, st, r));
+  if (!few) EFQAT_TRY(launch_rows(r, k.counts, st));
 
   const XentStageArgs tokens = xent_stage_tokens(p, k, h, ldh, D);
   XentStageArgs classes = xent_stage_classes(p, k, w, ldw, D);
@@ -599,7 +637,7 @@ extern "C" int efqat_linear_xent_bwd(const void* h, int64_t ldh, const void* w, 
   r.lse_in = lse; r.slot_lse = k.slot_lse;
   r.dloss = own ? dloss : nullptr; r.slot_scale = own ? k.slot_scale : nullptr;
   const bool few = T <= kXentFew;
-  if (!few) EFQAT_TRY(launch(k_xent_rows, dim3((unsigned)ceil_div(T, kXentOwn * 1024)), dim3(1024), 0, st, r));
+  if (!few) EFQAT_TRY(launch_rows(r, k.counts, st));
 
   XentStageArgs tokens = xent_stage_tokens(p, k, h, ldh, D), classes = xent_stage_classes(p, k, w, ldw, D);
   tokens.targets = targets; tokens.T = T; tokens.V = V; tokens.ignore = ignore_index; tokens.clear = dh; tokens.ld_clear = lddh;

@@ -261,3 +261,12 @@ def test_the_count_of_tokens(T):
     t[[0, T - 1]] = [-100, 3]
     r = check_all(h, w, t, hd, wd, torch.from_numpy(t).cuda(), "bf16")
     assert (r["dh"][0] == 0).all() and (r["dh"][T - 1] != 0).any()
+
+
+@pytest.mark.parametrize("T", [32767, 32768, 133123])
+def test_many_tokens(T):
+    """as many that the blocks' counts are taken first, and one fewer"""
+    h, w, t, hd, wd, td = make(T, 8, 9, "bf16", T, ignored=0.4)
+    t[[0, T - 1]] = [-100, 3]
+    r = check_all(h, w, t, hd, wd, torch.from_numpy(t).cuda(), "bf16")
+    assert (r["dh"][0] == 0).all() and (r["dh"][T - 1] != 0).any()

@@ -12,9 +12,16 @@
 // halves of a wavefront, instead of a reduction over 32 lanes for every row.
 //
 // Square tiles: 256 by eight wavefronts of 128 x 64 (the accumulators are half of a lane's registers, two wavefronts a SIMD),
-// 128 and 64 by four.  K stages of 64 in two LDS buffers; a stage's copies go out in the last sub-step of the stage before the
+// 128 by four of 64 x 64.  K stages of 64 in two LDS buffers; a stage's copies go out in the last sub-step of the stage before the
 // previous one's end and in the first of the previous, so that they have two sub-steps to land; fragment reads run a sub-step ahead
-// of the matrix instructions.  The order is pinned, one group per matrix instruction.
+// of the matrix instructions.  The order is pinned, one group per matrix instruction.  64 by four wavefronts that each walk K stages of
+// their own.
+//
+// Bound by the matrix cores where the tiles are large: 8028 tokens of width 4096 against 32000 classes (2.1 T operations a product), the
+// logits with their sums 1.62 ms (1.30 POP/s; 8192^3 takes a library product 1.38), the logits and G 1.79 ms (1.18), both products of G
+// 3.28 ms (1.28).  A 256-tile of logits costs 1.6 us a K stage and 8.5 us besides (128 exponentials a lane in the epilogue, the first
+// loads): 12 stages, as in a width of 768, reach 0.79 POP/s.  A round of four stages of a 64-tile takes 0.67 us, which the copies into LDS
+// (64 KB at 64 bytes a clock: 0.43 us) are most of.  LDS bank conflicts: none that a counter shows.
 //
 // fp32 operands are three bf16 parts each (x = x0 + x1 + x2 with 24 bits), side by side in a row; the product of two is the six
 // largest of the nine products of parts, smallest first: `segments` walks them, each a contraction of its own over the same rows.
@@ -79,7 +86,9 @@ struct XentGemmArgs {
   const int32_t* rows;            // XG_DH: rows of the output, by slot
 };
 
-// Slices of K of a product of G of so many tiles: about `blocks` blocks, none with fewer than 12 stages
+// Slices of K of a product of G of so many tiles: about `blocks` blocks, none with fewer than 12 stages.  Shorter ones cost more at the
+// join than they save, longer ones leave CUs without work: at least 6 / 12 / 24 stages, backward of 256 fp32 tokens of width 256 against
+// 1000 classes 37.6 / 31.8 / 30.7 us, of 128 of 1920 against 786 71.2 / 71.2 / 72.9, of 65 bf16 of 768 against 30522 73.0 / 66.5 / 69.7.
 __host__ __device__ inline int xent_split(int64_t tiles, int stages, int segments, int blocks) {
   const int by_blocks = tiles > blocks || tiles < 1 ? 1 : blocks / (int)tiles;
   const int by_stages = (int)((int64_t)stages * segments / 12);
@@ -199,14 +208,14 @@ struct XentOperand {
 template <int BT>
 struct XentCfg {
   static constexpr int NW = BT == 256 ? 8 : 4, WGM = 2, WGN = NW / 2;       // wavefronts of a tile
-  static constexpr int KG = BT == 64 ? 2 : 1;         // groups of them that take the K stages in turn
-  static constexpr int THREADS = NW * KG * 64;
+  static constexpr int THREADS = NW * 64;
   static constexpr int CHIP = BT == 128 ? 512 : 256;  // blocks that the chip holds at once
   static constexpr int WM = BT / WGM, WN = BT / WGN, TM = WM / 32, TN = WN / 32;
   static constexpr int STAGE = BT * 256;              // bytes of both operands' stage, a power of two
-  static constexpr int NST = BT == 64 ? 4 : 2;        // LDS stages of a group
+  static constexpr bool OWN = BT == 64;               // every wavefront works on K stages of its own, of the whole tile
+  static constexpr int RINGS = OWN ? NW : 1;          // rings of two LDS stages
   static constexpr int OUT_PITCH = WM * 2 + 16;       // bytes of a row of a wavefront's bf16 results in LDS
-  static constexpr int LDS = KG * NST * STAGE > NW * WN * OUT_PITCH ? KG * NST * STAGE : NW * WN * OUT_PITCH;
+  static constexpr int LDS = RINGS * 2 * STAGE > NW * WN * OUT_PITCH ? RINGS * 2 * STAGE : NW * WN * OUT_PITCH;
 };
 
 // bf16 parts of x: x0 + x1 + x2 = x up to 2^-24.  A NaN is its first part.  What bf16 has no finite value for, infinities among it,
@@ -240,8 +249,7 @@ __device__ __forceinline__ void xent_gemm_block(const XentGemmArgs& g, const Xen
   constexpr bool LOGITS = MODE == XG_LSE || MODE == XG_GRAD;
   constexpr bool ATR = !LOGITS, BTR = MODE == XG_DW;
   const int tid = threadIdx.x, lane = tid & 63;
-  const int all_wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int kg = all_wave / C::NW, wave = all_wave % C::NW;         // group along K, wavefront of the tile
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / C::WGN, wn = wave % C::WGN;
 
   const int M = z.M, N = z.N, nks = z.nks;
@@ -285,17 +293,18 @@ __device__ __forceinline__ void xent_gemm_block(const XentGemmArgs& g, const Xen
     }
   }
 
-  XentOperand<BT, C::WM, C::NW, ATR> A;
-  XentOperand<BT, C::WN, C::NW, BTR> B;
-  A.setup(lda, ATR ? (int)g.Dp - m0 : M - m0, wave, wm, lane, 0);
-  B.setup(ldb, BTR ? z.piece - n0 : N - n0, wave, wn, lane, BT * 128);
+  XentOperand<BT, C::OWN ? BT : C::WM, C::OWN ? 1 : C::NW, ATR> A;
+  XentOperand<BT, C::OWN ? BT : C::WN, C::OWN ? 1 : C::NW, BTR> B;
+  const int copier = C::OWN ? 0 : wave;               // among the wavefronts that copy a stage together
+  A.setup(lda, ATR ? (int)g.Dp - m0 : M - m0, copier, C::OWN ? 0 : wm, lane, 0);
+  B.setup(ldb, BTR ? z.piece - n0 : N - n0, copier, C::OWN ? 0 : wn, lane, BT * 128);
   const int64_t a_step = ATR ? lda * 128 : 128, b_step = BTR ? ldb * 128 : 128;
   const char* a_base = (const char*)opA + (ATR ? (int64_t)m0 * 2 : (int64_t)m0 * lda * 2) + k_first * a_step;
   const char* b_base = (const char*)opB + (BTR ? (int64_t)n0 * 2 : (int64_t)n0 * ldb * 2) + k_first * b_step;
   // the copy stream: stage, its place in its segment, its sources
   int c_seg = 0, c_kt = 0;
-  auto seg_a = [&](int s) { return (int)((0x001102u >> (4 * (g.segments == 6 ? s : 5))) & 15u); };
-  auto seg_b = [&](int s) { return (int)((0x010120u >> (4 * (g.segments == 6 ? s : 5))) & 15u); };
+  auto seg_a = [&](int s) { return (int)((0x001102u >> (4 * (g.segments == 6 && s < 5 ? s : 5))) & 15u); };
+  auto seg_b = [&](int s) { return (int)((0x010120u >> (4 * (g.segments == 6 && s < 5 ? s : 5))) & 15u); };
   const char* a_src = a_base + (int64_t)seg_a(0) * a_part * 2;
   const char* b_src = b_base + (int64_t)seg_b(0) * b_part * 2;
   auto next_stage = [&]() {
@@ -316,10 +325,10 @@ __device__ __forceinline__ void xent_gemm_block(const XentGemmArgs& g, const Xen
 #pragma unroll
     for (int t = t0; t < t1; ++t) {
       if (t < AG) {
-        if constexpr (decltype(lastc)::value) A.copy_last(a_src, l, wave, lane, t, lda, a_rows - (k_end - 1) * 64);
-        else A.copy(a_src, l, wave, t);
+        if constexpr (decltype(lastc)::value) A.copy_last(a_src, l, copier, lane, t, lda, a_rows - (k_end - 1) * 64);
+        else A.copy(a_src, l, copier, t);
       } else {
-        B.copy(b_src, l + BT * 128, wave, t - AG);
+        B.copy(b_src, l + BT * 128, copier, t - AG);
       }
     }
   };
@@ -336,9 +345,10 @@ __device__ __forceinline__ void xent_gemm_block(const XentGemmArgs& g, const Xen
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
 
-  typename decltype(A)::Frag af[2][C::TM];
-  typename decltype(B)::Frag bf[2][C::TN];
-  constexpr int RA = decltype(A)::READS, RBR = decltype(B)::READS, NRD = RA + RBR, MF = C::TM * C::TN;
+  constexpr int TM = decltype(A)::T, TN = decltype(B)::T;             // fragments of a wavefront in the product
+  typename decltype(A)::Frag af[2][TM];
+  typename decltype(B)::Frag bf[2][TN];
+  constexpr int RA = decltype(A)::READS, RBR = decltype(B)::READS, NRD = RA + RBR, MF = TM * TN;
   auto read_one = [&](int sub, int rb, int r) {
     if (r < RBR) B.read(smem, sub, r, bf[rb]);
     else A.read(smem, sub, r - RBR, af[rb]);
@@ -347,10 +357,10 @@ __device__ __forceinline__ void xent_gemm_block(const XentGemmArgs& g, const Xen
 #pragma unroll
     for (int r = 0; r < NRD; ++r) read_one(sub, rb, r);
   };
-  auto mfma_one = [&](int rb, int i, int j) {
-    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, af[rb][i].v),
-                                                        __builtin_bit_cast(bf16x8_t, bf[rb][j].v), acc[i][j], 0, 0, 0);
+  auto mfma_into = [&](floatx16_t& d, const auto& a, const auto& b) {
+    d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a.v), __builtin_bit_cast(bf16x8_t, b.v), d, 0, 0, 0);
   };
+  auto mfma_one = [&](int rb, int i, int j) { mfma_into(acc[i][j], af[rb][i], bf[rb][j]); };
   auto mfma_all = [&](int rb) {
 #pragma unroll
     for (int i = 0; i < C::TM; ++i)
@@ -381,86 +391,80 @@ __device__ __forceinline__ void xent_gemm_block(const XentGemmArgs& g, const Xen
     }
   };
 
-  if constexpr (C::NST > 2) {
-    // Few matrix instructions a stage: what a stage costs is the way from its barrier over the LDS reads to the last of them.  Two groups
-    // of wavefronts take every other stage, each into a ring of its own; the copies of two stages and more stay in flight across a
-    // barrier, behind which those of the group's stage NST - 1 further on go into the buffer that it has read.
-    const int mine = (nstage - kg + C::KG - 1) / C::KG, rounds = (nstage + C::KG - 1) / C::KG;     // stages of this group, of the first
-    const int ring = kg * C::NST;
-    floatx16_t odd[C::TM][C::TN];                     // every other sub-step: two chains of dependent instructions
+  if constexpr (C::OWN) {
+    // Few tiles: what counts is how long one takes.  Every wavefront walks K stages of its own, with all 64 x 64 results: a stage is read
+    // from LDS once (wavefronts of 32 x 32 read it twice), and nobody waits for anybody at a barrier.  The copies of a stage are under way
+    // while the one before is worked on.  128 fp32 tokens of width 1920 against 786 classes, forward: 49 us; two groups of four wavefronts
+    // of 32 x 32 that take every other stage in rings of four: 62 us.
+    const int mine = (nstage - wave + C::NW - 1) / C::NW, ring = wave * 2;           // stages of this wavefront
+    floatx16_t own[TM][TN];
 #pragma unroll
-    for (int i = 0; i < C::TM; ++i)
+    for (int i = 0; i < TM; ++i)
 #pragma unroll
-      for (int j = 0; j < C::TN; ++j) odd[i][j] = acc[i][j];
-    for (int k = 0; k < kg && k < nstage; ++k) next_stage();
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) own[i][j][r] = 0.0f;
+    for (int k = 0; k < wave && k < nstage; ++k) next_stage();
     auto issue_stage = [&](int r) {
-      const int s = r * C::KG + kg, buf = ring + r % C::NST;
-      if (s < nfull) issue(Whole{}, buf, 0, LPS);
-      else issue(Last{}, buf, 0, LPS);
+      if (r * C::NW + wave < nfull) issue(Whole{}, ring + (r & 1), 0, LPS);
+      else issue(Last{}, ring + (r & 1), 0, LPS);
 #pragma unroll
-      for (int k = 0; k < C::KG; ++k) next_stage();
+      for (int k = 0; k < C::NW; ++k) next_stage();
     };
-#pragma unroll
-    for (int r = 0; r < C::NST - 1; ++r)
-      if (r < mine) issue_stage(r);
-    for (int r = 0; r < rounds; ++r) {
-      if (r + C::NST - 2 < mine) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((C::NST - 2) * LPS) : "memory");
+    if (mine > 0) issue_stage(0);
+    if (mine > 1) issue_stage(1);
+    for (int r = 0; r < mine; ++r) {
+      if (r + 1 < mine) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LPS) : "memory");
       else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __builtin_amdgcn_s_barrier();
       __builtin_amdgcn_sched_barrier(0);
-      if (r + C::NST - 1 < mine) issue_stage(r + C::NST - 1);
-      if (r < mine) {
-        const char* at = smem + (ring + r % C::NST) * C::STAGE;
-        typename decltype(A)::Frag a4[4][C::TM];
-        typename decltype(B)::Frag b4[4][C::TN];
+      const char* at = smem + (ring + (r & 1)) * C::STAGE;
+      typename decltype(A)::Frag a4[4][TM];
+      typename decltype(B)::Frag b4[4][TN];
 #pragma unroll
-        for (int sub = 0; sub < 4; ++sub) {
+      for (int sub = 0; sub < 4; ++sub) {
 #pragma unroll
-          for (int q = 0; q < RBR; ++q) B.read(at, sub, q, b4[sub]);
+        for (int q = 0; q < RBR; ++q) B.read(at, sub, q, b4[sub]);
 #pragma unroll
-          for (int q = 0; q < RA; ++q) A.read(at, sub, q, a4[sub]);
+        for (int q = 0; q < RA; ++q) A.read(at, sub, q, a4[sub]);
+      }
+#pragma unroll
+      for (int sub = 0; sub < 4; ++sub) {
+        if (sub == 3) {                               // everything has been read: the stage after the next takes the place
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          __builtin_amdgcn_sched_barrier(0);
+          if (r + 2 < mine) issue_stage(r + 2);
         }
 #pragma unroll
-        for (int sub = 0; sub < 4; ++sub)
+        for (int i = 0; i < TM; ++i)
 #pragma unroll
-          for (int i = 0; i < C::TM; ++i)
-#pragma unroll
-            for (int j = 0; j < C::TN; ++j) {
-              floatx16_t& d = sub & 1 ? odd[i][j] : acc[i][j];
-              d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a4[sub][i].v),
-                                                          __builtin_bit_cast(bf16x8_t, b4[sub][j].v), d, 0, 0, 0);
-            }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_sched_barrier(0);
+          for (int j = 0; j < TN; ++j) mfma_into(own[i][j], a4[sub][i], b4[sub][j]);
       }
     }
-    // the sums of the groups, in the first one
-#pragma unroll
-    for (int i = 0; i < C::TM; ++i)
-#pragma unroll
-      for (int j = 0; j < C::TN; ++j)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) acc[i][j][r] += odd[i][j][r];
+    // each wavefront adds up 32 x 32 of the results, in the order of the wavefronts
     __syncthreads();
-    float* sum = reinterpret_cast<float*>(smem);
-    if (kg > 0) {
+    float4* sum = reinterpret_cast<float4*>(smem);    // [wavefront][32 x 32][4][lane]
+    if (mine > 0) {
 #pragma unroll
-      for (int i = 0; i < C::TM; ++i)
+      for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int j = 0; j < C::TN; ++j)
+        for (int j = 0; j < TN; ++j)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) sum[(((kg - 1) * C::NW + wave) * C::TM * C::TN + i * C::TN + j) * 1024 + r * 64 + lane] = acc[i][j][r];
+          for (int q = 0; q < 4; ++q)
+            sum[((wave * C::NW + i * C::WGN + j) * 4 + q) * 64 + lane] =
+                make_float4(own[i][j][4 * q], own[i][j][4 * q + 1], own[i][j][4 * q + 2], own[i][j][4 * q + 3]);
     }
     __syncthreads();
-    if (kg == 0) {
 #pragma unroll
-      for (int k = 1; k < C::KG; ++k)
+    for (int k = 0; k < C::NW; ++k) {
+      if (k >= nstage) break;
 #pragma unroll
-        for (int i = 0; i < C::TM; ++i)
-#pragma unroll
-          for (int j = 0; j < C::TN; ++j)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[i][j][r] += sum[(((k - 1) * C::NW + wave) * C::TM * C::TN + i * C::TN + j) * 1024 + r * 64 + lane];
+      for (int q = 0; q < 4; ++q) {
+        const float4 v = sum[((k * C::NW + wave) * 4 + q) * 64 + lane];
+        acc[0][0][4 * q] += v.x;
+        acc[0][0][4 * q + 1] += v.y;
+        acc[0][0][4 * q + 2] += v.z;
+        acc[0][0][4 * q + 3] += v.w;
+      }
     }
   } else
   // On entry to stage s the first H0 copies of stage s + 1 are under way if and only if s + 1 < nfull.
@@ -519,7 +523,6 @@ __device__ __forceinline__ void xent_gemm_block(const XentGemmArgs& g, const Xen
     const bool edge = m0 + BT > M;
 #pragma unroll
     for (int j = 0; j < C::TN; ++j) {
-      if (kg > 0) break;
       const int n = nw + 32 * j;
       float top = -INFINITY;
 #pragma unroll
@@ -558,7 +561,7 @@ __device__ __forceinline__ void xent_gemm_block(const XentGemmArgs& g, const Xen
       a.x = top;
       g.part[(z.class0 / BT + tm) * g.slots + n0 + tid] = a;
     }
-  } else if (kg == 0) {
+  } else {
     // a wavefront's results as rows of WM values in LDS, from where they leave 16 bytes a lane
     char* tile = smem + wave * (C::WN * C::OUT_PITCH);
     constexpr int CPR = C::WM * 2 / 16, RPI = 64 / CPR;            // chunks of a row, rows of an access

@@ -5,8 +5,13 @@
 //
 // Forward: one product whose epilogue keeps the largest logit and the sum of exponentials of every token and tile of classes
 // (8 bytes for 256 logits), joined by a second pass.  Backward: the classes in pieces; a piece's logits are formed again, leave as
-// G in bf16 (a buffer that the last-level cache holds) and are multiplied by w and by h.  8 T D V operations of a training step
-// are products on the matrix cores and bound it.
+// G in bf16 (a buffer that the last-level cache holds) and are multiplied by w and by h.  G in fewer bits than 32 is what lets both
+// products run on the matrix cores at their bf16 rate, like the operands; its rounding is as large as that of the results, each of which
+// sums thousands of its entries.  fp32 operands, and then G too, are three bf16 parts: 24 bits.
+//
+// 8 T D V operations of a training step are products on the matrix cores and bound it; with few tokens, reading w does.  bf16, 8192
+// tokens of width 4096 against 32000 classes, 98 % of them with one: 6.7 ms forward and backward, 1.25 POP/s.  12288 of width 768 against
+// 30522, 15 % of them with one: 0.44 ms, 0.78 POP/s.  One token of width 4096: 74 us forward, of which 50 are w at 5.2 TB/s.
 //
 // Tokens without a class (ignored, or a class outside [0, V)) take no part: the rows that do are counted and copied together
 // first, on the device, and every grid is cut to their number there.  What an ignored row holds - NaN included - touches nothing.
@@ -382,12 +387,18 @@ struct XentPlan {
   int64_t acc_dh, acc_dw;         // fp32 partial results
 };
 
+// Tile of the logits: the largest that gives three CUs in four something to do (of 64: whatever is left).  A larger tile reads its operands
+// fewer times, a smaller one leaves fewer CUs idle in the last round.  Width 4096, 32000 classes, forward: 65 tokens by 128 / 64 rows 88 /
+// 105 us, 256 by 256 / 128 / 64 125 / 102 / 173 us, 1280 by 256 / 128 324 / 342 us.  Up to 64 tokens take 71 to 74 us, of which reading the
+// classes is 50.
 static int logits_tile(int64_t T, int64_t V) {
   if (T > 128 && ceil_div(V, 256) * ceil_div(T, 256) >= 192) return 256;
   if (T > 64 && ceil_div(V, 128) * ceil_div(T, 128) >= 128) return 128;
   return 64;
 }
-// tile and blocks of a product of G [N][M] over so many stages
+// Tile and blocks of a product of G [N][M] over so many stages, by the same rule, with the slices of K that there may be.  The backward
+// pass of 256 / 768 / 2048 tokens of width 4096 against 32000 classes: tiles of 256 339 / 635 / 1384 us, of 128 360 / 712 / 1593 us; of 128
+// tokens 245 us by tiles of 128, 273 by 64.
 static int out_tile(int64_t M, int64_t N, int64_t stages, int* blocks) {
   const int64_t t256 = ceil_div(M, 256) * ceil_div(N, 256), t128 = ceil_div(M, 128) * ceil_div(N, 128);
   if (t256 * std::max<int64_t>(1, stages / 12) >= 192 && N > 128) { *blocks = 256; return 256; }

@@ -8,6 +8,11 @@
 // A block keeps its columns' parameters and, backward, their sums over all its rows in registers; the rows that come next are
 // requested before the present ones are worked on.  The sums of the blocks are added in a second pass, in a fixed order.
 // Rows longer than the registers hold (kNormMaxCols, kNormBwdMaxCols), and shorter than a chunk, are read again for every step.
+//
+// bf16, one call after another on the same buffers (which the last-level cache holds).  8192 x 4096: forward 22.5 us (134 MB, 6.0 TB/s),
+// input kept 28.0, backward 37.7 (201 MB, 5.3 TB/s), from the checkpoint 33.6.  12288 x 768: 9.7, 12.3, 16.6 (57 MB, 3.4 TB/s) and 16.4 us:
+// narrow rows are bound by the instructions a value takes (two sums, the code) and by the way through a row, load to store, that a block
+// walks a few times; 4 us of the backward are the second pass, mostly its launch.  1 x 4096: 2.5 us of kernel in 6.4 us a call.
 #include "rows.hpp"
 
 #include <algorithm>

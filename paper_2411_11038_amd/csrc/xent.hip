@@ -241,21 +241,27 @@ __global__ __launch_bounds__(256) void k_xent_stage(const XentStageArgs tokens, 
   }
 }
 
-// ---- forward: the tiles of classes joined, 64 tokens a block, four groups of tiles
+// ---- forward: the tiles of classes joined, TOK tokens a block, by 1024 / TOK groups of lanes that take the tiles in turn.  Up to 64 tokens
+// are one block, which takes their mean or sum too: 64 tokens of width 64 against 8000 classes 14.4 us forward, with a launch for the mean
+// and four groups of lanes 17.1; 18 of 32 against 68688 (1074 tiles) 36.8 and 46.5.  One block for 256 tokens, in turn, took 28.6, not 19.3.
 struct XentJoinArgs {
   const float2* part;
   int tiles;
   int64_t slots;
   const int32_t *n_valid, *rows;
   const float* target_logit;
-  float *lse, *loss, *slot_loss;                      // loss of the tokens by row, or (NULL) by slot
+  float *lse, *loss, *slot_loss;                      // loss of the tokens by row, or by slot (each nullable)
+  float* total;                                       // of all tokens: one block, or NULL
+  int mean;
 };
-__global__ __launch_bounds__(256) void k_xent_join(const XentJoinArgs g) {
-  __shared__ float2 red[4][64];
-  const int lane = threadIdx.x & 63, grp = threadIdx.x >> 6;
-  const int n = blockIdx.x * 64 + lane;
+template <int TOK>
+__global__ __launch_bounds__(1024) void k_xent_join(const XentJoinArgs g) {
+  constexpr int GROUPS = 1024 / TOK;
+  __shared__ float2 red[16][TOK];
+  const int lane = threadIdx.x % TOK, grp = threadIdx.x / TOK, wave = threadIdx.x >> 6;
   const int valid = g.n_valid[0];
-  if ((int)blockIdx.x * 64 >= valid) return;
+  if ((int)blockIdx.x * TOK >= valid && !g.total) return;
+  const int n = blockIdx.x * TOK + lane;
   float top = -INFINITY, sum = 0.0f;
   auto join = [&](float2 o) {
     const float t = fmaxf(top, o.x), b = t == -INFINITY ? 0.0f : t;
@@ -264,25 +270,38 @@ __global__ __launch_bounds__(256) void k_xent_join(const XentJoinArgs g) {
   };
   if (n < valid) {
     int i = grp;
-    for (; i + 28 < g.tiles; i += 32) {
+    for (; i + 7 * GROUPS < g.tiles; i += 8 * GROUPS) {
       float2 v[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) v[u] = g.part[(i + 4 * u) * g.slots + n];
+      for (int u = 0; u < 8; ++u) v[u] = g.part[(i + u * GROUPS) * g.slots + n];
 #pragma unroll
       for (int u = 0; u < 8; ++u) join(v[u]);
     }
-    for (; i < g.tiles; i += 4) join(g.part[i * g.slots + n]);
+    for (; i < g.tiles; i += GROUPS) join(g.part[i * g.slots + n]);
   }
-  red[grp][lane] = make_float2(top, sum);
-  __syncthreads();
-  if (grp != 0 || n >= valid) return;
 #pragma unroll
-  for (int i = 1; i < 4; ++i) join(red[i][lane]);
-  const float l = top + logf(sum), d = l - g.target_logit[n];
-  const int row = g.rows[n];
-  g.lse[row] = l;
-  if (g.loss) g.loss[row] = d;
-  else g.slot_loss[n] = d;
+  for (int o = TOK; o < 64; o <<= 1) {                // the groups of a wavefront
+    const float2 other = make_float2(__shfl_xor(top, o), __shfl_xor(sum, o));
+    join(other);
+  }
+  if ((threadIdx.x & 63) < TOK) red[wave][lane] = make_float2(top, sum);
+  __syncthreads();
+  if (wave != 0) return;
+  double total = 0.0;
+  if (threadIdx.x < TOK && n < valid) {
+#pragma unroll
+    for (int i = 1; i < 16; ++i) join(red[i][lane]);
+    const float l = top + logf(sum), d = l - g.target_logit[n];
+    const int row = g.rows[n];
+    g.lse[row] = l;
+    if (g.loss) g.loss[row] = d;
+    if (g.slot_loss) g.slot_loss[n] = d;
+    total = (double)d;
+  }
+  if (g.total) {
+    total = wave_sum(total);
+    if (threadIdx.x == 0) g.total[0] = valid == 0 ? 0.0f : (float)(g.mean ? total / valid : total);
+  }
 }
 
 // mean or sum over the tokens, in double precision
@@ -622,10 +641,15 @@ extern "C" int efqat_linear_xent_fwd(const void* h, int64_t ldh, const void* w, 
   // tiles of a piece are whole but for the last piece's: pieces are multiples of 256 classes
   XentJoinArgs j = {};
   j.part = k.part; j.tiles = (int)ceil_div(V, p.bt); j.slots = p.slots; j.n_valid = k.n_valid; j.rows = k.rows;
-  j.target_logit = k.target_logit; j.lse = lse; j.loss = none ? loss : nullptr; j.slot_loss = k.slot_loss;
-  EFQAT_TRY(launch(k_xent_join, dim3((unsigned)ceil_div(T, 64)), dim3(256), 0, st, j));
-  if (none) return EFQAT_OK;
-  return launch(k_xent_reduce_loss, dim3(1), dim3(1024), 0, st, k.slot_loss, k.n_valid, reduction == EFQAT_XENT_MEAN ? 1 : 0, loss);
+  j.target_logit = k.target_logit; j.lse = lse; j.loss = none ? loss : nullptr;
+  const int mean = reduction == EFQAT_XENT_MEAN ? 1 : 0;
+  const bool one = !none && T <= 64;
+  if (one) { j.total = loss; j.mean = mean; }
+  else if (!none) j.slot_loss = k.slot_loss;
+  if (T <= 16) EFQAT_TRY(launch(k_xent_join<16>, dim3(1), dim3(1024), 0, st, j));
+  else EFQAT_TRY(launch(k_xent_join<64>, dim3((unsigned)ceil_div(T, 64)), dim3(1024), 0, st, j));
+  if (none || one) return EFQAT_OK;
+  return launch(k_xent_reduce_loss, dim3(1), dim3(1024), 0, st, k.slot_loss, k.n_valid, mean, loss);
 }
 
 extern "C" int efqat_linear_xent_bwd(const void* h, int64_t ldh, const void* w, int64_t ldw, int dtype, int64_t T, int64_t D, int64_t V,
@@ -677,7 +701,8 @@ extern "C" int efqat_linear_xent_bwd(const void* h, int64_t ldh, const void* w, 
     if (!p.join_dh || g.piece < p.n_pieces - 1) gh.out = nullptr;
     if (!p.join_dw) gw.out = nullptr;
     if (gh.out || gw.out) {
-      const dim3 grid(1024, gw.out ? 2 : 1);
+      const int64_t most = std::max(gh.out ? T : 0, gw.out ? std::min(V, (int64_t)p.pieces.size(0)) : 0) * D;
+      const dim3 grid((unsigned)std::min<int64_t>(ceil_div(most, 8 * 256), 1024), gw.out ? 2 : 1);
       EFQAT_TRY(dtype == EFQAT_F32 ? launch(k_xent_join_slices<float>, grid, dim3(256), 0, st, gh, p.bt_dh, gw, p.bt_dw)
                                    : launch(k_xent_join_slices<bf16_t>, grid, dim3(256), 0, st, gh, p.bt_dh, gw, p.bt_dw));
     }

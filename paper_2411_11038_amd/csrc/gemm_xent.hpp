@@ -2,7 +2,7 @@
 //
 //   out[n][m] = sum_k A[m][k] B[n][k]
 //
-//   logits (XG_LSE, XG_GRAD)  A = class weights W [m = class][k = feature], B = features H [n = token][k]
+//   logits (XG_LSE, XG_GRAD, XG_PART)  A = class weights W [m = class][k = feature], B = features H [n = token][k]
 //   dH     (XG_DH)            A = W read as [k = class][m = feature], B = G [n = token][k = class]
 //   dW     (XG_DW)            A = H read as [k = token][m = feature], B = G read as [k = token][n = class]
 //
@@ -36,7 +36,7 @@
 
 namespace efqat {
 
-enum XentMode { XG_LSE = 0, XG_GRAD = 1, XG_DH = 2, XG_DW = 3 };
+enum XentMode { XG_LSE = 0, XG_GRAD = 1, XG_DH = 2, XG_DW = 3, XG_PART = 4 };
 
 // The classes are taken in pieces, whose size follows from the number of tokens that have a class: a piece's G has about `elems`
 // elements (of all its parts), and its classes, where they are laid out anew, are `cap` at most.  The host knows the number of tokens
@@ -68,14 +68,14 @@ struct XentGemmArgs {
   XentPieces pieces;
   int piece;                      // number of the piece
   const int32_t* n_valid;
-  int split_blocks;               // products of G: K is cut so that about that many blocks work (xent_split)
+  int split_blocks;               // XG_PART and products of G: K is cut so that about that many blocks work (xent_split)
   // logits, per token slot
   const int32_t* target;
   float2* part;                   // XG_LSE: [tile of classes][slots] (largest logit, sum of exp(logit - largest))
   float* target_logit;            // XG_LSE
   int64_t slots;
   const float *lse, *scale;       // XG_GRAD, by slot; scale NULL: ones
-  // products of G: fp32 partial results [slice][n][D], and the output; the result is multiplied by *factor (NULL: 1), and divided by the
+  // XG_PART and products of G: fp32 partial results [slice][n][M], and the output; the result is multiplied by *factor (NULL: 1), and divided by the
   // number of tokens (mean)
   const float* factor;
   int mean;
@@ -86,7 +86,7 @@ struct XentGemmArgs {
   const int32_t* rows;            // XG_DH: rows of the output, by slot
 };
 
-// Slices of K of a product of G of so many tiles: about `blocks` blocks, none with fewer than 12 stages.  Shorter ones cost more at the
+// Slices of K of a product of so many tiles: about `blocks` blocks, none with fewer than 12 stages.  Shorter ones cost more at the
 // join than they save, longer ones leave CUs without work: at least 6 / 12 / 24 stages, backward of 256 fp32 tokens of width 256 against
 // 1000 classes 37.6 / 31.8 / 30.7 us, of 128 of 1920 against 786 71.2 / 71.2 / 72.9, of 65 bf16 of 768 against 30522 73.0 / 66.5 / 69.7.
 __host__ __device__ inline int xent_split(int64_t tiles, int stages, int segments, int blocks) {
@@ -108,7 +108,7 @@ struct XentShape {
     class0 = (int64_t)piece * g.piece;
     const int64_t left = g.pieces.V - class0;
     classes = (int)(left < 0 ? 0 : left < piece ? left : piece);
-    M = mode == XG_LSE || mode == XG_GRAD ? classes : (int)g.D;
+    M = mode == XG_DH || mode == XG_DW ? (int)g.D : classes;
     N = mode == XG_DW ? classes : valid;
     K = mode == XG_DW ? valid : mode == XG_DH ? classes : (int)g.Dp;
     nks = (K + 63) / 64;
@@ -235,7 +235,7 @@ struct XentTiles {
   __device__ __forceinline__ XentTiles(const XentGemmArgs& g, const XentShape& z, XentMode mode, int bt) {
     m = (z.M + bt - 1) / bt;
     n = (z.N + bt - 1) / bt;
-    const bool cut = mode == XG_DH || mode == XG_DW;
+    const bool cut = mode == XG_DH || mode == XG_DW || mode == XG_PART;
     slices = cut ? __builtin_amdgcn_readfirstlane(xent_split(z.split_tiles(bt), z.split_stages, g.segments, g.split_blocks)) : 1;
   }
   __device__ __forceinline__ int total() const { return m * n * slices; }
@@ -246,7 +246,7 @@ template <int BT, XentMode MODE>
 __device__ __forceinline__ void xent_gemm_block(const XentGemmArgs& g, const XentShape& z, const XentTiles& tiles_of, int valid, int bid, char* smem) {
 #if defined(__HIP_DEVICE_COMPILE__)
   using C = XentCfg<BT>;
-  constexpr bool LOGITS = MODE == XG_LSE || MODE == XG_GRAD;
+  constexpr bool LOGITS = MODE == XG_LSE || MODE == XG_GRAD || MODE == XG_PART, SOFT = LOGITS && MODE != XG_PART;
   constexpr bool ATR = !LOGITS, BTR = MODE == XG_DW;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -279,9 +279,9 @@ __device__ __forceinline__ void xent_gemm_block(const XentGemmArgs& g, const Xen
 
   // what the epilogue needs of the tokens: on its way while the product runs
   const int n_lane = n0 + wn * C::WN + (lane & 31);
-  int tok_class[LOGITS ? C::TN : 1];
+  int tok_class[SOFT ? C::TN : 1];
   float tok_lse[MODE == XG_GRAD ? C::TN : 1], tok_scale[MODE == XG_GRAD ? C::TN : 1];
-  if constexpr (LOGITS) {
+  if constexpr (SOFT) {
 #pragma unroll
     for (int j = 0; j < C::TN; ++j) {
       const int n = n_lane + 32 * j;
@@ -640,12 +640,14 @@ __device__ __forceinline__ void xent_gemm_block(const XentGemmArgs& g, const Xen
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       }
     } else {
-      // dH: the pieces are added up in acc, the last one leaves for the output.  Slices leave for acc in any case, and are joined later.
+      // dH: the pieces are added up in acc, the last one leaves for the output.  Slices, and logits, leave for acc in any case, and are
+      // joined later.
       float* part = g.acc + (int64_t)slice * N * M;
       const bool add = MODE == XG_DH && g.piece > 0;
-      const bool to_acc = nslice > 1 || (MODE == XG_DH && z.class0 + z.piece < g.pieces.V);
+      const bool to_acc = MODE == XG_PART || nslice > 1 || (MODE == XG_DH && z.class0 + z.piece < g.pieces.V);
       char* const out = (char*)g.out + (MODE == XG_DW ? z.class0 * g.ldo * (g.out_dtype == EFQAT_F32 ? 4 : 2) : 0);
       auto row_of = [&](int n) -> int64_t { return MODE == XG_DH ? g.rows[n] : n; };
+      if constexpr (MODE != XG_PART) {
       const float factor = (g.factor ? g.factor[0] : 1.0f) / (g.mean && valid > 0 ? (float)valid : 1.0f);
       if (g.factor || g.mean) {
 #pragma unroll
@@ -654,6 +656,7 @@ __device__ __forceinline__ void xent_gemm_block(const XentGemmArgs& g, const Xen
           for (int j = 0; j < C::TN; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] *= factor;
+      }
       }
       if (add || to_acc || g.out_dtype == EFQAT_F32) {
 #pragma unroll

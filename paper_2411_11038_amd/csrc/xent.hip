@@ -304,6 +304,130 @@ __global__ __launch_bounds__(1024) void k_xent_join(const XentJoinArgs g) {
   }
 }
 
+// ---- logits whose contraction was cut: the slices added in their order.  Forward: a token a block, its log-sum-exp and loss.
+struct XentLogitsArgs {
+  XentGemmArgs gemm;              // of the product that made them
+  int bt;
+  const int32_t* rows;
+  float *lse, *loss, *slot_loss;                      // forward; loss of the tokens by row, or by slot
+};
+// 4 logits of a token from class m on, of which n exist (the others: -inf)
+__device__ __forceinline__ void xent_sum_slices(const float* part, int64_t slice, int slices, int n, float (&v)[4]) {
+  typedef float vec __attribute__((ext_vector_type(4), aligned(4)));
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = 0.0f;
+  if (n >= 4) {
+    for (int k = 0; k < slices; k += 4) {             // four loads in flight
+      vec o[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) o[u] = *reinterpret_cast<const vec*>(part + (k + u < slices ? k + u : k) * slice);
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += k + u < slices ? o[u][e] : 0.0f;
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (e < n)
+        for (int k = 0; k < slices; ++k) v[e] += part[k * slice + e];
+      else
+        v[e] = -INFINITY;
+    }
+  }
+}
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void k_xent_logits_lse(const XentLogitsArgs g) {
+  constexpr int WAVES = THREADS / 64;
+  __shared__ float2 red[WAVES];
+  const int valid = g.gemm.n_valid[0], lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const XentShape z(g.gemm, XG_PART, valid);
+  const int slices = XentTiles(g.gemm, z, XG_PART, g.bt).slices;
+  const int64_t slice = (int64_t)z.N * z.M;
+  for (int n = blockIdx.x; n < valid; n += gridDim.x) {
+    const float* row = g.gemm.acc + (int64_t)n * z.M;
+    const int cls = g.gemm.target[n];
+    float top = -INFINITY, sum = 0.0f, at_class = -INFINITY;
+    auto join = [&](float t2, float s2) {
+      const float t = fmaxf(top, t2), b = t == -INFINITY ? 0.0f : t;
+      sum = sum * __builtin_amdgcn_exp2f((top - b) * 1.4426950408889634f) + s2 * __builtin_amdgcn_exp2f((t2 - b) * 1.4426950408889634f);
+      top = t;
+    };
+    for (int m = 4 * threadIdx.x; m < z.M; m += 4 * THREADS) {
+      float v[4];
+      xent_sum_slices(row + m, slice, slices, z.M - m, v);
+      const float t = fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), b = t == -INFINITY ? 0.0f : t;
+      float s = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s += __builtin_amdgcn_exp2f((v[e] - b) * 1.4426950408889634f);
+        at_class = m + e == cls ? v[e] : at_class;
+      }
+      join(t, s);
+    }
+    // the one lane that met the class knows its logit
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const float t2 = __shfl_xor(top, o), s2 = __shfl_xor(sum, o);
+      join(t2, s2);
+    }
+    if (lane == 0) red[wave] = make_float2(top, sum);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) {
+      const float2 o = red[i];
+      if (i == 0) { top = o.x; sum = o.y; }
+      else join(o.x, o.y);
+    }
+    const float l = top + logf(sum);
+    if (cls >> 2 == (cls >> 2) / THREADS * THREADS + (int)threadIdx.x) {
+      const int r = g.rows[n];
+      g.lse[r] = l;
+      if (g.loss) g.loss[r] = l - at_class;
+      if (g.slot_loss) g.slot_loss[n] = l - at_class;
+    }
+    __syncthreads();
+  }
+}
+// Backward: G from them, zeros up to whole stages of classes and tokens.  Chunks of 8 classes.
+__global__ __launch_bounds__(256) void k_xent_logits_grad(const XentLogitsArgs g) {
+  const int valid = g.gemm.n_valid[0];
+  const XentShape z(g.gemm, XG_PART, valid);
+  const int slices = XentTiles(g.gemm, z, XG_PART, g.bt).slices;
+  const int64_t slice = (int64_t)z.N * z.M;
+  const int parts = g.gemm.segments == 6 ? 3 : 1;
+  const int64_t ldg = (int64_t)parts * z.piece;
+  const uint32_t per_row = (uint32_t)(z.M + 63) / 64 * 8;
+  const int64_t all = (int64_t)((z.N + 63) / 64 * 64) * per_row;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+    const int n = (int)(i / per_row), m = (int)(i - (int64_t)n * per_row) * 8;
+    float v[8] = {};
+    if (n < z.N && m < z.M) {
+      const float lse = g.gemm.lse[n], scale = g.gemm.scale ? g.gemm.scale[n] : 1.0f;
+      const int cls = g.gemm.target[n] - m;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float x[4];
+        xent_sum_slices(g.gemm.acc + (int64_t)n * z.M + m + 4 * h, slice, slices, z.M - m - 4 * h, x);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float p = __builtin_amdgcn_exp2f((x[e] - lse) * 1.4426950408889634f);
+          v[4 * h + e] = m + 4 * h + e < z.M ? (cls == 4 * h + e ? p - 1.0f : p) * scale : 0.0f;
+        }
+      }
+    }
+    bf16_t* to = g.gemm.G + n * ldg + m;
+    for (int part = 0; part < parts; ++part) {
+      store_chunk(to + (int64_t)part * z.piece, 8, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float head = __uint_as_float(pack_bf16x2(v[e], v[e]) << 16);
+        v[e] = fabsf(head) < INFINITY ? v[e] - head : 0.0f;
+      }
+    }
+  }
+}
+
 // mean or sum over the tokens, in double precision
 __global__ __launch_bounds__(1024) void k_xent_reduce_loss(const float* __restrict__ slot_loss, const int32_t* __restrict__ n_valid, int mean,
                                                            float* __restrict__ loss) {
@@ -390,6 +514,7 @@ constexpr int64_t kXentMany = INT64_C(1) << 15;
 // a pass over the sums of dh: pieces of 128 / 256 / 512 MiB took 505 / 482 / 476 us for 12288 tokens, one in seven with a class, of
 // width 768 against 30522 classes, and 6.77 / 6.73 / 6.66 ms for 8192 of width 4096 against 32000.
 constexpr int64_t kXentGradLeast = INT64_C(1) << 26, kXentGradMost = INT64_C(1) << 28;
+constexpr int64_t kXentCutStages = 48;
 constexpr int64_t kXentStageElems = INT64_C(1) << 26; // most elements of a staged piece of W
 
 struct XentPlan {
@@ -400,10 +525,11 @@ struct XentPlan {
   int n_pieces;                   // most there can be
   int64_t grad_elems, stage_rows; // of G, of a staged piece
   int bt, bt_dh, bt_dw;           // tiles of the logits and of the two products
-  int blocks_dh, blocks_dw;
+  int blocks, blocks_dh, blocks_dw;
   int64_t grid, grid_dh, grid_dw; // tiles and slices, at most
-  bool join_dh, join_dw;          // K may be cut
-  int64_t acc_dh, acc_dw;         // fp32 partial results
+  bool cut;                       // the logits' contraction may be cut
+  bool join_dh, join_dw;          // that of a product of G may
+  int64_t acc_z, acc_dh, acc_dw;  // fp32 partial results
 };
 
 // Tile of the logits: the largest that gives three CUs in four something to do (of 64: whatever is left).  A larger tile reads its operands
@@ -450,13 +576,21 @@ static XentPlan xent_plan(int64_t T, int64_t D, int64_t V, int dtype, bool backw
   p.n_pieces = (int)ceil_div(V, piece);
   p.stage_rows = p.stage_w ? widest : 0;
   p.bt = logits_tile(T, std::min(V, piece));
+  const int64_t stages = p.Dp / 64 * p.segments, tiles = ceil_div(std::min(V, piece), p.bt) * ceil_div(T, p.bt);
+  p.blocks = p.bt == 128 ? 512 : 256;
+  p.cut = p.n_pieces == 1 && stages >= kXentCutStages && tiles < p.blocks;
+  if (p.cut) {
+    bool join;
+    p.acc_z = std::max(out_acc_elems(V, 1, T, p.Dp / 64, p.segments, p.bt, p.blocks, false, &join), T * V);
+  }
   if (!backward) {
-    p.grid = ceil_div(piece, p.bt) * ceil_div(T, p.bt);
+    p.grid = p.cut ? p.blocks : ceil_div(piece, p.bt) * ceil_div(T, p.bt);
     return p;
   }
   // a piece of G: `elems`, or 1024 classes of many tokens, or all classes
   p.grad_elems = std::min(p.slots * p.parts * round_up(V, 256), std::max<int64_t>(p.pieces.elems, p.slots * p.parts * 1024));
   p.grid = std::min(ceil_div(V, p.bt) * ceil_div(T, p.bt), p.grad_elems / p.parts / (p.bt * p.bt) + 1);
+  if (p.cut) p.grid = p.blocks;
   p.bt_dh = out_tile(D, T, ceil_div(piece, 64) * p.segments, &p.blocks_dh);
   p.bt_dw = out_tile(D, std::min(V, piece), ceil_div(T, 64) * p.segments, &p.blocks_dw);
   p.grid_dh = std::max<int64_t>(ceil_div(D, p.bt_dh) * ceil_div(T, p.bt_dh), p.blocks_dh);
@@ -470,7 +604,7 @@ struct XentWs {
   int32_t *n_valid, *rows, *target, *counts;
   bf16_t *h, *w, *grad;
   float2* part;
-  float *target_logit, *slot_loss, *slot_lse, *slot_scale, *acc_dh, *acc_dw;
+  float *target_logit, *slot_loss, *slot_lse, *slot_scale, *acc_z, *acc_dh, *acc_dw;
   size_t bytes;
 };
 static XentWs xent_ws(void* ws, const XentPlan& p, int64_t T, int64_t V, bool backward) {
@@ -482,6 +616,7 @@ static XentWs xent_ws(void* ws, const XentPlan& p, int64_t T, int64_t V, bool ba
   if (T >= kXentMany) w.counts = (int32_t*)c.take((size_t)ceil_div(T, kXentBlock) * sizeof(int32_t));
   w.h = (bf16_t*)c.take((size_t)(p.slots * p.parts * p.Dp) * 2);
   if (p.stage_w) w.w = (bf16_t*)c.take((size_t)(p.stage_rows * p.parts * p.Dp) * 2);
+  w.acc_z = (float*)c.take((size_t)p.acc_z * sizeof(float));
   if (backward) {
     w.slot_lse = (float*)c.take((size_t)T * sizeof(float));
     w.slot_scale = (float*)c.take((size_t)T * sizeof(float));
@@ -635,14 +770,25 @@ extern "C" int efqat_linear_xent_fwd(const void* h, int64_t ldh, const void* w, 
   for (g.piece = 0; g.piece < p.n_pieces; ++g.piece) {
     classes.piece = g.piece;
     if (p.stage_w || g.piece == 0) EFQAT_TRY(launch_stage(g.piece == 0 ? &tokens : nullptr, p.stage_w ? &classes : nullptr, few && g.piece == 0 ? &r : nullptr, dtype, st));
-    EFQAT_TRY(launch_xent_tile<XG_LSE>(p.bt, g, p.grid, st));
+    if (!p.cut) EFQAT_TRY(launch_xent_tile<XG_LSE>(p.bt, g, p.grid, st));
+  }
+  const int mean = reduction == EFQAT_XENT_MEAN ? 1 : 0;
+  if (p.cut) {
+    g.piece = 0;
+    g.acc = k.acc_z;
+    g.split_blocks = p.blocks;
+    EFQAT_TRY(launch_xent_tile<XG_PART>(p.bt, g, p.grid, st));
+    const XentLogitsArgs z = {g, p.bt, k.rows, lse, none ? loss : nullptr, none ? nullptr : k.slot_loss};
+    EFQAT_TRY(T <= 256 ? launch(k_xent_logits_lse<1024>, dim3((unsigned)T), dim3(1024), 0, st, z)
+                       : launch(k_xent_logits_lse<256>, dim3((unsigned)std::min<int64_t>(T, 2048)), dim3(256), 0, st, z));
+    if (none) return EFQAT_OK;
+    return launch(k_xent_reduce_loss, dim3(1), dim3(1024), 0, st, k.slot_loss, k.n_valid, mean, loss);
   }
 
   // tiles of a piece are whole but for the last piece's: pieces are multiples of 256 classes
   XentJoinArgs j = {};
   j.part = k.part; j.tiles = (int)ceil_div(V, p.bt); j.slots = p.slots; j.n_valid = k.n_valid; j.rows = k.rows;
   j.target_logit = k.target_logit; j.lse = lse; j.loss = none ? loss : nullptr;
-  const int mean = reduction == EFQAT_XENT_MEAN ? 1 : 0;
   const bool one = !none && T <= 64;
   if (one) { j.total = loss; j.mean = mean; }
   else if (!none) j.slot_loss = k.slot_loss;
@@ -685,7 +831,17 @@ extern "C" int efqat_linear_xent_bwd(const void* h, int64_t ldh, const void* w, 
   for (g.piece = 0; g.piece < p.n_pieces; ++g.piece) {
     classes.piece = g.piece;
     if (p.stage_w || g.piece == 0) EFQAT_TRY(launch_stage(g.piece == 0 ? &tokens : nullptr, p.stage_w ? &classes : nullptr, few && g.piece == 0 ? &r : nullptr, dtype, st));
-    EFQAT_TRY(launch_xent_tile<XG_GRAD>(p.bt, g, p.grid, st));
+    if (p.cut) {
+      XentGemmArgs gz = g;
+      gz.acc = k.acc_z;
+      gz.split_blocks = p.blocks;
+      EFQAT_TRY(launch_xent_tile<XG_PART>(p.bt, gz, p.grid, st));
+      const XentLogitsArgs z = {gz, p.bt, nullptr, nullptr, nullptr, nullptr};
+      const int64_t chunks = round_up(T, 64) * (round_up(V, 64) / 8);
+      EFQAT_TRY(launch(k_xent_logits_grad, dim3((unsigned)std::min<int64_t>(ceil_div(chunks, 256), 2048)), dim3(256), 0, st, z));
+    } else {
+      EFQAT_TRY(launch_xent_tile<XG_GRAD>(p.bt, g, p.grid, st));
+    }
     XentGemmArgs gh = g, gw = g;
     gh.split_blocks = p.blocks_dh; gh.acc = k.acc_dh; gh.out = dh; gh.ldo = lddh; gh.rows = k.rows;
     gw.split_blocks = p.blocks_dw; gw.acc = k.acc_dw; gw.out = dw; gw.ldo = lddw;

@@ -270,3 +270,40 @@ def test_many_tokens(T):
     t[[0, T - 1]] = [-100, 3]
     r = check_all(h, w, t, hd, wd, torch.from_numpy(t).cuda(), "bf16")
     assert (r["dh"][0] == 0).all() and (r["dh"][T - 1] != 0).any()
+
+
+# logits of few tiles and long rows: their contraction is cut, the softmax follows the join; tiles of 64 and 128, whole and ragged
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,D,V", [(1, 4096, 1), (1, 4096, 3), (5, 3200, 1001), (64, 3136, 64), (70, 4160, 333), (300, 3136, 130), (200, 3500, 999), (700, 3200, 2050)])
+def test_contractions_of_logits_in_slices(T, D, V, dtype):
+    check_all(*make(T, D, V, dtype, T + D + V, ignored=0.2 if T > 1 else 0.0), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("reduction", [ef.XENT_NONE, ef.XENT_MEAN, ef.XENT_SUM])
+def test_reductions_of_logits_in_slices(reduction, dtype):
+    h, w, t, hd, wd, td = make(90, 3200, 150, dtype, 7, ignored=0.3)
+    rng = np.random.default_rng(8)
+    up = rng.standard_normal(90 if reduction == ef.XENT_NONE else 1)
+    out = t < 0
+    hd[out] = float("nan")
+    r = check_all(h, w, t, hd, wd, td, dtype, reduction=reduction, dloss=up)
+    assert (r["dh"][torch.from_numpy(out).cuda()] == 0).all()
+    td.fill_(-100)
+    r = ef.linear_xent_fwd(hd, wd, td, reduction=reduction)
+    r.update(ef.linear_xent_bwd(hd, wd, td, r["lse"], reduction=reduction))
+    assert all((r[k] == 0).all() for k in ("loss", "lse", "n_valid", "dh", "dw"))
+
+
+def test_masked_classes_of_logits_in_slices():
+    """logits of -inf: no probability, no gradient of their own"""
+    h, w, t, hd, wd, td = make(40, 4096, 100, "bf16", 9)
+    t[:] = 3 + t % 90
+    td = torch.from_numpy(t).cuda()
+    hd[:, 0] = 1.0
+    wd[:3, 0] = float("-inf")
+    r = ef.linear_xent_fwd(hd, wd, td)
+    ref = ef.linear_xent_fwd(hd, wd[3:].contiguous(), td - 3)
+    assert torch.allclose(r["lse"], ref["lse"], rtol=1e-6, atol=1e-6) and torch.isfinite(r["loss"]).all()
+    g = ef.linear_xent_bwd(hd, wd, td, r["lse"])
+    assert (g["dw"][:3] == 0).all() and torch.isfinite(g["dw"]).all()

@@ -441,7 +441,8 @@ int efqat_layer_norm_bwd(const void* dy, int64_t lddy, int dtype, const void* x,
  *   lse[t] = log sum_v exp(z[t][v]),   loss of token t = lse[t] - z[t][targets[t]]
  *   G = (exp(z - lse) - [v = targets[t]]) * (upstream gradient of token t's loss),  dh = G w,  dw = G^T h
  *   h        in  [T][D], w in [V][D], dtype F32 or BF16 (both); BF16 with D a multiple of 64: w 16-byte
- *                aligned and ldw a multiple of 8
+ *                aligned and ldw a multiple of 8.  BF16 rows of w of whole 16 bytes are read as they lie, others
+ *                (and F32) are laid out anew in the workspace
  *   targets  in  int64[T].  A token whose target is ignore_index, or outside [0, V), has no class: it takes no
  *                part, whatever its row of h holds; its loss, lse and row of dh are 0
  *   reduction    loss is float[T] (NONE), or float[1]: the mean or the sum over the tokens with a class (0

@@ -174,7 +174,8 @@ struct XentOperand {
         addr[sub] = lds0 + (wpos * WW + fr) * 128 + (((2 * sub + fh) ^ ((fr >> 1) & 7)) << 4);
     }
   }
-  // copy j of a stage; last: rows k >= left of a TR operand do not exist, the last one is repeated (the other operand's are zero)
+  // copy j of a stage; last: of a TR operand, rows k >= left do not exist, the last one is repeated (the other operand's are zero); of
+  // another, columns >= left (whole chunks) do not, they are zeros
   __device__ __forceinline__ void copy(const char* base, uint32_t lds, int wave, int j) const {
     dma16_at(base, voff[j], lds + (wave + NW * j) * 1024);
   }
@@ -183,8 +184,13 @@ struct XentOperand {
     if constexpr (TR) {
       const int k = (wave + NW * j) * RPC + lane / CPR;
       if (k >= left) off -= (uint32_t)(k - left + 1) * (uint32_t)(ld * 2);
+      dma16_at(base, off, lds + (wave + NW * j) * 1024);
+    } else {
+      const int r = (wave + NW * j) * 8 + (lane >> 3), c = (lane & 7) ^ ((r >> 1) & 7);
+      const char* from = c * 8 < left ? base + off : zero_page();
+      asm volatile("s_mov_b32 m0, %0" ::"s"(lds + (wave + NW * j) * 1024) : "m0");
+      asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from));
     }
-    dma16_at(base, off, lds + (wave + NW * j) * 1024);
   }
   // read number r of sub-step sub
   __device__ __forceinline__ void read(const char* smem, int sub, int r, Frag (&f)[T]) const {
@@ -274,8 +280,8 @@ __device__ __forceinline__ void xent_gemm_block(const XentGemmArgs& g, const Xen
   const bf16_t* opB = LOGITS ? g.H : g.G;
   const int64_t lda = MODE == XG_DW ? ldh : g.ldw, ldb = LOGITS ? ldh : ldg;
   const int64_t a_part = g.Dp, b_part = LOGITS ? g.Dp : z.piece;
-  // the rows of W end inside the last stage of dH
-  const int a_rows = MODE == XG_DH && !g.w_piece ? z.K : 0;
+  // classes as they lie end inside the last stage: rows in dH, columns in the logits
+  const int a_end = g.w_piece || MODE == XG_DW ? 0 : MODE == XG_DH ? z.K : (int)g.D;
 
   // what the epilogue needs of the tokens: on its way while the product runs
   const int n_lane = n0 + wn * C::WN + (lane & 31);
@@ -296,7 +302,7 @@ __device__ __forceinline__ void xent_gemm_block(const XentGemmArgs& g, const Xen
   XentOperand<BT, C::OWN ? BT : C::WM, C::OWN ? 1 : C::NW, ATR> A;
   XentOperand<BT, C::OWN ? BT : C::WN, C::OWN ? 1 : C::NW, BTR> B;
   const int copier = C::OWN ? 0 : wave;               // among the wavefronts that copy a stage together
-  A.setup(lda, ATR ? (int)g.Dp - m0 : M - m0, copier, C::OWN ? 0 : wm, lane, 0);
+  A.setup(lda, ATR ? (int)g.D - m0 : M - m0, copier, C::OWN ? 0 : wm, lane, 0);
   B.setup(ldb, BTR ? z.piece - n0 : N - n0, copier, C::OWN ? 0 : wn, lane, BT * 128);
   const int64_t a_step = ATR ? lda * 128 : 128, b_step = BTR ? ldb * 128 : 128;
   const char* a_base = (const char*)opA + (ATR ? (int64_t)m0 * 2 : (int64_t)m0 * lda * 2) + k_first * a_step;
@@ -325,7 +331,7 @@ __device__ __forceinline__ void xent_gemm_block(const XentGemmArgs& g, const Xen
 #pragma unroll
     for (int t = t0; t < t1; ++t) {
       if (t < AG) {
-        if constexpr (decltype(lastc)::value) A.copy_last(a_src, l, copier, lane, t, lda, a_rows - (k_end - 1) * 64);
+        if constexpr (decltype(lastc)::value) A.copy_last(a_src, l, copier, lane, t, lda, a_end - (k_end - 1) * 64);
         else A.copy(a_src, l, copier, t);
       } else {
         B.copy(b_src, l + BT * 128, copier, t - AG);
@@ -334,8 +340,8 @@ __device__ __forceinline__ void xent_gemm_block(const XentGemmArgs& g, const Xen
   };
   using Last = std::integral_constant<bool, true>;
   using Whole = std::integral_constant<bool, false>;
-  // the last stage of a TR A whose rows end inside it is copied apart
-  const int nfull = a_rows && k_end == nks && (a_rows & 63) ? nstage - 1 : nstage;
+  // the last stage is copied apart if they do
+  const int nfull = a_end && k_end == nks && (a_end & 63) ? nstage - 1 : nstage;
 
   floatx16_t acc[C::TM][C::TN];
 #pragma unroll

@@ -8,6 +8,7 @@
 // G in bf16 (a buffer that the last-level cache holds) and are multiplied by w and by h.  G in fewer bits than 32 is what lets both
 // products run on the matrix cores at their bf16 rate, like the operands; its rounding is as large as that of the results, each of which
 // sums thousands of its entries.  fp32 operands, and then G too, are three bf16 parts: 24 bits.
+// Few tiles of many stages: the logits' contraction is cut over the blocks, and the softmax follows the join of the slices.
 //
 // 8 T D V operations of a training step are products on the matrix cores and bound it; with few tokens, reading w does.  bf16, 8192
 // tokens of width 4096 against 32000 classes, 98 % of them with one: 6.7 ms forward and backward, 1.25 POP/s.  12288 of width 768 against
@@ -514,6 +515,11 @@ constexpr int64_t kXentMany = INT64_C(1) << 15;
 // a pass over the sums of dh: pieces of 128 / 256 / 512 MiB took 505 / 482 / 476 us for 12288 tokens, one in seven with a class, of
 // width 768 against 30522 classes, and 6.77 / 6.73 / 6.66 ms for 8192 of width 4096 against 32000.
 constexpr int64_t kXentGradLeast = INT64_C(1) << 26, kXentGradMost = INT64_C(1) << 28;
+// K stages (of all products of parts) from which on the logits' contraction is cut, where their tiles are fewer than the blocks that the
+// chip holds: the slices leave as fp32 sums and the softmax is a pass of its own over them.  Whole / cut, forward and backward, us: 128 fp32
+// tokens of width 1920 against 786 classes (180 stages, 26 tiles) 48 + 72 / 29 + 57, 557 bf16 (of 3712, the host knows no better) of 6400
+// against 1408 85 + 122 / 38 + 77, 1024 of 4096 against 4096 62 + 145 / 55 + 141.  It costs where there is one slice after all: all 3712 of
+// those tokens 103 + 317 / 115 + 263.  With 24 to 32 stages both take the same (512 bf16 of 2048 against 2000 22 + 43 / 23 + 43).
 constexpr int64_t kXentCutStages = 48;
 constexpr int64_t kXentStageElems = INT64_C(1) << 26; // most elements of a staged piece of W
 
@@ -560,13 +566,19 @@ static int64_t out_acc_elems(int64_t M, int64_t fewest, int64_t N, int64_t stage
   return std::max(N, std::min(most * N, blocks * (int64_t)bt / tm)) * M;
 }
 
-static XentPlan xent_plan(int64_t T, int64_t D, int64_t V, int dtype, bool backward) {
+// Classes that the products read as they lie: bf16, in rows of whole 16 bytes.  Others are laid out anew, piece by piece, in both passes: of
+// width 1360, 53730 of them, 16 tokens, that takes 97 + 196 us forward and backward instead of 46 + 122 (8192 tokens of width 1000 against
+// 32000 1 % less: rows of whole 128 bytes).
+static bool xent_direct(int dtype, int64_t D, const void* w, int64_t ldw) {
+  return dtype == EFQAT_BF16 && D % 8 == 0 && aligned16(w) && ldw % 8 == 0;
+}
+static XentPlan xent_plan(int64_t T, int64_t D, int64_t V, int dtype, bool direct, bool backward) {
   XentPlan p = {};
   p.parts = dtype == EFQAT_F32 ? 3 : 1;
   p.segments = dtype == EFQAT_F32 ? 6 : 1;
   p.Dp = round_up(D, 64);
   p.slots = round_up(T, 256);
-  p.stage_w = p.parts == 3 || D % 64 != 0;
+  p.stage_w = !direct;
   p.pieces.V = (int)V;
   p.pieces.parts = p.parts;
   p.pieces.elems = backward ? (uint32_t)std::min(std::max(p.slots * p.parts * round_up(ceil_div(V, 2), 256), kXentGradLeast), kXentGradMost) : 0;
@@ -630,6 +642,17 @@ static XentWs xent_ws(void* ws, const XentPlan& p, int64_t T, int64_t V, bool ba
   }
   w.bytes = c.off;
   return w;
+}
+
+static bool xent_sizes_ok(int64_t T, int64_t D, int64_t V) {
+  return T > 0 && D > 0 && V > 0 && T <= INT64_C(1) << 30 && V <= INT64_C(1) << 30 && D <= INT64_C(1) << 20;
+}
+// of a call whose pointers are not known yet
+static size_t xent_bytes(int64_t T, int64_t D, int64_t V, int dtype, bool backward) {
+  if (!xent_sizes_ok(T, D, V) || !known_dtype(dtype)) return 256;
+  const bool may = xent_direct(dtype, D, nullptr, 0), must = may && D % 64 == 0;
+  const size_t as_is = may ? xent_ws(nullptr, xent_plan(T, D, V, dtype, true, backward), T, V, backward).bytes : 0;
+  return must ? as_is : std::max(as_is, xent_ws(nullptr, xent_plan(T, D, V, dtype, false, backward), T, V, backward).bytes);
 }
 
 template <int BT, XentMode MODE>
@@ -712,9 +735,6 @@ static XentStageArgs xent_stage_classes(const XentPlan& p, const XentWs& k, cons
   return s;
 }
 
-static bool xent_sizes_ok(int64_t T, int64_t D, int64_t V) {
-  return T > 0 && D > 0 && V > 0 && T <= INT64_C(1) << 30 && V <= INT64_C(1) << 30 && D <= INT64_C(1) << 20;
-}
 static int check_xent(const void* h, int64_t ldh, const void* w, int64_t ldw, int dtype, int64_t T, int64_t D, int64_t V,
                       const int64_t* targets, int reduction, const void* ws) {
   // token slots and classes are 32-bit numbers, offsets inside a tile of 256 rows too
@@ -733,14 +753,8 @@ static int check_xent(const void* h, int64_t ldh, const void* w, int64_t ldw, in
 
 using namespace efqat;
 
-extern "C" size_t efqat_linear_xent_fwd_workspace_bytes(int64_t T, int64_t D, int64_t V, int dtype) {
-  if (!xent_sizes_ok(T, D, V) || !known_dtype(dtype)) return 256;
-  return xent_ws(nullptr, xent_plan(T, D, V, dtype, false), T, V, false).bytes;
-}
-extern "C" size_t efqat_linear_xent_bwd_workspace_bytes(int64_t T, int64_t D, int64_t V, int dtype) {
-  if (!xent_sizes_ok(T, D, V) || !known_dtype(dtype)) return 256;
-  return xent_ws(nullptr, xent_plan(T, D, V, dtype, true), T, V, true).bytes;
-}
+extern "C" size_t efqat_linear_xent_fwd_workspace_bytes(int64_t T, int64_t D, int64_t V, int dtype) { return xent_bytes(T, D, V, dtype, false); }
+extern "C" size_t efqat_linear_xent_bwd_workspace_bytes(int64_t T, int64_t D, int64_t V, int dtype) { return xent_bytes(T, D, V, dtype, true); }
 
 extern "C" int efqat_linear_xent_fwd(const void* h, int64_t ldh, const void* w, int64_t ldw, int dtype, int64_t T, int64_t D, int64_t V,
                                      const int64_t* targets, int64_t ignore_index, int reduction, float* loss, float* lse,
@@ -748,7 +762,7 @@ extern "C" int efqat_linear_xent_fwd(const void* h, int64_t ldh, const void* w, 
   if (const int rc = check_xent(h, ldh, w, ldw, dtype, T, D, V, targets, reduction, ws)) return rc;
   if (!loss || !lse) return EFQAT_ERR_NULL_PTR;
   if (!aligned4(loss) || !aligned4(lse) || !aligned4(n_valid)) return EFQAT_ERR_ALIGNMENT;
-  const XentPlan p = xent_plan(T, D, V, dtype, false);
+  const XentPlan p = xent_plan(T, D, V, dtype, xent_direct(dtype, D, w, ldw), false);
   const XentWs k = xent_ws(ws, p, T, V, false);
   if (ws_bytes < k.bytes) return EFQAT_ERR_WORKSPACE;
   if (std::max({p.grid, p.grid_dh, p.grid_dw}) > INT32_MAX / 2) return EFQAT_ERR_BAD_SHAPE;
@@ -805,7 +819,7 @@ extern "C" int efqat_linear_xent_bwd(const void* h, int64_t ldh, const void* w, 
   if ((dh && lddh < D) || (dw && lddw < D)) return EFQAT_ERR_BAD_SHAPE;
   if (!lse || (!dh && !dw)) return EFQAT_ERR_NULL_PTR;
   if (!aligned4(lse) || !aligned4(dloss) || !aligned_for(dh, dtype) || !aligned_for(dw, dtype)) return EFQAT_ERR_ALIGNMENT;
-  const XentPlan p = xent_plan(T, D, V, dtype, true);
+  const XentPlan p = xent_plan(T, D, V, dtype, xent_direct(dtype, D, w, ldw), true);
   const XentWs k = xent_ws(ws, p, T, V, true);
   if (ws_bytes < k.bytes) return EFQAT_ERR_WORKSPACE;
   if (std::max({p.grid, p.grid_dh, p.grid_dw}) > INT32_MAX / 2) return EFQAT_ERR_BAD_SHAPE;

@@ -307,3 +307,29 @@ def test_masked_classes_of_logits_in_slices():
     assert torch.allclose(r["lse"], ref["lse"], rtol=1e-6, atol=1e-6) and torch.isfinite(r["loss"]).all()
     g = ef.linear_xent_bwd(hd, wd, td, r["lse"])
     assert (g["dw"][:3] == 0).all() and torch.isfinite(g["dw"]).all()
+
+
+@pytest.mark.parametrize("D,V", [(8, 300), (72, 900), (72, 20011), (520, 20011), (3144, 90)])
+@pytest.mark.parametrize("at,ld", [(16, 40), (3, 40), (8, 37)])
+def test_classes_as_they_lie(at, ld, D, V):
+    """rows of whole 16 bytes that end inside a stage, between NaNs; rows that begin or lie at other addresses"""
+    T = 150 if V < 20000 else 600
+    h, w, t, hd, wd, td = make(T, D, V, "bf16", D + V + at, ignored=0.1)
+    big_w = torch.full((V, D + ld), float("nan"), dtype=wd.dtype, device="cuda")
+    ws_ = big_w[:, at: at + D]
+    ws_.copy_(wd)
+    check_all(h, w, t, hd, ws_, td, "bf16")
+
+
+@pytest.mark.parametrize("D", [72, 520])
+def test_masked_classes_whose_rows_end_inside_a_stage(D):
+    h, w, t, hd, wd, td = make(300, D, 20000, "bf16", 12)
+    t[:] = 3 + t % 19990
+    td = torch.from_numpy(t).cuda()
+    hd[:, 0] = 1.0
+    wd[:3, 0] = float("-inf")
+    r = ef.linear_xent_fwd(hd, wd, td)
+    ref = ef.linear_xent_fwd(hd, wd[3:].contiguous(), td - 3)
+    assert torch.allclose(r["lse"], ref["lse"], rtol=1e-6, atol=1e-6) and torch.isfinite(r["loss"]).all()
+    g = ef.linear_xent_bwd(hd, wd, td, r["lse"])
+    assert (g["dw"][:3] == 0).all() and torch.isfinite(g["dw"]).all()

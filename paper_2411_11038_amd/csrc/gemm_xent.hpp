@@ -2,7 +2,7 @@
 //
 //   out[n][m] = sum_k A[m][k] B[n][k]
 //
-//   logits (XG_LSE, XG_GRAD, XG_PART)  A = class weights W [m = class][k = feature], B = features H [n = token][k]
+//   logits (XG_LSE, XG_GRAD, XG_GRAD3 for G in three parts, XG_PART)  A = class weights W [m = class][k = feature], B = features H [n = token][k]
 //   dH     (XG_DH)            A = W read as [k = class][m = feature], B = G [n = token][k = class]
 //   dW     (XG_DW)            A = H read as [k = token][m = feature], B = G read as [k = token][n = class]
 //
@@ -36,7 +36,7 @@
 
 namespace efqat {
 
-enum XentMode { XG_LSE = 0, XG_GRAD = 1, XG_DH = 2, XG_DW = 3, XG_PART = 4 };
+enum XentMode { XG_LSE = 0, XG_GRAD = 1, XG_DH = 2, XG_DW = 3, XG_PART = 4, XG_GRAD3 = 5 };
 
 // The classes are taken in pieces, whose size follows from the number of tokens that have a class: a piece's G has about `elems`
 // elements (of all its parts), and its classes, where they are laid out anew, are `cap` at most.  The host knows the number of tokens
@@ -252,7 +252,7 @@ template <int BT, XentMode MODE>
 __device__ __forceinline__ void xent_gemm_block(const XentGemmArgs& g, const XentShape& z, const XentTiles& tiles_of, int valid, int bid, char* smem) {
 #if defined(__HIP_DEVICE_COMPILE__)
   using C = XentCfg<BT>;
-  constexpr bool LOGITS = MODE == XG_LSE || MODE == XG_GRAD || MODE == XG_PART, SOFT = LOGITS && MODE != XG_PART;
+  constexpr bool GRAD = MODE == XG_GRAD || MODE == XG_GRAD3, LOGITS = MODE == XG_LSE || GRAD || MODE == XG_PART, SOFT = MODE == XG_LSE || GRAD;
   constexpr bool ATR = !LOGITS, BTR = MODE == XG_DW;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -286,13 +286,13 @@ __device__ __forceinline__ void xent_gemm_block(const XentGemmArgs& g, const Xen
   // what the epilogue needs of the tokens: on its way while the product runs
   const int n_lane = n0 + wn * C::WN + (lane & 31);
   int tok_class[SOFT ? C::TN : 1];
-  float tok_lse[MODE == XG_GRAD ? C::TN : 1], tok_scale[MODE == XG_GRAD ? C::TN : 1];
+  float tok_lse[GRAD ? C::TN : 1], tok_scale[GRAD ? C::TN : 1];
   if constexpr (SOFT) {
 #pragma unroll
     for (int j = 0; j < C::TN; ++j) {
       const int n = n_lane + 32 * j;
       tok_class[j] = n < N ? g.target[n] : -1;
-      if constexpr (MODE == XG_GRAD) {
+      if constexpr (GRAD) {
         tok_lse[j] = n < N ? g.lse[n] : 0.0f;
         tok_scale[j] = n < N && g.scale ? g.scale[n] : 1.0f;
       }
@@ -519,14 +519,23 @@ __device__ __forceinline__ void xent_gemm_block(const XentGemmArgs& g, const Xen
   __syncthreads();
 
   // ---- accumulators: column n = lane & 31, rows m = 8 (r / 4) + 4 (lane / 32) + r % 4 of their 32 x 32
-  const int fr = lane & 31, fh = lane >> 5;
+  int late = lane;                                    // not known to be the same for every tile: addresses that follow from it are made
+  asm volatile("" : "+v"(late));                      // here, not kept in registers through the products
+  const int fr = late & 31, fh = late >> 5;
   const int mw = m0 + wm * C::WM + 4 * fh, nw = n0 + wn * C::WN + fr;
   auto m_of = [&](int i, int r) { return mw + 32 * i + 8 * (r >> 2) + (r & 3); };
 
   if constexpr (MODE == XG_LSE) {
     // largest logit and sum of exponentials of the tile's classes, for every token; the tile's wavefronts join theirs in LDS
     float2* red = reinterpret_cast<float2*>(smem);    // [WGM][BT]
-    const bool edge = m0 + BT > M;
+    if (m0 + BT > M) {                                // the last class is repeated
+#pragma unroll
+      for (int j = 0; j < C::TN; ++j)
+#pragma unroll
+        for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[i][j][r] = m_of(i, r) < M ? acc[i][j][r] : -INFINITY;
+    }
 #pragma unroll
     for (int j = 0; j < C::TN; ++j) {
       const int n = nw + 32 * j;
@@ -534,10 +543,7 @@ __device__ __forceinline__ void xent_gemm_block(const XentGemmArgs& g, const Xen
 #pragma unroll
       for (int i = 0; i < C::TM; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          if (edge && m_of(i, r) >= M) acc[i][j][r] = -INFINITY;
-          top = fmaxf(top, acc[i][j][r]);
-        }
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, acc[i][j][r]);
       top = fmaxf(top, __shfl_xor(top, 32));
       // a token whose logits are all -inf has sum 0; a NaN makes the sum NaN
       const float base = top == -INFINITY ? 0.0f : top;
@@ -575,75 +581,91 @@ __device__ __forceinline__ void xent_gemm_block(const XentGemmArgs& g, const Xen
       *reinterpret_cast<uint2*>(tile + (32 * j + fr) * C::OUT_PITCH + (32 * i + 8 * q + 4 * fh) * 2) =
           make_uint2(pack_bf16x2(a, b), pack_bf16x2(c, d));
     };
-    if constexpr (MODE == XG_GRAD) {
+    if constexpr (GRAD) {
       // G = (softmax - [class of the token]) scale, in bf16; zero outside the classes and behind the last token.  A factor that all tokens
       // share is left to the products of G: without it the -1 for the class of a token that the model knows nothing about is exact in
       // bf16, while the same factor on all of them is the same rounding error for all, which no sum averages out.  dh and dw of 8028 tokens
       // against 32000 classes are 0.17 % off in the 2-norm (the rounding of the results themselves), and were 0.24 to 0.32 % off with
       // 1 / 8028 inside G.
-      const bool edge = m0 + BT > M;
-#pragma unroll
-      for (int j = 0; j < C::TN; ++j) {
-        const int n = nw + 32 * j;
-        const bool in = n < N;
-        const float lse = tok_lse[j], scale = tok_scale[j];
-        const int rel = in ? tok_class[j] - (int)z.class0 - m0 - wm * C::WM : -1;   // row of the wavefront's tile that is the class
-#pragma unroll
-        for (int i = 0; i < C::TM; ++i)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) acc[i][j][r] = __builtin_amdgcn_exp2f((acc[i][j][r] - lse) * 1.4426950408889634f);
-        if (__any(rel >= 0 && rel < C::WM)) {
-          const int mine = rel - 4 * fh;
-#pragma unroll
-          for (int i = 0; i < C::TM; ++i)
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-              if (mine == 32 * i + 8 * (r >> 2) + (r & 3)) acc[i][j][r] -= 1.0f;
-        }
-        if (g.scale) {
-#pragma unroll
-          for (int i = 0; i < C::TM; ++i)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[i][j][r] *= scale;
-        }
-        if (edge) {                                   // a repeated class may be anything
-#pragma unroll
-          for (int i = 0; i < C::TM; ++i)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[i][j][r] = m_of(i, r) < M ? acc[i][j][r] : 0.0f;
-        }
-        if (!in) {                                    // a repeated token too
-#pragma unroll
-          for (int i = 0; i < C::TM; ++i)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
-        }
-      }
-      for (int part = 0; part < parts; ++part) {
-#pragma unroll
-        for (int j = 0; j < C::TN; ++j)
-#pragma unroll
-          for (int i = 0; i < C::TM; ++i)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              float p[4];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                p[e] = acc[i][j][4 * q + e];
-                const float head = __uint_as_float(pack_bf16x2(p[e], p[e]) << 16);
-                if (part + 1 < parts) acc[i][j][4 * q + e] = fabsf(head) < INFINITY ? p[e] - head : 0.0f;
-              }
-              put(i, j, q, p[0], p[1], p[2], p[3]);
-            }
+      auto leave = [&](int part) {                      // of all lanes: what `put` has laid out
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
         for (int r0 = 0; r0 < C::WN; r0 += RPI) {
-          const int r = r0 + lane / CPR, c = lane % CPR;
+          const int r = r0 + late / CPR, c = late % CPR;
           const uint4 v = *reinterpret_cast<const uint4*>(tile + r * C::OUT_PITCH + c * 16);
           bf16_t* to = g.G + (n0 + wn * C::WN + r) * ldg + (int64_t)part * z.piece + m0 + wm * C::WM + c * 8;
           *reinterpret_cast<uint4*>(to) = v;
         }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      };
+      auto softmax = [&](float v, float lse) { return __builtin_amdgcn_exp2f((v - lse) * 1.4426950408889634f); };
+      if (MODE == XG_GRAD && m0 + BT <= M && n0 + BT <= N && !g.scale) {
+        // Straight through, no accumulator is written: the entry of a token's class, which few tiles have, is put over the others in LDS.
+#pragma unroll
+        for (int j = 0; j < C::TN; ++j) {
+          const float lse = tok_lse[j];
+#pragma unroll
+          for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              put(i, j, q, softmax(acc[i][j][4 * q], lse), softmax(acc[i][j][4 * q + 1], lse), softmax(acc[i][j][4 * q + 2], lse),
+                  softmax(acc[i][j][4 * q + 3], lse));
+          const int rel = tok_class[j] - (int)z.class0 - m0 - wm * C::WM;              // row of the wavefront's tile that is the class
+          if (__any(rel >= 0 && rel < C::WM)) {
+            const int mine = rel - 4 * fh;
+            float at_class = 0.0f;
+#pragma unroll
+            for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+              for (int r = 0; r < 16; ++r) at_class = mine == 32 * i + 8 * (r >> 2) + (r & 3) ? acc[i][j][r] : at_class;
+            asm volatile("" ::: "memory");
+            if (mine >= 0 && mine < C::WM && !(mine & 4))
+              *reinterpret_cast<bf16_t*>(tile + (32 * j + fr) * C::OUT_PITCH + rel * 2) = from_f32<bf16_t>(softmax(at_class, lse) - 1.0f);
+          }
+        }
+        leave(0);
+      } else {
+        const int m_left = M - mw;
+        auto entry = [&](int i, int j, int r) {
+          const int at = 32 * i + 8 * (r >> 2) + (r & 3);
+          float p = softmax(acc[i][j][r], tok_lse[j]);
+          p -= tok_class[j] - (int)z.class0 - mw == at ? 1.0f : 0.0f;
+          return at < m_left && nw + 32 * j < N ? p * tok_scale[j] : 0.0f;           // a repeated class or token may be anything
+        };
+        if constexpr (MODE == XG_GRAD) {
+#pragma unroll
+          for (int j = 0; j < C::TN; ++j)
+#pragma unroll
+            for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+              for (int q = 0; q < 4; ++q) put(i, j, q, entry(i, j, 4 * q), entry(i, j, 4 * q + 1), entry(i, j, 4 * q + 2), entry(i, j, 4 * q + 3));
+          leave(0);
+        } else {
+#pragma unroll
+          for (int j = 0; j < C::TN; ++j)
+#pragma unroll
+            for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+              for (int r = 0; r < 16; ++r) acc[i][j][r] = entry(i, j, r);
+#pragma unroll
+          for (int part = 0; part < 3; ++part) {
+#pragma unroll
+            for (int j = 0; j < C::TN; ++j)
+#pragma unroll
+              for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                  floatx16_t& v = acc[i][j];
+                  put(i, j, q, v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+#pragma unroll
+                  for (int e = 4 * q; e < 4 * q + 4 && part < 2; ++e) {
+                    const float head = __uint_as_float(pack_bf16x2(v[e], v[e]) << 16);
+                    v[e] = fabsf(head) < INFINITY ? v[e] - head : 0.0f;
+                  }
+                }
+            leave(part);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          }
+        }
       }
     } else {
       // dH: the pieces are added up in acc, the last one leaves for the output.  Slices, and logits, leave for acc in any case, and are
@@ -727,7 +749,7 @@ __device__ __forceinline__ void xent_gemm_block(const XentGemmArgs& g, const Xen
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
         for (int r0 = 0; r0 < C::WN; r0 += RPI) {
-          const int r = r0 + lane / CPR, c = lane % CPR;
+          const int r = r0 + late / CPR, c = late % CPR;
           const int n = n0 + wn * C::WN + r, m = m0 + wm * C::WM + c * 8;
           const uint4 v = *reinterpret_cast<const uint4*>(tile + r * C::OUT_PITCH + c * 16);
           const int left = n < N ? M - m : 0;

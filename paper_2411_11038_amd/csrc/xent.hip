@@ -854,7 +854,7 @@ extern "C" int efqat_linear_xent_bwd(const void* h, int64_t ldh, const void* w, 
       const int64_t chunks = round_up(T, 64) * (round_up(V, 64) / 8);
       EFQAT_TRY(launch(k_xent_logits_grad, dim3((unsigned)std::min<int64_t>(ceil_div(chunks, 256), 2048)), dim3(256), 0, st, z));
     } else {
-      EFQAT_TRY(launch_xent_tile<XG_GRAD>(p.bt, g, p.grid, st));
+      EFQAT_TRY(p.parts == 3 ? launch_xent_tile<XG_GRAD3>(p.bt, g, p.grid, st) : launch_xent_tile<XG_GRAD>(p.bt, g, p.grid, st));
     }
     XentGemmArgs gh = g, gw = g;
     gh.split_blocks = p.blocks_dh; gh.acc = k.acc_dh; gh.out = dh; gh.ldo = lddh; gh.rows = k.rows;

@@ -557,11 +557,12 @@ __device__ __forceinline__ void xent_gemm_block(const XentGemmArgs& g, const Xen
       const int rel = n < N ? tok_class[j] - (int)z.class0 - m0 - wm * C::WM : -1;   // row of the wavefront's tile that is the class
       if (__any(rel >= 0 && rel < C::WM)) {
         const int mine = rel - 4 * fh;
+        float at_class = 0.0f;
 #pragma unroll
         for (int i = 0; i < C::TM; ++i)
 #pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (mine == 32 * i + 8 * (r >> 2) + (r & 3)) g.target_logit[n] = acc[i][j][r];
+          for (int r = 0; r < 16; ++r) at_class = mine == 32 * i + 8 * (r >> 2) + (r & 3) ? acc[i][j][r] : at_class;
+        if (mine >= 0 && mine < C::WM && !(mine & 4)) g.target_logit[n] = at_class;
       }
     }
     __syncthreads();

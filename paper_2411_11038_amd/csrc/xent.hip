@@ -244,7 +244,8 @@ __global__ __launch_bounds__(256) void k_xent_stage(const XentStageArgs tokens, 
 
 // ---- forward: the tiles of classes joined, TOK tokens a block, by 1024 / TOK groups of lanes that take the tiles in turn.  Up to 64 tokens
 // are one block, which takes their mean or sum too: 64 tokens of width 64 against 8000 classes 14.4 us forward, with a launch for the mean
-// and four groups of lanes 17.1; 18 of 32 against 68688 (1074 tiles) 36.8 and 46.5.  One block for 256 tokens, in turn, took 28.6, not 19.3.
+// and four groups of lanes 17.1; 18 of 32 against 68688 (1074 tiles) 36.8 and 46.5.  So are up to 256 of at most 32 tiles (256 of width 64 against 1000 classes 17.2 -> 15.0 us); 256
+// tokens 64 at a time took 28.6, not 19.3.
 struct XentJoinArgs {
   const float2* part;
   int tiles;
@@ -257,8 +258,9 @@ struct XentJoinArgs {
 };
 template <int TOK>
 __global__ __launch_bounds__(1024) void k_xent_join(const XentJoinArgs g) {
-  constexpr int GROUPS = 1024 / TOK;
-  __shared__ float2 red[16][TOK];
+  constexpr int GROUPS = 1024 / TOK, ROWS = TOK < 64 ? 16 : GROUPS;
+  __shared__ float2 red[ROWS][TOK];
+  __shared__ double sums[TOK < 64 ? 1 : TOK / 64];
   const int lane = threadIdx.x % TOK, grp = threadIdx.x / TOK, wave = threadIdx.x >> 6;
   const int valid = g.n_valid[0];
   if ((int)blockIdx.x * TOK >= valid && !g.total) return;
@@ -285,13 +287,12 @@ __global__ __launch_bounds__(1024) void k_xent_join(const XentJoinArgs g) {
     const float2 other = make_float2(__shfl_xor(top, o), __shfl_xor(sum, o));
     join(other);
   }
-  if ((threadIdx.x & 63) < TOK) red[wave][lane] = make_float2(top, sum);
+  if ((threadIdx.x & 63) < TOK) red[TOK < 64 ? wave : grp][lane] = make_float2(top, sum);
   __syncthreads();
-  if (wave != 0) return;
   double total = 0.0;
   if (threadIdx.x < TOK && n < valid) {
 #pragma unroll
-    for (int i = 1; i < 16; ++i) join(red[i][lane]);
+    for (int i = 1; i < ROWS; ++i) join(red[i][lane]);
     const float l = top + logf(sum), d = l - g.target_logit[n];
     const int row = g.rows[n];
     g.lse[row] = l;
@@ -301,6 +302,13 @@ __global__ __launch_bounds__(1024) void k_xent_join(const XentJoinArgs g) {
   }
   if (g.total) {
     total = wave_sum(total);
+    if constexpr (TOK > 64) {
+      if (threadIdx.x < TOK && (threadIdx.x & 63) == 0) sums[wave] = total;
+      __syncthreads();
+      total = 0.0;
+#pragma unroll
+      for (int i = 0; i < TOK / 64; ++i) total += sums[i];
+    }
     if (threadIdx.x == 0) g.total[0] = valid == 0 ? 0.0f : (float)(g.mean ? total / valid : total);
   }
 }
@@ -803,10 +811,11 @@ extern "C" int efqat_linear_xent_fwd(const void* h, int64_t ldh, const void* w, 
   XentJoinArgs j = {};
   j.part = k.part; j.tiles = (int)ceil_div(V, p.bt); j.slots = p.slots; j.n_valid = k.n_valid; j.rows = k.rows;
   j.target_logit = k.target_logit; j.lse = lse; j.loss = none ? loss : nullptr;
-  const bool one = !none && T <= 64;
+  const bool one = !none && (T <= 64 || (T <= 256 && j.tiles <= 32));
   if (one) { j.total = loss; j.mean = mean; }
   else if (!none) j.slot_loss = k.slot_loss;
   if (T <= 16) EFQAT_TRY(launch(k_xent_join<16>, dim3(1), dim3(1024), 0, st, j));
+  else if (T > 64 && one) EFQAT_TRY(launch(k_xent_join<256>, dim3(1), dim3(1024), 0, st, j));
   else EFQAT_TRY(launch(k_xent_join<64>, dim3((unsigned)ceil_div(T, 64)), dim3(1024), 0, st, j));
   if (none || one) return EFQAT_OK;
   return launch(k_xent_reduce_loss, dim3(1), dim3(1024), 0, st, k.slot_loss, k.n_valid, mean, loss);

@@ -333,3 +333,10 @@ def test_masked_classes_whose_rows_end_inside_a_stage(D):
     assert torch.allclose(r["lse"], ref["lse"], rtol=1e-6, atol=1e-6) and torch.isfinite(r["loss"]).all()
     g = ef.linear_xent_bwd(hd, wd, td, r["lse"])
     assert (g["dw"][:3] == 0).all() and torch.isfinite(g["dw"]).all()
+
+
+@pytest.mark.parametrize("reduction", [ef.XENT_NONE, ef.XENT_MEAN, ef.XENT_SUM])
+@pytest.mark.parametrize("T,V", [(16, 900), (17, 900), (64, 900), (65, 900), (256, 2048), (256, 2049), (257, 2048)])
+def test_the_join_of_few_tokens(T, V, reduction):
+    """one block that takes 16, 64 or 256 tokens and their mean, or several"""
+    check_all(*make(T, 64, V, "bf16", T + V, ignored=0.3), "bf16", reduction=reduction)

@@ -18,9 +18,11 @@
 // their own.
 //
 // Bound by the matrix cores where the tiles are large: 8028 tokens of width 4096 against 32000 classes (2.1 T operations a product), the
-// logits with their sums 1.62 ms (1.30 POP/s; 8192^3 takes a library product 1.38), the logits and G 1.79 ms (1.18), both products of G
-// 3.28 ms (1.28).  A 256-tile of logits costs 1.6 us a K stage and 8.5 us besides (128 exponentials a lane in the epilogue, the first
-// loads): 12 stages, as in a width of 768, reach 0.79 POP/s.  A round of four stages of a 64-tile takes 0.67 us, which the copies into LDS
+// logits with their sums 1.58 ms (1.33 POP/s; a library product of 8192^3 reaches 1.38), the logits and G 1.67 ms (1.26), both products of
+// G 3.23 ms (1.30).  A 256-tile of logits costs 1.6 us a K stage and 5.5 us besides (128 exponentials a lane in the epilogue, the first
+// loads): 12 stages, as in a width of 768, reach 0.87 POP/s.  The epilogues are written so that no accumulator changes under a branch (copies
+// of all of them) and their addresses are not kept through the products: 217 registers, no spills; with both, G's had 256 and spilled, and
+// 1843 tokens of width 768 against 30522 classes took 313 us backward instead of 291.  A round of four stages of a 64-tile takes 0.67 us, which the copies into LDS
 // (64 KB at 64 bytes a clock: 0.43 us) are most of.  LDS bank conflicts: none that a counter shows.
 //
 // fp32 operands are three bf16 parts each (x = x0 + x1 + x2 with 24 bits), side by side in a row; the product of two is the six

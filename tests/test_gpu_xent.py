@@ -340,3 +340,21 @@ def test_masked_classes_whose_rows_end_inside_a_stage(D):
 def test_the_join_of_few_tokens(T, V, reduction):
     """one block that takes 16, 64 or 256 tokens and their mean, or several"""
     check_all(*make(T, 64, V, "bf16", T + V, ignored=0.3), "bf16", reduction=reduction)
+
+
+@pytest.mark.parametrize("T,D,V,dtype", [(90, 3200, 150, "bf16"), (90, 3200, 150, "f32"), (300, 72, 9000, "bf16"), (700, 640, 7000, "f32"),
+                                         (2050, 64, 130, "bf16"), (40, 520, 30000, "bf16"), (33000, 8, 20, "bf16")])
+def test_what_the_workspace_held(T, D, V, dtype):
+    """NaN in every word of it, in every way that the logits are made: the same bits"""
+    h, w, t, hd, wd, td = make(T, D, V, dtype, T + V, ignored=0.3)
+    lib, code = ef.lib(), 1 if dtype == "bf16" else 0
+
+    def run(fill):
+        ws = [torch.full((n(T, D, V, code),), fill, dtype=torch.uint8, device="cuda")
+              for n in (lib.efqat_linear_xent_fwd_workspace_bytes, lib.efqat_linear_xent_bwd_workspace_bytes)]
+        r = ef.linear_xent_fwd(hd, wd, td, ws=ws[0])
+        r.update(ef.linear_xent_bwd(hd, wd, td, r["lse"], ws=ws[1]))
+        return r
+
+    a, b = run(0), run(255)
+    assert all(torch.equal(a[k], b[k]) for k in a) and torch.isfinite(b["dw"]).all() and torch.isfinite(b["dh"]).all()

@@ -794,7 +794,34 @@ __global__ __launch_bounds__(XentCfg<BT>::THREADS) void k_xent_gemm(const XentGe
 #endif
 }
 
-// both products of G in one grid, the longer contraction first: neither has to wait for the other's last, partly filled round
+// Which tiles of the second product a block takes in a launch of `grid` blocks, whose first `first` have one of the first product's: the
+// blocks that have none take `others` each, the rest is shared among those that do.  Blocks and tiles go by eights: a tile stays on the
+// XCD whose neighbours it has.
+struct XentShare {
+  int head, tail, others, last;   // blocks that have (rounded up), that do not; tiles of each of the latter; tiles from which the former share
+  // a, b: K stages of a tile of the first and the second product
+  __device__ __forceinline__ XentShare(int first, int second, int a, int b, int grid) {
+    head = (first + 7) / 8 * 8;
+    head = head < grid ? head : grid;
+    tail = grid - head;
+    others = 0;
+    if (tail > 0) {
+      const int most = (second + tail - 1) / tail;
+      int best = INT32_MAX;
+      for (int q = most; q >= 0 && q > most - 8; --q) {
+        const int rest = second - q * tail, each = rest > 0 ? (rest + head - 1) / (head > 0 ? head : 1) : 0;
+        const int cost = max(q * b, a + each * b);
+        if (head == 0 && rest > 0) break;
+        if (cost < best) { best = cost; others = q; }
+      }
+    }
+    last = min(second, others * tail);
+  }
+};
+
+// Both products of G in one grid: neither has to wait for the other's last, partly filled round.  They have as many operations, so dH's
+// contraction is cut for half of the blocks, and the others begin with dW: 1843 tokens of width 768 against 30522 classes backward 316 ->
+// 296 us (against slices of dH for all blocks, with every block's share of dW on top), 1024 of 1024 against 4096 66 -> 56.
 template <int BT>
 __global__ __launch_bounds__(XentCfg<BT>::THREADS) void k_xent_gemm_pair(const XentGemmArgs h, const XentGemmArgs w) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -803,14 +830,24 @@ __global__ __launch_bounds__(XentCfg<BT>::THREADS) void k_xent_gemm_pair(const X
   const XentShape zh(h, XG_DH, valid), zw(w, XG_DW, valid);
   if (zh.classes == 0) return;
   const XentTiles th(h, zh, XG_DH, BT), tw(w, zw, XG_DW, BT);
-  const int first = th.total(), total = first + tw.total();
-  int bid = blockIdx.x;
-  for (; bid < first; bid += gridDim.x) {
+  const int first = th.total(), second = tw.total(), grid = gridDim.x, block = blockIdx.x;
+  for (int bid = block; bid < first; bid += grid) {
     xent_gemm_block<BT, XG_DH>(h, zh, th, valid, bid, smem);
     __syncthreads();
   }
-  for (; bid < total; bid += gridDim.x) {
-    xent_gemm_block<BT, XG_DW>(w, zw, tw, valid, bid - first, smem);
+  // tiles begin .. end - 1 of dW in steps
+  int begin = block, end = second, step = grid;
+  if (first <= grid) {
+    const XentShare share(first, second, zh.nks * h.segments / th.slices, zw.nks * w.segments / tw.slices, grid);
+    const bool tail = block >= share.head;
+    begin = tail ? block - share.head : share.last + block;
+    end = tail ? share.last : second;
+    step = tail ? share.tail : share.head;
+  } else {
+    begin = (block + grid - first % grid) % grid;     // where the first product's last round ends
+  }
+  for (int bid = begin; bid < end; bid += step) {
+    xent_gemm_block<BT, XG_DW>(w, zw, tw, valid, bid, smem);
     __syncthreads();
   }
 #endif

@@ -870,6 +870,7 @@ extern "C" int efqat_linear_xent_bwd(const void* h, int64_t ldh, const void* w, 
     gw.split_blocks = p.blocks_dw; gw.acc = k.acc_dw; gw.out = dw; gw.ldo = lddw;
     if (dh && dw && p.bt_dh == p.bt_dw) {
       const int64_t blocks = p.grid_dh + p.grid_dw;
+      gh.split_blocks /= 2;                           // as many operations in each: half of the blocks for dH's slices
       EFQAT_TRY(p.bt_dh == 256   ? launch_xent_pair<256>(gh, gw, blocks, st)
                 : p.bt_dh == 128 ? launch_xent_pair<128>(gh, gw, blocks, st)
                                  : launch_xent_pair<64>(gh, gw, blocks, st));

@@ -358,3 +358,9 @@ def test_what_the_workspace_held(T, D, V, dtype):
 
     a, b = run(0), run(255)
     assert all(torch.equal(a[k], b[k]) for k in a) and torch.isfinite(b["dw"]).all() and torch.isfinite(b["dh"]).all()
+
+
+@pytest.mark.parametrize("T,D,V", [(8200, 2112, 520), (1843, 768, 9000), (260, 264, 40000)])
+def test_both_products_share_the_blocks(T, D, V):
+    """more tiles of dh than blocks; some blocks with slices of dh and the others with dw; few of either"""
+    check_all(*make(T, D, V, "bf16", 13, ignored=0.1), "bf16")

@@ -12,7 +12,7 @@
 //
 // 8 T D V operations of a training step are products on the matrix cores and bound it; with few tokens, reading w does.  bf16, 8192
 // tokens of width 4096 against 32000 classes, 98 % of them with one: 6.6 ms forward and backward, 1.28 POP/s.  12288 of width 768 against
-// 30522, 15 % of them with one: 0.42 ms, 0.83 POP/s.  One token of width 4096: 74 us forward, of which 50 are w at 5.2 TB/s.
+// 30522, 15 % of them with one: 0.40 ms, 0.87 POP/s.  One token of width 4096: 74 us forward, of which 50 are w at 5.2 TB/s.
 //
 // Tokens without a class (ignored, or a class outside [0, V)) take no part: the rows that do are counted and copied together
 // first, on the device, and every grid is cut to their number there.  What an ignored row holds - NaN included - touches nothing.

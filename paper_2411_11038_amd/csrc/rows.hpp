@@ -171,12 +171,12 @@ __device__ __forceinline__ uint2 ckpt_encode(const float (&v)[8], float* scale) 
   };
   return make_uint2(four(0), four(4));
 }
-// code * scale, rounded once: with the sign bit turned a byte is code + 128, and 128 * scale is exact
+// code * scale, rounded once.  The product is formed from the signed code: 128 * scale may be infinite where 127 * scale, the largest
+// kept value, is not.  A byte's sign is extended by the conversion itself.
 __device__ __forceinline__ void ckpt_decode(uint2 codes, float scale, float (&v)[8]) {
-  const float base = -128.0f * scale;
-  const uint32_t w[2] = {codes.x ^ 0x80808080u, codes.y ^ 0x80808080u};
+  const uint32_t w[2] = {codes.x, codes.y};
 #pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] = fmaf((float)((w[j >> 2] >> (8 * (j & 3))) & 0xFFu), scale, base);
+  for (int j = 0; j < 8; ++j) v[j] = (float)(int8_t)(w[j >> 2] >> (8 * (j & 3))) * scale;
 }
 
 // Launches a kernel and says whether that went well by what the launch itself returns: the last error of the thread may be one

@@ -56,11 +56,12 @@ struct RowSum {
 };
 
 // From the sums of d = x - mean and of d^2: what the mean has lost to rounding is put back (the sum of d is not quite zero), and what
-// that adds to the squares taken off.
+// that adds to the squares taken off.  A row with a NaN or an infinity has the mean that its sum says and a NaN for rstd; one whose
+// squares alone leave fp32 has rstd 0 (the product of the second step is not rounded before it is taken off an infinite sum).
 __device__ __forceinline__ float norm_rstd(float2 sums, float inv_cols, float eps, float* mean) {
-  const float more = sums.x * inv_cols;
-  *mean += more;
-  return 1.0f / sqrtf(fmaxf(fmaf(sums.y, inv_cols, -more * more), 0.0f) + eps);
+  const float more = sums.x * inv_cols, var = fmaf(-more, more, sums.y * inv_cols);
+  *mean += fabsf(more) < INFINITY ? more : 0.0f;
+  return 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + eps);
 }
 
 struct NormFwdArgs {

@@ -402,7 +402,8 @@ int efqat_ckpt8_load(const int8_t* codes, const float* scales, int64_t rows, int
 
 /* ------------------------------------------------------------------ activation of a feed-forward block
  *   y = f(x)  or, with up,  y = f(x) * up;   f: GELU x Phi(x), or SiLU x / (1 + exp(-x))
- * computed in fp32 and rounded once.  The backward pass reads the checkpoints of x and up:
+ * computed in fp32 and rounded once: f to 2^-20 of its value (GELU; bf16: 2^-24 x^2 / 2 more), to 2^-24 (6 + 2 |x|)
+ * of it (SiLU of x < 0), results below 2^-126 may be 0.  The backward pass reads the checkpoints of x and up:
  *   dx = dy f'(x) [* up],   dup = dy f(x)
  *   x, up, y, dy, dx, dup  [rows][cols], dtype F32 or BF16 (one for all); up NULL: not gated
  *   x_codes, x_scales, up_codes, up_scales   see efqat_ckpt8_save.  Forward: out, in the pass that reads

@@ -34,6 +34,18 @@ long long integer(PyObject* o, const char* what) {
   return v;
 }
 
+// as a C type: what it does not hold is refused, not cut to its lowest bits
+template <class T>
+T integer_as(PyObject* o, const char* what) {
+  static_assert(std::is_integral_v<T>);
+  const long long v = integer(o, what);
+  if ((v < 0 && std::is_unsigned_v<T>) || (long long)(T)v != v) {
+    PyErr_Format(PyExc_OverflowError, "%s: out of range", what);
+    throw BadArgument();
+  }
+  return (T)v;
+}
+
 void* tensor_address(PyObject* o) {
   if (o == Py_None) return nullptr;
   if (!THPVariable_Check(o)) refuse(PyExc_TypeError, "tensor", o);
@@ -78,7 +90,7 @@ T from_python(PyObject* o) {
   } else if constexpr (std::is_pointer_v<T>) {
     return (T)(ROWS ? rows_address(o) : tensor_address(o));
   } else {
-    return (T)integer(o, "integer");
+    return integer_as<T>(o, "integer");
   }
 }
 
@@ -131,7 +143,7 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) { return call_n<
 template <class... A, size_t... I>
 PyObject* ask(size_t (*fn)(A...), PyObject* const* args, std::index_sequence<I...>) {
   try {
-    std::tuple<A...> a{(A)integer(args[I], "integer")...};
+    std::tuple<A...> a{integer_as<A>(args[I], "integer")...};
     return PyLong_FromSize_t(std::apply(fn, a));
   } catch (const BadArgument&) {
     return nullptr;
@@ -351,7 +363,7 @@ PyObject* ckpt8_load(PyObject* const* a, PyObject* const* out) {
 PyObject* act_fwd(PyObject* const* a, PyObject* const* out) {
   const at::Tensor& t = gpu_tensor(a[0]);
   const Rows x = rows_of(t);
-  const int kind = (int)integer(a[1], "integer");
+  const int kind = integer_as<int>(a[1], "kind");
   const bool gated = given(a[2]), keep = PyObject_IsTrue(a[3]);
   const Rows up = gated ? rows_like(a[2], x, "up") : Rows{};
   Results r(5, t);
@@ -367,7 +379,7 @@ PyObject* act_fwd(PyObject* const* a, PyObject* const* out) {
 PyObject* act_bwd(PyObject* const* a, PyObject* const* out) {
   const at::Tensor& t = gpu_tensor(a[0]);
   const Rows dy = rows_of(t);
-  const int kind = (int)integer(a[1], "integer");
+  const int kind = integer_as<int>(a[1], "kind");
   const int8_t* xc = codes_of(a[2], dy, "x_codes");
   const float* xs = scales_of(a[3], dy, "x_scales");
   const bool gated = given(a[4]);

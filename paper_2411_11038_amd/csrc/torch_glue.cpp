@@ -46,6 +46,13 @@ T integer_as(PyObject* o, const char* what) {
   return (T)v;
 }
 
+// what has no truth (an array of several elements) is an error of the call
+bool truth(PyObject* o) {
+  const int v = PyObject_IsTrue(o);
+  if (v < 0) throw BadArgument();
+  return v != 0;
+}
+
 void* tensor_address(PyObject* o) {
   if (o == Py_None) return nullptr;
   if (!THPVariable_Check(o)) refuse(PyExc_TypeError, "tensor", o);
@@ -350,7 +357,7 @@ PyObject* ckpt8_save(PyObject* const* a, PyObject* const* out) {
 PyObject* ckpt8_load(PyObject* const* a, PyObject* const* out) {
   const at::Tensor& t = gpu_tensor(a[0]);
   const int64_t cols = integer(a[2], "integer");
-  Rows x = {nullptr, t.dim() > 0 ? t.size(0) : 0, cols, cols, PyObject_IsTrue(a[3]) ? at::kBFloat16 : at::kFloat};
+  Rows x = {nullptr, t.dim() > 0 ? t.size(0) : 0, cols, cols, truth(a[3]) ? at::kBFloat16 : at::kFloat};
   const int8_t* codes = codes_of(a[0], x, "codes");
   const float* scales = scales_of(a[1], x, "scales");
   Results r(1, t);
@@ -364,7 +371,7 @@ PyObject* act_fwd(PyObject* const* a, PyObject* const* out) {
   const at::Tensor& t = gpu_tensor(a[0]);
   const Rows x = rows_of(t);
   const int kind = integer_as<int>(a[1], "kind");
-  const bool gated = given(a[2]), keep = PyObject_IsTrue(a[3]);
+  const bool gated = given(a[2]), keep = truth(a[3]);
   const Rows up = gated ? rows_like(a[2], x, "up") : Rows{};
   Results r(5, t);
   const Rows y = r.rows(0, out[0], x, "y");
@@ -399,7 +406,7 @@ PyObject* layer_norm_fwd(PyObject* const* a, PyObject* const* out) {
   const float* b = given(a[2]) ? (const float*)dense(a[2], at::kFloat, x.cols, -1, "bias") : nullptr;
   const double eps = PyFloat_AsDouble(a[3]);
   if (eps == -1.0 && PyErr_Occurred()) throw BadArgument();
-  const bool keep = PyObject_IsTrue(a[4]);
+  const bool keep = truth(a[4]);
   Results r(5, t);
   const Rows y = r.rows(0, out[0], x, "y");
   float* mean = (float*)r.dense_at(1, out[1], at::kFloat, x.rows, -1, "mean");

@@ -425,7 +425,8 @@ int efqat_act_bwd(const void* dy, int64_t lddy, int dtype, int64_t rows, int64_t
  *   dweight = sum over the rows of dy xhat,  dbias = sum over the rows of dy   (never frozen: Sec. 3.4)
  *   x, y, dy, dx    [rows][cols], dtype F32 or BF16
  *   weight, bias    float[cols]; NULL: 1, 0
- *   mean, rstd      float[rows]; forward: out, nullable (evaluation)
+ *   mean, rstd      float[rows]; forward: out, nullable (evaluation).  rstd of a row with a NaN or an infinity is NaN; of one whose
+ *                   squares leave fp32 it is 0
  *   x_codes, x_scales   8-bit checkpoint of x.  Forward: out, nullable.  Backward: read where x is NULL
  *   dweight, dbias  out float[cols], nullable; summed in a fixed order (bit-reproducible) */
 int efqat_layer_norm_fwd(const void* x, int64_t ldx, int dtype, int64_t rows, int64_t cols, const float* weight,
@@ -438,7 +439,8 @@ int efqat_layer_norm_bwd(const void* dy, int64_t lddy, int dtype, const void* x,
                          void* stream);
 
 /* ------------------------------------------------------------------ softmax cross entropy over a vocabulary
- * Of the logits z = h w^T, which are not kept:
+ * Of the logits z = h w^T, which are not kept (where they are few tiles of long rows, the workspace of a call holds slices of them in
+ * fp32 while it runs, 64 MiB at most):
  *   lse[t] = log sum_v exp(z[t][v]),   loss of token t = lse[t] - z[t][targets[t]]
  *   G = (exp(z - lse) - [v = targets[t]]) * (upstream gradient of token t's loss),  dh = G w,  dw = G^T h
  *   h        in  [T][D], w in [V][D], dtype F32 or BF16 (both); BF16 with D a multiple of 64: w 16-byte

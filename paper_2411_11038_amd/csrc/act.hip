@@ -6,8 +6,9 @@
 // is written once: y and the codes leave in the pass that reads x and u.
 //
 // bf16, 8192 x 11008, gated: forward with both inputs kept 135 us (726 MB, 5.4 TB/s; a copy of 1 GiB reaches 5.0, of 256 MiB 5.4),
-// backward 129 us (726 MB, 5.6 TB/s), a checkpoint read back 53 us (273 MB, 5.2 TB/s).  Small calls are a launch: 16 x 11008 forward
-// 2.8 us of kernel in 5.0 us a call.  fp32 2049 x 1001, rows of any alignment, backward 5.8 us (18 MB).
+// backward 124 us (726 MB, 5.8 TB/s), a checkpoint read back 53 us (273 MB, 5.2 TB/s).  Small calls are a launch: 16 x 11008 forward
+// 2.6 us of kernel in 4.8 us a call.  fp32 2049 x 1001, rows of any alignment, backward 5.9 us (18 MB).  GELU of one input in bf16 is bound by
+// its operations beside the bytes: 8192 x 11008 forward 84 us (361 MB, 4.3 TB/s).
 #include "rows.hpp"
 
 namespace efqat {

@@ -9,8 +9,8 @@
 // requested before the present ones are worked on.  The sums of the blocks are added in a second pass, in a fixed order.
 // Rows longer than the registers hold (kNormMaxCols, kNormBwdMaxCols), and shorter than a chunk, are read again for every step.
 //
-// bf16, one call after another on the same buffers (which the last-level cache holds).  8192 x 4096: forward 22.5 us (134 MB, 6.0 TB/s),
-// input kept 28.0, backward 37.7 (201 MB, 5.3 TB/s), from the checkpoint 33.6.  12288 x 768: 9.7, 12.3, 16.6 (57 MB, 3.4 TB/s) and 16.4 us:
+// bf16, one call after another on the same buffers (which the last-level cache holds).  8192 x 4096: forward 22.6 us (134 MB, 5.9 TB/s),
+// input kept 28.4, backward 38.1 (201 MB, 5.3 TB/s), from the checkpoint 34.2.  12288 x 768: 9.6, 12.4, 16.8 (57 MB, 3.4 TB/s) and 17.0 us:
 // narrow rows are bound by the instructions a value takes (two sums, the code) and by the way through a row, load to store, that a block
 // walks a few times; 4 us of the backward are the second pass, mostly its launch.  1 x 4096: 2.5 us of kernel in 6.4 us a call.
 #include "rows.hpp"
@@ -384,7 +384,8 @@ __global__ __launch_bounds__(THREADS, 4) void k_norm_bwd(const NormBwdArgs g) {
   }
 }
 
-// Long rows, first pass: the two means of a row.
+// Long rows, first pass: the two means of a row.  Two readings of the rows and three launches: 2048 x 12288 bf16 41.0 us (floor of the bytes,
+// read once, 29), 16 / 64 / 128 rows 13.8 / 14.3 / 16.0 us, where the second pass has 12 to 96 blocks and each walks its eight rows.
 template <typename T, bool CKPT>
 __global__ __launch_bounds__(1024) void k_norm_bwd_long_rows(const NormBwdArgs g) {
   __shared__ float2 sums[2][16];

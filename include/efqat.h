@@ -12,7 +12,9 @@
  *   efqat_conv_bwd         the same two contractions with Eq. 8's shapes
  *
  * and what a language model needs between its quantized layers: layer norm, the activation of
- * a feed-forward block with its inputs kept in 8 bits, and the loss over the vocabulary.
+ * a feed-forward block with its inputs kept in 8 bits, the loss over the vocabulary, and of an
+ * attention block norms of queries and keys with the position rotation, attention with a window
+ * and first tokens that stay visible, and dropout.
  *
  * Conventions common to every call
  *   - Every tensor pointer is a DEVICE pointer owned by the caller; the library
@@ -471,6 +473,88 @@ int efqat_linear_xent_bwd(const void* h, int64_t ldh, const void* w, int64_t ldw
                           const int64_t* targets, int64_t ignore_index, int reduction, const float* lse,
                           const float* dloss, void* dh, int64_t lddh, void* dw, int64_t lddw, void* ws, size_t ws_bytes,
                           void* stream);
+
+/* ------------------------------------------------------------------ norms of queries and keys, position rotation
+ * Both in one pass over the heads of the queries and the keys, in fp32, rounded once:
+ *   n = x w / sqrt(mean of x^2 over the head + eps)  (norm 0: n = x),   then for the `freqs` pairs (a, b) of a head
+ *   y_a = n_a cos t - n_b sin t,  y_b = n_b cos t + n_a sin t,   t = positions[axis[j]][token] * inv_freq[j] for pair j
+ * the features behind the pairs are n.  Angles are formed in 64 bits, cosine and sine good to 2^-23 however far the position.  The
+ * backward reads the forward's inputs:
+ *   dn = the rotation back of dy,  g = dn w,  dx = (g - xhat mean(g xhat)) / sqrt(mean x^2 + eps),  xhat = n / w
+ *   dq_weight, dk_weight = sums over tokens and heads of dn xhat (fixed order, bit-reproducible)
+ *   q [T][heads * dim], k [T][kv_heads * dim], and yq, yk, dyq, dyk, dq, dk alike, dtype F32 or BF16; rows may lie apart, any element
+ *              alignment.  kv_heads 0: no keys.  yq may be q, dq may be dyq (the same rows), and so for the keys.  dim <= 256
+ *   norm       0 or 1.  q_weight, k_weight  float[dim], NULL: 1.  A head whose squares leave fp32 is 0 behind its norm
+ *   positions  int32 [axes][T], any value; axes 1 .. 16 positions of a token (text: 1; images and video: time, height, width)
+ *   axis       int32 [freqs] the axis whose position turns a pair, cut to 0 .. axes - 1; not read (may be NULL) with one axis
+ *   inv_freq   float [freqs]; 2 freqs <= dim, freqs 0: no rotation (positions, inv_freq not read)
+ *   neighbours 0: pair j is features j and j + freqs; 1: 2 j and 2 j + 1
+ *   dq_weight, dk_weight  out, nullable float[dim] (NULL without norm); with both NULL ws is not used
+ *   q, k of the backward are not read without norm (may be NULL) */
+int efqat_head_norm_rope_fwd(const void* q, int64_t ldq, const void* k, int64_t ldk, int dtype, int64_t T, int64_t heads,
+                             int64_t kv_heads, int64_t dim, int norm, const float* q_weight, const float* k_weight, float eps,
+                             const int32_t* positions, int64_t axes, const int32_t* axis, const float* inv_freq, int64_t freqs,
+                             int neighbours, void* yq, int64_t ldyq, void* yk, int64_t ldyk, void* stream);
+size_t efqat_head_norm_rope_bwd_workspace_bytes(int64_t T, int64_t heads, int64_t kv_heads, int64_t dim);
+int efqat_head_norm_rope_bwd(const void* dyq, int64_t lddyq, const void* dyk, int64_t lddyk, const void* q, int64_t ldq, const void* k,
+                             int64_t ldk, int dtype, int64_t T, int64_t heads, int64_t kv_heads, int64_t dim, int norm,
+                             const float* q_weight, const float* k_weight, float eps, const int32_t* positions, int64_t axes,
+                             const int32_t* axis, const float* inv_freq, int64_t freqs, int neighbours, void* dq, int64_t lddq,
+                             void* dk, int64_t lddk, float* dq_weight, float* dk_weight, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------ attention
+ * Of n_seq sequences packed into rows, heads grouped (heads / kv_heads query heads share a key head: head h reads key head
+ * h / (heads / kv_heads)):
+ *   s_ij = scale q_i . k_j,  o_i = sum_j softmax_j(s_ij) v_j,  lse_i = log sum_j exp(s_ij),  over the keys j that token i sees
+ * The queries of a sequence are its last tokens: query i of lq is at position p = i + lk - lq of lk keys, and sees key j if
+ *   (causal 0 or j <= p)  and  (window 0 or |p - j| < window or j < sinks)
+ * A token that sees nothing (or whose scores are all -infinity) has o = 0 and lse = -infinity and takes no part in the backward:
+ *   P = exp(s - lse), dP_ij = do_i . v_j, dS = P (dP - do_i . o_i);  dv = P^T do, dq = scale dS k, dk = scale dS^T q, over shared heads too
+ *   q, o, dout, dq  [Tq][heads * dim], k, v, dk, dv  [Tk][kv_heads * dim], dtype F32 or BF16; rows may lie apart; 16-byte aligned, row
+ *                strides in whole 16 bytes.  dim a multiple of 8, at most 128
+ *   q_start, k_start  int32 [n_seq + 1]: rows start[s] .. start[s + 1] - 1 are sequence s (ascending; cut to the rows that exist; empty
+ *                ones are allowed).  Both NULL: n_seq sequences of Tq / n_seq and Tk / n_seq rows.  Rows of no sequence are neither read
+ *                nor written
+ *   window       0: no window; sinks: first keys that stay visible beside a window
+ *   lse          float [heads][Tq]; forward: out, nullable.  Backward: in, with o, as the forward left them
+ * Scores, their maxima and sums, and all accumulators are fp32.  With BF16 the probabilities and dS are rounded to bf16 for the
+ * matrix cores (their sum is taken before); with F32 the products are fp32 too.  Sums have a fixed order (bit-reproducible).  A key or
+ * value in a sequence that is not finite may make undefined what tokens of that sequence and head hold that do not see it; other sequences
+ * and heads do not notice.  scale is positive; at most 2^28 rows, 65535 heads, row strides 2^24. */
+int efqat_attention_fwd(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, int dtype, int64_t Tq,
+                        int64_t Tk, int64_t n_seq, const int32_t* q_start, const int32_t* k_start, int64_t heads, int64_t kv_heads,
+                        int64_t dim, float scale, int causal, int64_t window, int64_t sinks, void* o, int64_t ldo, float* lse,
+                        void* stream);
+size_t efqat_attention_bwd_workspace_bytes(int64_t Tq, int64_t heads);
+int efqat_attention_bwd(const void* dout, int64_t lddo, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v,
+                        int64_t ldv, const void* o, int64_t ldo, const float* lse, int dtype, int64_t Tq, int64_t Tk, int64_t n_seq,
+                        const int32_t* q_start, const int32_t* k_start, int64_t heads, int64_t kv_heads, int64_t dim, float scale,
+                        int causal, int64_t window, int64_t sinks, void* dq, int64_t lddq, void* dk, int64_t lddk, void* dv,
+                        int64_t lddv, void* ws, size_t ws_bytes, void* stream);
+/* The same for one new token a sequence over its cache: query s at position lengths[s] - 1, causal.
+ *   q, o         [n_seq][heads * dim]
+ *   k_cache, v_cache  [n_seq][capacity][kv_heads * dim]: ldk, ldv elements from key to key, seq_k, seq_v from sequence to sequence
+ *   lengths      int32 [n_seq] keys of a sequence, the new one among them (cut to 0 .. capacity; 0: o = 0).  What lies behind them, or
+ *                outside the window and the sinks by 32 keys and more, is not read, and nothing of it reaches o
+ *   at most 65535 sequences */
+size_t efqat_attention_decode_workspace_bytes(int64_t n_seq, int64_t capacity, int64_t heads, int64_t kv_heads, int64_t dim,
+                                              int64_t window, int64_t sinks);
+int efqat_attention_decode(const void* q, int64_t ldq, const void* k_cache, int64_t ldk, int64_t seq_k, const void* v_cache,
+                           int64_t ldv, int64_t seq_v, int dtype, int64_t n_seq, int64_t capacity, const int32_t* lengths,
+                           int64_t heads, int64_t kv_heads, int64_t dim, float scale, int64_t window, int64_t sinks, void* o,
+                           int64_t ldo, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------ dropout
+ *   y = [residual +] (kept ? x 65536 / (65536 - t) : 0),   t = rne(65536 p), an element is kept if its 16-bit number is >= t
+ * in fp32, rounded once.  The numbers come from Philox4x32-10 with key = seed: columns 8 c .. 8 c + 7 of row r take the four words of
+ * the counter (r ceil(cols / 8) + c, offset), 64 bits each, the lower half of a word first.  The mask is never stored: the gradient of x
+ * is the same call on dy without residual (that of residual is dy).
+ *   x, residual, y  [rows][cols], dtype F32 or BF16; rows may lie apart, any element alignment.  residual NULL: not added.  y may be x or
+ *            residual (the same rows)
+ *   p        0 .. 1; 1 drops everything
+ *   state    int64[2] {seed, offset} on the device, so that a captured graph draws anew when they are changed */
+int efqat_dropout(const void* x, int64_t ldx, const void* residual, int64_t ldr, int dtype, int64_t rows, int64_t cols, double p,
+                  const int64_t* state, void* y, int64_t ldy, void* stream);
 
 /* ------------------------------------------------------------------ kernel timing (benchmarks)
  * To report each kernel class against its roofline a benchmark can have the library bracket its

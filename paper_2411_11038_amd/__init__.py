@@ -14,4 +14,5 @@ from .binding import (  # noqa: F401
     PROF_QUANT_ACT, PROF_QUANT_W, PROF_IMPORTANCE, PROF_TOPK, PROF_BIAS, PROF_CLASSES,
     ckpt8_save, ckpt8_load, act_fwd, act_bwd, layer_norm_fwd, layer_norm_bwd, linear_xent_fwd, linear_xent_bwd, CKPT8_GROUP, ACT_GELU,
     ACT_SILU, XENT_NONE, XENT_MEAN, XENT_SUM,
+    head_norm_rope_fwd, head_norm_rope_bwd, attention_fwd, attention_bwd, attention_decode, dropout_fwd, dropout_bwd,
 )

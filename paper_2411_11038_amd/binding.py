@@ -34,6 +34,9 @@ EXPORTS = [
     "efqat_layer_norm_fwd", "efqat_layer_norm_bwd_workspace_bytes", "efqat_layer_norm_bwd",
     "efqat_linear_xent_fwd_workspace_bytes", "efqat_linear_xent_fwd",
     "efqat_linear_xent_bwd_workspace_bytes", "efqat_linear_xent_bwd",
+    "efqat_head_norm_rope_fwd", "efqat_head_norm_rope_bwd_workspace_bytes", "efqat_head_norm_rope_bwd",
+    "efqat_attention_fwd", "efqat_attention_bwd_workspace_bytes", "efqat_attention_bwd",
+    "efqat_attention_decode_workspace_bytes", "efqat_attention_decode", "efqat_dropout",
 ]
 
 
@@ -160,6 +163,26 @@ def lib():
     L.efqat_linear_xent_bwd_workspace_bytes.argtypes = [i64, i64, i64, ci]
     L.efqat_linear_xent_bwd.restype = ci
     L.efqat_linear_xent_bwd.argtypes = [vp, i64, vp, i64, ci, i64, i64, i64, vp, i64, ci, vp, vp, vp, i64, vp, i64, vp, sz, vp]
+    L.efqat_head_norm_rope_fwd.restype = ci
+    rope = [ci, i64, i64, i64, i64, ci, vp, vp, C.c_float, vp, i64, vp, vp, i64, ci]     # dtype, sizes, norm, positions
+    L.efqat_head_norm_rope_fwd.argtypes = [vp, i64] * 2 + rope + [vp, i64] * 2 + [vp]
+    L.efqat_head_norm_rope_bwd_workspace_bytes.restype = sz
+    L.efqat_head_norm_rope_bwd_workspace_bytes.argtypes = [i64] * 4
+    L.efqat_head_norm_rope_bwd.restype = ci
+    L.efqat_head_norm_rope_bwd.argtypes = [vp, i64] * 4 + rope + [vp, i64] * 2 + [vp, vp, vp, sz, vp]
+    attn = [ci, i64, i64, i64, vp, vp, i64, i64, i64, C.c_float, ci, i64, i64]           # dtype, sizes, offsets, heads, scale, mask
+    L.efqat_attention_fwd.restype = ci
+    L.efqat_attention_fwd.argtypes = [vp, i64] * 3 + attn + [vp, i64, vp, vp]
+    L.efqat_attention_bwd_workspace_bytes.restype = sz
+    L.efqat_attention_bwd_workspace_bytes.argtypes = [i64, i64]
+    L.efqat_attention_bwd.restype = ci
+    L.efqat_attention_bwd.argtypes = [vp, i64] * 5 + [vp] + attn + [vp, i64] * 3 + [vp, sz, vp]
+    L.efqat_attention_decode_workspace_bytes.restype = sz
+    L.efqat_attention_decode_workspace_bytes.argtypes = [i64] * 7
+    L.efqat_attention_decode.restype = ci
+    L.efqat_attention_decode.argtypes = ([vp, i64] + [vp, i64, i64] * 2 + [ci, i64, i64, vp, i64, i64, i64, C.c_float, i64, i64, vp, i64, vp, sz, vp])
+    L.efqat_dropout.restype = ci
+    L.efqat_dropout.argtypes = [vp, i64, vp, i64, ci, i64, i64, C.c_double, vp, vp, i64, vp]
     _LIB = L
     return L
 
@@ -676,3 +699,67 @@ def linear_xent_bwd(h, w, targets, lse, dloss=None, ignore_index=-100, reduction
     _check(native.linear_xent_bwd(h, _ld(h), w, _ld(w), dt, T, D, V, targets, ignore_index, reduction, lse, dloss, dh, lddh, dw, lddw,
                                   ws, ws.numel(), _STREAM), "efqat_linear_xent_bwd")
     return dict(dh=dh, dw=dw)
+
+
+# ------------------------------------------------------------------ attention block
+# As with the layer norm, the marshalling module reads sizes, strides and types, checks the arguments and makes what `out` does not have.
+# All tensors of a call live on the current device.
+def head_norm_rope_fwd(q, heads, k=None, kv_heads=0, q_weight=None, k_weight=None, norm=True, eps=1e-6, positions=None, inv_freq=None,
+                       axis=None, neighbours=False, out=None):
+    """Norm (root mean square; norm=False: none) of every head of q [T, heads * dim] and k [T, kv_heads * dim] and the rotation by their
+    positions, in one pass; rows may lie apart.  q_weight, k_weight fp32 [dim] or None; positions int32 [T] or [axes, T] with
+    inv_freq fp32 [pairs] (None: no rotation) and, for several axes, axis int32 [pairs]; neighbours: pairs are features 2 j and 2 j + 1,
+    else j and j + pairs.  Returns dict(q, k); `out` may carry them, q and k themselves too."""
+    more = (out.get("q"), out.get("k")) if out else ()
+    yq, yk = _results((_NATIVE or _native()).head_norm_rope_fwd(q, heads, k, kv_heads, q_weight, k_weight, norm, eps, positions, inv_freq, axis,
+                                                                neighbours, *more), "efqat_head_norm_rope_fwd")
+    return {"q": yq, "k": yk}
+
+
+def head_norm_rope_bwd(dq, q, heads, dk=None, k=None, kv_heads=0, q_weight=None, k_weight=None, norm=True, eps=1e-6, positions=None,
+                       inv_freq=None, axis=None, neighbours=False, ws=None, out=None):
+    """Backward of head_norm_rope_fwd from its inputs q, k (not read without norm) and the gradients dq, dk of what it returned.  Returns
+    dict(dq, dk, dq_weight, dk_weight) (the last two None without norm); `out` may carry them, dq and dk themselves too."""
+    more = (out.get("dq"), out.get("dk"), out.get("dq_weight"), out.get("dk_weight")) if out else ()
+    xq, xk, wq, wk = _results((_NATIVE or _native()).head_norm_rope_bwd(dq, q, heads, dk, k, kv_heads, q_weight, k_weight, norm, eps, positions,
+                                                                        inv_freq, axis, neighbours, ws, *more), "efqat_head_norm_rope_bwd")
+    return {"dq": xq, "dk": xk, "dq_weight": wq, "dk_weight": wk}
+
+
+def attention_fwd(q, k, v, heads, kv_heads=None, q_start=None, k_start=None, sequences=1, causal=True, window=0, sinks=0, scale=None, out=None):
+    """Attention of q [Tq, heads * dim] over k, v [Tk, kv_heads * dim] (rows may lie apart) within packed sequences: q_start, k_start
+    int32 [sequences + 1] (k_start None: q_start), or `sequences` of equal lengths.  The queries of a sequence are its last tokens; a token
+    at p sees key j if j <= p (causal) and, with a window, |p - j| < window or j < sinks.  scale None: dim ** -0.5.  Returns
+    dict(o, lse [heads, Tq]); `out` may carry them."""
+    more = (out.get("o"), out.get("lse")) if out else ()
+    o, lse = _results((_NATIVE or _native()).attention_fwd(q, k, v, heads, kv_heads, q_start, k_start, sequences, causal, window, sinks, scale, *more),
+                      "efqat_attention_fwd")
+    return {"o": o, "lse": lse}
+
+
+def attention_bwd(do, q, k, v, o, lse, heads, kv_heads=None, q_start=None, k_start=None, sequences=1, causal=True, window=0, sinks=0, scale=None,
+                  ws=None, out=None):
+    """Backward of attention_fwd from its inputs and results.  Returns dict(dq, dk, dv); `out` may carry them (rows may lie apart)."""
+    more = (out.get("dq"), out.get("dk"), out.get("dv")) if out else ()
+    dq, dk, dv = _results((_NATIVE or _native()).attention_bwd(do, q, k, v, o, lse, heads, kv_heads, q_start, k_start, sequences, causal, window,
+                                                               sinks, scale, ws, *more), "efqat_attention_bwd")
+    return {"dq": dq, "dk": dk, "dv": dv}
+
+
+def attention_decode(q, k_cache, v_cache, lengths, heads, kv_heads=None, window=0, sinks=0, scale=None, ws=None, out=None):
+    """Attention of one new token a sequence, q [sequences, heads * dim], over its cache: k_cache, v_cache
+    [sequences, capacity, kv_heads * dim] (keys and sequences may lie apart), of which sequence s has lengths[s] keys (int32, the new one
+    among them).  Returns o [sequences, heads * dim]."""
+    return _results((_NATIVE or _native()).attention_decode(q, k_cache, v_cache, lengths, heads, kv_heads, window, sinks, scale, ws, out),
+                    "efqat_attention_decode")[0]
+
+
+def dropout_fwd(x, p, state, residual=None, out=None):
+    """Drops elements of x [rows, cols] with probability p (in steps of 2 ** -16), scales the others by its inverse and adds the residual.
+    state: int64 [2] on the device, seed and offset, of which the mask is a function.  `out`: x or residual too."""
+    return _results((_NATIVE or _native()).dropout(x, p, state, residual, out), "efqat_dropout")[0]
+
+
+def dropout_bwd(dy, p, state, out=None):
+    """Gradient of dropout_fwd's x from that of its result, with the mask drawn again; the residual's is dy itself."""
+    return _results((_NATIVE or _native()).dropout(dy, p, state, None, out), "efqat_dropout")[0]

@@ -10,7 +10,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB_DIR = os.path.join(HERE, "lib")
 LIB_PATH = os.path.join(LIB_DIR, "libefqat.so")
 SOURCES = ["api.hip", "fakequant.hip", "select.hip", "gemm.hip", "gemm_tn.hip", "gemm_kk.hip", "pair.hip", "bwd.hip", "fwd.hip", "bias.hip",
-           "act.hip", "norm.hip", "xent.hip"]
+           "act.hip", "norm.hip", "xent.hip", "rope.hip", "attn.hip", "attn_bwd.hip", "dropout.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

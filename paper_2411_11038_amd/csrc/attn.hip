@@ -1,0 +1,389 @@
+// Attention with a sliding window and first tokens that stay visible, forward, and its form for one new token a sequence.
+//
+//   s_ij = scale q_i . k_j over the keys that token i sees,  m_i = max_j s_ij,  l_i = sum_j exp(s_ij - m_i),
+//   o_i = sum_j exp(s_ij - m_i) v_j / l_i,  lse_i = m_i + log l_i
+//
+// One pass over the keys: with a new largest score m', l and o are multiplied by exp(m - m').  Scores are formed transposed, keys as
+// rows and queries as columns of a result: a lane then holds 16 scores of one query, its maximum and sum need one exchange between the
+// halves of a wavefront, and the probabilities are the second product's operand where they are.
+#include "attn_tile.hpp"
+
+namespace efqat {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
+
+template <typename T>
+struct FwdTile {
+  static constexpr int BM = 128, BN = sizeof(T) == 2 ? 64 : 32;       // queries of a block, keys of a stage
+};
+
+// scores of a wavefront's 32 queries (columns) against BN keys; what is not seen is -inf
+template <int NT>
+__device__ __forceinline__ void mask_scores(floatx16_t (&s)[NT], const AttnMask& m, int p, int j0, int end) {
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int j = j0 + 32 * n + result_row(i);
+      s[n][i] = j < end && m.sees(p, j) ? s[n][i] : -INFINITY;
+    }
+}
+
+template <typename T, int DP>
+__global__ __launch_bounds__(256, sizeof(T) == 2 || DP == 64 ? 2 : 1) void k_attn_fwd(AttnArgs a, T* __restrict__ o, int64_t ldo, float* __restrict__ lse, int tiles) {
+  using R = RowTile<T, DP>;
+  constexpr int BM = FwdTile<T>::BM, BN = FwdTile<T>::BN, NT = BN / 32, STAGE = 2 * BN * R::ROW;
+  __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+
+  // blocks that share keys are neighbours, late tiles (the long ones under a causal mask) come first
+  const int id = xcd_contiguous_index(blockIdx.x, gridDim.x);
+  const int per_head = tiles * a.group, kvh = id / per_head, at = id - kvh * per_head;
+  const int head = kvh * a.group + at % a.group;
+  int seq, tile;
+  if (!find_tile(a.qs, BM, tiles - 1 - at / a.group, &seq, &tile)) return;
+  const int2 qp = a.qs.place(seq), kp = a.ks.place(seq);
+  const int shift = kp.y - qp.y, r0 = tile * BM + wave * 32, qrow = r0 + (lane & 31);
+  const int p = qrow + shift, rows = min(BM, qp.y - tile * BM);
+  const KeyTiles kt(a.mask, kp.y, tile * BM + shift, tile * BM + rows - 1 + shift, BN);
+
+  const char* kbase = (const char*)((const T*)a.k + (int64_t)kp.x * a.ldk + kvh * a.dim);
+  const char* vbase = (const char*)((const T*)a.v + (int64_t)kp.x * a.ldv + kvh * a.dim);
+  const int64_t ldk = a.ldk * (int)sizeof(T), ldv = a.ldv * (int)sizeof(T);
+  const int pieces = a.dim * (int)sizeof(T) / 16;
+  auto issue = [&](int t, char* buf) {
+    const int j0 = kt.tile(t) * BN, valid = kp.y - j0;
+#pragma unroll
+    for (int s = 0; s < BN / R::RPI / 4; ++s) R::copy(kbase + j0 * ldk, ldk, valid, pieces, buf, wave + 4 * s);
+#pragma unroll
+    for (int s = 0; s < BN / R::RPI / 4; ++s) R::copy(vbase + j0 * ldv, ldv, valid, pieces, buf + BN * R::ROW, wave + 4 * s);
+  };
+
+  Frag<T> q[R::KS];
+  {
+    const T* row = (const T*)a.q + (int64_t)(qp.x + qrow) * a.ldq + head * a.dim;
+#pragma unroll
+    for (int ks = 0; ks < R::KS; ++ks) {
+      const int d = 16 * ks + 8 * (lane >> 5);
+      q[ks] = load_frag(row + d, qrow < qp.y && d < a.dim);
+    }
+  }
+  floatx16_t acc[R::ND];
+#pragma unroll
+  for (int i = 0; i < R::ND; ++i) acc[i] = zero16();
+  float m = -INFINITY, l = 0.0f;
+  const float c = a.scale * kLog2e;
+
+  if (kt.count > 0) issue(0, smem);
+  tile_sync();
+  for (int t = 0; t < kt.count; ++t) {
+    char* buf = smem + (t & 1) * STAGE;
+    if (t + 1 < kt.count) issue(t + 1, smem + ((t + 1) & 1) * STAGE);
+    const int j0 = kt.tile(t) * BN;
+    const int p0 = r0 + shift, p1 = p0 + 31;
+    if (a.mask.sees_some(p0, p1, j0, j0 + BN - 1)) {
+      floatx16_t s[NT];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        s[n] = zero16();
+#pragma unroll
+        for (int ks = 0; ks < R::KS; ++ks) mma(R::row_frag(buf, 32 * n, ks), q[ks], s[n]);
+      }
+      if (j0 + BN > kp.y || !a.mask.sees_all(p0, p1, j0, j0 + BN - 1)) mask_scores(s, a.mask, p, j0, kp.y);
+      float top = m;
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
+      top = half_max(top);
+      const float base = top == -INFINITY ? 0.0f : top * c;       // nothing seen so far: exp2(-inf) is 0 for all of it
+      const float shrink = __builtin_amdgcn_exp2f(fmaf(m, c, -base));
+      m = top;
+      l *= shrink;
+#pragma unroll
+      for (int i = 0; i < R::ND; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[i][r] *= shrink;
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          s[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], c, -base));
+          l += s[n][i];
+        }
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const Frag<T> pf = frag_of<T>(s[n], h);
+#pragma unroll
+          for (int i = 0; i < R::ND; ++i) mma(R::col_frag(buf + BN * R::ROW, 32 * n + 16 * h, i), pf, acc[i]);
+        }
+    }
+    tile_sync();
+  }
+  l = half_sum(l);
+  if (qrow < qp.y) {
+    const int64_t row = (int64_t)qp.x + qrow;
+    const float f = l == 0.0f ? 0.0f : 1.0f / l;                   // a token that sees nothing: zeros
+    T* to = o + row * ldo + head * a.dim;
+#pragma unroll
+    for (int i = 0; i < R::ND; ++i) store_col(to, acc[i], i, a.dim, f);
+    if (lse && lane < 32) lse[(int64_t)head * a.qs.rows + row] = l == 0.0f ? -INFINITY : fmaf(m, a.scale, kLn2 * __builtin_amdgcn_logf(l));
+  }
+}
+
+// ---- one new token a sequence
+// A block takes one sequence, one key head with up to 32 of its query heads (the columns of a result) and a share of the keys;
+// its wavefronts take 32 keys at a time by themselves, each with its own part of LDS, and are joined at the end.  Shares of more
+// than one block are joined by k_attn_join.
+struct DecodeArgs {
+  const void *q, *k, *v;
+  int64_t ldq, ldk, ldv, seq_k, seq_v;
+  const int32_t* lengths;
+  int capacity, heads, group, dim, window, sinks, splits;
+  float scale;
+};
+
+template <typename T, int DP>
+struct DecodeTile {
+  using R = RowTile<T, DP>;
+  static constexpr int BN = 32, STAGE = 2 * BN * R::ROW, STAGES = sizeof(T) == 2 || DP <= 64 ? 2 : 1;
+  static constexpr int LDS = 4 * STAGE * STAGES;
+};
+
+template <typename T, int DP>
+__global__ __launch_bounds__(256) void k_attn_decode(DecodeArgs a, T* __restrict__ o, int64_t ldo, float* __restrict__ part) {
+  using C = DecodeTile<T, DP>;
+  using R = RowTile<T, DP>;
+  constexpr int BN = C::BN, COPIES = 2 * BN / R::RPI;                    // of a stage, in flight behind the one that is waited for
+  __shared__ __attribute__((aligned(1024))) char smem[C::LDS];
+  __shared__ float s_m[4][32], s_l[4][32];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int split = blockIdx.x, seq = blockIdx.z, row_tiles = (a.group + 31) / 32;
+  const int kvh = blockIdx.y / row_tiles, g0 = (blockIdx.y - kvh * row_tiles) * 32, g = g0 + (lane & 31);
+  int keys = a.lengths[seq];
+  keys = keys < 0 ? 0 : keys > a.capacity ? a.capacity : keys;
+  const AttnMask mask = {1, a.window, a.sinks};
+  const int p = keys - 1;
+  const KeyTiles kt(mask, keys, p, p, BN);
+  const int first = (int)((int64_t)kt.count * split / a.splits), last = (int)((int64_t)kt.count * (split + 1) / a.splits);
+
+  const char* kbase = (const char*)((const T*)a.k + seq * a.seq_k + kvh * a.dim);
+  const char* vbase = (const char*)((const T*)a.v + seq * a.seq_v + kvh * a.dim);
+  const int64_t ldk = a.ldk * (int)sizeof(T), ldv = a.ldv * (int)sizeof(T);
+  const int pieces = a.dim * (int)sizeof(T) / 16;
+  char* own = smem + wave * C::STAGE * C::STAGES;
+  auto issue = [&](int t, char* buf) {
+    const int j0 = kt.tile(t) * BN, valid = keys - j0;
+#pragma unroll
+    for (int s = 0; s < BN / R::RPI; ++s) R::copy(kbase + j0 * ldk, ldk, valid, pieces, buf, s);
+#pragma unroll
+    for (int s = 0; s < BN / R::RPI; ++s) R::copy(vbase + j0 * ldv, ldv, valid, pieces, buf + BN * R::ROW, s);
+  };
+  Frag<T> q[R::KS];
+  {
+    const T* row = (const T*)a.q + seq * a.ldq + (int64_t)(kvh * a.group + g) * a.dim;
+#pragma unroll
+    for (int ks = 0; ks < R::KS; ++ks) {
+      const int d = 16 * ks + 8 * (lane >> 5);
+      q[ks] = load_frag(row + d, g < a.group && d < a.dim);
+    }
+  }
+  floatx16_t acc[R::ND];
+#pragma unroll
+  for (int i = 0; i < R::ND; ++i) acc[i] = zero16();
+  float m = -INFINITY, l = 0.0f;
+  const float c = a.scale * kLog2e;
+  int n = 0;
+  if (first + wave < last) issue(first + wave, own);
+  for (int t = first + wave; t < last; t += 4, ++n) {
+    char* buf = own + (C::STAGES == 2 ? (n & 1) * C::STAGE : 0);
+    const bool more = C::STAGES == 2 && t + 4 < last;
+    if (more) issue(t + 4, own + ((n + 1) & 1) * C::STAGE);
+#if defined(__HIP_DEVICE_COMPILE__)
+    __builtin_amdgcn_sched_barrier(0);
+    if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+#endif
+    const int j0 = kt.tile(t) * BN;
+    floatx16_t s[1] = {zero16()};
+#pragma unroll
+    for (int ks = 0; ks < R::KS; ++ks) mma(R::row_frag(buf, 0, ks), q[ks], s[0]);
+    if (!mask.sees_all(p, p, j0, j0 + BN - 1)) mask_scores(s, mask, p, j0, keys);
+    float top = m;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = fmaxf(top, s[0][i]);
+    top = half_max(top);
+    const float base = top == -INFINITY ? 0.0f : top * c;
+    const float shrink = __builtin_amdgcn_exp2f(fmaf(m, c, -base));
+    m = top;
+    l *= shrink;
+#pragma unroll
+    for (int i = 0; i < R::ND; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][r] *= shrink;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[0][i] = __builtin_amdgcn_exp2f(fmaf(s[0][i], c, -base));
+      l += s[0][i];
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const Frag<T> pf = frag_of<T>(s[0], h);
+#pragma unroll
+      for (int i = 0; i < R::ND; ++i) mma(R::col_frag(buf + BN * R::ROW, 16 * h, i), pf, acc[i]);
+    }
+#if defined(__HIP_DEVICE_COMPILE__)
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");              // its tile is read: the next copies may overwrite it
+    __builtin_amdgcn_sched_barrier(0);
+#endif
+    if (C::STAGES == 1 && t + 4 < last) issue(t + 4, own);
+  }
+  l = half_sum(l);
+  if (lane < 32) {
+    s_m[wave][lane] = m;
+    s_l[wave][lane] = l;
+  }
+  tile_sync();
+  // the wavefronts' outputs on a common base, [wave][column][DP] in the tiles' place (columns one bank apart)
+  constexpr int PITCH = DP + 4;
+  static_assert(4 * 32 * PITCH * 4 <= C::LDS, "the joined columns lie where the tiles were");
+  float top = -INFINITY;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) top = fmaxf(top, s_m[w][lane & 31]);
+  const float base = top == -INFINITY ? 0.0f : top * c;
+  float* mine = (float*)smem + (wave * 32 + (lane & 31)) * PITCH;
+  const float f = __builtin_amdgcn_exp2f(fmaf(m, c, -base));
+#pragma unroll
+  for (int i = 0; i < R::ND; ++i) store_col(mine, acc[i], i, DP, f);
+  tile_sync();
+  const int cols = min(32, a.group - g0);
+  for (int e = threadIdx.x; e < cols * (DP / 4); e += 256) {
+    const int col = e / (DP / 4), d = (e - col * (DP / 4)) * 4;
+    float tm = -INFINITY, tl = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) tm = fmaxf(tm, s_m[w][col]);
+    const float tb = tm == -INFINITY ? 0.0f : tm * c;
+    float4 sum = make_float4(0, 0, 0, 0);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      tl += s_l[w][col] * __builtin_amdgcn_exp2f(fmaf(s_m[w][col], c, -tb));
+      const float4 v = *(const float4*)((const float*)smem + (w * 32 + col) * PITCH + d);
+      sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
+    }
+    const int head = kvh * a.group + g0 + col;
+    if (a.splits == 1) {
+      const float r = tl == 0.0f ? 0.0f : 1.0f / tl;
+      if (d < a.dim) store4(o + seq * ldo + (int64_t)head * a.dim + d, sum.x * r, sum.y * r, sum.z * r, sum.w * r);
+    } else {
+      float* to = part + ((int64_t)(seq * a.heads + head) * a.splits + split) * (DP + 4);
+      *(float4*)(to + d) = sum;
+      if (d == 0) *(float4*)(to + DP) = make_float4(tm, tl, 0, 0);
+    }
+  }
+}
+
+// the shares of a head's keys put together: a block of 64 lanes for each sequence and head
+template <typename T, int DP>
+__global__ __launch_bounds__(64) void k_attn_join(const float* __restrict__ part, int splits, int heads, int dim, float c, T* __restrict__ o,
+                                                  int64_t ldo) {
+  const int lane = threadIdx.x, head = blockIdx.x, seq = blockIdx.y;
+  const float* from = part + (int64_t)(seq * heads + head) * splits * (DP + 4);
+  float top = -INFINITY;
+  for (int s = lane; s < splits; s += 64) top = fmaxf(top, from[s * (DP + 4) + DP]);
+  top = wave_max(top);
+  const float base = top == -INFINITY ? 0.0f : top * c;
+  float l = 0.0f;
+  float v[DP / 64 > 0 ? DP / 64 : 1] = {};
+  for (int s = 0; s < splits; ++s) {
+    const float* at = from + s * (DP + 4);
+    const float f = __builtin_amdgcn_exp2f(fmaf(at[DP], c, -base));
+    l = fmaf(at[DP + 1], f, l);
+#pragma unroll
+    for (int i = 0; i < DP / 64; ++i) v[i] = fmaf(at[lane + 64 * i], f, v[i]);
+  }
+  const float r = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+  for (int i = 0; i < DP / 64; ++i)
+    if (lane + 64 * i < dim) o[seq * ldo + (int64_t)head * dim + lane + 64 * i] = from_f32<T>(v[i] * r);
+}
+
+static int attn_dp(int64_t dim) { return dim <= 64 ? 64 : 128; }
+
+static int decode_splits(int64_t n_seq, int64_t capacity, int64_t heads, int64_t kv_heads, int64_t window, int64_t sinks) {
+  const int64_t most = window > 0 && window + sinks + 64 < capacity ? window + sinks + 64 : capacity;
+  const int64_t tiles = ceil_div(most, 32), blocks = n_seq * kv_heads * ceil_div(heads / kv_heads, 32);
+  int64_t s = ceil_div(512, blocks);
+  if (s > ceil_div(tiles, 4)) s = ceil_div(tiles, 4);
+  return (int)(s < 1 ? 1 : s);
+}
+
+}  // namespace efqat
+
+using namespace efqat;
+
+extern "C" int efqat_attention_fwd(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, int dtype, int64_t Tq,
+                                   int64_t Tk, int64_t n_seq, const int32_t* q_start, const int32_t* k_start, int64_t heads,
+                                   int64_t kv_heads, int64_t dim, float scale, int causal, int64_t window, int64_t sinks, void* o,
+                                   int64_t ldo, float* lse, void* stream) {
+  AttnArgs a;
+  EFQAT_TRY(attn_args(&a, q, ldq, k, ldk, v, ldv, dtype, Tq, Tk, n_seq, q_start, k_start, heads, kv_heads, dim, scale, causal, window, sinks));
+  EFQAT_TRY(attn_rows(o, ldo, heads * dim, dtype));
+  if (!aligned4(lse)) return EFQAT_ERR_ALIGNMENT;
+  const int64_t tiles = a.qs.most_tiles(128), blocks = tiles * heads;
+  if (blocks > kAttnMostBlocks) return EFQAT_ERR_BAD_SHAPE;
+  hipStream_t st = (hipStream_t)stream;
+#define EFQAT_FWD(E, DP) return launch(k_attn_fwd<E, DP>, dim3((unsigned)blocks), dim3(256), 0, st, a, (E*)o, ldo, lse, (int)tiles)
+  if (dtype == EFQAT_F32) { if (dim <= 64) EFQAT_FWD(float, 64); EFQAT_FWD(float, 128); }
+  if (dim <= 64) EFQAT_FWD(bf16_t, 64);
+  EFQAT_FWD(bf16_t, 128);
+#undef EFQAT_FWD
+}
+
+extern "C" size_t efqat_attention_decode_workspace_bytes(int64_t n_seq, int64_t capacity, int64_t heads, int64_t kv_heads, int64_t dim,
+                                                         int64_t window, int64_t sinks) {
+  if (n_seq <= 0 || capacity <= 0 || heads <= 0 || kv_heads <= 0 || heads % kv_heads || dim <= 0 || dim > 128 || window < 0 || sinks < 0 ||
+      n_seq > 65535 || capacity > kAttnMostRows || heads > 65535)
+    return 256;
+  const int splits = decode_splits(n_seq, capacity, heads, kv_heads, window, sinks);
+  if (splits == 1) return 256;
+  return (size_t)round_up(n_seq * heads * splits * (attn_dp(dim) + 4) * 4, 256);
+}
+
+extern "C" int efqat_attention_decode(const void* q, int64_t ldq, const void* k_cache, int64_t ldk, int64_t seq_k, const void* v_cache,
+                                      int64_t ldv, int64_t seq_v, int dtype, int64_t n_seq, int64_t capacity, const int32_t* lengths,
+                                      int64_t heads, int64_t kv_heads, int64_t dim, float scale, int64_t window, int64_t sinks, void* o,
+                                      int64_t ldo, void* ws, size_t ws_bytes, void* stream) {
+  AttnArgs a;
+  EFQAT_TRY(attn_args(&a, q, ldq, k_cache, ldk, v_cache, ldv, dtype, n_seq, capacity, 1, nullptr, nullptr, heads, kv_heads, dim, scale, 1, window, sinks));
+  EFQAT_TRY(attn_rows(o, ldo, heads * dim, dtype));
+  if (n_seq > 65535 || (n_seq > 1 && (seq_k < (capacity - 1) * ldk + kv_heads * dim || seq_v < (capacity - 1) * ldv + kv_heads * dim)))
+    return EFQAT_ERR_BAD_SHAPE;
+  if (!lengths || !ws) return EFQAT_ERR_NULL_PTR;
+  if (!aligned4(lengths) || (uintptr_t)ws % 256) return EFQAT_ERR_ALIGNMENT;
+  const int per16 = dtype == EFQAT_F32 ? 4 : 8;
+  if (n_seq > 1 && (seq_k % per16 || seq_v % per16)) return EFQAT_ERR_ALIGNMENT;
+  if (ws_bytes < efqat_attention_decode_workspace_bytes(n_seq, capacity, heads, kv_heads, dim, window, sinks)) return EFQAT_ERR_WORKSPACE;
+  const int splits = decode_splits(n_seq, capacity, heads, kv_heads, window, sinks);
+  const DecodeArgs d = {q, k_cache, v_cache, ldq, ldk, ldv, n_seq > 1 ? seq_k : 0, n_seq > 1 ? seq_v : 0, lengths, (int)capacity, (int)heads,
+                        a.group, (int)dim, a.mask.window, a.mask.sinks, splits, scale};
+  const int64_t ny = kv_heads * ceil_div(a.group, 32);
+  const dim3 grid((unsigned)splits, (unsigned)ny, (unsigned)n_seq);
+  hipStream_t st = (hipStream_t)stream;
+  float* part = (float*)ws;
+#define EFQAT_DEC(E, DP)                                                                                                           \
+  do {                                                                                                                             \
+    EFQAT_TRY(launch(k_attn_decode<E, DP>, grid, dim3(256), 0, st, d, (E*)o, ldo, part));                                          \
+    if (splits > 1)                                                                                                                \
+      EFQAT_TRY(launch(k_attn_join<E, DP>, dim3((unsigned)heads, (unsigned)n_seq), dim3(64), 0, st, part, splits, (int)heads,      \
+                       (int)dim, scale * kLog2e, (E*)o, ldo));                                                                     \
+    return EFQAT_OK;                                                                                                               \
+  } while (0)
+  if (dtype == EFQAT_F32) { if (dim <= 64) EFQAT_DEC(float, 64); EFQAT_DEC(float, 128); }
+  if (dim <= 64) EFQAT_DEC(bf16_t, 64);
+  EFQAT_DEC(bf16_t, 128);
+#undef EFQAT_DEC
+}

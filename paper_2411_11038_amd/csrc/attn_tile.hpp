@@ -1,0 +1,316 @@
+// Pieces that the attention kernels share: which keys a query sees, places of blocks in packed sequences, tiles of rows in LDS and the
+// fragments of the matrix instructions that are read from them.
+//
+// All kernels use v_mfma_f32_32x32x16_bf16 or, for fp32, eight v_mfma_f32_32x32x2_f32 on the same fragments: a lane holds 8 of the 16
+// contraction elements of one row (column) of an operand, elements 8 (lane / 32) .. + 7 of row (column) lane % 32.  The result has column
+// lane % 32 and, in register i, row (i & 3) + 8 (i >> 2) + 4 (lane / 32).  Eight neighbouring registers of a result are thus a fragment
+// of the next product's operand, if that product's other operand takes its 16 contraction elements in the same order (col_frag does):
+// probabilities go from one product to the next without leaving their lane.
+#pragma once
+#include "gemm_epilogue.hpp"
+#include "lds_copy.hpp"
+#include "rows.hpp"
+
+namespace efqat {
+
+constexpr int64_t kAttnMostRows = INT64_C(1) << 28;          // sums of three such fit 32 bits
+
+// token at position p sees key j (< keys of the sequence)
+struct AttnMask {
+  int causal, window, sinks;
+  __device__ __forceinline__ bool sees(int p, int j) const {
+    const int d = p - j;
+    return (!causal || d >= 0) & (!window || (d < window && -d < window) || j < sinks);
+  }
+  // all of p0 .. p1 see all of j0 .. j1
+  __device__ __forceinline__ bool sees_all(int p0, int p1, int j0, int j1) const {
+    return (!causal || j1 <= p0) && (!window || (p1 - j0 < window && j1 - p0 < window) || j1 < sinks);
+  }
+  // some of p0 .. p1 may see some of j0 .. j1
+  __device__ __forceinline__ bool sees_some(int p0, int p1, int j0, int j1) const {
+    return (!causal || j0 <= p1) && (!window || (p0 - j1 < window && j0 - p1 < window) || j0 < sinks);
+  }
+};
+
+// Sequences packed into rows: sequence s is rows start[s] .. start[s + 1] - 1, or rows / n rows each (start NULL).  Offsets are data of the
+// device: they are cut to the rows that exist.
+struct Packed {
+  const int32_t* start;
+  int rows, n;
+  __device__ __forceinline__ int2 place(int s) const {               // first row, rows
+    if (!start) {
+      const int each = rows / n;
+      return make_int2(s * each, each);
+    }
+    int a = start[s], b = start[s + 1];
+    a = a < 0 ? 0 : a > rows ? rows : a;
+    b = b < a ? a : b > rows ? rows : b;
+    return make_int2(a, b - a);
+  }
+  // at most so many tiles have rows
+  __host__ int64_t most_tiles(int tile) const {
+    return start ? ceil_div(rows, tile) + n - 1 : n * ceil_div(rows / n, tile);
+  }
+};
+// Sequence and tile in it of tile number t of all sequences; false: there are not so many.  A wavefront looks at 64 sequences at a time.
+__device__ __forceinline__ bool find_tile(const Packed& p, int tile_rows, int t, int* seq, int* tile) {
+  if (!p.start) {
+    const int each = (int)((p.rows / p.n + tile_rows - 1) / tile_rows);
+    *seq = t / each;
+    *tile = t - *seq * each;
+    return true;
+  }
+  const int lane = threadIdx.x & 63;
+  for (int base = 0; base < p.n; base += 64) {
+    int n = 0;
+    if (base + lane < p.n) n = (p.place(base + lane).y + tile_rows - 1) / tile_rows;
+    int end = n;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(end, o, 64);
+      end += lane >= o ? v : 0;
+    }
+    const uint64_t past = __ballot(end > t);
+    if (past) {
+      const int l = __builtin_ctzll(past);
+      *seq = base + l;
+      *tile = t - __builtin_amdgcn_readlane(end - n, l);
+      return true;
+    }
+    t -= __builtin_amdgcn_readlane(end, 63);
+  }
+  return false;
+}
+
+// ---- fragments
+template <typename T>
+struct Frag;
+template <>
+struct Frag<bf16_t> {
+  bf16x8_t v;
+};
+template <>
+struct Frag<float> {
+  float v[8];
+};
+__device__ __forceinline__ void mma(const Frag<bf16_t>& a, const Frag<bf16_t>& b, floatx16_t& c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b.v, c, 0, 0, 0);
+#endif
+}
+__device__ __forceinline__ void mma(const Frag<float>& a, const Frag<float>& b, floatx16_t& c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+#pragma unroll
+  for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[e], b.v[e], c, 0, 0, 0);
+#endif
+}
+// registers 8 s .. 8 s + 7 of a result as an operand; bf16: rounded to nearest even
+template <typename T>
+__device__ __forceinline__ Frag<T> frag_of(const floatx16_t& c, int s) {
+  Frag<T> f;
+  if constexpr (sizeof(T) == 2) {
+    uint4 w;
+    w.x = pack_bf16x2(c[8 * s], c[8 * s + 1]);
+    w.y = pack_bf16x2(c[8 * s + 2], c[8 * s + 3]);
+    w.z = pack_bf16x2(c[8 * s + 4], c[8 * s + 5]);
+    w.w = pack_bf16x2(c[8 * s + 6], c[8 * s + 7]);
+    f.v = __builtin_bit_cast(bf16x8_t, w);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f.v[e] = c[8 * s + e];
+  }
+  return f;
+}
+__device__ __forceinline__ floatx16_t zero16() {
+  floatx16_t z;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) z[i] = 0.0f;
+  return z;
+}
+// row of a result that register i holds in this lane
+__device__ __forceinline__ int result_row(int i) { return (i & 3) + 8 * (i >> 2) + 4 * ((threadIdx.x >> 5) & 1); }
+
+// 8 elements of a row of a matrix in memory as an operand, 16-byte aligned; not `ok`: zeros
+template <typename T>
+__device__ __forceinline__ Frag<T> load_frag(const T* p, bool ok) {
+  Frag<T> f;
+  if constexpr (sizeof(T) == 2) {
+    uint4 w = make_uint4(0, 0, 0, 0);
+    if (ok) w = *reinterpret_cast<const uint4*>(p);
+    f.v = __builtin_bit_cast(bf16x8_t, w);
+  } else {
+    float4 a = make_float4(0, 0, 0, 0), b = a;
+    if (ok) {
+      a = *reinterpret_cast<const float4*>(p);
+      b = *reinterpret_cast<const float4*>(p + 4);
+    }
+    f.v[0] = a.x; f.v[1] = a.y; f.v[2] = a.z; f.v[3] = a.w;
+    f.v[4] = b.x; f.v[5] = b.y; f.v[6] = b.z; f.v[7] = b.w;
+  }
+  return f;
+}
+
+// ---- a tile of rows of DP features in LDS.  Its 16-byte pieces are swizzled by row so that both ways of reading it spread over the
+// banks: neighbouring rows at the same piece (row_frag), and four rows at four neighbouring pieces (col_frag, bf16, transposing reads)
+// or two rows four apart at eight neighbouring pieces (col_frag, fp32).
+template <typename T, int DP>
+struct RowTile {
+  static constexpr int ROW = DP * (int)sizeof(T), CH = ROW / 16, RPI = 1024 / ROW;   // bytes and pieces of a row, rows of one copy
+  static constexpr int KS = DP / 16, ND = DP / 32;                                   // contraction steps, result tiles of a row
+  __device__ static __forceinline__ int swz(int row) {
+    if constexpr (sizeof(T) == 4) return ((row >> 2) & 1) << 3 | ((row >> 3) & 1) << 2 | (row & 3);
+    else if constexpr (DP == 128) return (row & 3) << 2 | ((row >> 2) & 3);
+    else return ((row >> 1) & 1) << 2 | ((row >> 2) & 3);
+  }
+  // copy number `slot` of a tile: the rows slot * RPI .. + RPI - 1, those at `valid` and behind and pieces behind `pieces` as zeros
+  __device__ static __forceinline__ void copy(const char* base, int64_t ld_bytes, int valid, int pieces, char* lds, int slot) {
+    const int lane = threadIdx.x & 63;
+    const int row = slot * RPI + lane / CH, piece = (lane % CH) ^ swz(row);
+    const char* src = row < valid && piece < pieces ? base + row * ld_bytes + piece * 16 : zero_page();
+    dma16(src, lds + slot * 1024);
+  }
+  // contraction step ks of row `row` (a multiple of 32) + lane % 32
+  __device__ static __forceinline__ Frag<T> row_frag(const char* lds, int row, int ks) {
+    const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
+    const char* p = lds + (row + r) * ROW;
+    Frag<T> f;
+    if constexpr (sizeof(T) == 2) {
+      f.v = *reinterpret_cast<const bf16x8_t*>(p + (((2 * ks + h) ^ swz(r)) << 4));
+    } else {
+      const float4 a = *reinterpret_cast<const float4*>(p + (((4 * ks + 2 * h) ^ swz(r)) << 4));
+      const float4 b = *reinterpret_cast<const float4*>(p + (((4 * ks + 2 * h + 1) ^ swz(r)) << 4));
+      f.v[0] = a.x; f.v[1] = a.y; f.v[2] = a.z; f.v[3] = a.w;
+      f.v[4] = b.x; f.v[5] = b.y; f.v[6] = b.z; f.v[7] = b.w;
+    }
+    return f;
+  }
+  // feature 32 i + lane % 32 of the 16 rows from `row` (a multiple of 16) on, in the order of a result's registers: element e is row
+  // 8 (e >> 2) + 4 (lane / 32) + (e & 3)
+  __device__ static __forceinline__ Frag<T> col_frag(const char* lds, int row, int i) {
+    const int lane = threadIdx.x & 63, h = lane >> 5;
+    Frag<T> f;
+    if constexpr (sizeof(T) == 2) {
+#if defined(__HIP_DEVICE_COMPILE__)
+      const int s = lane & 15, piece = 4 * i + 2 * ((lane >> 4) & 1) + ((s & 3) >> 1);
+      shortx4_t v[2];
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int k = row + 8 * r + 4 * h + (s >> 2);
+        v[r] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) shortx4_t*)(lds + k * ROW + ((piece ^ swz(k)) << 4) + 8 * (s & 1)));
+      }
+      struct { shortx4_t lo, hi; } both = {v[0], v[1]};
+      f.v = __builtin_bit_cast(bf16x8_t, both);
+#endif
+    } else {
+      const int d = lane & 31;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int k = row + 8 * (e >> 2) + 4 * h + (e & 3);
+        f.v[e] = *reinterpret_cast<const float*>(lds + k * ROW + (((8 * i + (d >> 2)) ^ swz(k)) << 4) + 4 * (d & 3));
+      }
+    }
+    return f;
+  }
+};
+
+// everything that was copied and read is there, for all wavefronts of the block
+__device__ __forceinline__ void tile_sync() {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+#endif
+}
+
+// the other half's value: lane l gets that of lane l ^ 32
+__device__ __forceinline__ float half_max(float v) { return fmaxf(v, __shfl_xor(v, 32, 64)); }
+__device__ __forceinline__ float half_sum(float v) { return v + __shfl_xor(v, 32, 64); }
+
+// four neighbouring elements of a result's column, as features of a row
+template <typename T>
+__device__ __forceinline__ void store4(T* p, float a, float b, float c, float d) {
+  if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(a, b), pack_bf16x2(c, d));
+  else *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d);
+}
+// a result tile whose columns are tokens and whose rows are features 32 i .. + 31: times f into row p of `dim` features
+template <typename T>
+__device__ __forceinline__ void store_col(T* p, const floatx16_t& c, int i, int dim, float f) {
+#pragma unroll
+  for (int r = 0; r < 16; r += 4) {
+    const int d = 32 * i + result_row(r);
+    if (d < dim) store4(p + d, c[r] * f, c[r + 1] * f, c[r + 2] * f, c[r + 3] * f);
+  }
+}
+
+// Tiles of BN keys that some of the positions p0 .. p1 see: those of the first `sinks` keys, then those of the window
+struct KeyTiles {
+  int sink, first, count, end;                        // tiles of the sinks that lie before tile `first`; tiles in all; keys that count
+  __device__ __forceinline__ KeyTiles(const AttnMask& m, int keys, int p0, int p1, int bn) {
+    int lo = 0, hi = keys;
+    if (m.window) {
+      lo = p0 - m.window + 1;
+      hi = p1 + m.window < hi ? p1 + m.window : hi;
+      if (hi < m.sinks) hi = m.sinks < keys ? m.sinks : keys;
+    }
+    if (m.causal && p1 + 1 < hi) hi = p1 + 1;
+    if (hi < 0) hi = 0;
+    if (lo < 0) lo = 0;
+    if (lo > hi) lo = hi;
+    end = hi;
+    first = lo / bn;
+    const int s = m.window && m.sinks > 0 ? (m.sinks - 1) / bn + 1 : 0;
+    if (s >= first) {
+      if (s > 0) first = 0;
+      sink = 0;
+    } else {
+      sink = s;
+    }
+    count = (hi + bn - 1) / bn - first;
+    if (count < 0) count = 0;
+    count += sink;
+  }
+  __device__ __forceinline__ int tile(int t) const { return t < sink ? t : first + t - sink; }
+};
+
+// ---- host side
+struct AttnArgs {
+  const void *q, *k, *v;
+  int64_t ldq, ldk, ldv;
+  Packed qs, ks;
+  int heads, group, dim;                             // query heads, of them for one key head, features of a head
+  AttnMask mask;
+  float scale;
+};
+constexpr int64_t kAttnMostBlocks = (1 << 24) - 1;    // of 256 lanes: a grid has fewer than 2^32
+// rows of heads: at least `cols` wide, in whole 16 bytes from a 16-byte aligned address
+inline int attn_rows(const void* p, int64_t ld, int64_t cols, int dtype) {
+  if (ld < cols || ld > (INT64_C(1) << 24)) return EFQAT_ERR_BAD_SHAPE;
+  if (!p) return EFQAT_ERR_NULL_PTR;
+  if (!aligned16(p) || ld % (dtype == EFQAT_F32 ? 4 : 8)) return EFQAT_ERR_ALIGNMENT;
+  return EFQAT_OK;
+}
+inline int attn_args(AttnArgs* a, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, int dtype, int64_t Tq,
+                     int64_t Tk, int64_t n_seq, const int32_t* q_start, const int32_t* k_start, int64_t heads, int64_t kv_heads, int64_t dim,
+                     float scale, int causal, int64_t window, int64_t sinks) {
+  if (Tq <= 0 || Tk <= 0 || Tq > kAttnMostRows || Tk > kAttnMostRows || n_seq <= 0 || n_seq > (1 << 24) || heads <= 0 || kv_heads <= 0 ||
+      heads > 65535 || heads % kv_heads || dim <= 0 || dim > 128 || dim % 8 || window < 0 || sinks < 0)
+    return EFQAT_ERR_BAD_SHAPE;
+  if (!(scale > 0.0f) || !(scale < INFINITY)) return EFQAT_ERR_BAD_SHAPE;
+  if (!known_dtype(dtype)) return EFQAT_ERR_BAD_DTYPE;
+  if (causal != 0 && causal != 1) return EFQAT_ERR_BAD_LAYOUT;
+  if (!q_start != !k_start) return EFQAT_ERR_NULL_PTR;                    // both packed by offsets, or both evenly
+  if (!q_start && (Tq % n_seq || Tk % n_seq)) return EFQAT_ERR_BAD_SHAPE;
+  EFQAT_TRY(attn_rows(q, ldq, heads * dim, dtype));
+  EFQAT_TRY(attn_rows(k, ldk, kv_heads * dim, dtype));
+  EFQAT_TRY(attn_rows(v, ldv, kv_heads * dim, dtype));
+  if (!aligned4(q_start) || !aligned4(k_start)) return EFQAT_ERR_ALIGNMENT;
+  const int64_t far = kAttnMostRows;
+  *a = {q, k, v, ldq, ldk, ldv, {q_start, (int)Tq, (int)n_seq}, {k_start, (int)Tk, (int)n_seq}, (int)heads, (int)(heads / kv_heads), (int)dim,
+        {causal, window >= far ? 0 : (int)window, sinks >= far ? (int)far : (int)sinks}, scale};
+  return EFQAT_OK;
+}
+
+}  // namespace efqat

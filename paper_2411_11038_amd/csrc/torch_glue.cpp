@@ -10,6 +10,8 @@
 #include <ATen/ops/empty.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <c10/hip/HIPFunctions.h>
+#include <cmath>
 #include <cstdint>
 #include <tuple>
 #include <type_traits>
@@ -443,6 +445,247 @@ PyObject* layer_norm_bwd(PyObject* const* a, PyObject* const* out) {
   }));
 }
 
+// ---- Calls of an attention block.  Their tensors have to live on the current device, whose stream they are launched on.
+const at::Tensor& here(PyObject* o) {
+  const at::Tensor& t = gpu_tensor(o);
+  if (t.device().index() != c10::hip::current_device()) refuse_value("tensor must live on the current device", "");
+  return t;
+}
+Rows rows_here(PyObject* o) { return rows_of(here(o)); }
+// rows of the type of x
+Rows rows_at(PyObject* o, const Rows& x, int64_t rows, int64_t cols, const char* what) {
+  const Rows r = rows_here(o);
+  if (r.type != x.type) {
+    PyErr_Format(PyExc_TypeError, "%s: another dtype than the call's", what);
+    throw BadArgument();
+  }
+  if (r.rows != rows || (cols >= 0 && r.cols != cols)) refuse_value("%s: another shape than the call's", what);
+  return r;
+}
+template <class T>
+T* dense_here(PyObject* o, at::ScalarType type, int64_t rows, int64_t cols, const char* what) {
+  if (!given(o)) return nullptr;
+  here(o);
+  return (T*)dense(o, type, rows, cols, what);
+}
+double real(PyObject* o) {
+  const double v = PyFloat_AsDouble(o);
+  if (v == -1.0 && PyErr_Occurred()) throw BadArgument();
+  return v;
+}
+int64_t heads_in(PyObject* o, int64_t cols, int64_t* dim, const char* what) {
+  const int64_t heads = integer_as<int64_t>(o, "heads");
+  if (heads < 1 || cols % heads) refuse_value("%s: no whole number of features for each head", what);
+  *dim = cols / heads;
+  return heads;
+}
+// a given result of a call here, or a new one: rows of x's type
+Rows result(Results& r, Py_ssize_t i, PyObject* o, const Rows& x, int64_t rows, int64_t cols, const char* what) {
+  if (given(o)) here(o);
+  return r.rows(i, o, Rows{nullptr, rows, cols, cols, x.type}, what);
+}
+float* result_f32(Results& r, Py_ssize_t i, PyObject* o, int64_t rows, int64_t cols, const char* what) {
+  if (given(o)) here(o);
+  return (float*)r.dense_at(i, o, at::kFloat, rows, cols, what);
+}
+struct Scratch {
+  at::Tensor t;
+  void* p;
+  size_t bytes;
+};
+Scratch scratch(Results& r, PyObject* o, size_t need) {
+  Scratch s;
+  s.t = given(o) ? here(o) : r.make(at::kByte, (int64_t)need, -1);
+  if (!s.t.is_contiguous()) refuse_value("%s: tensor must be contiguous", "ws");
+  s.p = s.t.data_ptr();
+  s.bytes = s.t.nbytes();
+  return s;
+}
+
+// weights, norm, eps, positions, inv_freq, axis, neighbours
+struct RopeCall {
+  const float *wq, *wk, *inv_freq;
+  const int32_t *positions, *axis;
+  int64_t axes, freqs;
+  int norm, neighbours;
+  float eps;
+};
+RopeCall rope_call(PyObject* const* a, int64_t rows, int64_t dim) {
+  RopeCall c = {};
+  c.wq = dense_here<const float>(a[0], at::kFloat, dim, -1, "q_weight");
+  c.wk = dense_here<const float>(a[1], at::kFloat, dim, -1, "k_weight");
+  c.norm = truth(a[2]);
+  c.eps = (float)real(a[3]);
+  if (given(a[5])) {
+    const at::Tensor& f = here(a[5]);
+    c.freqs = f.numel();
+    c.inv_freq = dense_here<const float>(a[5], at::kFloat, c.freqs, -1, "inv_freq");
+    if (!given(a[4])) refuse_value("inv_freq without positions", "");
+    const at::Tensor& p = here(a[4]);
+    c.axes = p.dim() == 1 ? 1 : p.size(0);
+    c.positions = p.dim() == 1 ? dense_here<const int32_t>(a[4], at::kInt, rows, -1, "positions")
+                               : dense_here<const int32_t>(a[4], at::kInt, c.axes, rows, "positions");
+    c.axis = dense_here<const int32_t>(a[6], at::kInt, c.freqs, -1, "axis");
+  } else if (given(a[4]) || given(a[6])) {
+    refuse_value("positions without inv_freq", "");
+  }
+  c.neighbours = truth(a[7]);
+  return c;
+}
+// q, heads, k, kv_heads, q_weight, k_weight, norm, eps, positions, inv_freq, axis, neighbours -> yq, yk
+PyObject* head_norm_rope_fwd(PyObject* const* a, PyObject* const* out) {
+  const at::Tensor& t = here(a[0]);
+  const Rows q = rows_of(t);
+  int64_t dim;
+  const int64_t heads = heads_in(a[1], q.cols, &dim, "q"), kv = given(a[2]) ? integer_as<int64_t>(a[3], "kv_heads") : 0;
+  if (given(a[2]) && (kv < 1 || kv > 65535)) refuse_value("%s: kv_heads expected", "k");
+  const Rows k = given(a[2]) ? rows_at(a[2], q, q.rows, kv * dim, "k") : Rows{};
+  const RopeCall c = rope_call(a + 4, q.rows, dim);
+  Results r(2, t);
+  const Rows yq = result(r, 0, out[0], q, q.rows, q.cols, "q"), yk = kv ? result(r, 1, out[1], q, q.rows, k.cols, "k") : Rows{};
+  void* st = stream_now();
+  return r.take(unlocked([&] {
+    return efqat_head_norm_rope_fwd(q.p, q.ld, k.p, k.ld, q.dtype(), q.rows, heads, kv, dim, c.norm, c.wq, c.wk, c.eps, c.positions, c.axes, c.axis,
+                                    c.inv_freq, c.freqs, c.neighbours, yq.p, yq.ld, yk.p, yk.ld, st);
+  }));
+}
+// dq, q, heads, dk, k, kv_heads, q_weight, k_weight, norm, eps, positions, inv_freq, axis, neighbours, ws -> dq, dk, dq_weight, dk_weight
+PyObject* head_norm_rope_bwd(PyObject* const* a, PyObject* const* out) {
+  const at::Tensor& t = here(a[0]);
+  const Rows dq = rows_of(t);
+  int64_t dim;
+  const int64_t heads = heads_in(a[2], dq.cols, &dim, "dq"), kv = given(a[3]) ? integer_as<int64_t>(a[5], "kv_heads") : 0;
+  if (given(a[3]) && (kv < 1 || kv > 65535)) refuse_value("%s: kv_heads expected", "dk");
+  const Rows dk = given(a[3]) ? rows_at(a[3], dq, dq.rows, kv * dim, "dk") : Rows{};
+  const RopeCall c = rope_call(a + 6, dq.rows, dim);
+  if (c.norm && (!given(a[1]) || (kv && !given(a[4])))) refuse_value("the inputs of the norm expected", "");
+  const Rows q = given(a[1]) ? rows_at(a[1], dq, dq.rows, dq.cols, "q") : Rows{}, k = kv && given(a[4]) ? rows_at(a[4], dq, dq.rows, kv * dim, "k") : Rows{};
+  Results r(4, t);
+  const Rows xq = result(r, 0, out[0], dq, dq.rows, dq.cols, "dq"), xk = kv ? result(r, 1, out[1], dq, dq.rows, dk.cols, "dk") : Rows{};
+  float* wq = c.norm ? result_f32(r, 2, out[2], dim, -1, "dq_weight") : nullptr;
+  float* wk = c.norm && kv ? result_f32(r, 3, out[3], dim, -1, "dk_weight") : nullptr;
+  const Scratch ws = scratch(r, a[14], efqat_head_norm_rope_bwd_workspace_bytes(dq.rows, heads, kv, dim));
+  void* st = stream_now();
+  return r.take(unlocked([&] {
+    return efqat_head_norm_rope_bwd(dq.p, dq.ld, dk.p, dk.ld, q.p, q.ld, k.p, k.ld, dq.dtype(), dq.rows, heads, kv, dim, c.norm, c.wq, c.wk, c.eps,
+                                    c.positions, c.axes, c.axis, c.inv_freq, c.freqs, c.neighbours, xq.p, xq.ld, xk.p, xk.ld, wq, wk, ws.p, ws.bytes, st);
+  }));
+}
+
+// heads, kv_heads, q_start, k_start, sequences, causal, window, sinks, scale
+struct AttnCall {
+  int64_t heads, kv, dim, n_seq, window, sinks;
+  const int32_t *q_start, *k_start;
+  int causal;
+  float scale;
+};
+AttnCall attn_call(PyObject* const* a, const Rows& q, const Rows& k) {
+  AttnCall c = {};
+  c.heads = heads_in(a[0], q.cols, &c.dim, "q");
+  c.kv = given(a[1]) ? integer_as<int64_t>(a[1], "kv_heads") : c.heads;
+  if (c.kv < 1 || c.kv > 65535 || k.cols != c.kv * c.dim) refuse_value("%s: another shape than the call's", "k");
+  if (given(a[2])) {
+    const at::Tensor& s = here(a[2]);
+    c.n_seq = s.numel() - 1;
+    if (c.n_seq < 1) refuse_value("%s: the offsets of one sequence at least expected", "q_start");
+    c.q_start = dense_here<const int32_t>(a[2], at::kInt, c.n_seq + 1, -1, "q_start");
+    c.k_start = given(a[3]) ? dense_here<const int32_t>(a[3], at::kInt, c.n_seq + 1, -1, "k_start") : c.q_start;
+  } else {
+    if (given(a[3])) refuse_value("k_start without q_start", "");
+    c.n_seq = integer_as<int64_t>(a[4], "sequences");
+  }
+  c.causal = truth(a[5]);
+  c.window = integer_as<int64_t>(a[6], "window");
+  c.sinks = integer_as<int64_t>(a[7], "sinks");
+  c.scale = given(a[8]) ? (float)real(a[8]) : (float)(1.0 / std::sqrt((double)c.dim));
+  return c;
+}
+// q, k, v, heads, kv_heads, q_start, k_start, sequences, causal, window, sinks, scale -> o, lse
+PyObject* attention_fwd(PyObject* const* a, PyObject* const* out) {
+  const at::Tensor& t = here(a[0]);
+  const Rows q = rows_of(t), k = rows_here(a[1]);
+  rows_at(a[1], q, k.rows, k.cols, "k");
+  const Rows v = rows_at(a[2], q, k.rows, k.cols, "v");
+  const AttnCall c = attn_call(a + 3, q, k);
+  Results r(2, t);
+  const Rows o = result(r, 0, out[0], q, q.rows, q.cols, "o");
+  float* lse = result_f32(r, 1, out[1], c.heads, q.rows, "lse");
+  void* st = stream_now();
+  return r.take(unlocked([&] {
+    return efqat_attention_fwd(q.p, q.ld, k.p, k.ld, v.p, v.ld, q.dtype(), q.rows, k.rows, c.n_seq, c.q_start, c.k_start, c.heads, c.kv, c.dim, c.scale,
+                               c.causal, c.window, c.sinks, o.p, o.ld, lse, st);
+  }));
+}
+// do, q, k, v, o, lse, heads, kv_heads, q_start, k_start, sequences, causal, window, sinks, scale, ws -> dq, dk, dv
+PyObject* attention_bwd(PyObject* const* a, PyObject* const* out) {
+  const at::Tensor& t = here(a[1]);
+  const Rows q = rows_of(t), k = rows_here(a[2]), g = rows_at(a[0], q, q.rows, q.cols, "do"), o = rows_at(a[4], q, q.rows, q.cols, "o");
+  rows_at(a[2], q, k.rows, k.cols, "k");
+  const Rows v = rows_at(a[3], q, k.rows, k.cols, "v");
+  const AttnCall c = attn_call(a + 6, q, k);
+  if (!given(a[5])) refuse(PyExc_TypeError, "tensor", a[5]);
+  const float* lse = dense_here<const float>(a[5], at::kFloat, c.heads, q.rows, "lse");
+  Results r(3, t);
+  const Rows dq = result(r, 0, out[0], q, q.rows, q.cols, "dq"), dk = result(r, 1, out[1], q, k.rows, k.cols, "dk"),
+             dv = result(r, 2, out[2], q, k.rows, k.cols, "dv");
+  const Scratch ws = scratch(r, a[15], efqat_attention_bwd_workspace_bytes(q.rows, c.heads));
+  void* st = stream_now();
+  return r.take(unlocked([&] {
+    return efqat_attention_bwd(g.p, g.ld, q.p, q.ld, k.p, k.ld, v.p, v.ld, o.p, o.ld, lse, q.dtype(), q.rows, k.rows, c.n_seq, c.q_start, c.k_start,
+                               c.heads, c.kv, c.dim, c.scale, c.causal, c.window, c.sinks, dq.p, dq.ld, dk.p, dk.ld, dv.p, dv.ld, ws.p, ws.bytes, st);
+  }));
+}
+// a cache [sequences][capacity][columns] whose rows may lie apart
+struct Cache {
+  void* p;
+  int64_t seqs, capacity, cols, ld, seq;
+};
+Cache cache_of(PyObject* o, const Rows& q, const char* what) {
+  const at::Tensor& t = here(o);
+  if (t.scalar_type() != q.type) {
+    PyErr_Format(PyExc_TypeError, "%s: another dtype than the call's", what);
+    throw BadArgument();
+  }
+  if (t.dim() != 3 || t.size(0) != q.rows || (t.size(2) > 1 && t.stride(2) != 1)) refuse_value("%s: [sequences, capacity, features] with contiguous rows expected", what);
+  const int64_t cols = t.size(2), ld = t.size(1) > 1 ? t.stride(1) : cols;
+  return {t.data_ptr(), t.size(0), t.size(1), cols, ld, t.size(0) > 1 ? t.stride(0) : 0};
+}
+// q, k_cache, v_cache, lengths, heads, kv_heads, window, sinks, scale, ws -> o
+PyObject* attention_decode(PyObject* const* a, PyObject* const* out) {
+  const at::Tensor& t = here(a[0]);
+  const Rows q = rows_of(t);
+  const Cache k = cache_of(a[1], q, "k_cache"), v = cache_of(a[2], q, "v_cache");
+  int64_t dim;
+  const int64_t heads = heads_in(a[4], q.cols, &dim, "q"), kv = given(a[5]) ? integer_as<int64_t>(a[5], "kv_heads") : heads;
+  if (kv < 1 || kv > 65535 || k.cols != kv * dim) refuse_value("%s: another shape than the call's", "k_cache");
+  if (v.cols != k.cols || v.capacity != k.capacity) refuse_value("%s: another shape than the call's", "v_cache");
+  if (!given(a[3])) refuse(PyExc_TypeError, "tensor", a[3]);
+  const int32_t* lengths = dense_here<const int32_t>(a[3], at::kInt, q.rows, -1, "lengths");
+  const int64_t window = integer_as<int64_t>(a[6], "window"), sinks = integer_as<int64_t>(a[7], "sinks");
+  const float scale = given(a[8]) ? (float)real(a[8]) : (float)(1.0 / std::sqrt((double)dim));
+  Results r(1, t);
+  const Rows o = result(r, 0, out[0], q, q.rows, q.cols, "out");
+  const Scratch ws = scratch(r, a[9], efqat_attention_decode_workspace_bytes(q.rows, k.capacity, heads, kv, dim, window, sinks));
+  void* st = stream_now();
+  return r.take(unlocked([&] {
+    return efqat_attention_decode(q.p, q.ld, k.p, k.ld, k.seq, v.p, v.ld, v.seq, q.dtype(), q.rows, k.capacity, lengths, heads, kv, dim, scale, window,
+                                  sinks, o.p, o.ld, ws.p, ws.bytes, st);
+  }));
+}
+// x, p, state, residual -> y
+PyObject* dropout(PyObject* const* a, PyObject* const* out) {
+  const at::Tensor& t = here(a[0]);
+  const Rows x = rows_of(t);
+  const double p = real(a[1]);
+  if (!given(a[2])) refuse(PyExc_TypeError, "tensor", a[2]);
+  const int64_t* state = dense_here<const int64_t>(a[2], at::kLong, 2, -1, "state");
+  const Rows res = given(a[3]) ? rows_at(a[3], x, x.rows, x.cols, "residual") : Rows{};
+  Results r(1, t);
+  const Rows y = result(r, 0, out[0], x, x.rows, x.cols, "out");
+  void* st = stream_now();
+  return r.take(unlocked([&] { return efqat_dropout(x.p, x.ld, res.p, res.ld, x.dtype(), x.rows, x.cols, p, state, y.p, y.ld, st); }));
+}
+
 #define EFQAT_WHOLE(name, n, more) {#name, (PyCFunction)(void (*)(void))whole<name, n, more>, METH_FASTCALL, nullptr}
 #define EFQAT_QUERY(name) {#name, (PyCFunction)(void (*)(void))query<efqat_##name>, METH_FASTCALL, nullptr}
 #define EFQAT_ENTRY(name) {#name, (PyCFunction)(void (*)(void))entry<efqat_##name, false>, METH_FASTCALL, nullptr}
@@ -453,7 +696,9 @@ PyMethodDef methods[] = {
     EFQAT_ENTRY(bias_grad),      EFQAT_ENTRY(linear_bwd_ex),  EFQAT_ENTRY(linear_bwd_weight_operand),
     EFQAT_ENTRY(conv_bwd_ex),    EFQAT_ENTRY(linear_fwd),
     EFQAT_WHOLE(ckpt8_save, 1, 2), EFQAT_WHOLE(ckpt8_load, 4, 1), EFQAT_WHOLE(act_fwd, 4, 5), EFQAT_WHOLE(act_bwd, 6, 2),
-    EFQAT_WHOLE(layer_norm_fwd, 5, 5), EFQAT_WHOLE(layer_norm_bwd, 8, 3), EFQAT_ENTRY_ROWS(linear_xent_fwd),
+    EFQAT_WHOLE(layer_norm_fwd, 5, 5), EFQAT_WHOLE(layer_norm_bwd, 8, 3), EFQAT_WHOLE(head_norm_rope_fwd, 12, 2),
+    EFQAT_WHOLE(head_norm_rope_bwd, 15, 4), EFQAT_WHOLE(attention_fwd, 12, 2), EFQAT_WHOLE(attention_bwd, 16, 3),
+    EFQAT_WHOLE(attention_decode, 10, 1), EFQAT_WHOLE(dropout, 4, 1), EFQAT_ENTRY_ROWS(linear_xent_fwd),
     EFQAT_ENTRY_ROWS(linear_xent_bwd), EFQAT_QUERY(linear_xent_fwd_workspace_bytes),
     EFQAT_QUERY(linear_xent_bwd_workspace_bytes), {"empty", (PyCFunction)(void (*)(void))empty, METH_FASTCALL, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_efqat_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -10,12 +10,18 @@
 
 namespace efqat {
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f, kLn2Rest = -1.9046542999e-9f;      // ln 2 = kLn2 + kLn2Rest
 
 template <typename T>
 struct FwdTile {
   static constexpr int BM = 128, BN = sizeof(T) == 2 ? 64 : 32;       // queries of a block, keys of a stage
 };
+
+// log of l exp2(m c), the sum that l stands for: m c as it was rounded where l was summed
+__device__ __forceinline__ float log_sum(float m, float c, float l) {
+  const float base = m * c;
+  return l == 0.0f ? -INFINITY : fmaf(base, kLn2, fmaf(base, kLn2Rest, kLn2 * __builtin_amdgcn_logf(l)));
+}
 
 // scores of a wavefront's 32 queries (columns) against BN keys; what is not seen is -inf
 template <int NT>
@@ -25,7 +31,7 @@ __device__ __forceinline__ void mask_scores(floatx16_t (&s)[NT], const AttnMask&
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const int j = j0 + 32 * n + result_row(i);
-      s[n][i] = j < end && m.sees(p, j) ? s[n][i] : -INFINITY;
+      s[n][i] = (j < end) & m.sees(p, j) ? s[n][i] : -INFINITY;
     }
 }
 
@@ -79,9 +85,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || DP == 64 ? 2 : 1) void k_att
   for (int t = 0; t < kt.count; ++t) {
     char* buf = smem + (t & 1) * STAGE;
     if (t + 1 < kt.count) issue(t + 1, smem + ((t + 1) & 1) * STAGE);
-    const int j0 = kt.tile(t) * BN;
-    const int p0 = r0 + shift, p1 = p0 + 31;
-    if (a.mask.sees_some(p0, p1, j0, j0 + BN - 1)) {
+    const int j0 = kt.tile(t) * BN, p0 = r0 + shift, p1 = p0 + 31;
+    auto tile = [&](auto masked) {
       floatx16_t s[NT];
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
@@ -89,7 +94,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || DP == 64 ? 2 : 1) void k_att
 #pragma unroll
         for (int ks = 0; ks < R::KS; ++ks) mma(R::row_frag(buf, 32 * n, ks), q[ks], s[n]);
       }
-      if (j0 + BN > kp.y || !a.mask.sees_all(p0, p1, j0, j0 + BN - 1)) mask_scores(s, a.mask, p, j0, kp.y);
+      if constexpr (decltype(masked)::value) mask_scores(s, a.mask, p, j0, kp.y);
       float top = m;
 #pragma unroll
       for (int n = 0; n < NT; ++n)
@@ -99,18 +104,18 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || DP == 64 ? 2 : 1) void k_att
       const float base = top == -INFINITY ? 0.0f : top * c;       // nothing seen so far: exp2(-inf) is 0 for all of it
       const float shrink = __builtin_amdgcn_exp2f(fmaf(m, c, -base));
       m = top;
-      l *= shrink;
 #pragma unroll
       for (int i = 0; i < R::ND; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[i][r] *= shrink;
+      float sum = 0.0f;
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+      for (int n = 0; n < NT; ++n) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          s[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], c, -base));
-          l += s[n][i];
-        }
+        for (int i = 0; i < 16; ++i) s[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], c, -base));
+        sum += sum16(s[n]);
+      }
+      l = fmaf(l, shrink, sum);
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -119,9 +124,14 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || DP == 64 ? 2 : 1) void k_att
 #pragma unroll
           for (int i = 0; i < R::ND; ++i) mma(R::col_frag(buf + BN * R::ROW, 32 * n + 16 * h, i), pf, acc[i]);
         }
+    };
+    if (a.mask.sees_some(p0, p1, j0, j0 + BN - 1)) {
+      if (j0 + BN <= kp.y && a.mask.sees_all(p0, p1, j0, j0 + BN - 1)) tile(std::false_type{});
+      else tile(std::true_type{});
     }
     tile_sync();
   }
+  results_settle();
   l = half_sum(l);
   if (qrow < qp.y) {
     const int64_t row = (int64_t)qp.x + qrow;
@@ -129,7 +139,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || DP == 64 ? 2 : 1) void k_att
     T* to = o + row * ldo + head * a.dim;
 #pragma unroll
     for (int i = 0; i < R::ND; ++i) store_col(to, acc[i], i, a.dim, f);
-    if (lse && lane < 32) lse[(int64_t)head * a.qs.rows + row] = l == 0.0f ? -INFINITY : fmaf(m, a.scale, kLn2 * __builtin_amdgcn_logf(l));
+    if (lse && lane < 32) lse[(int64_t)head * a.qs.rows + row] = log_sum(m, c, l);
   }
 }
 
@@ -208,33 +218,34 @@ __global__ __launch_bounds__(256) void k_attn_decode(DecodeArgs a, T* __restrict
     __builtin_amdgcn_sched_barrier(0);
 #endif
     const int j0 = kt.tile(t) * BN;
-    floatx16_t s[1] = {zero16()};
+    auto tile = [&](auto masked) {
+      floatx16_t s[1] = {zero16()};
 #pragma unroll
-    for (int ks = 0; ks < R::KS; ++ks) mma(R::row_frag(buf, 0, ks), q[ks], s[0]);
-    if (!mask.sees_all(p, p, j0, j0 + BN - 1)) mask_scores(s, mask, p, j0, keys);
-    float top = m;
+      for (int ks = 0; ks < R::KS; ++ks) mma(R::row_frag(buf, 0, ks), q[ks], s[0]);
+      if constexpr (decltype(masked)::value) mask_scores(s, mask, p, j0, keys);
+      float top = m;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) top = fmaxf(top, s[0][i]);
-    top = half_max(top);
-    const float base = top == -INFINITY ? 0.0f : top * c;
-    const float shrink = __builtin_amdgcn_exp2f(fmaf(m, c, -base));
-    m = top;
-    l *= shrink;
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[0][i]);
+      top = half_max(top);
+      const float base = top == -INFINITY ? 0.0f : top * c;
+      const float shrink = __builtin_amdgcn_exp2f(fmaf(m, c, -base));
+      m = top;
 #pragma unroll
-    for (int i = 0; i < R::ND; ++i)
+      for (int i = 0; i < R::ND; ++i)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) acc[i][r] *= shrink;
+        for (int r = 0; r < 16; ++r) acc[i][r] *= shrink;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      s[0][i] = __builtin_amdgcn_exp2f(fmaf(s[0][i], c, -base));
-      l += s[0][i];
-    }
+      for (int i = 0; i < 16; ++i) s[0][i] = __builtin_amdgcn_exp2f(fmaf(s[0][i], c, -base));
+      l = fmaf(l, shrink, sum16(s[0]));
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const Frag<T> pf = frag_of<T>(s[0], h);
+      for (int h = 0; h < 2; ++h) {
+        const Frag<T> pf = frag_of<T>(s[0], h);
 #pragma unroll
-      for (int i = 0; i < R::ND; ++i) mma(R::col_frag(buf + BN * R::ROW, 16 * h, i), pf, acc[i]);
-    }
+        for (int i = 0; i < R::ND; ++i) mma(R::col_frag(buf + BN * R::ROW, 16 * h, i), pf, acc[i]);
+      }
+    };
+    if (mask.sees_all(p, p, j0, j0 + BN - 1)) tile(std::false_type{});
+    else tile(std::true_type{});
 #if defined(__HIP_DEVICE_COMPILE__)
     __builtin_amdgcn_sched_barrier(0);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");              // its tile is read: the next copies may overwrite it
@@ -242,6 +253,7 @@ __global__ __launch_bounds__(256) void k_attn_decode(DecodeArgs a, T* __restrict
 #endif
     if (C::STAGES == 1 && t + 4 < last) issue(t + 4, own);
   }
+  results_settle();
   l = half_sum(l);
   if (lane < 32) {
     s_m[wave][lane] = m;

@@ -22,6 +22,20 @@ struct AttnGrads {
   int64_t lddq, lddk, lddv;
 };
 
+// What prob() takes of a token's lse, and the factor of the scores.  bf16: exp2(s c - lse log2 e), one operation beside the exponential.
+// fp32: exp2((s scale - lse) log2 e), whose argument is small wherever the result is not, and exact to 2^-24 of it.
+template <typename T>
+__device__ __forceinline__ float prob_base(float lse) {
+  return lse == -INFINITY ? INFINITY : sizeof(T) == 2 ? lse * kLog2e : lse;       // a token that sees nothing: P = 0
+}
+template <typename T>
+__device__ __forceinline__ float prob(float s, float c, float base) {
+  const float x = fmaf(s, c, -base);
+  return __builtin_amdgcn_exp2f(sizeof(T) == 2 ? x : x * kLog2e);
+}
+template <typename T>
+__device__ __forceinline__ float prob_factor(float scale) { return sizeof(T) == 2 ? scale * kLog2e : scale; }
+
 // dq, and delta for the other kernel.  Blocks, tiles and layout as in k_attn_fwd.
 template <typename T, int DP>
 __global__ __launch_bounds__(256, 1) void k_attn_dq(AttnArgs a, AttnGrads g, int tiles) {
@@ -55,7 +69,7 @@ __global__ __launch_bounds__(256, 1) void k_attn_dq(AttnArgs a, AttnGrads g, int
   const bool in = qrow < qp.y;
   const int64_t row = (int64_t)qp.x + qrow;
   Frag<T> q[R::KS], d[R::KS];
-  float delta = 0.0f, lse2 = INFINITY;
+  float delta = 0.0f, lse = INFINITY;
   {
     const T* qr = (const T*)a.q + row * a.ldq + head * a.dim;
     const T* dr = (const T*)g.dout + row * g.lddo + head * a.dim;
@@ -72,15 +86,14 @@ __global__ __launch_bounds__(256, 1) void k_attn_dq(AttnArgs a, AttnGrads g, int
     }
     delta = half_sum(delta);
     if (in) {
-      const float x = g.lse[(int64_t)head * a.qs.rows + row];
-      lse2 = x == -INFINITY ? INFINITY : x * kLog2e;                // a token that sees nothing: P = 0
+      lse = prob_base<T>(g.lse[(int64_t)head * a.qs.rows + row]);
       if (lane < 32) g.delta[(int64_t)head * a.qs.rows + row] = delta;
     }
   }
   floatx16_t acc[R::ND];
 #pragma unroll
   for (int i = 0; i < R::ND; ++i) acc[i] = zero16();
-  const float c = a.scale * kLog2e;
+  const float c = prob_factor<T>(a.scale);
   tile_sync();
   for (int t = 0; t < kt.count; ++t) {
     char* buf = smem + (t & 1) * STAGE;
@@ -89,31 +102,36 @@ __global__ __launch_bounds__(256, 1) void k_attn_dq(AttnArgs a, AttnGrads g, int
 #pragma unroll
     for (int n = 0; n < BN / 32; ++n) {
       const int j0 = kt.tile(t) * BN + 32 * n;
-      if (!a.mask.sees_some(p0, p1, j0, j0 + 31)) continue;
-      floatx16_t s = zero16(), dp = zero16();
+      auto tile = [&](auto masked) {
+        floatx16_t s = zero16(), dp = zero16();
 #pragma unroll
-      for (int ks = 0; ks < R::KS; ++ks) {
-        mma(R::row_frag(buf, 32 * n, ks), q[ks], s);
-        mma(R::row_frag(buf + BN * R::ROW, 32 * n, ks), d[ks], dp);
-      }
-      const bool all = j0 + 32 <= kp.y && a.mask.sees_all(p0, p1, j0, j0 + 31);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -lse2)) * (dp[i] - delta);
-        if (!all) {
-          const int j = j0 + result_row(i);
-          s[i] = j < kp.y && a.mask.sees(p, j) ? s[i] : 0.0f;
+        for (int ks = 0; ks < R::KS; ++ks) {
+          mma(R::row_frag(buf, 32 * n, ks), q[ks], s);
+          mma(R::row_frag(buf + BN * R::ROW, 32 * n, ks), d[ks], dp);
         }
-      }
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const Frag<T> f = frag_of<T>(s, h);
+        for (int i = 0; i < 16; ++i) {
+          s[i] = prob<T>(s[i], c, lse) * (dp[i] - delta);
+          if constexpr (decltype(masked)::value) {
+            const int j = j0 + result_row(i);
+            s[i] = (j < kp.y) & a.mask.sees(p, j) ? s[i] : 0.0f;
+          }
+        }
 #pragma unroll
-        for (int i = 0; i < R::ND; ++i) mma(R::col_frag(buf, 32 * n + 16 * h, i), f, acc[i]);
+        for (int h = 0; h < 2; ++h) {
+          const Frag<T> f = frag_of<T>(s, h);
+#pragma unroll
+          for (int i = 0; i < R::ND; ++i) mma(R::col_frag(buf, 32 * n + 16 * h, i), f, acc[i]);
+        }
+      };
+      if (a.mask.sees_some(p0, p1, j0, j0 + 31)) {
+        if (j0 + 32 <= kp.y && a.mask.sees_all(p0, p1, j0, j0 + 31)) tile(std::false_type{});
+        else tile(std::true_type{});
       }
     }
     tile_sync();
   }
+  results_settle();
   if (in) {
     T* to = (T*)g.dq + row * g.lddq + head * a.dim;
 #pragma unroll
@@ -171,8 +189,7 @@ __global__ __launch_bounds__(256, 1) void k_attn_dkv(AttnArgs a, AttnGrads g, in
       next_lse = INFINITY;                                          // rows behind the sequence and tokens that see nothing: P = 0
       next_delta = 0.0f;
       if (i < valid) {
-        const float x = g.lse[from];
-        next_lse = x == -INFINITY ? INFINITY : x * kLog2e;
+        next_lse = prob_base<T>(g.lse[from]);
         next_delta = g.delta[from];
       }
     }
@@ -200,7 +217,7 @@ __global__ __launch_bounds__(256, 1) void k_attn_dkv(AttnArgs a, AttnGrads g, in
   floatx16_t dk[R::ND], dv[R::ND];
 #pragma unroll
   for (int i = 0; i < R::ND; ++i) dk[i] = dv[i] = zero16();
-  const float c = a.scale * kLog2e;
+  const float c = prob_factor<T>(a.scale);
   tile_sync();
   for (int t = 0; t < count; ++t) {
     const int b = t & 1;
@@ -210,40 +227,50 @@ __global__ __launch_bounds__(256, 1) void k_attn_dkv(AttnArgs a, AttnGrads g, in
 #pragma unroll
     for (int n = 0; n < BQ / 32; ++n) {
       const int p0 = i0 + 32 * n + shift, p1 = p0 + 31;
-      if (i0 + 32 * n >= qp.y || !a.mask.sees_some(p0, p1, k0, k0 + 31)) continue;
-      floatx16_t s = zero16(), dp = zero16();
+      auto tile = [&](auto masked) {
+        floatx16_t s = zero16(), dp = zero16();
 #pragma unroll
-      for (int ks = 0; ks < R::KS; ++ks) {
-        mma(R::row_frag(buf, 32 * n, ks), k[ks], s);
-        mma(R::row_frag(buf + BQ * R::ROW, 32 * n, ks), v[ks], dp);
-      }
-      const bool all = a.mask.sees_all(p0, p1, k0, k0 + 31);
-#pragma unroll
-      for (int i = 0; i < 16; i += 4) {
-        const float4 l4 = *(const float4*)&s_lse[b][32 * n + result_row(i)];
-        const float4 d4 = *(const float4*)&s_delta[b][32 * n + result_row(i)];
-        const float ls[4] = {l4.x, l4.y, l4.z, l4.w}, ds[4] = {d4.x, d4.y, d4.z, d4.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const bool seen = all || a.mask.sees(p0 + result_row(i + j), krow);
-          const float e = __builtin_amdgcn_exp2f(fmaf(s[i + j], c, -ls[j]));
-          s[i + j] = seen ? e : 0.0f;
-          dp[i + j] = seen ? e * (dp[i + j] - ds[j]) : 0.0f;
+        for (int ks = 0; ks < R::KS; ++ks) {
+          mma(R::row_frag(buf, 32 * n, ks), k[ks], s);
+          mma(R::row_frag(buf + BQ * R::ROW, 32 * n, ks), v[ks], dp);
         }
-      }
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const Frag<T> pf = frag_of<T>(s, h), df = frag_of<T>(dp, h);
+        for (int i = 0; i < 16; i += 4) {
+          const float4 l4 = *(const float4*)&s_lse[b][32 * n + result_row(i)];
+          const float4 d4 = *(const float4*)&s_delta[b][32 * n + result_row(i)];
+          const float ls[4] = {l4.x, l4.y, l4.z, l4.w}, ds[4] = {d4.x, d4.y, d4.z, d4.w};
 #pragma unroll
-        for (int i = 0; i < R::ND; ++i) {
-          mma(R::col_frag(buf + BQ * R::ROW, 32 * n + 16 * h, i), pf, dv[i]);
-          mma(R::col_frag(buf, 32 * n + 16 * h, i), df, dk[i]);
+          for (int j = 0; j < 4; ++j) {
+            const float e = prob<T>(s[i + j], c, ls[j]), f = e * (dp[i + j] - ds[j]);
+            if constexpr (decltype(masked)::value) {
+              const bool seen = a.mask.sees(p0 + result_row(i + j), krow);
+              s[i + j] = seen ? e : 0.0f;
+              dp[i + j] = seen ? f : 0.0f;
+            } else {
+              s[i + j] = e;
+              dp[i + j] = f;
+            }
+          }
         }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const Frag<T> pf = frag_of<T>(s, h), df = frag_of<T>(dp, h);
+#pragma unroll
+          for (int i = 0; i < R::ND; ++i) {
+            mma(R::col_frag(buf + BQ * R::ROW, 32 * n + 16 * h, i), pf, dv[i]);
+            mma(R::col_frag(buf, 32 * n + 16 * h, i), df, dk[i]);
+          }
+        }
+      };
+      if (i0 + 32 * n < qp.y && a.mask.sees_some(p0, p1, k0, k0 + 31)) {
+        if (a.mask.sees_all(p0, p1, k0, k0 + 31)) tile(std::false_type{});
+        else tile(std::true_type{});
       }
     }
     if (t + 1 < count) keep(b ^ 1);
     tile_sync();
   }
+  results_settle();
   if (in) {
     T* tk = (T*)g.dk + row * g.lddk + kvh * a.dim;
     T* tv = (T*)g.dv + row * g.lddv + kvh * a.dim;

@@ -19,8 +19,8 @@ constexpr int64_t kAttnMostRows = INT64_C(1) << 28;          // sums of three su
 struct AttnMask {
   int causal, window, sinks;
   __device__ __forceinline__ bool sees(int p, int j) const {
-    const int d = p - j;
-    return (!causal || d >= 0) & (!window || (d < window && -d < window) || j < sinks);
+    const int d = p - j;                             // no short cuts: no branch may lie between a product and what reads its result
+    return ((causal == 0) | (d >= 0)) & ((window == 0) | ((d < window) & (-d < window)) | (j < sinks));
   }
   // all of p0 .. p1 see all of j0 .. j1
   __device__ __forceinline__ bool sees_all(int p0, int p1, int j0, int j1) const {
@@ -225,9 +225,28 @@ __device__ __forceinline__ void tile_sync() {
 #endif
 }
 
+// A result of the matrix cores is there 19 wait states after the instruction, and the compiler counts them on one of the ways that lead
+// to a reader only (of a tile of 32 keys the last register was read too early behind a skipped branch).  So whatever reads results stands
+// in one block with the products, or behind this.
+__device__ __forceinline__ void results_settle() {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_nop 15\n\ts_nop 7" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+#endif
+}
+
 // the other half's value: lane l gets that of lane l ^ 32
 __device__ __forceinline__ float half_max(float v) { return fmaxf(v, __shfl_xor(v, 32, 64)); }
 __device__ __forceinline__ float half_sum(float v) { return v + __shfl_xor(v, 32, 64); }
+
+// the sum of a result's registers, pairs first
+__device__ __forceinline__ float sum16(const floatx16_t& c) {
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = c[2 * i] + c[2 * i + 1];
+  return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+}
 
 // four neighbouring elements of a result's column, as features of a row
 template <typename T>

@@ -209,6 +209,29 @@ def test_decode(kind, heads, kv, dim, window, sinks):
             # partial sums are put together with two more factors of exponentials each
             tol = 1.01 * u * np.abs(ref) + 1.01 * (p * (u + eta + eta.max() + (m + 8 + 32) * ck.E)) @ np.abs(V[g]) + 1e-30
             ck.within(O[h], ref, tol, f"sequence {s} head {h}")
+            if kind == "bf16":
+                ck.near(O[h], ref, u * np.sqrt(ref ** 2 + p ** 2 @ V[g] ** 2), (p * (eta + eta.max() + (m + 8 + 32) * ck.E)) @ np.abs(V[g]),
+                        f"sequence {s} head {h}")
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_every_key_has_its_weight(kind, dim):
+    """values that say which key they belong to, at every length of a last tile of 32, and at windows that begin anywhere in one"""
+    for n, window in [(64 + i, 0) for i in range(33)] + [(200, 100 + i) for i in range(33)]:
+        q, k = rand(n, 1, dim, kind, 2.0), rand(n + 1, n, dim, kind)
+        lo = n - window if window else 0
+        p = ao.attention_fwd(host(q), host(k), np.zeros((n, 1)), ao.default_scale(dim), ao.seen(1, n, True, window, 0))[2][0]
+        got = np.zeros(n)
+        for b in range(0, n, dim):
+            v = torch.zeros(n, dim, device="cuda", dtype=KINDS[kind])
+            m = min(dim, n - b)
+            v[torch.arange(b, b + m), torch.arange(m)] = 1
+            o = ef.attention_decode(q, k[None], v[None], torch.tensor([n], dtype=torch.int32, device="cuda"), 1, window=window)
+            got[b: b + m] = host(o)[0, :m]
+        # P and the result are rounded, the score is off by (dim + 8) 2^-24 of at most 40
+        u = 2 * ck.half_step(kind) + 2.0 ** -15
+        assert (got[:lo] == 0).all() and (np.abs(got - p) <= u * p).all(), (n, window, np.argmax(np.abs(got - p) / np.maximum(p, 1e-30)))
 
 
 def test_decode_cache_strides_and_one_sequence():

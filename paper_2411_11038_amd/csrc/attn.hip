@@ -12,17 +12,21 @@ namespace efqat {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f, kLn2Rest = -1.9046542999e-9f;      // ln 2 = kLn2 + kLn2Rest
 
-template <typename T>
-struct FwdTile {
-  static constexpr int BM = 128, BN = sizeof(T) == 2 ? 64 : 32;       // queries of a block, keys of a stage
-};
-
 // log of l exp2(m c), the sum that l stands for: m c as it was rounded where l was summed
 __device__ __forceinline__ float log_sum(float m, float c, float l) {
   const float base = m * c;
   return l == 0.0f ? -INFINITY : fmaf(base, kLn2, fmaf(base, kLn2Rest, kLn2 * __builtin_amdgcn_logf(l)));
 }
 
+template <int NT>
+__device__ __forceinline__ float max_of(const floatx16_t (&s)[NT]) {
+  float top = -INFINITY;
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
+  return top;
+}
 // scores of a wavefront's 32 queries (columns) against BN keys; what is not seen is -inf
 template <int NT>
 __device__ __forceinline__ void mask_scores(floatx16_t (&s)[NT], const AttnMask& m, int p, int j0, int end) {
@@ -31,116 +35,143 @@ __device__ __forceinline__ void mask_scores(floatx16_t (&s)[NT], const AttnMask&
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const int j = j0 + 32 * n + result_row(i);
-      s[n][i] = (j < end) & m.sees(p, j) ? s[n][i] : -INFINITY;
+      s[n][i] = ((j < end) & m.sees(p, j)) ? s[n][i] : -INFINITY;
     }
 }
 
-template <typename T, int DP>
-__global__ __launch_bounds__(256, sizeof(T) == 2 || DP == 64 ? 2 : 1) void k_attn_fwd(AttnArgs a, T* __restrict__ o, int64_t ldo, float* __restrict__ lse, int tiles) {
+// A block of NW wavefronts of 32 queries each: `hb` of the heads that share keys, 32 NW / hb queries of each, so that what is copied into
+// LDS serves 32 NW rows of scores.
+//
+// A lane's maximum is not followed exactly: l and o refer to the score m, which moves only where a score passes it by 8 / log2 e, so that
+// probabilities stay below 2^8 and the accumulators are hardly ever multiplied.
+template <typename T, int DP, int NW>
+__global__ __launch_bounds__(64 * NW, (kWideBlocks<T, DP> ? 2 : 1)) void k_attn_fwd(AttnArgs a, T* __restrict__ o, int64_t ldo,
+                                                                                         float* __restrict__ lse, int tiles, int hb) {
   using R = RowTile<T, DP>;
-  constexpr int BM = FwdTile<T>::BM, BN = FwdTile<T>::BN, NT = BN / 32, STAGE = 2 * BN * R::ROW;
-  __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
+  constexpr int BN = kKeyStage<T>, NT = BN / 32, TILE = BN * R::ROW;
+  __shared__ __attribute__((aligned(1024))) char smem[4 * TILE];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-
-  // blocks that share keys are neighbours, late tiles (the long ones under a causal mask) come first
-  const int id = xcd_contiguous_index(blockIdx.x, gridDim.x);
-  const int per_head = tiles * a.group, kvh = id / per_head, at = id - kvh * per_head;
-  const int head = kvh * a.group + at % a.group;
-  int seq, tile;
-  if (!find_tile(a.qs, BM, tiles - 1 - at / a.group, &seq, &tile)) return;
-  const int2 qp = a.qs.place(seq), kp = a.ks.place(seq);
-  const int shift = kp.y - qp.y, r0 = tile * BM + wave * 32, qrow = r0 + (lane & 31);
-  const int p = qrow + shift, rows = min(BM, qp.y - tile * BM);
-  const KeyTiles kt(a.mask, kp.y, tile * BM + shift, tile * BM + rows - 1 + shift, BN);
-
-  const char* kbase = (const char*)((const T*)a.k + (int64_t)kp.x * a.ldk + kvh * a.dim);
-  const char* vbase = (const char*)((const T*)a.v + (int64_t)kp.x * a.ldv + kvh * a.dim);
-  const int64_t ldk = a.ldk * (int)sizeof(T), ldv = a.ldv * (int)sizeof(T);
-  const int pieces = a.dim * (int)sizeof(T) / 16;
-  auto issue = [&](int t, char* buf) {
-    const int j0 = kt.tile(t) * BN, valid = kp.y - j0;
-#pragma unroll
-    for (int s = 0; s < BN / R::RPI / 4; ++s) R::copy(kbase + j0 * ldk, ldk, valid, pieces, buf, wave + 4 * s);
-#pragma unroll
-    for (int s = 0; s < BN / R::RPI / 4; ++s) R::copy(vbase + j0 * ldv, ldv, valid, pieces, buf + BN * R::ROW, wave + 4 * s);
-  };
+  HeadTile w;
+  if (!w.find(a, NW, hb, tiles, wave)) return;
+  const int p = w.row + (lane & 31) + w.shift;
+  const KeyTiles kt(a.mask, w.keys.y, w.block_row + w.shift, w.block_row + w.block_rows - 1 + w.shift, BN);
+  KeyCopies<T, DP, NW> copies(a, w.keys, w.kvh, wave);
 
   Frag<T> q[R::KS];
   {
-    const T* row = (const T*)a.q + (int64_t)(qp.x + qrow) * a.ldq + head * a.dim;
+    const T* row = (const T*)a.q + w.token(lane) * a.ldq + w.head * a.dim;
 #pragma unroll
     for (int ks = 0; ks < R::KS; ++ks) {
       const int d = 16 * ks + 8 * (lane >> 5);
-      q[ks] = load_frag(row + d, qrow < qp.y && d < a.dim);
+      q[ks] = load_frag(row + d, w.in(lane) && d < a.dim);
     }
   }
   floatx16_t acc[R::ND];
 #pragma unroll
   for (int i = 0; i < R::ND; ++i) acc[i] = zero16();
   float m = -INFINITY, l = 0.0f;
-  const float c = a.scale * kLog2e;
+  const float c = a.scale * kLog2e, slack = 8.0f / c;
 
-  if (kt.count > 0) issue(0, smem);
-  tile_sync();
-  for (int t = 0; t < kt.count; ++t) {
-    char* buf = smem + (t & 1) * STAGE;
-    if (t + 1 < kt.count) issue(t + 1, smem + ((t + 1) & 1) * STAGE);
-    const int j0 = kt.tile(t) * BN, p0 = r0 + shift, p1 = p0 + 31;
-    auto tile = [&](auto masked) {
-      floatx16_t s[NT];
+  // Keys are a tile ahead of values: while tile t's scores become probabilities, the scores of tile t + 1 are formed.  Two places in LDS for
+  // keys, two for values; what was copied during a step is there at its end.
+  char* const vals = smem + 2 * TILE;
+  float top = -INFINITY;
+  // scores of the tile whose keys lie at `keys`, and beside each product a share of tile t's probabilities, as operands of the next product
+  auto scores = [&](const char* keys, floatx16_t (&u)[NT], floatx16_t (&s)[NT], Frag<T> (&pf)[2 * NT], float base, auto both) {
+    constexpr int GROUPS = R::KS * NT, PER = 16 * NT / GROUPS;
+    Frag<T> kf[2][NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      u[n] = zero16();
+      kf[0][n] = R::row_frag(keys, 32 * n, 0);
+    }
+#pragma unroll
+    for (int ks = 0; ks < R::KS; ++ks)
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        s[n] = zero16();
+        if (ks + 1 < R::KS) kf[(ks + 1) & 1][n] = R::row_frag(keys, 32 * n, ks + 1);
+        mma(kf[ks & 1][n], q[ks], u[n]);
+        if constexpr (decltype(both)::value) {
 #pragma unroll
-        for (int ks = 0; ks < R::KS; ++ks) mma(R::row_frag(buf, 32 * n, ks), q[ks], s[n]);
+          for (int e = (ks * NT + n) * PER; e < (ks * NT + n + 1) * PER; ++e) {
+            s[e >> 4][e & 15] = __builtin_amdgcn_exp2f(fmaf(s[e >> 4][e & 15], c, -base));
+            if ((e & 7) == 7) {
+              l += sum8(s[e >> 4], (e >> 3) & 1);
+              pf[e >> 3] = frag_of<T>(s[e >> 4], (e >> 3) & 1);
+              hold(pf[e >> 3]);
+            }
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
-      if constexpr (decltype(masked)::value) mask_scores(s, a.mask, p, j0, kp.y);
-      float top = m;
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
-      top = half_max(top);
-      const float base = top == -INFINITY ? 0.0f : top * c;       // nothing seen so far: exp2(-inf) is 0 for all of it
-      const float shrink = __builtin_amdgcn_exp2f(fmaf(m, c, -base));
-      m = top;
+    top = max_of(u);
+    hold(top);                                       // all results are read here, before a branch
+  };
+  auto hide = [&](int t, floatx16_t (&u)[NT]) {
+    const int j0 = kt.tile(t) * BN, p0 = w.row + w.shift;
+    if (j0 + BN > w.keys.y || !a.mask.sees_all(p0, p0 + 31, j0, j0 + BN - 1)) {
+      mask_scores(u, a.mask, p, j0, w.keys.y);
+      top = max_of(u);
+    }
+  };
+  auto step = [&](int t, floatx16_t (&s)[NT], floatx16_t (&u)[NT]) {
+    if (t + 2 < kt.count) copies.issue_keys(kt.tile(t + 2), smem + (t & 1) * TILE, wave);
+    if (t + 1 < kt.count) copies.issue_values(kt.tile(t + 1), vals + ((t + 1) & 1) * TILE, wave);
+    top = half_max(top);
+    if (__any(top > m + slack)) {
+      results_settle();
+      const float next = fmaxf(m, top);
+      const float shrink = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - next) * c);
+      m = next;
+      l *= shrink;
 #pragma unroll
       for (int i = 0; i < R::ND; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[i][r] *= shrink;
-      float sum = 0.0f;
+    }
+    const float base = m == -INFINITY ? 0.0f : m * c;              // nothing seen so far: exp2(-inf) is 0 for all of it
+    Frag<T> pf[2 * NT];
+    scores(smem + ((t + 1) & 1) * TILE, u, s, pf, base, std::true_type{});      // behind the last tile: of what lies there, not used
+    if (t + 1 < kt.count) hide(t + 1, u);
+    // values are read a step ahead of the products that take them
+    const char* at = vals + (t & 1) * TILE;
+    Frag<T> v[2][R::ND];
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
+    for (int i = 0; i < R::ND; ++i) v[0][i] = R::col_frag(at, 0, i);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], c, -base));
-        sum += sum16(s[n]);
+    for (int x = 0; x < 2 * NT; ++x) {
+      if (x + 1 < 2 * NT) {
+#pragma unroll
+        for (int i = 0; i < R::ND; ++i) v[(x + 1) & 1][i] = R::col_frag(at, 16 * (x + 1), i);
       }
-      l = fmaf(l, shrink, sum);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const Frag<T> pf = frag_of<T>(s[n], h);
-#pragma unroll
-          for (int i = 0; i < R::ND; ++i) mma(R::col_frag(buf + BN * R::ROW, 32 * n + 16 * h, i), pf, acc[i]);
-        }
-    };
-    if (a.mask.sees_some(p0, p1, j0, j0 + BN - 1)) {
-      if (j0 + BN <= kp.y && a.mask.sees_all(p0, p1, j0, j0 + BN - 1)) tile(std::false_type{});
-      else tile(std::true_type{});
+      for (int i = 0; i < R::ND; ++i) mma(v[x & 1][i], pf[x], acc[i]);
     }
     tile_sync();
+  };
+  if (kt.count > 0) {
+    floatx16_t s[NT], u[NT];
+    Frag<T> none[2 * NT];
+    copies.issue_keys(kt.tile(0), smem, wave);
+    tile_sync();
+    if (kt.count > 1) copies.issue_keys(kt.tile(1), smem + TILE, wave);
+    copies.issue_values(kt.tile(0), vals, wave);
+    scores(smem, s, u, none, 0.0f, std::false_type{});
+    hide(0, s);
+    tile_sync();
+    for (int t = 0;; t += 2) {
+      step(t, s, u);
+      if (t + 1 >= kt.count) break;
+      step(t + 1, u, s);
+      if (t + 2 >= kt.count) break;
+    }
   }
   results_settle();
   l = half_sum(l);
-  if (qrow < qp.y) {
-    const int64_t row = (int64_t)qp.x + qrow;
-    const float f = l == 0.0f ? 0.0f : 1.0f / l;                   // a token that sees nothing: zeros
-    T* to = o + row * ldo + head * a.dim;
-#pragma unroll
-    for (int i = 0; i < R::ND; ++i) store_col(to, acc[i], i, a.dim, f);
-    if (lse && lane < 32) lse[(int64_t)head * a.qs.rows + row] = log_sum(m, c, l);
-  }
+  const float f = l == 0.0f ? 0.0f : 1.0f / l;                     // a token that sees nothing: zeros
+  store_rows<T, DP>(o + w.token(0) * ldo + w.head * a.dim, ldo, w.rows_left(), a.dim, acc, f, smem + wave * (sizeof(smem) / NW));
+  if (lse && lane < 32 && w.in(lane)) lse[(int64_t)w.head * a.qs.rows + w.token(lane)] = log_sum(m, c, l);
 }
 
 // ---- one new token a sequence
@@ -345,10 +376,15 @@ extern "C" int efqat_attention_fwd(const void* q, int64_t ldq, const void* k, in
   EFQAT_TRY(attn_args(&a, q, ldq, k, ldk, v, ldv, dtype, Tq, Tk, n_seq, q_start, k_start, heads, kv_heads, dim, scale, causal, window, sinks));
   EFQAT_TRY(attn_rows(o, ldo, heads * dim, dtype));
   if (!aligned4(lse)) return EFQAT_ERR_ALIGNMENT;
-  const int64_t tiles = a.qs.most_tiles(128), blocks = tiles * heads;
-  if (blocks > kAttnMostBlocks) return EFQAT_ERR_BAD_SHAPE;
+  const HeadPlan h = head_plan(a, kv_heads, dtype);
+  if (h.blocks > kAttnMostBlocks) return EFQAT_ERR_BAD_SHAPE;
   hipStream_t st = (hipStream_t)stream;
-#define EFQAT_FWD(E, DP) return launch(k_attn_fwd<E, DP>, dim3((unsigned)blocks), dim3(256), 0, st, a, (E*)o, ldo, lse, (int)tiles)
+#define EFQAT_FWD(E, DP)                                                                                                                \
+  do {                                                                                                                                  \
+    if constexpr (kWideBlocks<E, DP>)                                                                                                   \
+      if (h.waves == 8) return launch(k_attn_fwd<E, DP, 8>, dim3((unsigned)h.blocks), dim3(512), 0, st, a, (E*)o, ldo, lse, h.tiles, h.hb); \
+    return launch(k_attn_fwd<E, DP, 4>, dim3((unsigned)h.blocks), dim3(256), 0, st, a, (E*)o, ldo, lse, h.tiles, h.hb);                  \
+  } while (0)
   if (dtype == EFQAT_F32) { if (dim <= 64) EFQAT_FWD(float, 64); EFQAT_FWD(float, 128); }
   if (dim <= 64) EFQAT_FWD(bf16_t, 64);
   EFQAT_FWD(bf16_t, 128);

@@ -36,38 +36,22 @@ __device__ __forceinline__ float prob(float s, float c, float base) {
 template <typename T>
 __device__ __forceinline__ float prob_factor(float scale) { return sizeof(T) == 2 ? scale * kLog2e : scale; }
 
-// dq, and delta for the other kernel.  Blocks, tiles and layout as in k_attn_fwd.
-template <typename T, int DP>
-__global__ __launch_bounds__(256, 1) void k_attn_dq(AttnArgs a, AttnGrads g, int tiles) {
+// dq, and delta for the other kernel.  Blocks and layout as in k_attn_fwd.
+template <typename T, int DP, int NW>
+__global__ __launch_bounds__(64 * NW, (kWideBlocks<T, DP> ? 2 : 1)) void k_attn_dq(AttnArgs a, AttnGrads g, int tiles, int hb) {
   using R = RowTile<T, DP>;
-  constexpr int BM = 128, BN = sizeof(T) == 2 ? 64 : 32, STAGE = 2 * BN * R::ROW;
+  constexpr int BN = kKeyStage<T>, STAGE = 2 * BN * R::ROW;
   __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int id = xcd_contiguous_index(blockIdx.x, gridDim.x);
-  const int per_head = tiles * a.group, kvh = id / per_head, at = id - kvh * per_head;
-  const int head = kvh * a.group + at % a.group;
-  int seq, tile;
-  if (!find_tile(a.qs, BM, tiles - 1 - at / a.group, &seq, &tile)) return;
-  const int2 qp = a.qs.place(seq), kp = a.ks.place(seq);
-  const int shift = kp.y - qp.y, r0 = tile * BM + wave * 32, qrow = r0 + (lane & 31);
-  const int p = qrow + shift, rows = min(BM, qp.y - tile * BM);
-  const KeyTiles kt(a.mask, kp.y, tile * BM + shift, tile * BM + rows - 1 + shift, BN);
+  HeadTile w;
+  if (!w.find(a, NW, hb, tiles, wave)) return;
+  const int p = w.row + (lane & 31) + w.shift, head = w.head;
+  const KeyTiles kt(a.mask, w.keys.y, w.block_row + w.shift, w.block_row + w.block_rows - 1 + w.shift, BN);
+  KeyCopies<T, DP, NW> copies(a, w.keys, w.kvh, wave);
+  if (kt.count > 0) copies.issue(kt.tile(0), smem, wave);
 
-  const char* kbase = (const char*)((const T*)a.k + (int64_t)kp.x * a.ldk + kvh * a.dim);
-  const char* vbase = (const char*)((const T*)a.v + (int64_t)kp.x * a.ldv + kvh * a.dim);
-  const int64_t ldk = a.ldk * (int)sizeof(T), ldv = a.ldv * (int)sizeof(T);
-  const int pieces = a.dim * (int)sizeof(T) / 16;
-  auto issue = [&](int t, char* buf) {
-    const int j0 = kt.tile(t) * BN, valid = kp.y - j0;
-#pragma unroll
-    for (int s = 0; s < BN / R::RPI / 4; ++s) R::copy(kbase + j0 * ldk, ldk, valid, pieces, buf, wave + 4 * s);
-#pragma unroll
-    for (int s = 0; s < BN / R::RPI / 4; ++s) R::copy(vbase + j0 * ldv, ldv, valid, pieces, buf + BN * R::ROW, wave + 4 * s);
-  };
-  if (kt.count > 0) issue(0, smem);
-
-  const bool in = qrow < qp.y;
-  const int64_t row = (int64_t)qp.x + qrow;
+  const bool in = w.in(lane);
+  const int64_t row = w.token(lane);
   Frag<T> q[R::KS], d[R::KS];
   float delta = 0.0f, lse = INFINITY;
   {
@@ -97,8 +81,8 @@ __global__ __launch_bounds__(256, 1) void k_attn_dq(AttnArgs a, AttnGrads g, int
   tile_sync();
   for (int t = 0; t < kt.count; ++t) {
     char* buf = smem + (t & 1) * STAGE;
-    if (t + 1 < kt.count) issue(t + 1, smem + ((t + 1) & 1) * STAGE);
-    const int p0 = r0 + shift, p1 = p0 + 31;
+    if (t + 1 < kt.count) copies.issue(kt.tile(t + 1), smem + ((t + 1) & 1) * STAGE, wave);
+    const int p0 = w.row + w.shift, p1 = p0 + 31;
 #pragma unroll
     for (int n = 0; n < BN / 32; ++n) {
       const int j0 = kt.tile(t) * BN + 32 * n;
@@ -114,7 +98,7 @@ __global__ __launch_bounds__(256, 1) void k_attn_dq(AttnArgs a, AttnGrads g, int
           s[i] = prob<T>(s[i], c, lse) * (dp[i] - delta);
           if constexpr (decltype(masked)::value) {
             const int j = j0 + result_row(i);
-            s[i] = (j < kp.y) & a.mask.sees(p, j) ? s[i] : 0.0f;
+            s[i] = ((j < w.keys.y) & a.mask.sees(p, j)) ? s[i] : 0.0f;
           }
         }
 #pragma unroll
@@ -125,18 +109,14 @@ __global__ __launch_bounds__(256, 1) void k_attn_dq(AttnArgs a, AttnGrads g, int
         }
       };
       if (a.mask.sees_some(p0, p1, j0, j0 + 31)) {
-        if (j0 + 32 <= kp.y && a.mask.sees_all(p0, p1, j0, j0 + 31)) tile(std::false_type{});
+        if (j0 + 32 <= w.keys.y && a.mask.sees_all(p0, p1, j0, j0 + 31)) tile(std::false_type{});
         else tile(std::true_type{});
       }
     }
     tile_sync();
   }
   results_settle();
-  if (in) {
-    T* to = (T*)g.dq + row * g.lddq + head * a.dim;
-#pragma unroll
-    for (int i = 0; i < R::ND; ++i) store_col(to, acc[i], i, a.dim, a.scale);
-  }
+  store_rows<T, DP>((T*)g.dq + w.token(0) * g.lddq + head * a.dim, g.lddq, w.rows_left(), a.dim, acc, a.scale, smem + wave * (sizeof(smem) / NW));
 }
 
 // Queries first .. last - 1 of a sequence that see some of the keys j0 .. j1
@@ -306,13 +286,16 @@ extern "C" int efqat_attention_bwd(const void* dout, int64_t lddo, const void* q
   if (!lse || !ws) return EFQAT_ERR_NULL_PTR;
   if (!aligned4(lse) || (uintptr_t)ws % 256) return EFQAT_ERR_ALIGNMENT;
   if (ws_bytes < efqat_attention_bwd_workspace_bytes(Tq, heads)) return EFQAT_ERR_WORKSPACE;
-  const int64_t qt = a.qs.most_tiles(128), kt = a.ks.most_tiles(128);
-  if (qt * heads > kAttnMostBlocks || kt * kv_heads > kAttnMostBlocks) return EFQAT_ERR_BAD_SHAPE;
+  const HeadPlan h = head_plan(a, kv_heads, dtype);
+  const int64_t kt = a.ks.most_tiles(128);
+  if (h.blocks > kAttnMostBlocks || kt * kv_heads > kAttnMostBlocks) return EFQAT_ERR_BAD_SHAPE;
   const AttnGrads g = {dout, o, lddo, ldo, lse, (float*)ws, dq, dk, dv, lddq, lddk, lddv};
   hipStream_t st = (hipStream_t)stream;
 #define EFQAT_BWD(E, DP)                                                                                             \
   do {                                                                                                               \
-    EFQAT_TRY(launch(k_attn_dq<E, DP>, dim3((unsigned)(qt * heads)), dim3(256), 0, st, a, g, (int)qt));              \
+    if (h.waves == 8) {                                                                                              \
+      if constexpr (kWideBlocks<E, DP>) EFQAT_TRY(launch(k_attn_dq<E, DP, 8>, dim3((unsigned)h.blocks), dim3(512), 0, st, a, g, h.tiles, h.hb)); \
+    } else EFQAT_TRY(launch(k_attn_dq<E, DP, 4>, dim3((unsigned)h.blocks), dim3(256), 0, st, a, g, h.tiles, h.hb));    \
     return launch(k_attn_dkv<E, DP>, dim3((unsigned)(kt * kv_heads)), dim3(256), 0, st, a, g, (int)kt);              \
   } while (0)
   if (dtype == EFQAT_F32) { if (dim <= 64) EFQAT_BWD(float, 64); EFQAT_BWD(float, 128); }

@@ -121,6 +121,21 @@ __device__ __forceinline__ Frag<T> frag_of(const floatx16_t& c, int s) {
   }
   return f;
 }
+// made where this stands: the compiler may not move it behind a branch, nearer to where it is used
+__device__ __forceinline__ void hold(float& v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("" : "+v"(v));
+#endif
+}
+__device__ __forceinline__ void hold(Frag<bf16_t>& f) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("" : "+v"(f.v));
+#endif
+}
+__device__ __forceinline__ void hold(Frag<float>& f) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) hold(f.v[e]);
+}
 __device__ __forceinline__ floatx16_t zero16() {
   floatx16_t z;
 #pragma unroll
@@ -236,10 +251,29 @@ __device__ __forceinline__ void results_settle() {
 #endif
 }
 
-// the other half's value: lane l gets that of lane l ^ 32
-__device__ __forceinline__ float half_max(float v) { return fmaxf(v, __shfl_xor(v, 32, 64)); }
-__device__ __forceinline__ float half_sum(float v) { return v + __shfl_xor(v, 32, 64); }
+// a value and that of the other half of the wavefront, lane l ^ 32's
+__device__ __forceinline__ float2 halves(float v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return make_float2(__uint_as_float(r[0]), __uint_as_float(r[1]));
+#else
+  return make_float2(v, v);
+#endif
+}
+__device__ __forceinline__ float half_max(float v) {
+  const float2 h = halves(v);
+  return fmaxf(h.x, h.y);
+}
+__device__ __forceinline__ float half_sum(float v) {
+  const float2 h = halves(v);
+  return h.x + h.y;
+}
 
+// the sum of eight of a result's registers
+__device__ __forceinline__ float sum8(const floatx16_t& c, int half) {
+  const int i = 8 * half;
+  return ((c[i] + c[i + 1]) + (c[i + 2] + c[i + 3])) + ((c[i + 4] + c[i + 5]) + (c[i + 6] + c[i + 7]));
+}
 // the sum of a result's registers, pairs first
 __device__ __forceinline__ float sum16(const floatx16_t& c) {
   float v[8];
@@ -294,7 +328,6 @@ struct KeyTiles {
   __device__ __forceinline__ int tile(int t) const { return t < sink ? t : first + t - sink; }
 };
 
-// ---- host side
 struct AttnArgs {
   const void *q, *k, *v;
   int64_t ldq, ldk, ldv;
@@ -303,6 +336,127 @@ struct AttnArgs {
   AttnMask mask;
   float scale;
 };
+template <typename T>
+constexpr int kKeyStage = sizeof(T) == 2 ? 64 : 32;    // keys of a stage of LDS
+// eight wavefronts a block, two a SIMD: what they hold fits 256 registers
+template <typename T, int DP>
+constexpr bool kWideBlocks = sizeof(T) == 2 || DP == 64;
+
+// Rows of a wavefront in a block of `waves`, each with 32 queries of a head: hb heads that share keys, 32 waves / hb queries.
+// Blocks that share keys are neighbours, late tiles (the long ones under a causal mask) come first.
+struct HeadTile {
+  int2 queries, keys;                                // rows of the sequence: first, count
+  int kvh, head, shift, block_row, block_rows, row;  // row: the wavefront's first query
+  __device__ __forceinline__ bool find(const AttnArgs& a, int waves, int hb, int tiles, int wave) {
+    const int id = xcd_contiguous_index(blockIdx.x, gridDim.x);
+    const int groups = a.group / hb, per_head = tiles * groups, at = id % per_head, bq = 32 * waves / hb;
+    kvh = id / per_head;
+    head = kvh * a.group + at % groups * hb + wave % hb;
+    int seq, tile;
+    if (!find_tile(a.qs, bq, tiles - 1 - at / groups, &seq, &tile)) return false;
+    queries = a.qs.place(seq);
+    keys = a.ks.place(seq);
+    shift = keys.y - queries.y;
+    block_row = tile * bq;
+    block_rows = min(bq, queries.y - block_row);
+    row = block_row + wave / hb * 32;
+    return true;
+  }
+  __device__ __forceinline__ bool in(int lane) const { return row + (lane & 31) < queries.y; }
+  __device__ __forceinline__ int64_t token(int lane) const { return (int64_t)queries.x + row + (lane & 31); }
+  __device__ __forceinline__ int rows_left() const { return queries.y - row; }
+};
+
+// one copy of 16 bytes a lane (see dma16) from a base that the wavefront shares and an offset of the lane's own
+__device__ __forceinline__ void dma16_at(const char* base, uint32_t offset, char* lds_dst) {
+  const uint32_t m = (uint32_t)(uintptr_t)(lds_ptr_t)lds_dst;
+  asm volatile("s_mov_b32 m0, %0" ::"s"(m) : "m0");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base));
+}
+
+// Copies of ROWS rows of a matrix into a tile by NW wavefronts.  Rows that all exist, of DP features, less than 2^31 bytes apart in all: a
+// scalar address and a lane's offset, which stay the same from tile to tile.  Others choose between the row and zeros lane by lane.
+template <typename T, int DP, int NW, int ROWS>
+struct RowCopies {
+  using R = RowTile<T, DP>;
+  static constexpr int N = ROWS / R::RPI / NW;
+  static_assert(N * R::RPI * NW == ROWS, "whole copies");
+  int64_t ld;                                        // bytes
+  int pieces;
+  bool plain;
+  static constexpr bool SAME = NW * R::RPI % 16 == 0;           // the swizzle of a wavefront's copies: one offset serves all
+  uint32_t at[SAME ? 1 : N];
+  __device__ __forceinline__ RowCopies(int64_t ld_elements, int dim, int wave)
+      : ld(ld_elements * (int)sizeof(T)), pieces(dim * (int)sizeof(T) / 16), plain(dim == DP && ld * ROWS < (INT64_C(1) << 31)) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int s = 0; s < (SAME ? 1 : N); ++s) {
+      const int row = (wave + NW * s) * R::RPI + lane / R::CH;
+      at[s] = (uint32_t)(row * ld) + (((lane % R::CH) ^ R::swz(row)) << 4);
+    }
+  }
+  // base: the tile's first row, of which `valid` exist
+  __device__ __forceinline__ void issue(const char* base, int valid, char* lds, int wave) const {
+    if (plain && valid >= ROWS) {
+#pragma unroll
+      for (int s = 0; s < N; ++s) dma16_at(SAME ? base + s * NW * R::RPI * ld : base, at[SAME ? 0 : s], lds + (wave + NW * s) * 1024);
+    } else {
+#pragma unroll
+      for (int s = 0; s < N; ++s) R::copy(base, ld, valid, pieces, lds, wave + NW * s);
+    }
+  }
+};
+// of a stage's keys and values
+template <typename T, int DP, int NW>
+struct KeyCopies {
+  using R = RowTile<T, DP>;
+  static constexpr int BN = kKeyStage<T>;
+  const char *k, *v;
+  RowCopies<T, DP, NW, BN> ck, cv;
+  int keys;
+  __device__ __forceinline__ KeyCopies(const AttnArgs& a, int2 place, int kvh, int wave)
+      : k((const char*)((const T*)a.k + (int64_t)place.x * a.ldk + kvh * a.dim)), v((const char*)((const T*)a.v + (int64_t)place.x * a.ldv + kvh * a.dim)),
+        ck(a.ldk, a.dim, wave), cv(a.ldv, a.dim, wave), keys(place.y) {}
+  __device__ __forceinline__ void issue_keys(int tile, char* buf, int wave) const { ck.issue(k + tile * BN * ck.ld, keys - tile * BN, buf, wave); }
+  __device__ __forceinline__ void issue_values(int tile, char* buf, int wave) const { cv.issue(v + tile * BN * cv.ld, keys - tile * BN, buf, wave); }
+  __device__ __forceinline__ void issue(int tile, char* buf, int wave) const {
+    issue_keys(tile, buf, wave);
+    issue_values(tile, buf + BN * R::ROW, wave);
+  }
+};
+
+// A wavefront's 32 tokens (columns) of DP features times f, `rows` of them, into rows of memory.  bf16: through its own 8 (4) KB of LDS, so that
+// 16 bytes of a row leave at once and neighbouring lanes write neighbouring pieces; fp32: four features are 16 bytes as they are.
+template <typename T, int DP>
+__device__ __forceinline__ void store_rows(T* to, int64_t ld, int rows, int dim, const floatx16_t (&acc)[DP / 32], float f, char* lds) {
+  const int lane = threadIdx.x & 63;
+  if constexpr (sizeof(T) == 4) {
+    if ((lane & 31) < rows) {
+#pragma unroll
+      for (int i = 0; i < DP / 32; ++i) store_col(to + (lane & 31) * ld, acc[i], i, dim, f);
+    }
+  } else {
+    constexpr int CH = DP / 8;
+    const int r = lane & 31;
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+      for (int x = 0; x < 16; x += 4) {
+        const int d = 32 * i + result_row(x);          // four features: half a piece
+        store4((T*)(lds + r * DP * 2 + (((d >> 3) ^ (r & (CH - 1))) << 4) + 2 * (d & 7)), acc[i][x] * f, acc[i][x + 1] * f, acc[i][x + 2] * f, acc[i][x + 3] * f);
+      }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int s = 0; s < 32 * CH / 64; ++s) {
+      const int row = s * (64 / CH) + lane / CH, piece = lane % CH;
+      const uint4 v = *(const uint4*)(lds + row * DP * 2 + ((piece ^ (row & (CH - 1))) << 4));
+      if (row < rows && piece * 8 < dim) *(uint4*)(to + row * ld + piece * 8) = v;
+    }
+  }
+}
+
+// ---- host side
 constexpr int64_t kAttnMostBlocks = (1 << 24) - 1;    // of 256 lanes: a grid has fewer than 2^32
 // rows of heads: at least `cols` wide, in whole 16 bytes from a 16-byte aligned address
 inline int attn_rows(const void* p, int64_t ld, int64_t cols, int dtype) {
@@ -330,6 +484,22 @@ inline int attn_args(AttnArgs* a, const void* q, int64_t ldq, const void* k, int
   *a = {q, k, v, ldq, ldk, ldv, {q_start, (int)Tq, (int)n_seq}, {k_start, (int)Tk, (int)n_seq}, (int)heads, (int)(heads / kv_heads), (int)dim,
         {causal, window >= far ? 0 : (int)window, sinks >= far ? (int)far : (int)sinks}, scale};
   return EFQAT_OK;
+}
+
+// Blocks of the kernels that walk keys: eight wavefronts, whose 256 rows halve what L2 delivers, where these fill the chip; else four.
+struct HeadPlan {
+  int waves, hb, tiles;
+  int64_t blocks;
+};
+inline HeadPlan head_plan(const AttnArgs& a, int64_t kv_heads, int dtype) {
+  HeadPlan h;
+  for (int waves = 4;; waves = 4) {
+    int hb = 1;
+    while (hb < waves && a.group % (2 * hb) == 0) hb *= 2;
+    const int64_t tiles = a.qs.most_tiles(32 * waves / hb);
+    h = {waves, hb, (int)tiles, tiles * (a.group / hb) * kv_heads};
+    if (waves == 4 || h.blocks >= 512) return h;
+  }
 }
 
 }  // namespace efqat

@@ -517,6 +517,7 @@ int efqat_head_norm_rope_bwd(const void* dyq, int64_t lddyq, const void* dyk, in
  *                nor written
  *   window       0: no window; sinks: first keys that stay visible beside a window
  *   lse          float [heads][Tq]; forward: out, nullable.  Backward: in, with o, as the forward left them
+ *   packed       of the workspace query: whether offsets will be given (0 or 1)
  * Scores, their maxima and sums, and all accumulators are fp32.  With BF16 the probabilities and dS are rounded to bf16 for the
  * matrix cores (their sum is taken before); with F32 the products are fp32 too.  Sums have a fixed order (bit-reproducible).  A key or
  * value in a sequence that is not finite may make undefined what tokens of that sequence and head hold that do not see it; other sequences
@@ -525,7 +526,8 @@ int efqat_attention_fwd(const void* q, int64_t ldq, const void* k, int64_t ldk, 
                         int64_t Tk, int64_t n_seq, const int32_t* q_start, const int32_t* k_start, int64_t heads, int64_t kv_heads,
                         int64_t dim, float scale, int causal, int64_t window, int64_t sinks, void* o, int64_t ldo, float* lse,
                         void* stream);
-size_t efqat_attention_bwd_workspace_bytes(int64_t Tq, int64_t heads);
+size_t efqat_attention_bwd_workspace_bytes(int64_t Tq, int64_t Tk, int64_t n_seq, int packed, int64_t heads, int64_t kv_heads,
+                                           int64_t dim, int dtype, int causal, int64_t window, int64_t sinks);
 int efqat_attention_bwd(const void* dout, int64_t lddo, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v,
                         int64_t ldv, const void* o, int64_t ldo, const float* lse, int dtype, int64_t Tq, int64_t Tk, int64_t n_seq,
                         const int32_t* q_start, const int32_t* k_start, int64_t heads, int64_t kv_heads, int64_t dim, float scale,

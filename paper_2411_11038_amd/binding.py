@@ -174,7 +174,7 @@ def lib():
     L.efqat_attention_fwd.restype = ci
     L.efqat_attention_fwd.argtypes = [vp, i64] * 3 + attn + [vp, i64, vp, vp]
     L.efqat_attention_bwd_workspace_bytes.restype = sz
-    L.efqat_attention_bwd_workspace_bytes.argtypes = [i64, i64]
+    L.efqat_attention_bwd_workspace_bytes.argtypes = [i64, i64, i64, ci, i64, i64, i64, ci, ci, i64, i64]
     L.efqat_attention_bwd.restype = ci
     L.efqat_attention_bwd.argtypes = [vp, i64] * 5 + [vp] + attn + [vp, i64] * 3 + [vp, sz, vp]
     L.efqat_attention_decode_workspace_bytes.restype = sz

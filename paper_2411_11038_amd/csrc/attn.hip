@@ -30,32 +30,33 @@ __device__ __forceinline__ float max_of(const floatx16_t (&s)[NT]) {
 // scores of a wavefront's 32 queries (columns) against BN keys; what is not seen is -inf
 template <int NT>
 __device__ __forceinline__ void mask_scores(floatx16_t (&s)[NT], const AttnMask& m, int p, int j0, int end) {
+  j0 += row_here();
 #pragma unroll
   for (int n = 0; n < NT; ++n)
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const int j = j0 + 32 * n + result_row(i);
+      const int j = j0 + 32 * n + row_of(i);
       s[n][i] = ((j < end) & m.sees(p, j)) ? s[n][i] : -INFINITY;
     }
 }
 
-// A block of NW wavefronts of 32 queries each: `hb` of the heads that share keys, 32 NW / hb queries of each, so that what is copied into
-// LDS serves 32 NW rows of scores.
+// A block takes 128 rows of scores: `hb` of the heads that share keys, 128 / hb queries of each.  (256 rows halve what L2 delivers, but
+// their eight wavefronts wait for each other: no faster at 32768 tokens, a third slower at 384.)
 //
 // A lane's maximum is not followed exactly: l and o refer to the score m, which moves only where a score passes it by 8 / log2 e, so that
 // probabilities stay below 2^8 and the accumulators are hardly ever multiplied.
-template <typename T, int DP, int NW>
-__global__ __launch_bounds__(64 * NW, (kWideBlocks<T, DP> ? 2 : 1)) void k_attn_fwd(AttnArgs a, T* __restrict__ o, int64_t ldo,
+template <typename T, int DP>
+__global__ __launch_bounds__(256, (kTwoWaves<T, DP> ? 2 : 1)) void k_attn_fwd(AttnArgs a, T* __restrict__ o, int64_t ldo,
                                                                                          float* __restrict__ lse, int tiles, int hb) {
   using R = RowTile<T, DP>;
   constexpr int BN = kKeyStage<T>, NT = BN / 32, TILE = BN * R::ROW;
   __shared__ __attribute__((aligned(1024))) char smem[4 * TILE];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   HeadTile w;
-  if (!w.find(a, NW, hb, tiles, wave)) return;
+  if (!w.find(a, hb, tiles, wave)) return;
   const int p = w.row + (lane & 31) + w.shift;
   const KeyTiles kt(a.mask, w.keys.y, w.block_row + w.shift, w.block_row + w.block_rows - 1 + w.shift, BN);
-  KeyCopies<T, DP, NW> copies(a, w.keys, w.kvh, wave);
+  KeyCopies<T, DP, BN> copies(a, w.keys, w.kvh, wave);
 
   Frag<T> q[R::KS];
   {
@@ -170,7 +171,7 @@ __global__ __launch_bounds__(64 * NW, (kWideBlocks<T, DP> ? 2 : 1)) void k_attn_
   results_settle();
   l = half_sum(l);
   const float f = l == 0.0f ? 0.0f : 1.0f / l;                     // a token that sees nothing: zeros
-  store_rows<T, DP>(o + w.token(0) * ldo + w.head * a.dim, ldo, w.rows_left(), a.dim, acc, f, smem + wave * (sizeof(smem) / NW));
+  store_rows<T, DP>(o + w.token(0) * ldo + w.head * a.dim, ldo, w.rows_left(), a.dim, acc, f, smem + wave * (sizeof(smem) / kWaves));
   if (lse && lane < 32 && w.in(lane)) lse[(int64_t)w.head * a.qs.rows + w.token(lane)] = log_sum(m, c, l);
 }
 
@@ -376,15 +377,10 @@ extern "C" int efqat_attention_fwd(const void* q, int64_t ldq, const void* k, in
   EFQAT_TRY(attn_args(&a, q, ldq, k, ldk, v, ldv, dtype, Tq, Tk, n_seq, q_start, k_start, heads, kv_heads, dim, scale, causal, window, sinks));
   EFQAT_TRY(attn_rows(o, ldo, heads * dim, dtype));
   if (!aligned4(lse)) return EFQAT_ERR_ALIGNMENT;
-  const HeadPlan h = head_plan(a, kv_heads, dtype);
+  const HeadPlan h = head_plan(a, kv_heads);
   if (h.blocks > kAttnMostBlocks) return EFQAT_ERR_BAD_SHAPE;
   hipStream_t st = (hipStream_t)stream;
-#define EFQAT_FWD(E, DP)                                                                                                                \
-  do {                                                                                                                                  \
-    if constexpr (kWideBlocks<E, DP>)                                                                                                   \
-      if (h.waves == 8) return launch(k_attn_fwd<E, DP, 8>, dim3((unsigned)h.blocks), dim3(512), 0, st, a, (E*)o, ldo, lse, h.tiles, h.hb); \
-    return launch(k_attn_fwd<E, DP, 4>, dim3((unsigned)h.blocks), dim3(256), 0, st, a, (E*)o, ldo, lse, h.tiles, h.hb);                  \
-  } while (0)
+#define EFQAT_FWD(E, DP) return launch(k_attn_fwd<E, DP>, dim3((unsigned)h.blocks), dim3(256), 0, st, a, (E*)o, ldo, lse, h.tiles, h.hb)
   if (dtype == EFQAT_F32) { if (dim <= 64) EFQAT_FWD(float, 64); EFQAT_FWD(float, 128); }
   if (dim <= 64) EFQAT_FWD(bf16_t, 64);
   EFQAT_FWD(bf16_t, 128);

@@ -36,18 +36,39 @@ __device__ __forceinline__ float prob(float s, float c, float base) {
 template <typename T>
 __device__ __forceinline__ float prob_factor(float scale) { return sizeof(T) == 2 ? scale * kLog2e : scale; }
 
-// dq, and delta for the other kernel.  Blocks and layout as in k_attn_fwd.
-template <typename T, int DP, int NW>
-__global__ __launch_bounds__(64 * NW, (kWideBlocks<T, DP> ? 2 : 1)) void k_attn_dq(AttnArgs a, AttnGrads g, int tiles, int hb) {
+// What k_attn_dkv does with 32 x 32 scores: P and dS, whose results S and dP are, as operands of the sums, a share of 16 / GROUPS elements
+// beside each of the GROUPS products that are formed meanwhile.  rows(i) says what lse and delta register i has.
+template <typename T, int GROUPS, class Rows>
+__device__ __forceinline__ void grads_of(int group, floatx16_t& s, floatx16_t& dp, float c, Frag<T> (&pf)[2], Frag<T> (&df)[2], const Rows& rows) {
+  constexpr int PER = 16 / GROUPS;
+#pragma unroll
+  for (int i = group * PER; i < (group + 1) * PER; ++i) {
+    const float2 r = rows(i);
+    const float e = prob<T>(s[i], c, r.x);
+    dp[i] = e * (dp[i] - r.y);
+    s[i] = e;
+    if ((i & 7) == 7) {
+      pf[i >> 3] = frag_of<T>(s, i >> 3);
+      hold(pf[i >> 3]);
+      df[i >> 3] = frag_of<T>(dp, i >> 3);
+      hold(df[i >> 3]);
+    }
+  }
+}
+
+// dq, and delta for the other kernel.  Blocks as in k_attn_fwd.  (Forming the next 32 keys' scores beside dS, as the other kernels do, needs
+// more registers than two wavefronts a SIMD have: 380 instead of 250 us for a window of 1024 in 2 x 4096 tokens, 32 heads of 128.)
+template <typename T, int DP>
+__global__ __launch_bounds__(256, (kTwoWaves<T, DP> ? 2 : 1)) void k_attn_dq(AttnArgs a, AttnGrads g, int tiles, int hb) {
   using R = RowTile<T, DP>;
   constexpr int BN = kKeyStage<T>, STAGE = 2 * BN * R::ROW;
   __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   HeadTile w;
-  if (!w.find(a, NW, hb, tiles, wave)) return;
+  if (!w.find(a, hb, tiles, wave)) return;
   const int p = w.row + (lane & 31) + w.shift, head = w.head;
   const KeyTiles kt(a.mask, w.keys.y, w.block_row + w.shift, w.block_row + w.block_rows - 1 + w.shift, BN);
-  KeyCopies<T, DP, NW> copies(a, w.keys, w.kvh, wave);
+  KeyCopies<T, DP, BN> copies(a, w.keys, w.kvh, wave);
   if (kt.count > 0) copies.issue(kt.tile(0), smem, wave);
 
   const bool in = w.in(lane);
@@ -93,11 +114,12 @@ __global__ __launch_bounds__(64 * NW, (kWideBlocks<T, DP> ? 2 : 1)) void k_attn_
           mma(R::row_frag(buf, 32 * n, ks), q[ks], s);
           mma(R::row_frag(buf + BN * R::ROW, 32 * n, ks), d[ks], dp);
         }
+        const int first = j0 + row_here();
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           s[i] = prob<T>(s[i], c, lse) * (dp[i] - delta);
           if constexpr (decltype(masked)::value) {
-            const int j = j0 + result_row(i);
+            const int j = first + row_of(i);
             s[i] = ((j < w.keys.y) & a.mask.sees(p, j)) ? s[i] : 0.0f;
           }
         }
@@ -116,15 +138,15 @@ __global__ __launch_bounds__(64 * NW, (kWideBlocks<T, DP> ? 2 : 1)) void k_attn_
     tile_sync();
   }
   results_settle();
-  store_rows<T, DP>((T*)g.dq + w.token(0) * g.lddq + head * a.dim, g.lddq, w.rows_left(), a.dim, acc, a.scale, smem + wave * (sizeof(smem) / NW));
+  store_rows<T, DP>((T*)g.dq + w.token(0) * g.lddq + head * a.dim, g.lddq, w.rows_left(), a.dim, acc, a.scale, smem + wave * (sizeof(smem) / kWaves));
 }
 
-// Queries first .. last - 1 of a sequence that see some of the keys j0 .. j1
+// Queries first .. last - 1 of a sequence that see some of the keys j0 .. j1; near: those that do beside what sinks add
 struct QuerySpan {
   int first, last;
-  __device__ __forceinline__ QuerySpan(const AttnMask& m, int queries, int shift, int j0, int j1) {
+  __device__ __forceinline__ QuerySpan(const AttnMask& m, bool near, int queries, int shift, int j0, int j1) {
     int lo = m.causal ? j0 - shift : 0, hi = queries;
-    if (m.window && j0 >= m.sinks) {
+    if (m.window && (near || j0 >= m.sinks)) {
       const int past = j1 + m.window - shift, before = j0 - m.window + 1 - shift;
       hi = past < hi ? past : hi;
       lo = before > lo ? before : lo;
@@ -134,35 +156,76 @@ struct QuerySpan {
   }
 };
 
-// dk and dv of 128 keys, 32 a wavefront: scores with queries as rows and keys as columns, so that P and dS are operands of the sums over
-// the queries where they are.
-template <typename T, int DP>
-__global__ __launch_bounds__(256, 1) void k_attn_dkv(AttnArgs a, AttnGrads g, int tiles) {
-  using R = RowTile<T, DP>;
-  constexpr int BM = 128, BQ = sizeof(T) == 2 ? 64 : 32, STAGE = 2 * BQ * R::ROW;
-  __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
-  __shared__ __attribute__((aligned(16))) float s_lse[2][BQ], s_delta[2][BQ];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int id = xcd_contiguous_index(blockIdx.x, gridDim.x);
-  const int kvh = id / tiles;
-  int seq, tile;
-  if (!find_tile(a.ks, BM, id - kvh * tiles, &seq, &tile)) return;
-  const int2 qp = a.qs.place(seq), kp = a.ks.place(seq);
-  const int shift = kp.y - qp.y, k0 = tile * BM + wave * 32, krow = k0 + (lane & 31);
-  const QuerySpan span(a.mask, qp.y, shift, tile * BM, min(tile * BM + BM, kp.y) - 1);
-  const int nq = span.last > span.first ? (span.last - span.first + BQ - 1) / BQ : 0, count = nq * a.group;
+// How the work of dk and dv is cut.  `parts` blocks share a tile of 128 keys where there are few tiles.  Keys that stay visible beside a window
+// have the queries of the whole sequence behind them, which one block would walk long after the others have ended: what lies outside their
+// window is the work of `far` blocks of its own.  Parts leave fp32 sums in the workspace, which k_attn_dkv_join adds in their order.
+struct KeyPlan {
+  int tiles, parts, far, sink_tiles;
+  int64_t near_blocks, far_blocks, slots;            // slots: sums of a block in the workspace
+};
+constexpr int kKeyRows = 128;
+// sums of a block of (tile, head) and part; far parts and, where tiles are not cut, the near part of a tile with sinks lie behind them
+__host__ __device__ inline int64_t near_slot(const KeyPlan& k, int64_t block) { return k.parts > 1 ? block : 0; }
+__host__ __device__ inline int64_t far_slot(const KeyPlan& k, int kv_heads, int seq, int tile, int kvh, int part) {
+  return (k.parts > 1 ? k.near_blocks : 0) + (((int64_t)seq * k.sink_tiles + tile) * kv_heads + kvh) * (k.far + 1) + part;
+}
 
-  const int64_t ldq = a.ldq * (int)sizeof(T), lddo = g.lddo * (int)sizeof(T);
-  const int pieces = a.dim * (int)sizeof(T) / 16;
+// dk and dv of 128 keys, 32 a wavefront: scores with queries as rows and keys as columns, so that P and dS are operands of the sums over
+// the queries where they are.  A ring of three stages of queries and their gradients, walked in steps of 32 rows; beside the products that form
+// a step's scores and dP stands the arithmetic of the step before.
+template <typename T, int DP>
+__global__ __launch_bounds__(256, (sizeof(T) == 2 && DP == 64 ? 2 : 1)) void k_attn_dkv(AttnArgs a, AttnGrads g, KeyPlan plan, float* __restrict__ sums) {
+  using R = RowTile<T, DP>;
+  constexpr int BQ = sizeof(T) == 2 ? 64 : 32, NQ = BQ / 32, TILE = BQ * R::ROW, STAGE = 2 * TILE;
+  __shared__ __attribute__((aligned(1024))) char smem[3 * STAGE];
+  __shared__ __attribute__((aligned(16))) float s_lse[3][BQ], s_delta[3][BQ];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kv_heads = a.heads / a.group;
+  const bool far = blockIdx.x >= plan.near_blocks;                   // short ones, behind the others: they even out the end
+  int seq, tile, kvh, part;
+  int64_t slot;
+  if (far) {
+    int id = blockIdx.x - (int)plan.near_blocks;
+    part = id % plan.far;
+    id /= plan.far;
+    kvh = id % kv_heads;
+    id /= kv_heads;
+    tile = id % plan.sink_tiles;
+    seq = id / plan.sink_tiles;
+    slot = far_slot(plan, kv_heads, seq, tile, kvh, part + 1);
+  } else {
+    const int id = xcd_contiguous_index(blockIdx.x, (int)plan.near_blocks);
+    const int per_head = plan.tiles * plan.parts, at = id % per_head;
+    kvh = id / per_head;
+    part = at % plan.parts;
+    if (!find_tile(a.ks, kKeyRows, at / plan.parts, &seq, &tile)) return;
+    slot = near_slot(plan, id);
+  }
+  const int2 qp = a.qs.place(seq), kp = a.ks.place(seq);
+  if (tile * kKeyRows >= kp.y) return;
+  const bool near = plan.far > 0;                                    // what sinks add is not this block's, or all that is
+  const int shift = kp.y - qp.y, k0 = tile * kKeyRows + wave * 32, krow = k0 + (lane & 31);
+  const QuerySpan span(a.mask, near && !far, qp.y, shift, tile * kKeyRows, min(tile * kKeyRows + kKeyRows, kp.y) - 1);
+  const int nq = span.last > span.first ? (span.last - span.first + BQ - 1) / BQ : 0;
+  const int cuts = far ? plan.far : plan.parts;
+  const int begin = (int)((int64_t)nq * a.group * part / cuts), count = (int)((int64_t)nq * a.group * (part + 1) / cuts) - begin;
+  // which pairs count: all that see each other; without sinks; sinks outside the window alone
+  AttnMask mask = a.mask;
+  if (near && !far) mask.sinks = 0;
+  const AttnMask window_alone = {0, a.mask.window, 0};
+  auto seen = [&](int p, int j) {
+    const bool yes = mask.sees(p, j);
+    return (bool)((int)yes & ((int)!far | ((int)(j < mask.sinks) & (int)!window_alone.sees(p, j))));
+  };
+  auto all = [&](int p0) { return !far && mask.sees_all(p0, p0 + 31, k0, k0 + 31); };
+
+  RowCopies<T, DP, BQ> cq(a.ldq, a.dim, wave), cd(g.lddo, a.dim, wave);
   float next_lse = 0.0f, next_delta = 0.0f;
+  auto first_row = [&](int t) { return span.first + (begin + t) % nq * BQ; };
   auto issue = [&](int t, char* buf) {
-    const int head = kvh * a.group + t / nq, i0 = span.first + (t % nq) * BQ, valid = qp.y - i0;
-    const char* qbase = (const char*)((const T*)a.q + (int64_t)(qp.x + i0) * a.ldq + head * a.dim);
-    const char* dbase = (const char*)((const T*)g.dout + (int64_t)(qp.x + i0) * g.lddo + head * a.dim);
-#pragma unroll
-    for (int s = 0; s < BQ / R::RPI / 4; ++s) R::copy(qbase, ldq, valid, pieces, buf, wave + 4 * s);
-#pragma unroll
-    for (int s = 0; s < BQ / R::RPI / 4; ++s) R::copy(dbase, lddo, valid, pieces, buf + BQ * R::ROW, wave + 4 * s);
+    const int head = kvh * a.group + (begin + t) / nq, i0 = first_row(t), valid = qp.y - i0;
+    cq.issue((const char*)((const T*)a.q + (int64_t)(qp.x + i0) * a.ldq + head * a.dim), valid, buf, wave);
+    cd.issue((const char*)((const T*)g.dout + (int64_t)(qp.x + i0) * g.lddo + head * a.dim), valid, buf + TILE, wave);
     if (threadIdx.x < BQ) {
       const int i = threadIdx.x;
       const int64_t from = (int64_t)head * a.qs.rows + qp.x + i0 + i;
@@ -184,6 +247,10 @@ __global__ __launch_bounds__(256, 1) void k_attn_dkv(AttnArgs a, AttnGrads g, in
     issue(0, smem);
     keep(0);
   }
+  if (count > 1) {
+    issue(1, smem + STAGE);
+    keep(1);
+  }
 
   const bool in = krow < kp.y;
   const int64_t row = (int64_t)kp.x + krow;
@@ -198,77 +265,199 @@ __global__ __launch_bounds__(256, 1) void k_attn_dkv(AttnArgs a, AttnGrads g, in
 #pragma unroll
   for (int i = 0; i < R::ND; ++i) dk[i] = dv[i] = zero16();
   const float c = prob_factor<T>(a.scale);
-  tile_sync();
-  for (int t = 0; t < count; ++t) {
-    const int b = t & 1;
-    char* buf = smem + b * STAGE;
-    if (t + 1 < count) issue(t + 1, smem + (b ^ 1) * STAGE);
-    const int i0 = span.first + (t % nq) * BQ;
+
+  // scores and dP of the 32 rows at `at`, and beside them P and dS of the rows before, whose lse and delta lie at l and e
+  auto scores = [&](const char* at, floatx16_t& u, floatx16_t& up, floatx16_t& s, floatx16_t& dp, Frag<T> (&pf)[2], Frag<T> (&df)[2], const float* l,
+                    const float* e, auto both) {
+    float4 l4[4], e4[4];
+    if constexpr (decltype(both)::value) {
 #pragma unroll
-    for (int n = 0; n < BQ / 32; ++n) {
-      const int p0 = i0 + 32 * n + shift, p1 = p0 + 31;
-      auto tile = [&](auto masked) {
-        floatx16_t s = zero16(), dp = zero16();
-#pragma unroll
-        for (int ks = 0; ks < R::KS; ++ks) {
-          mma(R::row_frag(buf, 32 * n, ks), k[ks], s);
-          mma(R::row_frag(buf + BQ * R::ROW, 32 * n, ks), v[ks], dp);
-        }
-#pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-          const float4 l4 = *(const float4*)&s_lse[b][32 * n + result_row(i)];
-          const float4 d4 = *(const float4*)&s_delta[b][32 * n + result_row(i)];
-          const float ls[4] = {l4.x, l4.y, l4.z, l4.w}, ds[4] = {d4.x, d4.y, d4.z, d4.w};
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float e = prob<T>(s[i + j], c, ls[j]), f = e * (dp[i + j] - ds[j]);
-            if constexpr (decltype(masked)::value) {
-              const bool seen = a.mask.sees(p0 + result_row(i + j), krow);
-              s[i + j] = seen ? e : 0.0f;
-              dp[i + j] = seen ? f : 0.0f;
-            } else {
-              s[i + j] = e;
-              dp[i + j] = f;
-            }
-          }
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const Frag<T> pf = frag_of<T>(s, h), df = frag_of<T>(dp, h);
-#pragma unroll
-          for (int i = 0; i < R::ND; ++i) {
-            mma(R::col_frag(buf + BQ * R::ROW, 32 * n + 16 * h, i), pf, dv[i]);
-            mma(R::col_frag(buf, 32 * n + 16 * h, i), df, dk[i]);
-          }
-        }
-      };
-      if (i0 + 32 * n < qp.y && a.mask.sees_some(p0, p1, k0, k0 + 31)) {
-        if (a.mask.sees_all(p0, p1, k0, k0 + 31)) tile(std::false_type{});
-        else tile(std::true_type{});
+      for (int i = 0; i < 4; ++i) {
+        l4[i] = *(const float4*)(l + result_row(4 * i));
+        e4[i] = *(const float4*)(e + result_row(4 * i));
       }
     }
-    if (t + 1 < count) keep(b ^ 1);
-    tile_sync();
-  }
-  results_settle();
-  if (in) {
-    T* tk = (T*)g.dk + row * g.lddk + kvh * a.dim;
-    T* tv = (T*)g.dv + row * g.lddv + kvh * a.dim;
+    const auto rows = [&](int i) {
+      const float4 x = l4[i >> 2], y = e4[i >> 2];
+      switch (i & 3) {
+        case 0: return make_float2(x.x, y.x);
+        case 1: return make_float2(x.y, y.y);
+        case 2: return make_float2(x.z, y.z);
+        default: return make_float2(x.w, y.w);
+      }
+    };
+    Frag<T> qf[2], of[2];
+    u = zero16();
+    up = zero16();
+    qf[0] = R::row_frag(at, 0, 0);
+    of[0] = R::row_frag(at + TILE, 0, 0);
 #pragma unroll
-    for (int i = 0; i < R::ND; ++i) {
-      store_col(tk, dk[i], i, a.dim, a.scale);
-      store_col(tv, dv[i], i, a.dim, 1.0f);
+    for (int ks = 0; ks < R::KS; ++ks) {
+      if (ks + 1 < R::KS) {
+        qf[(ks + 1) & 1] = R::row_frag(at, 0, ks + 1);
+        of[(ks + 1) & 1] = R::row_frag(at + TILE, 0, ks + 1);
+      }
+      mma(qf[ks & 1], k[ks], u);
+      if constexpr (decltype(both)::value) grads_of<T, 2 * R::KS>(2 * ks, s, dp, c, pf, df, rows);
+      __builtin_amdgcn_sched_barrier(0);
+      mma(of[ks & 1], v[ks], up);
+      if constexpr (decltype(both)::value) grads_of<T, 2 * R::KS>(2 * ks + 1, s, dp, c, pf, df, rows);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  auto hide = [&](int p0, floatx16_t& u) {
+    if (!all(p0)) {
+      results_settle();
+      const int first = p0 + row_here();
+#pragma unroll
+      for (int i = 0; i < 16; ++i) u[i] = seen(first + row_of(i), krow) ? u[i] : -INFINITY;
+    }
+  };
+  int place = 0;                                     // of stage t
+  // rows 32 n of stage t, and the scores of the 32 behind them
+  auto step = [&](int t, int n, floatx16_t& s, floatx16_t& dp, floatx16_t& u, floatx16_t& up) {
+    const int next = place == 2 ? 0 : place + 1;
+    const bool over = n + 1 == NQ, more = !over || t + 1 < count;
+    const int after = over ? next : place, m = over ? 0 : n + 1;
+    Frag<T> pf[2], df[2];
+    scores(smem + after * STAGE + 32 * m * R::ROW, u, up, s, dp, pf, df, s_lse[place] + 32 * n, s_delta[place] + 32 * n, std::true_type{});
+    if (more) hide(first_row(over ? t + 1 : t) + 32 * m + shift, u);
+    const char* at = smem + place * STAGE + 32 * n * R::ROW;
+    Frag<T> qf[2][R::ND], of[2][R::ND];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < R::ND; ++i) {
+        of[h][i] = R::col_frag(at + TILE, 16 * h, i);
+        qf[h][i] = R::col_frag(at, 16 * h, i);
+      }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < R::ND; ++i) {
+        mma(of[h][i], pf[h], dv[i]);
+        mma(qf[h][i], df[h], dk[i]);
+      }
+  };
+  tile_sync();
+  if (count > 0) {
+    floatx16_t s, dp, u, up;
+    Frag<T> nothing[2];
+    scores(smem, s, dp, u, up, nothing, nothing, nullptr, nullptr, std::false_type{});
+    hide(first_row(0) + shift, s);
+    results_settle();
+    for (int t = 0; t < count; ++t) {
+      const int last = place == 0 ? 2 : place - 1;
+      if (t + 2 < count) issue(t + 2, smem + last * STAGE);
+      step(t, 0, s, dp, u, up);
+      if constexpr (NQ == 2) {
+        step(t, 1, u, up, s, dp);
+      } else {
+        s = u;
+        dp = up;
+      }
+      if (t + 2 < count) keep(last);
+      place = place == 2 ? 0 : place + 1;
+      tile_sync();
     }
   }
+  results_settle();
+  const bool direct = plan.parts == 1 && !far && !(plan.far > 0 && tile < plan.sink_tiles);
+  if (direct) {
+    const int left = kp.y - k0;
+    char* own = smem + wave * (sizeof(smem) / kWaves);
+    store_rows<T, DP>((T*)g.dk + ((int64_t)kp.x + k0) * g.lddk + kvh * a.dim, g.lddk, left, a.dim, dk, a.scale, own);
+    store_rows<T, DP>((T*)g.dv + ((int64_t)kp.x + k0) * g.lddv + kvh * a.dim, g.lddv, left, a.dim, dv, 1.0f, own);
+    return;
+  }
+  if (!far && plan.parts == 1) slot = far_slot(plan, kv_heads, seq, tile, kvh, 0);
+  float* to = sums + slot * (2 * kKeyRows * DP) + (int64_t)(wave * 32 + (lane & 31)) * DP;
+#pragma unroll
+  for (int i = 0; i < R::ND; ++i) {
+    store_col(to, dk[i], i, DP, a.scale);
+    store_col(to + kKeyRows * DP, dv[i], i, DP, 1.0f);
+  }
+}
+
+// The sums of a tile's parts added in their order.  Blocks: the tiles, or (where tiles are not cut) those with sinks; eight for the rows of one.
+template <typename T, int DP>
+__global__ __launch_bounds__(256) void k_attn_dkv_join(AttnArgs a, AttnGrads g, KeyPlan plan, const float* __restrict__ sums) {
+  const int kv_heads = a.heads / a.group, id = blockIdx.x, kvh = id % kv_heads;
+  int seq, tile;
+  if (plan.parts > 1) {
+    if (!find_tile(a.ks, kKeyRows, id / kv_heads, &seq, &tile)) return;
+  } else {
+    seq = id / kv_heads / plan.sink_tiles;
+    tile = id / kv_heads - seq * plan.sink_tiles;
+  }
+  const int2 kp = a.ks.place(seq);
+  const bool sinks = plan.far > 0 && tile < plan.sink_tiles;
+  const int near = plan.parts > 1 ? plan.parts : 0, parts = near + (sinks ? plan.far + (near ? 0 : 1) : 0);
+  // near parts of the tile are neighbours among those of the head
+  const int64_t base = near ? ((int64_t)kvh * plan.tiles + id / kv_heads) * plan.parts : 0;
+  const int64_t far = sinks ? far_slot(plan, kv_heads, seq, tile, kvh, near ? 1 : 0) : 0;
+  constexpr int PER_ROW = DP / 4, ROWS = 256 / PER_ROW;              // four features a lane
+  for (int r = blockIdx.y * ROWS + threadIdx.x / PER_ROW; r < 2 * kKeyRows; r += gridDim.y * ROWS) {
+    const int d = threadIdx.x % PER_ROW * 4, krow = tile * kKeyRows + r % kKeyRows;
+    if (krow >= kp.y || d >= a.dim) continue;
+    float4 sum = make_float4(0, 0, 0, 0);
+    for (int x = 0; x < parts; ++x) {
+      const int64_t slot = x < near ? base + x : far + x - near;
+      const float4 v = *(const float4*)(sums + (slot * 2 * kKeyRows + r) * DP + d);
+      sum.x += v.x;
+      sum.y += v.y;
+      sum.z += v.z;
+      sum.w += v.w;
+    }
+    T* to = r < kKeyRows ? (T*)g.dk + ((int64_t)kp.x + krow) * g.lddk : (T*)g.dv + ((int64_t)kp.x + krow) * g.lddv;
+    store4(to + kvh * a.dim + d, sum.x, sum.y, sum.z, sum.w);
+  }
+}
+
+// far parts where a window's tiles have less to do than a tile with sinks, and few enough tiles that the chip does not fill by them; parts
+// where tiles do not fill it
+static KeyPlan key_plan(const Packed& qs, const Packed& ks, int64_t kv_heads, int64_t group, const AttnMask& m, int dtype) {
+  KeyPlan k = {};
+  const int64_t tiles = ks.most_tiles(kKeyRows), stage = dtype == EFQAT_BF16 ? 64 : 32, each = ceil_div(qs.rows, qs.n);
+  int64_t span = m.window && m.window + kKeyRows < each ? m.window + kKeyRows : each;      // queries of a tile
+  const int64_t steps = ceil_div(span, stage) * group, blocks = tiles * kv_heads;
+  int64_t parts = ceil_div(512, blocks);
+  if (blocks >= 256) parts = 1;
+  if (parts > ceil_div(steps, 4)) parts = ceil_div(steps, 4);
+  k.tiles = (int)tiles;
+  k.parts = (int)(parts < 1 ? 1 : parts);
+  if (m.window && m.sinks > 0 && each > 2 * span) {
+    const int64_t sink_tiles = ceil_div(m.sinks < ks.rows ? m.sinks : ks.rows, kKeyRows), sink_blocks = sink_tiles * qs.n * kv_heads;
+    if (sink_blocks < 256) {
+      const int64_t most = ceil_div(ceil_div(each - span, stage) * group, 8), want = ceil_div(256, sink_blocks);
+      k.sink_tiles = (int)sink_tiles;
+      k.far = (int)(most < want ? most : want);
+      k.far_blocks = sink_blocks * k.far;
+    }
+  }
+  k.near_blocks = blocks * k.parts;
+  k.slots = (k.parts > 1 ? k.near_blocks : 0) + (k.far ? k.far_blocks / k.far * (k.far + 1) : 0);
+  return k;
 }
 
 }  // namespace efqat
 
 using namespace efqat;
 
-extern "C" size_t efqat_attention_bwd_workspace_bytes(int64_t Tq, int64_t heads) {
-  if (Tq <= 0 || heads <= 0 || Tq > kAttnMostRows || heads > 65535) return 256;
-  return (size_t)round_up(Tq * heads * 4, 256);
+static size_t bwd_ws_bytes(const KeyPlan& k, int64_t Tq, int64_t heads, int64_t dim) {
+  return (size_t)round_up(Tq * heads * 4, 256) + (size_t)k.slots * 2 * kKeyRows * (dim <= 64 ? 64 : 128) * 4;
+}
+
+extern "C" size_t efqat_attention_bwd_workspace_bytes(int64_t Tq, int64_t Tk, int64_t n_seq, int packed, int64_t heads, int64_t kv_heads, int64_t dim,
+                                                      int dtype, int causal, int64_t window, int64_t sinks) {
+  AttnArgs a;
+  static const int32_t some[1] = {0};
+  void* const p = (void*)16;                         // any pointer and stride that would do
+  if (attn_args(&a, p, heads * dim, p, kv_heads * dim, p, kv_heads * dim, dtype, Tq, Tk, n_seq, packed ? some : nullptr, packed ? some : nullptr, heads,
+                kv_heads, dim, 1.0f, causal, window, sinks))
+    return 256;
+  return bwd_ws_bytes(key_plan(a.qs, a.ks, kv_heads, a.group, a.mask, dtype), Tq, heads, dim);
 }
 
 extern "C" int efqat_attention_bwd(const void* dout, int64_t lddo, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v,
@@ -285,18 +474,20 @@ extern "C" int efqat_attention_bwd(const void* dout, int64_t lddo, const void* q
   EFQAT_TRY(attn_rows(dv, lddv, kv_heads * dim, dtype));
   if (!lse || !ws) return EFQAT_ERR_NULL_PTR;
   if (!aligned4(lse) || (uintptr_t)ws % 256) return EFQAT_ERR_ALIGNMENT;
-  if (ws_bytes < efqat_attention_bwd_workspace_bytes(Tq, heads)) return EFQAT_ERR_WORKSPACE;
-  const HeadPlan h = head_plan(a, kv_heads, dtype);
-  const int64_t kt = a.ks.most_tiles(128);
-  if (h.blocks > kAttnMostBlocks || kt * kv_heads > kAttnMostBlocks) return EFQAT_ERR_BAD_SHAPE;
+  const KeyPlan plan = key_plan(a.qs, a.ks, kv_heads, a.group, a.mask, dtype);
+  if (ws_bytes < bwd_ws_bytes(plan, Tq, heads, dim)) return EFQAT_ERR_WORKSPACE;
+  const HeadPlan h = head_plan(a, kv_heads);
+  if (h.blocks > kAttnMostBlocks || plan.near_blocks + plan.far_blocks > kAttnMostBlocks) return EFQAT_ERR_BAD_SHAPE;
   const AttnGrads g = {dout, o, lddo, ldo, lse, (float*)ws, dq, dk, dv, lddq, lddk, lddv};
+  float* sums = (float*)((char*)ws + round_up(Tq * heads * 4, 256));
+  const unsigned joins = (unsigned)(plan.parts > 1 ? plan.tiles * kv_heads : plan.far ? plan.far_blocks / plan.far : 0);
   hipStream_t st = (hipStream_t)stream;
-#define EFQAT_BWD(E, DP)                                                                                             \
-  do {                                                                                                               \
-    if (h.waves == 8) {                                                                                              \
-      if constexpr (kWideBlocks<E, DP>) EFQAT_TRY(launch(k_attn_dq<E, DP, 8>, dim3((unsigned)h.blocks), dim3(512), 0, st, a, g, h.tiles, h.hb)); \
-    } else EFQAT_TRY(launch(k_attn_dq<E, DP, 4>, dim3((unsigned)h.blocks), dim3(256), 0, st, a, g, h.tiles, h.hb));    \
-    return launch(k_attn_dkv<E, DP>, dim3((unsigned)(kt * kv_heads)), dim3(256), 0, st, a, g, (int)kt);              \
+#define EFQAT_BWD(E, DP)                                                                                                           \
+  do {                                                                                                                             \
+    EFQAT_TRY(launch(k_attn_dq<E, DP>, dim3((unsigned)h.blocks), dim3(256), 0, st, a, g, h.tiles, h.hb));                          \
+    EFQAT_TRY(launch(k_attn_dkv<E, DP>, dim3((unsigned)(plan.near_blocks + plan.far_blocks)), dim3(256), 0, st, a, g, plan, sums)); \
+    if (joins) EFQAT_TRY(launch(k_attn_dkv_join<E, DP>, dim3(joins, 8), dim3(256), 0, st, a, g, plan, (const float*)sums));        \
+    return EFQAT_OK;                                                                                                               \
   } while (0)
   if (dtype == EFQAT_F32) { if (dim <= 64) EFQAT_BWD(float, 64); EFQAT_BWD(float, 128); }
   if (dim <= 64) EFQAT_BWD(bf16_t, 64);

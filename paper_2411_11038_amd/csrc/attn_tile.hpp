@@ -144,6 +144,15 @@ __device__ __forceinline__ floatx16_t zero16() {
 }
 // row of a result that register i holds in this lane
 __device__ __forceinline__ int result_row(int i) { return (i & 3) + 8 * (i >> 2) + 4 * ((threadIdx.x >> 5) & 1); }
+// first row of a result that this lane holds, made where this stands: rows made from it do not occupy registers elsewhere
+__device__ __forceinline__ int row_here() {
+  int r = 4 * ((threadIdx.x >> 5) & 1);
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("" : "+v"(r));
+#endif
+  return r;
+}
+__device__ __forceinline__ int row_of(int i) { return (i & 3) + 8 * (i >> 2); }
 
 // 8 elements of a row of a matrix in memory as an operand, 16-byte aligned; not `ok`: zeros
 template <typename T>
@@ -165,6 +174,14 @@ __device__ __forceinline__ Frag<T> load_frag(const T* p, bool ok) {
   return f;
 }
 
+#if defined(__HIP_DEVICE_COMPILE__)
+__device__ __forceinline__ uint32_t lds_address(const char* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p; }
+template <class V>
+__device__ __forceinline__ V lds_read(uint32_t at) {
+  return *(__attribute__((address_space(3))) const V*)(uintptr_t)at;
+}
+#endif
+
 // ---- a tile of rows of DP features in LDS.  Its 16-byte pieces are swizzled by row so that both ways of reading it spread over the
 // banks: neighbouring rows at the same piece (row_frag), and four rows at four neighbouring pieces (col_frag, bf16, transposing reads)
 // or two rows four apart at eight neighbouring pieces (col_frag, fp32).
@@ -184,47 +201,47 @@ struct RowTile {
     const char* src = row < valid && piece < pieces ? base + row * ld_bytes + piece * 16 : zero_page();
     dma16(src, lds + slot * 1024);
   }
+  // Addresses of pieces differ by exclusive ors with constants: tiles lie at multiples of a row, and so does everything that is added.
   // contraction step ks of row `row` (a multiple of 32) + lane % 32
   __device__ static __forceinline__ Frag<T> row_frag(const char* lds, int row, int ks) {
-    const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
-    const char* p = lds + (row + r) * ROW;
     Frag<T> f;
+#if defined(__HIP_DEVICE_COMPILE__)
+    const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
     if constexpr (sizeof(T) == 2) {
-      f.v = *reinterpret_cast<const bf16x8_t*>(p + (((2 * ks + h) ^ swz(r)) << 4));
+      const uint32_t base = lds_address(lds) + r * ROW + ((h ^ swz(r)) << 4);
+      f.v = lds_read<bf16x8_t>((base ^ (ks << 5)) + row * ROW);
     } else {
-      const float4 a = *reinterpret_cast<const float4*>(p + (((4 * ks + 2 * h) ^ swz(r)) << 4));
-      const float4 b = *reinterpret_cast<const float4*>(p + (((4 * ks + 2 * h + 1) ^ swz(r)) << 4));
+      const uint32_t base = lds_address(lds) + r * ROW + (((2 * h) ^ swz(r)) << 4);
+      const float4 a = lds_read<float4>((base ^ (ks << 6)) + row * ROW), b = lds_read<float4>((base ^ (ks << 6 | 16)) + row * ROW);
       f.v[0] = a.x; f.v[1] = a.y; f.v[2] = a.z; f.v[3] = a.w;
       f.v[4] = b.x; f.v[5] = b.y; f.v[6] = b.z; f.v[7] = b.w;
     }
+#endif
     return f;
   }
   // feature 32 i + lane % 32 of the 16 rows from `row` (a multiple of 16) on, in the order of a result's registers: element e is row
   // 8 (e >> 2) + 4 (lane / 32) + (e & 3)
   __device__ static __forceinline__ Frag<T> col_frag(const char* lds, int row, int i) {
-    const int lane = threadIdx.x & 63, h = lane >> 5;
     Frag<T> f;
-    if constexpr (sizeof(T) == 2) {
 #if defined(__HIP_DEVICE_COMPILE__)
-      const int s = lane & 15, piece = 4 * i + 2 * ((lane >> 4) & 1) + ((s & 3) >> 1);
+    const int lane = threadIdx.x & 63, h = lane >> 5;
+    if constexpr (sizeof(T) == 2) {
+      const int s = lane & 15, piece = 2 * ((lane >> 4) & 1) + ((s & 3) >> 1), k = 4 * h + (s >> 2);
+      const uint32_t base = lds_address(lds) + k * ROW + ((piece ^ swz(k)) << 4) + 8 * (s & 1);
       shortx4_t v[2];
 #pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const int k = row + 8 * r + 4 * h + (s >> 2);
+      for (int r = 0; r < 2; ++r)
         v[r] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (__attribute__((address_space(3))) shortx4_t*)(lds + k * ROW + ((piece ^ swz(k)) << 4) + 8 * (s & 1)));
-      }
+            (__attribute__((address_space(3))) shortx4_t*)(uintptr_t)((base ^ (i << 6 | r << 5)) + (row + 8 * r) * ROW));
       struct { shortx4_t lo, hi; } both = {v[0], v[1]};
       f.v = __builtin_bit_cast(bf16x8_t, both);
-#endif
     } else {
       const int d = lane & 31;
+      const uint32_t base = lds_address(lds) + 4 * h * ROW + (((d >> 2) ^ (h << 3)) << 4) + 4 * (d & 3);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int k = row + 8 * (e >> 2) + 4 * h + (e & 3);
-        f.v[e] = *reinterpret_cast<const float*>(lds + k * ROW + (((8 * i + (d >> 2)) ^ swz(k)) << 4) + 4 * (d & 3));
-      }
+      for (int e = 0; e < 8; ++e) f.v[e] = lds_read<float>((base ^ (i << 7 | e << 4)) + (row + 8 * (e >> 2) + (e & 3)) * ROW);
     }
+#endif
     return f;
   }
 };
@@ -338,18 +355,19 @@ struct AttnArgs {
 };
 template <typename T>
 constexpr int kKeyStage = sizeof(T) == 2 ? 64 : 32;    // keys of a stage of LDS
-// eight wavefronts a block, two a SIMD: what they hold fits 256 registers
+constexpr int kWaves = 4;                              // of a block, each with 32 rows of scores
+// what a wavefront holds fits 256 registers: two a SIMD
 template <typename T, int DP>
-constexpr bool kWideBlocks = sizeof(T) == 2 || DP == 64;
+constexpr bool kTwoWaves = sizeof(T) == 2 || DP == 64;
 
-// Rows of a wavefront in a block of `waves`, each with 32 queries of a head: hb heads that share keys, 32 waves / hb queries.
+// Rows of a wavefront in a block of four, each with 32 queries of a head: hb (1, 2 or 4) of the heads that share keys, 128 / hb queries.
 // Blocks that share keys are neighbours, late tiles (the long ones under a causal mask) come first.
 struct HeadTile {
   int2 queries, keys;                                // rows of the sequence: first, count
   int kvh, head, shift, block_row, block_rows, row;  // row: the wavefront's first query
-  __device__ __forceinline__ bool find(const AttnArgs& a, int waves, int hb, int tiles, int wave) {
+  __device__ __forceinline__ bool find(const AttnArgs& a, int hb, int tiles, int wave) {
     const int id = xcd_contiguous_index(blockIdx.x, gridDim.x);
-    const int groups = a.group / hb, per_head = tiles * groups, at = id % per_head, bq = 32 * waves / hb;
+    const int groups = a.group / hb, per_head = tiles * groups, at = id % per_head, bq = 32 * kWaves / hb;
     kvh = id / per_head;
     head = kvh * a.group + at % groups * hb + wave % hb;
     int seq, tile;
@@ -374,12 +392,12 @@ __device__ __forceinline__ void dma16_at(const char* base, uint32_t offset, char
   asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base));
 }
 
-// Copies of ROWS rows of a matrix into a tile by NW wavefronts.  Rows that all exist, of DP features, less than 2^31 bytes apart in all: a
+// Copies of ROWS rows of a matrix into a tile by the block.  Rows that all exist, of DP features, less than 2^31 bytes apart in all: a
 // scalar address and a lane's offset, which stay the same from tile to tile.  Others choose between the row and zeros lane by lane.
-template <typename T, int DP, int NW, int ROWS>
+template <typename T, int DP, int ROWS>
 struct RowCopies {
   using R = RowTile<T, DP>;
-  static constexpr int N = ROWS / R::RPI / NW;
+  static constexpr int NW = kWaves, N = ROWS / R::RPI / NW;
   static_assert(N * R::RPI * NW == ROWS, "whole copies");
   int64_t ld;                                        // bytes
   int pieces;
@@ -407,12 +425,11 @@ struct RowCopies {
   }
 };
 // of a stage's keys and values
-template <typename T, int DP, int NW>
+template <typename T, int DP, int BN>
 struct KeyCopies {
   using R = RowTile<T, DP>;
-  static constexpr int BN = kKeyStage<T>;
   const char *k, *v;
-  RowCopies<T, DP, NW, BN> ck, cv;
+  RowCopies<T, DP, BN> ck, cv;
   int keys;
   __device__ __forceinline__ KeyCopies(const AttnArgs& a, int2 place, int kvh, int wave)
       : k((const char*)((const T*)a.k + (int64_t)place.x * a.ldk + kvh * a.dim)), v((const char*)((const T*)a.v + (int64_t)place.x * a.ldv + kvh * a.dim)),
@@ -486,20 +503,16 @@ inline int attn_args(AttnArgs* a, const void* q, int64_t ldq, const void* k, int
   return EFQAT_OK;
 }
 
-// Blocks of the kernels that walk keys: eight wavefronts, whose 256 rows halve what L2 delivers, where these fill the chip; else four.
+// Blocks of the kernels that walk keys
 struct HeadPlan {
-  int waves, hb, tiles;
+  int hb, tiles;
   int64_t blocks;
 };
-inline HeadPlan head_plan(const AttnArgs& a, int64_t kv_heads, int dtype) {
-  HeadPlan h;
-  for (int waves = 4;; waves = 4) {
-    int hb = 1;
-    while (hb < waves && a.group % (2 * hb) == 0) hb *= 2;
-    const int64_t tiles = a.qs.most_tiles(32 * waves / hb);
-    h = {waves, hb, (int)tiles, tiles * (a.group / hb) * kv_heads};
-    if (waves == 4 || h.blocks >= 512) return h;
-  }
+inline HeadPlan head_plan(const AttnArgs& a, int64_t kv_heads) {
+  int hb = 1;
+  while (hb < kWaves && a.group % (2 * hb) == 0) hb *= 2;
+  const int64_t tiles = a.qs.most_tiles(32 * kWaves / hb);
+  return {hb, (int)tiles, tiles * (a.group / hb) * kv_heads};
 }
 
 }  // namespace efqat

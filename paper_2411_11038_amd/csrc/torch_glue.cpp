@@ -628,7 +628,8 @@ PyObject* attention_bwd(PyObject* const* a, PyObject* const* out) {
   Results r(3, t);
   const Rows dq = result(r, 0, out[0], q, q.rows, q.cols, "dq"), dk = result(r, 1, out[1], q, k.rows, k.cols, "dk"),
              dv = result(r, 2, out[2], q, k.rows, k.cols, "dv");
-  const Scratch ws = scratch(r, a[15], efqat_attention_bwd_workspace_bytes(q.rows, c.heads));
+  const Scratch ws = scratch(r, a[15], efqat_attention_bwd_workspace_bytes(q.rows, k.rows, c.n_seq, c.q_start != nullptr, c.heads, c.kv, c.dim, q.dtype(), c.causal,
+                                                                               c.window, c.sinks));
   void* st = stream_now();
   return r.take(unlocked([&] {
     return efqat_attention_bwd(g.p, g.ld, q.p, q.ld, k.p, k.ld, v.p, v.ld, o.p, o.ld, lse, q.dtype(), q.rows, k.rows, c.n_seq, c.q_start, c.k_start,

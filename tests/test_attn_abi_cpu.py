@@ -51,8 +51,11 @@ def _attn(**kw):
 
 def test_attention(L):
     extra = dict(o=FAKE, ldo=256, lse=FAKE, do=FAKE, lddo=256, dq=FAKE, lddq=256, dk=FAKE, lddk=128, dv=FAKE, lddv=128, ws=FAKE)
-    need = L.efqat_attention_bwd_workspace_bytes(12, 4)
-    assert need >= 12 * 4 * 4 and L.efqat_attention_bwd_workspace_bytes(0, 4) == 256
+    query = L.efqat_attention_bwd_workspace_bytes
+    need = max(query(12, 12, 2, packed, 4, 2, 64, dt, 1, 0, 0) for packed in (0, 1) for dt in (0, 1))
+    assert query(12, 12, 2, 0, 4, 2, 64, 1, 1, 0, 0) >= 12 * 4 * 4
+    assert query(0, 12, 2, 0, 4, 2, 64, 1, 1, 0, 0) == query(12, 13, 2, 0, 4, 2, 64, 1, 1, 0, 0) == query(12, 12, 2, 0, 4, 3, 64, 1, 1, 0, 0) == 256
+    least = query(12, 12, 2, 0, 4, 2, 64, 1, 1, 0, 0)
 
     def fwd(wsb=None, **kw):
         a = {**_attn(), **extra, **kw}
@@ -74,7 +77,7 @@ def test_attention(L):
         assert f(qs=FAKE + 2, ks=FAKE) == f(dt=0, ldq=258) == ALIGN
         assert f(Tq=1 << 28, Tk=1 << 28, n=1, H=16, KV=16, ldq=1024, ldk=1024, ldv=1024, ldo=1024, lddo=1024, lddq=1024, lddk=1024, lddv=1024, wsb=1 << 50) == SHAPE
     assert bwd(do=None) == bwd(lse=None) == bwd(dq=None) == bwd(dk=None) == bwd(dv=None) == bwd(ws=None) == NULL
-    assert bwd(lddo=248) == bwd(lddq=248) == bwd(lddk=120) == bwd(lddv=120) == SHAPE and bwd(wsb=need - 1) == WORKSPACE
+    assert bwd(lddo=248) == bwd(lddq=248) == bwd(lddk=120) == bwd(lddv=120) == SHAPE and bwd(wsb=least - 1) == WORKSPACE
     assert bwd(ws=FAKE + 128) == bwd(do=FAKE + 8) == bwd(lddv=132) == ALIGN
 
 

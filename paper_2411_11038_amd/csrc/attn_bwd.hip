@@ -36,26 +36,6 @@ __device__ __forceinline__ float prob(float s, float c, float base) {
 template <typename T>
 __device__ __forceinline__ float prob_factor(float scale) { return sizeof(T) == 2 ? scale * kLog2e : scale; }
 
-// What k_attn_dkv does with 32 x 32 scores: P and dS, whose results S and dP are, as operands of the sums, a share of 16 / GROUPS elements
-// beside each of the GROUPS products that are formed meanwhile.  rows(i) says what lse and delta register i has.
-template <typename T, int GROUPS, class Rows>
-__device__ __forceinline__ void grads_of(int group, floatx16_t& s, floatx16_t& dp, float c, Frag<T> (&pf)[2], Frag<T> (&df)[2], const Rows& rows) {
-  constexpr int PER = 16 / GROUPS;
-#pragma unroll
-  for (int i = group * PER; i < (group + 1) * PER; ++i) {
-    const float2 r = rows(i);
-    const float e = prob<T>(s[i], c, r.x);
-    dp[i] = e * (dp[i] - r.y);
-    s[i] = e;
-    if ((i & 7) == 7) {
-      pf[i >> 3] = frag_of<T>(s, i >> 3);
-      hold(pf[i >> 3]);
-      df[i >> 3] = frag_of<T>(dp, i >> 3);
-      hold(df[i >> 3]);
-    }
-  }
-}
-
 // dq, and delta for the other kernel.  Blocks as in k_attn_fwd.  (Forming the next 32 keys' scores beside dS, as the other kernels do, needs
 // more registers than two wavefronts a SIMD have: 380 instead of 250 us for a window of 1024 in 2 x 4096 tokens, 32 heads of 128.)
 template <typename T, int DP>
@@ -170,15 +150,26 @@ __host__ __device__ inline int64_t far_slot(const KeyPlan& k, int kv_heads, int 
   return (k.parts > 1 ? k.near_blocks : 0) + (((int64_t)seq * k.sink_tiles + tile) * kv_heads + kvh) * (k.far + 1) + part;
 }
 
-// dk and dv of 128 keys, 32 a wavefront: scores with queries as rows and keys as columns, so that P and dS are operands of the sums over
-// the queries where they are.  A ring of three stages of queries and their gradients, walked in steps of 32 rows; beside the products that form
-// a step's scores and dP stands the arithmetic of the step before.
+// Wavefronts of a block, and where they hold values.  bf16 heads of 128: eight, two a SIMD, so that one's arithmetic runs beside the other's products (one wavefront
+// a SIMD with twice the rows issues them one after the other: 550 us where two take 440, window of 1024 in 2 x 4096 tokens, 32 heads of 128).  Four take
+// the first 32 rows of a stage and four the second, for the same keys; the second ones' sums are added through LDS at the end.  They have
+// no registers left for the values, which stay in LDS.  Smaller heads and fp32: four, each with all rows.
 template <typename T, int DP>
-__global__ __launch_bounds__(256, (sizeof(T) == 2 && DP == 64 ? 2 : 1)) void k_attn_dkv(AttnArgs a, AttnGrads g, KeyPlan plan, float* __restrict__ sums) {
+struct DkvTile {
+  static constexpr int WAVES = sizeof(T) == 2 && DP == 128 ? 8 : 4, BQ = sizeof(T) == 2 ? 64 : 32;
+  static constexpr bool VALUES_IN_LDS = sizeof(T) == 2 && DP == 128;
+};
+
+// dk and dv of 128 keys, 32 a wavefront: scores with queries as rows and keys as columns, so that P and dS are operands of the sums over
+// the queries where they are.
+template <typename T, int DP>
+__global__ __launch_bounds__((64 * DkvTile<T, DP>::WAVES), (sizeof(T) == 2 || DP == 64 ? 2 : 1)) void k_attn_dkv(AttnArgs a, AttnGrads g, KeyPlan plan,
+                                                                                              float* __restrict__ sums) {
   using R = RowTile<T, DP>;
-  constexpr int BQ = sizeof(T) == 2 ? 64 : 32, NQ = BQ / 32, TILE = BQ * R::ROW, STAGE = 2 * TILE;
-  __shared__ __attribute__((aligned(1024))) char smem[3 * STAGE];
-  __shared__ __attribute__((aligned(16))) float s_lse[3][BQ], s_delta[3][BQ];
+  using C = DkvTile<T, DP>;
+  constexpr int BQ = C::BQ, NW = C::WAVES, TILE = BQ * R::ROW, STAGE = 2 * TILE, VALUES = C::VALUES_IN_LDS ? kKeyRows * R::ROW : 0;
+  __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE + VALUES];
+  __shared__ __attribute__((aligned(16))) float s_lse[2][BQ], s_delta[2][BQ];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kv_heads = a.heads / a.group;
   const bool far = blockIdx.x >= plan.near_blocks;                   // short ones, behind the others: they even out the end
@@ -204,7 +195,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 && DP == 64 ? 2 : 1)) void k_a
   const int2 qp = a.qs.place(seq), kp = a.ks.place(seq);
   if (tile * kKeyRows >= kp.y) return;
   const bool near = plan.far > 0;                                    // what sinks add is not this block's, or all that is
-  const int shift = kp.y - qp.y, k0 = tile * kKeyRows + wave * 32, krow = k0 + (lane & 31);
+  const int shift = kp.y - qp.y, own = wave & 3, sub = NW == 8 ? wave >> 2 : 0, k0 = tile * kKeyRows + own * 32, krow = k0 + (lane & 31);
   const QuerySpan span(a.mask, near && !far, qp.y, shift, tile * kKeyRows, min(tile * kKeyRows + kKeyRows, kp.y) - 1);
   const int nq = span.last > span.first ? (span.last - span.first + BQ - 1) / BQ : 0;
   const int cuts = far ? plan.far : plan.parts;
@@ -217,162 +208,145 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 && DP == 64 ? 2 : 1)) void k_a
     const bool yes = mask.sees(p, j);
     return (bool)((int)yes & ((int)!far | ((int)(j < mask.sinks) & (int)!window_alone.sees(p, j))));
   };
+  auto some = [&](int p0) { return mask.sees_some(p0, p0 + 31, k0, k0 + 31) && (!far || k0 < mask.sinks); };
   auto all = [&](int p0) { return !far && mask.sees_all(p0, p0 + 31, k0, k0 + 31); };
 
-  RowCopies<T, DP, BQ> cq(a.ldq, a.dim, wave), cd(g.lddo, a.dim, wave);
+  RowCopies<T, DP, BQ, NW> cq(a.ldq, a.dim, wave), cd(g.lddo, a.dim, wave);
   float next_lse = 0.0f, next_delta = 0.0f;
-  auto first_row = [&](int t) { return span.first + (begin + t) % nq * BQ; };
-  auto issue = [&](int t, char* buf) {
-    const int head = kvh * a.group + (begin + t) / nq, i0 = first_row(t), valid = qp.y - i0;
+  // stages are counted along the queries of a head, then along the heads: where the next copy, and the next scores, stand in that
+  int to_head = kvh * a.group + (count > 0 ? begin / nq : 0), to_tile = count > 0 ? begin % nq : 0;
+  int at_tile = to_tile;                             // of the stage that is worked on
+  auto issue = [&](char* buf) {
+    const int head = to_head, i0 = span.first + to_tile * BQ, valid = qp.y - i0;
+    if (++to_tile == nq) {
+      to_tile = 0;
+      ++to_head;
+    }
     cq.issue((const char*)((const T*)a.q + (int64_t)(qp.x + i0) * a.ldq + head * a.dim), valid, buf, wave);
     cd.issue((const char*)((const T*)g.dout + (int64_t)(qp.x + i0) * g.lddo + head * a.dim), valid, buf + TILE, wave);
     if (threadIdx.x < BQ) {
       const int i = threadIdx.x;
       const int64_t from = (int64_t)head * a.qs.rows + qp.x + i0 + i;
-      next_lse = INFINITY;                                          // rows behind the sequence and tokens that see nothing: P = 0
+      next_lse = -INFINITY;                                         // rows behind the sequence are as tokens that see nothing
       next_delta = 0.0f;
-      if (i < valid) {
-        next_lse = prob_base<T>(g.lse[from]);
+      if (i < valid) {                                              // not looked at before keep(): that would wait for the copies too
+        next_lse = g.lse[from];
         next_delta = g.delta[from];
       }
     }
   };
   auto keep = [&](int b) {
     if (threadIdx.x < BQ) {
-      s_lse[b][threadIdx.x] = next_lse;
+      s_lse[b][threadIdx.x] = prob_base<T>(next_lse);
       s_delta[b][threadIdx.x] = next_delta;
     }
   };
+  char* const vals = smem + 2 * STAGE;
+  if constexpr (C::VALUES_IN_LDS) {
+    const RowCopies<T, DP, kKeyRows, NW> cv(a.ldv, a.dim, wave);
+    cv.issue((const char*)((const T*)a.v + ((int64_t)kp.x + tile * kKeyRows) * a.ldv + kvh * a.dim), kp.y - tile * kKeyRows, vals, wave);
+  }
   if (count > 0) {
-    issue(0, smem);
+    issue(smem);
     keep(0);
   }
-  if (count > 1) {
-    issue(1, smem + STAGE);
-    keep(1);
-  }
-
   const bool in = krow < kp.y;
   const int64_t row = (int64_t)kp.x + krow;
-  Frag<T> k[R::KS], v[R::KS];
+  Frag<T> k[R::KS], v[C::VALUES_IN_LDS ? 1 : R::KS];
 #pragma unroll
   for (int ks = 0; ks < R::KS; ++ks) {
     const int c = 16 * ks + 8 * (lane >> 5);
     k[ks] = load_frag((const T*)a.k + row * a.ldk + kvh * a.dim + c, in && c < a.dim);
-    v[ks] = load_frag((const T*)a.v + row * a.ldv + kvh * a.dim + c, in && c < a.dim);
+    if constexpr (!C::VALUES_IN_LDS) v[ks] = load_frag((const T*)a.v + row * a.ldv + kvh * a.dim + c, in && c < a.dim);
   }
   floatx16_t dk[R::ND], dv[R::ND];
 #pragma unroll
   for (int i = 0; i < R::ND; ++i) dk[i] = dv[i] = zero16();
   const float c = prob_factor<T>(a.scale);
-
-  // scores and dP of the 32 rows at `at`, and beside them P and dS of the rows before, whose lse and delta lie at l and e
-  auto scores = [&](const char* at, floatx16_t& u, floatx16_t& up, floatx16_t& s, floatx16_t& dp, Frag<T> (&pf)[2], Frag<T> (&df)[2], const float* l,
-                    const float* e, auto both) {
-    float4 l4[4], e4[4];
-    if constexpr (decltype(both)::value) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        l4[i] = *(const float4*)(l + result_row(4 * i));
-        e4[i] = *(const float4*)(e + result_row(4 * i));
-      }
-    }
-    const auto rows = [&](int i) {
-      const float4 x = l4[i >> 2], y = e4[i >> 2];
-      switch (i & 3) {
-        case 0: return make_float2(x.x, y.x);
-        case 1: return make_float2(x.y, y.y);
-        case 2: return make_float2(x.z, y.z);
-        default: return make_float2(x.w, y.w);
-      }
-    };
-    Frag<T> qf[2], of[2];
-    u = zero16();
-    up = zero16();
-    qf[0] = R::row_frag(at, 0, 0);
-    of[0] = R::row_frag(at + TILE, 0, 0);
-#pragma unroll
-    for (int ks = 0; ks < R::KS; ++ks) {
-      if (ks + 1 < R::KS) {
-        qf[(ks + 1) & 1] = R::row_frag(at, 0, ks + 1);
-        of[(ks + 1) & 1] = R::row_frag(at + TILE, 0, ks + 1);
-      }
-      mma(qf[ks & 1], k[ks], u);
-      if constexpr (decltype(both)::value) grads_of<T, 2 * R::KS>(2 * ks, s, dp, c, pf, df, rows);
-      __builtin_amdgcn_sched_barrier(0);
-      mma(of[ks & 1], v[ks], up);
-      if constexpr (decltype(both)::value) grads_of<T, 2 * R::KS>(2 * ks + 1, s, dp, c, pf, df, rows);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-  };
-  auto hide = [&](int p0, floatx16_t& u) {
-    if (!all(p0)) {
-      results_settle();
-      const int first = p0 + row_here();
-#pragma unroll
-      for (int i = 0; i < 16; ++i) u[i] = seen(first + row_of(i), krow) ? u[i] : -INFINITY;
-    }
-  };
-  int place = 0;                                     // of stage t
-  // rows 32 n of stage t, and the scores of the 32 behind them
-  auto step = [&](int t, int n, floatx16_t& s, floatx16_t& dp, floatx16_t& u, floatx16_t& up) {
-    const int next = place == 2 ? 0 : place + 1;
-    const bool over = n + 1 == NQ, more = !over || t + 1 < count;
-    const int after = over ? next : place, m = over ? 0 : n + 1;
-    Frag<T> pf[2], df[2];
-    scores(smem + after * STAGE + 32 * m * R::ROW, u, up, s, dp, pf, df, s_lse[place] + 32 * n, s_delta[place] + 32 * n, std::true_type{});
-    if (more) hide(first_row(over ? t + 1 : t) + 32 * m + shift, u);
-    const char* at = smem + place * STAGE + 32 * n * R::ROW;
-    Frag<T> qf[2][R::ND], of[2][R::ND];
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int i = 0; i < R::ND; ++i) {
-        of[h][i] = R::col_frag(at + TILE, 16 * h, i);
-        qf[h][i] = R::col_frag(at, 16 * h, i);
-      }
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int i = 0; i < R::ND; ++i) {
-        mma(of[h][i], pf[h], dv[i]);
-        mma(qf[h][i], df[h], dk[i]);
-      }
-  };
   tile_sync();
-  if (count > 0) {
-    floatx16_t s, dp, u, up;
-    Frag<T> nothing[2];
-    scores(smem, s, dp, u, up, nothing, nothing, nullptr, nullptr, std::false_type{});
-    hide(first_row(0) + shift, s);
-    results_settle();
-    for (int t = 0; t < count; ++t) {
-      const int last = place == 0 ? 2 : place - 1;
-      if (t + 2 < count) issue(t + 2, smem + last * STAGE);
-      step(t, 0, s, dp, u, up);
-      if constexpr (NQ == 2) {
-        step(t, 1, u, up, s, dp);
-      } else {
-        s = u;
-        dp = up;
+  for (int t = 0; t < count; ++t) {
+    const int b = t & 1;
+    if (t + 1 < count) issue(smem + (b ^ 1) * STAGE);
+    const int stage_row = span.first + at_tile * BQ;
+    if (++at_tile == nq) at_tile = 0;
+#pragma unroll
+    for (int n = 0; n < BQ / 32 * 4 / NW; ++n) {
+      const int r0 = 32 * (sub + n), i0 = stage_row + r0, p0 = i0 + shift;
+      const char *const qs = smem + b * STAGE + r0 * R::ROW, *const ds = qs + TILE;
+      if (i0 < qp.y && some(p0)) {
+        floatx16_t s = zero16(), dp = zero16();
+#pragma unroll
+        for (int ks = 0; ks < R::KS; ++ks) {
+          mma(R::row_frag(qs, 0, ks), k[ks], s);
+          if constexpr (C::VALUES_IN_LDS) mma(R::row_frag(ds, 0, ks), R::row_frag(vals, own * 32, ks), dp);
+          else mma(R::row_frag(ds, 0, ks), v[ks], dp);
+        }
+        if (!all(p0)) {
+          results_settle();
+          const int first = p0 + row_here();
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[i] = seen(first + row_of(i), krow) ? s[i] : -INFINITY;
+        } else {
+          results_settle();
+        }
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          const float4 l4 = *(const float4*)&s_lse[b][r0 + result_row(i)], e4 = *(const float4*)&s_delta[b][r0 + result_row(i)];
+          const float ls[4] = {l4.x, l4.y, l4.z, l4.w}, es[4] = {e4.x, e4.y, e4.z, e4.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            s[i + j] = prob<T>(s[i + j], c, ls[j]);
+            dp[i + j] = s[i + j] * (dp[i + j] - es[j]);
+          }
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const Frag<T> pf = frag_of<T>(s, h), df = frag_of<T>(dp, h);
+#pragma unroll
+          for (int i = 0; i < R::ND; ++i) {
+            mma(R::col_frag(ds, 16 * h, i), pf, dv[i]);
+            mma(R::col_frag(qs, 16 * h, i), df, dk[i]);
+          }
+        }
       }
-      if (t + 2 < count) keep(last);
-      place = place == 2 ? 0 : place + 1;
-      tile_sync();
     }
+    if (t + 1 < count) keep(b ^ 1);
+    tile_sync();
   }
   results_settle();
+  if constexpr (NW == 8) {                           // the second four's sums, register by register
+    static_assert(2 * STAGE >= 4 * R::ND * 16 * 64 * 4, "the sums lie where the stages were");
+    float* const at = (float*)smem + own * (R::ND * 16 * 64) + lane;
+    auto join = [&](floatx16_t (&x)[R::ND]) {
+      if (sub == 1) {
+#pragma unroll
+        for (int i = 0; i < R::ND; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) at[(i * 16 + r) * 64] = x[i][r];
+      }
+      tile_sync();
+      if (sub == 0) {
+#pragma unroll
+        for (int i = 0; i < R::ND; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) x[i][r] += at[(i * 16 + r) * 64];
+      }
+      tile_sync();
+    };
+    join(dk);
+    join(dv);
+    if (sub == 1) return;
+  }
   const bool direct = plan.parts == 1 && !far && !(plan.far > 0 && tile < plan.sink_tiles);
   if (direct) {
     const int left = kp.y - k0;
-    char* own = smem + wave * (sizeof(smem) / kWaves);
-    store_rows<T, DP>((T*)g.dk + ((int64_t)kp.x + k0) * g.lddk + kvh * a.dim, g.lddk, left, a.dim, dk, a.scale, own);
-    store_rows<T, DP>((T*)g.dv + ((int64_t)kp.x + k0) * g.lddv + kvh * a.dim, g.lddv, left, a.dim, dv, 1.0f, own);
+    char* const place = smem + own * (2 * STAGE / kWaves);
+    store_rows<T, DP>((T*)g.dk + ((int64_t)kp.x + k0) * g.lddk + kvh * a.dim, g.lddk, left, a.dim, dk, a.scale, place);
+    store_rows<T, DP>((T*)g.dv + ((int64_t)kp.x + k0) * g.lddv + kvh * a.dim, g.lddv, left, a.dim, dv, 1.0f, place);
     return;
   }
   if (!far && plan.parts == 1) slot = far_slot(plan, kv_heads, seq, tile, kvh, 0);
-  float* to = sums + slot * (2 * kKeyRows * DP) + (int64_t)(wave * 32 + (lane & 31)) * DP;
+  float* to = sums + slot * (2 * kKeyRows * DP) + (int64_t)(own * 32 + (lane & 31)) * DP;
 #pragma unroll
   for (int i = 0; i < R::ND; ++i) {
     store_col(to, dk[i], i, DP, a.scale);
@@ -485,7 +459,7 @@ extern "C" int efqat_attention_bwd(const void* dout, int64_t lddo, const void* q
 #define EFQAT_BWD(E, DP)                                                                                                           \
   do {                                                                                                                             \
     EFQAT_TRY(launch(k_attn_dq<E, DP>, dim3((unsigned)h.blocks), dim3(256), 0, st, a, g, h.tiles, h.hb));                          \
-    EFQAT_TRY(launch(k_attn_dkv<E, DP>, dim3((unsigned)(plan.near_blocks + plan.far_blocks)), dim3(256), 0, st, a, g, plan, sums)); \
+    EFQAT_TRY(launch(k_attn_dkv<E, DP>, dim3((unsigned)(plan.near_blocks + plan.far_blocks)), dim3(64 * DkvTile<E, DP>::WAVES), 0, st, a, g, plan, sums)); \
     if (joins) EFQAT_TRY(launch(k_attn_dkv_join<E, DP>, dim3(joins, 8), dim3(256), 0, st, a, g, plan, (const float*)sums));        \
     return EFQAT_OK;                                                                                                               \
   } while (0)

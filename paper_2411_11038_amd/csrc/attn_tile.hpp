@@ -136,6 +136,12 @@ __device__ __forceinline__ void hold(Frag<float>& f) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) hold(f.v[e]);
 }
+// a result that is to be read by vector operations, in vector registers
+__device__ __forceinline__ void hold(floatx16_t& c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("" : "+v"(c));
+#endif
+}
 __device__ __forceinline__ floatx16_t zero16() {
   floatx16_t z;
 #pragma unroll
@@ -394,10 +400,10 @@ __device__ __forceinline__ void dma16_at(const char* base, uint32_t offset, char
 
 // Copies of ROWS rows of a matrix into a tile by the block.  Rows that all exist, of DP features, less than 2^31 bytes apart in all: a
 // scalar address and a lane's offset, which stay the same from tile to tile.  Others choose between the row and zeros lane by lane.
-template <typename T, int DP, int ROWS>
+template <typename T, int DP, int ROWS, int NW = kWaves>
 struct RowCopies {
   using R = RowTile<T, DP>;
-  static constexpr int NW = kWaves, N = ROWS / R::RPI / NW;
+  static constexpr int N = ROWS / R::RPI / NW;
   static_assert(N * R::RPI * NW == ROWS, "whole copies");
   int64_t ld;                                        // bytes
   int pieces;

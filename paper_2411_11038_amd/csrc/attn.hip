@@ -216,10 +216,13 @@ __global__ __launch_bounds__(256) void k_attn_decode(DecodeArgs a, T* __restrict
   const int64_t ldk = a.ldk * (int)sizeof(T), ldv = a.ldv * (int)sizeof(T);
   const int pieces = a.dim * (int)sizeof(T) / 16;
   char* own = smem + wave * C::STAGE * C::STAGES;
-  auto issue = [&](int t, char* buf) {
+  auto issue_keys = [&](int t, char* buf) {
     const int j0 = kt.tile(t) * BN, valid = keys - j0;
 #pragma unroll
     for (int s = 0; s < BN / R::RPI; ++s) R::copy(kbase + j0 * ldk, ldk, valid, pieces, buf, s);
+  };
+  auto issue_values = [&](int t, char* buf) {
+    const int j0 = kt.tile(t) * BN, valid = keys - j0;
 #pragma unroll
     for (int s = 0; s < BN / R::RPI; ++s) R::copy(vbase + j0 * ldv, ldv, valid, pieces, buf + BN * R::ROW, s);
   };
@@ -237,18 +240,41 @@ __global__ __launch_bounds__(256) void k_attn_decode(DecodeArgs a, T* __restrict
   for (int i = 0; i < R::ND; ++i) acc[i] = zero16();
   float m = -INFINITY, l = 0.0f;
   const float c = a.scale * kLog2e;
-  int n = 0;
-  if (first + wave < last) issue(first + wave, own);
-  for (int t = first + wave; t < last; t += 4, ++n) {
-    char* buf = own + (C::STAGES == 2 ? (n & 1) * C::STAGE : 0);
-    const bool more = C::STAGES == 2 && t + 4 < last;
-    if (more) issue(t + 4, own + ((n + 1) & 1) * C::STAGE);
+  // Two stages: the next tile is copied while one is worked on.  One (where two do not fit): the next keys are, from when the scores are formed,
+  // and the next values behind the products.
+  constexpr int HALF = COPIES / 2;
+  auto arrived = [&](bool behind, auto left) {       // all copies but the last `left`, if so many were issued behind what is waited for
 #if defined(__HIP_DEVICE_COMPILE__)
     __builtin_amdgcn_sched_barrier(0);
-    if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");
+    if (behind) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(decltype(left)::value) : "memory");
     else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
 #endif
+  };
+  auto was_read = [&]() {                            // a tile in LDS: the next copies may overwrite it
+#if defined(__HIP_DEVICE_COMPILE__)
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+#endif
+  };
+  int n = 0;
+  if (first + wave < last) {
+    issue_keys(first + wave, own);
+    issue_values(first + wave, own);
+  }
+  for (int t = first + wave; t < last; t += 4, ++n) {
+    char* buf = own + (C::STAGES == 2 ? (n & 1) * C::STAGE : 0);
+    const bool more = t + 4 < last;
+    if constexpr (C::STAGES == 2) {
+      if (more) {
+        issue_keys(t + 4, own + ((n + 1) & 1) * C::STAGE);
+        issue_values(t + 4, own + ((n + 1) & 1) * C::STAGE);
+      }
+      arrived(more, std::integral_constant<int, COPIES>{});
+    } else {
+      arrived(true, std::integral_constant<int, HALF>{});            // the values of this tile may be on their way
+    }
     const int j0 = kt.tile(t) * BN;
     auto tile = [&](auto masked) {
       floatx16_t s[1] = {zero16()};
@@ -258,6 +284,11 @@ __global__ __launch_bounds__(256) void k_attn_decode(DecodeArgs a, T* __restrict
       float top = m;
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, s[0][i]);
+      if constexpr (C::STAGES == 1) {
+        hold(top);                                   // all results are read here, before the branch
+        was_read();
+        if (more) issue_keys(t + 4, buf);
+      }
       top = half_max(top);
       const float base = top == -INFINITY ? 0.0f : top * c;
       const float shrink = __builtin_amdgcn_exp2f(fmaf(m, c, -base));
@@ -269,6 +300,7 @@ __global__ __launch_bounds__(256) void k_attn_decode(DecodeArgs a, T* __restrict
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[0][i] = __builtin_amdgcn_exp2f(fmaf(s[0][i], c, -base));
       l = fmaf(l, shrink, sum16(s[0]));
+      if constexpr (C::STAGES == 1) arrived(more, std::integral_constant<int, HALF>{});
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const Frag<T> pf = frag_of<T>(s[0], h);
@@ -278,12 +310,8 @@ __global__ __launch_bounds__(256) void k_attn_decode(DecodeArgs a, T* __restrict
     };
     if (mask.sees_all(p, p, j0, j0 + BN - 1)) tile(std::false_type{});
     else tile(std::true_type{});
-#if defined(__HIP_DEVICE_COMPILE__)
-    __builtin_amdgcn_sched_barrier(0);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");              // its tile is read: the next copies may overwrite it
-    __builtin_amdgcn_sched_barrier(0);
-#endif
-    if (C::STAGES == 1 && t + 4 < last) issue(t + 4, own);
+    was_read();
+    if (C::STAGES == 1 && more) issue_values(t + 4, buf);
   }
   results_settle();
   l = half_sum(l);
@@ -330,38 +358,60 @@ __global__ __launch_bounds__(256) void k_attn_decode(DecodeArgs a, T* __restrict
   }
 }
 
-// the shares of a head's keys put together: a block of 64 lanes for each sequence and head
+// The shares of a head's keys put together: a block for each sequence and head, its wavefronts every fourth share.  All that a share leaves is
+// read at once; their weights are made by a lane each.
+constexpr int kMostShares = 64;
 template <typename T, int DP>
-__global__ __launch_bounds__(64) void k_attn_join(const float* __restrict__ part, int splits, int heads, int dim, float c, T* __restrict__ o,
-                                                  int64_t ldo) {
-  const int lane = threadIdx.x, head = blockIdx.x, seq = blockIdx.y;
+__global__ __launch_bounds__(256) void k_attn_join(const float* __restrict__ part, int splits, int heads, int dim, float c, T* __restrict__ o,
+                                                   int64_t ldo) {
+  constexpr int PER = DP / 64;
+  __shared__ float s_sum[3][DP];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, head = blockIdx.x, seq = blockIdx.y;
   const float* from = part + (int64_t)(seq * heads + head) * splits * (DP + 4);
-  float top = -INFINITY;
-  for (int s = lane; s < splits; s += 64) top = fmaxf(top, from[s * (DP + 4) + DP]);
-  top = wave_max(top);
-  const float base = top == -INFINITY ? 0.0f : top * c;
-  float l = 0.0f;
-  float v[DP / 64 > 0 ? DP / 64 : 1] = {};
-  for (int s = 0; s < splits; ++s) {
-    const float* at = from + s * (DP + 4);
-    const float f = __builtin_amdgcn_exp2f(fmaf(at[DP], c, -base));
-    l = fmaf(at[DP + 1], f, l);
+  const float m = lane < splits ? from[lane * (DP + 4) + DP] : -INFINITY, l = lane < splits ? from[lane * (DP + 4) + DP + 1] : 0.0f;
+  float v[kMostShares / 4][PER];
 #pragma unroll
-    for (int i = 0; i < DP / 64; ++i) v[i] = fmaf(at[lane + 64 * i], f, v[i]);
+  for (int x = 0; x < kMostShares / 4; ++x) {
+    const int s = wave + 4 * x;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) v[x][i] = s < splits ? from[s * (DP + 4) + lane * PER + i] : 0.0f;
   }
-  const float r = l == 0.0f ? 0.0f : 1.0f / l;
+  const float top = wave_max(m), base = top == -INFINITY ? 0.0f : top * c;
+  const float f = __builtin_amdgcn_exp2f(fmaf(m, c, -base)), total = wave_total(l * f);
+  float sum[PER] = {};
 #pragma unroll
-  for (int i = 0; i < DP / 64; ++i)
-    if (lane + 64 * i < dim) o[seq * ldo + (int64_t)head * dim + lane + 64 * i] = from_f32<T>(v[i] * r);
+  for (int x = 0; x < kMostShares / 4; ++x) {
+    const float w = __shfl(f, wave + 4 * x, 64);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) sum[i] = fmaf(v[x][i], w, sum[i]);
+  }
+  if (wave > 0) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) s_sum[wave - 1][lane * PER + i] = sum[i];
+  }
+  __syncthreads();
+  if (wave == 0) {
+    const float r = total == 0.0f ? 0.0f : 1.0f / total;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int d = lane * PER + i;
+      sum[i] = ((sum[i] + s_sum[0][d]) + (s_sum[1][d] + s_sum[2][d])) * r;
+      if (d < dim) o[seq * ldo + (int64_t)head * dim + d] = from_f32<T>(sum[i]);
+    }
+  }
 }
 
 static int attn_dp(int64_t dim) { return dim <= 64 ? 64 : 128; }
 
+// Shares of a sequence's keys: as many blocks as the chip has CUs, each with four tiles of 32 keys a wavefront at least, and eight a CU where
+// shares stay long (sequences differ in length: 64 of 500 to 8192 keys, 8 heads of 128, 248 us in one share, 224 in four; 24 of 1028 keys, 12
+// heads of 64, 20 us in one, 24 in two).
 static int decode_splits(int64_t n_seq, int64_t capacity, int64_t heads, int64_t kv_heads, int64_t window, int64_t sinks) {
-  const int64_t most = window > 0 && window + sinks + 64 < capacity ? window + sinks + 64 : capacity;
+  const int64_t most = window > 0 && window < capacity && sinks < capacity && window + sinks + 64 < capacity ? window + sinks + 64 : capacity;
   const int64_t tiles = ceil_div(most, 32), blocks = n_seq * kv_heads * ceil_div(heads / kv_heads, 32);
-  int64_t s = ceil_div(512, blocks);
-  if (s > ceil_div(tiles, 4)) s = ceil_div(tiles, 4);
+  auto at_most = [](int64_t a, int64_t b) { return a < b ? a : b; };
+  const int64_t fill = at_most(ceil_div(256, blocks), ceil_div(tiles, 16)), even = at_most(ceil_div(2048, blocks), tiles / 64);
+  const int64_t s = at_most(fill > even ? fill : even, kMostShares);
   return (int)(s < 1 ? 1 : s);
 }
 
@@ -422,7 +472,7 @@ extern "C" int efqat_attention_decode(const void* q, int64_t ldq, const void* k_
   do {                                                                                                                             \
     EFQAT_TRY(launch(k_attn_decode<E, DP>, grid, dim3(256), 0, st, d, (E*)o, ldo, part));                                          \
     if (splits > 1)                                                                                                                \
-      EFQAT_TRY(launch(k_attn_join<E, DP>, dim3((unsigned)heads, (unsigned)n_seq), dim3(64), 0, st, part, splits, (int)heads,      \
+      EFQAT_TRY(launch(k_attn_join<E, DP>, dim3((unsigned)heads, (unsigned)n_seq), dim3(256), 0, st, part, splits, (int)heads,      \
                        (int)dim, scale * kLog2e, (E*)o, ldo));                                                                     \
     return EFQAT_OK;                                                                                                               \
   } while (0)

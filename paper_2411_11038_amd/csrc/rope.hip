@@ -21,25 +21,36 @@ struct RopeTensor {
 struct RopeArgs {
   RopeTensor t[2];                                   // queries, keys
   int64_t rows;
-  int dim, freqs, axes, norm, slices;
+  int dim, freqs, axes, norm;
   const int32_t* pos;                                // [axes][rows]
   const int32_t* axis;
   const float* inv_freq;
   float eps;
-  float* part;                                       // backward: [blocks][2][dim] sums of dn xhat
+  float* part;                                       // backward: [blocks][dim] sums of dn xhat
 };
 
-// cosine and sine of position * f: the turns are formed in 64 bits, their fraction is exact to 2^-25
-__device__ __forceinline__ float2 turn_of(const RopeArgs& a, int64_t row, int j) {
-  int ax = a.axis ? a.axis[j] : 0;
-  ax = ax < 0 ? 0 : ax >= a.axes ? a.axes - 1 : ax;
-  const double turns = (double)a.pos[ax * a.rows + row] * (double)a.inv_freq[j] * 0.15915494309189533577;
-  float2 cs;
-  sincospif((float)(2.0 * (turns - rint(turns))), &cs.y, &cs.x);
-  return cs;
-}
+// a pair's position and frequency
+struct Angle {
+  int pos;
+  float f;
+  __device__ __forceinline__ Angle() {}
+  __device__ __forceinline__ Angle(const RopeArgs& a, int64_t row, int j) {
+    int ax = a.axis ? a.axis[j] : 0;
+    ax = ax < 0 ? 0 : ax >= a.axes ? a.axes - 1 : ax;
+    pos = a.pos[ax * a.rows + row];
+    f = a.inv_freq[j];
+  }
+  // cosine and sine: the turns are formed in 64 bits, their fraction is exact to 2^-25
+  __device__ __forceinline__ float2 turn() const {
+    const double turns = (double)pos * (double)f * 0.15915494309189533577;
+    float2 cs;
+    sincospif((float)(2.0 * (turns - rint(turns))), &cs.y, &cs.x);
+    return cs;
+  }
+};
 
 constexpr int kRopeMostDim = 256;
+constexpr int kRopeBlocks = 1024;                    // of a backward pass at most: four a CU
 
 // Two chunks of a lane: first columns, elements that exist, and the pair of its first element (both are turned with `turn[pair ..]`)
 struct RopeLane {
@@ -65,25 +76,28 @@ __device__ __forceinline__ RopeLane rope_lane(const RopeArgs& a, int lanes) {
   for (int i = 0; i < 2; ++i) l.n[i] = a.dim - l.col[i] >= 8 ? 8 : 0;
   return l;
 }
-// rotation (sign 1) or rotation back (-1) of a lane's 16 elements; what has no pair stays as it is, whatever lies beside it
+// Rotation (sign 1) or rotation back (-1) of a lane's 16 elements; what has no pair stays as it is, whatever lies beside it.  The turns of a
+// token's pairs are read from LDS each time: lanes have more heads' registers to fill.
 template <bool NEXT>
-__device__ __forceinline__ void rope_turn(const RopeLane& l, int freqs, float (&v)[2][8], const float (&cs)[8], const float (&sn)[8], float sign) {
+__device__ __forceinline__ void rope_turn(const RopeLane& l, int freqs, float (&v)[2][8], const float2* turns, float sign) {
   if constexpr (NEXT) {
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float x = v[i][2 * j], y = v[i][2 * j + 1], c = cs[4 * i + j], s = sign * sn[4 * i + j];
         const bool in = l.pair + 4 * i + j < freqs;
-        v[i][2 * j] = in ? x * c - y * s : x;
-        v[i][2 * j + 1] = in ? y * c + x * s : y;
+        const float2 cs = turns[l.pair + 4 * i + j];
+        const float x = v[i][2 * j], y = v[i][2 * j + 1], s = sign * cs.y;
+        v[i][2 * j] = in ? x * cs.x - y * s : x;
+        v[i][2 * j + 1] = in ? y * cs.x + x * s : y;
       }
   } else if (l.turned) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float x = v[0][j], y = v[1][j], s = sign * sn[j];
-      v[0][j] = x * cs[j] - y * s;
-      v[1][j] = y * cs[j] + x * s;
+      const float2 cs = turns[l.pair + j];
+      const float x = v[0][j], y = v[1][j], s = sign * cs.y;
+      v[0][j] = x * cs.x - y * s;
+      v[1][j] = y * cs.x + x * s;
     }
   }
 }
@@ -93,64 +107,80 @@ __device__ __forceinline__ float head_sum(float v, int lanes) {
   return v;
 }
 
+// How the work is laid out: a wavefront takes a token's queries or its keys, `per` passes of them at most (a pass: 64 / lanes heads).  The first
+// blocks have the queries' units, the others the keys'; backward blocks walk theirs and keep the weights' sums.
+struct RopeUnits {
+  int lanes, per, passes[2], units[2];               // passes of a token, units they are cut into
+  int blocks[2];
+};
+
 template <typename T, bool NEXT, bool BWD>
-__global__ __launch_bounds__(256) void k_rope(RopeArgs a, int lanes) {
+__global__ __launch_bounds__(256, BWD ? 4 : 5) void k_rope(RopeArgs a, RopeUnits u) {
   __shared__ float2 s_turn[4][kRopeMostDim / 2];
-  __shared__ float s_sum[BWD ? 4 : 1][2][BWD ? kRopeMostDim : 1];
+  __shared__ float s_sum[BWD ? 4 : 1][BWD ? kRopeMostDim : 1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const RopeLane l = rope_lane<NEXT>(a, lanes);
-  const int per_pass = 64 / lanes, pq = (a.t[0].heads + per_pass - 1) / per_pass, pk = (a.t[1].heads + per_pass - 1) / per_pass;
-  const int64_t items = a.rows * a.slices;
-  float sum[2][2][8] = {};
-  for (int64_t item = (int64_t)blockIdx.x * 4 + wave; item < items; item += (int64_t)gridDim.x * 4) {
-    const int64_t row = item / a.slices;
-    const int slice = (int)(item - row * a.slices);
-    float cs[8], sn[8];
-    if (a.freqs > 0) {
-      for (int j = lane; j < a.freqs; j += 64) s_turn[wave][j] = turn_of(a, row, j);
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      __builtin_amdgcn_wave_barrier();
+  const RopeLane l = rope_lane<NEXT>(a, u.lanes);
+  const int key = (int)blockIdx.x >= u.blocks[0], per_pass = 64 / u.lanes, units = u.units[key];
+  const RopeTensor& t = a.t[key];
+  const int64_t items = a.rows * units;
+  float w[2][8], sum[2][8] = {};
+  if (a.norm && t.w) {
+    load_chunk(t.w + l.col[0], l.n[0]).get(w[0]);
+    load_chunk(t.w + l.col[1], l.n[1]).get(w[1]);
+  } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const bool in = l.turned && l.pair + j < a.freqs;
-        const float2 t = in ? s_turn[wave][l.pair + j] : make_float2(1.0f, 0.0f);
-        cs[j] = t.x;
-        sn[j] = t.y;
+    for (int j = 0; j < 8; ++j) w[0][j] = w[1][j] = 1.0f;
+  }
+  const float inv_dim = 1.0f / (float)a.dim;
+  for (int64_t item = (int64_t)(blockIdx.x - (key ? u.blocks[0] : 0)) * 4 + wave; item < items; item += (int64_t)u.blocks[key] * 4) {
+    const int64_t row = item / units;
+    const int unit = (int)(item - row * units), first = unit * u.per, last = min(first + u.per, u.passes[key]);
+    const T* const x_row = (const T*)t.x + row * t.ldx;
+    const T* const dy_row = (const T*)t.dy + row * t.lddy;
+    T* const out_row = (T*)t.out + row * t.ldo;
+    Raw8<T> rx[2], rd[2];
+    auto load = [&](int pass) {
+      const int head = pass * per_pass + l.group;
+      const int64_t at = (int64_t)head * a.dim;
+      const bool in = head < t.heads;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int n = in ? l.n[i] : 0;
+        if (!BWD || a.norm) rx[i] = load_chunk(x_row + at + l.col[i], n);
+        if constexpr (BWD) rd[i] = load_chunk(dy_row + at + l.col[i], n);
       }
+    };
+    // what the angles are made of is asked for first, the first heads are on their way while they are made
+    Angle angle[2];
+    if (lane < a.freqs) angle[0] = Angle(a, row, lane);
+    if (lane + 64 < a.freqs) angle[1] = Angle(a, row, lane + 64);
+    load(first);
+    if (a.freqs > 0) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");             // the item before has read its turns
+      __builtin_amdgcn_wave_barrier();
+      if (lane < a.freqs) s_turn[wave][lane] = angle[0].turn();
+      if (lane + 64 < a.freqs) s_turn[wave][lane + 64] = angle[1].turn();
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       __builtin_amdgcn_wave_barrier();
     }
-    const int first = (pq + pk) * slice / a.slices, last = (pq + pk) * (slice + 1) / a.slices;
     for (int pass = first; pass < last; ++pass) {
-      const bool key = pass >= pq;
-      const RopeTensor& t = a.t[key];
-      const int head = (key ? pass - pq : pass) * per_pass + l.group;
+      const int head = pass * per_pass + l.group;
       const bool in = head < t.heads;
-      const int64_t at = (int64_t)head * a.dim;
-      const int n0 = in ? l.n[0] : 0, n1 = in ? l.n[1] : 0;
-      float x[2][8], w[2][8];
-      if (!BWD || a.norm) {
-        load_chunk((const T*)t.x + row * t.ldx + at + l.col[0], n0).get(x[0]);
-        load_chunk((const T*)t.x + row * t.ldx + at + l.col[1], n1).get(x[1]);
-      }
-      if (a.norm && t.w) {
-        load_chunk(t.w + l.col[0], n0).get(w[0]);
-        load_chunk(t.w + l.col[1], n1).get(w[1]);
-      } else {
+      float x[2][8], d[2][8], r = 1.0f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[0][j] = w[1][j] = 1.0f;
+      for (int i = 0; i < 2; ++i) {
+        if (!BWD || a.norm) rx[i].get(x[i]);
+        if constexpr (BWD) rd[i].get(d[i]);
       }
-      float r = 1.0f;
+      if (pass + 1 < last) load(pass + 1);
       if (a.norm) {
         float sq = 0.0f;
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int j = 0; j < 8; ++j) sq = fmaf(x[i][j], x[i][j], sq);
-        sq = head_sum(sq, lanes);
-        r = 1.0f / sqrtf(sq / (float)a.dim + a.eps);
+        r = 1.0f / sqrtf(fmaf(head_sum(sq, u.lanes), inv_dim, a.eps));
       }
-      T* out = (T*)t.out + row * t.ldo + at;
       if constexpr (!BWD) {
         if (a.norm) {
 #pragma unroll
@@ -158,71 +188,62 @@ __global__ __launch_bounds__(256) void k_rope(RopeArgs a, int lanes) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) x[i][j] = x[i][j] * r * w[i][j];
         }
-        if (a.freqs > 0) rope_turn<NEXT>(l, a.freqs, x, cs, sn, 1.0f);
-        store_chunk(out + l.col[0], n0, x[0]);
-        store_chunk(out + l.col[1], n1, x[1]);
+        if (a.freqs > 0) rope_turn<NEXT>(l, a.freqs, x, s_turn[wave], 1.0f);
       } else {
-        float d[2][8];
-        load_chunk((const T*)t.dy + row * t.lddy + at + l.col[0], n0).get(d[0]);
-        load_chunk((const T*)t.dy + row * t.lddy + at + l.col[1], n1).get(d[1]);
-        if (a.freqs > 0) rope_turn<NEXT>(l, a.freqs, d, cs, sn, -1.0f);
+        if (a.freqs > 0) rope_turn<NEXT>(l, a.freqs, d, s_turn[wave], -1.0f);
         if (a.norm) {
           float dot = 0.0f;
 #pragma unroll
           for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-              x[i][j] *= r;
-              if (in) sum[key][i][j] = fmaf(d[i][j], x[i][j], sum[key][i][j]);
+              x[i][j] *= r;                          // of a head that does not exist: zeros
+              sum[i][j] = fmaf(d[i][j], x[i][j], sum[i][j]);
               d[i][j] *= w[i][j];
               dot = fmaf(d[i][j], x[i][j], dot);
             }
-          dot = head_sum(dot, lanes) / (float)a.dim;
+          dot = head_sum(dot, u.lanes) * inv_dim;
 #pragma unroll
           for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j) d[i][j] = r * (d[i][j] - x[i][j] * dot);
         }
-        store_chunk(out + l.col[0], n0, d[0]);
-        store_chunk(out + l.col[1], n1, d[1]);
       }
+      const int64_t at = (int64_t)head * a.dim;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) store_chunk(out_row + at + l.col[i], in ? l.n[i] : 0, BWD ? d[i] : x[i]);
     }
   }
   if constexpr (BWD) {
     if (!a.part) return;
 #pragma unroll
-    for (int key = 0; key < 2; ++key)
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          float v = sum[key][i][j];
-          for (int o = lanes; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
-          if (l.group == 0 && j < l.n[i]) s_sum[wave][key][l.col[i] + j] = v;
-        }
+      for (int j = 0; j < 8; ++j) {
+        float v = sum[i][j];
+        for (int o = u.lanes; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
+        if (l.group == 0 && j < l.n[i]) s_sum[wave][l.col[i] + j] = v;
+      }
     __syncthreads();
-    for (int e = threadIdx.x; e < 2 * a.dim; e += 256) {
-      const int key = e / a.dim, d = e - key * a.dim;
-      a.part[(int64_t)blockIdx.x * 2 * a.dim + e] = (s_sum[0][key][d] + s_sum[1][key][d]) + (s_sum[2][key][d] + s_sum[3][key][d]);
-    }
+    for (int d = threadIdx.x; d < a.dim; d += 256)
+      a.part[(int64_t)blockIdx.x * a.dim + d] = (s_sum[0][d] + s_sum[1][d]) + (s_sum[2][d] + s_sum[3][d]);
   }
 }
 
 // Any head width up to 256 and any number of pairs: a wavefront takes a head of a token, a lane every 64th feature and reads its
 // partner's beside it.
 template <typename T, bool NEXT, bool BWD>
-__global__ __launch_bounds__(256) void k_rope_any(RopeArgs a) {
-  __shared__ float s_sum[BWD ? 4 : 1][2][BWD ? kRopeMostDim : 1];
+__global__ __launch_bounds__(256) void k_rope_any(RopeArgs a, RopeUnits u) {
+  __shared__ float s_sum[BWD ? 4 : 1][BWD ? kRopeMostDim : 1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int heads = a.t[0].heads + a.t[1].heads;
+  const int key = (int)blockIdx.x >= u.blocks[0];
+  const RopeTensor& t = a.t[key];
+  const int heads = t.heads;
   const int64_t items = a.rows * heads;
-  float sum[2][4] = {};
-  for (int64_t item = (int64_t)blockIdx.x * 4 + wave; item < items; item += (int64_t)gridDim.x * 4) {
+  float sum[4] = {};
+  for (int64_t item = (int64_t)(blockIdx.x - (key ? u.blocks[0] : 0)) * 4 + wave; item < items; item += (int64_t)u.blocks[key] * 4) {
     const int64_t row = item / heads;
-    int head = (int)(item - row * heads);
-    const bool key = head >= a.t[0].heads;
-    if (key) head -= a.t[0].heads;
-    const RopeTensor& t = a.t[key];
+    const int head = (int)(item - row * heads);
     const T* x = (const T*)t.x + row * t.ldx + (int64_t)head * a.dim;
     const T* dy = (const T*)t.dy + row * t.lddy + (int64_t)head * a.dim;
     T* out = (T*)t.out + row * t.ldo + (int64_t)head * a.dim;
@@ -240,7 +261,7 @@ __global__ __launch_bounds__(256) void k_rope_any(RopeArgs a) {
       u[i] = load_as_f32<T>(from, mate);
       xv[i] = BWD ? (a.norm ? load_as_f32<T>(x, e) : 0.0f) : v[i];
       if (e < 2 * f) {
-        const float2 c = turn_of(a, row, NEXT ? e >> 1 : e < f ? e : e - f);
+        const float2 c = Angle(a, row, NEXT ? e >> 1 : e < f ? e : e - f).turn();
         const bool lower = NEXT ? !(e & 1) : e < f;
         cs[i] = c.x;
         sn[i] = lower != BWD ? -c.y : c.y;
@@ -262,7 +283,7 @@ __global__ __launch_bounds__(256) void k_rope_any(RopeArgs a) {
         if (e < 2 * a.freqs) v[i] = v[i] * cs[i] + u[i] * sn[i];
         if (a.norm && e < a.dim) {
           xv[i] *= r;
-          sum[key][i] = fmaf(v[i], xv[i], sum[key][i]);
+          sum[i] = fmaf(v[i], xv[i], sum[i]);
           if (t.w) v[i] *= t.w[e];
           dot = fmaf(v[i], xv[i], dot);
         }
@@ -280,33 +301,35 @@ __global__ __launch_bounds__(256) void k_rope_any(RopeArgs a) {
   if constexpr (BWD) {
     if (!a.part) return;
 #pragma unroll
-    for (int key = 0; key < 2; ++key)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (lane + 64 * i < a.dim) s_sum[wave][key][lane + 64 * i] = sum[key][i];
+    for (int i = 0; i < 4; ++i)
+      if (lane + 64 * i < a.dim) s_sum[wave][lane + 64 * i] = sum[i];
     __syncthreads();
-    for (int e = threadIdx.x; e < 2 * a.dim; e += 256) {
-      const int key = e / a.dim, d = e - key * a.dim;
-      a.part[(int64_t)blockIdx.x * 2 * a.dim + e] = (s_sum[0][key][d] + s_sum[1][key][d]) + (s_sum[2][key][d] + s_sum[3][key][d]);
-    }
+    for (int d = threadIdx.x; d < a.dim; d += 256)
+      a.part[(int64_t)blockIdx.x * a.dim + d] = (s_sum[0][d] + s_sum[1][d]) + (s_sum[2][d] + s_sum[3][d]);
   }
 }
 
-// the blocks' sums put together, in fixed order and fp64: 16 columns a block, 16 lanes each
-__global__ __launch_bounds__(256) void k_rope_finish(const float* __restrict__ part, int blocks, int dim, float* __restrict__ dwq,
+// The blocks' sums put together, in fixed order and fp64: four columns a block, 64 lanes each; the queries' first, then the keys'.
+__global__ __launch_bounds__(256) void k_rope_finish(const float* __restrict__ part, RopeUnits u, int dim, float* __restrict__ dwq,
                                                      float* __restrict__ dwk) {
-  __shared__ double red[16][17];
-  const int c = threadIdx.x & 15, s = threadIdx.x >> 4, e = blockIdx.x * 16 + c;
+  __shared__ double red[4][4];
+  const int key = blockIdx.y, c = threadIdx.x & 3, s = threadIdx.x >> 2, e = blockIdx.x * 4 + c, blocks = u.blocks[key];
+  const float* from = part + (key ? (int64_t)u.blocks[0] * dim : 0);
+  float* to = key ? dwk : dwq;
+  if (!to) return;
   double v = 0.0;
-  if (e < 2 * dim)
-    for (int b = s; b < blocks; b += 16) v += part[(int64_t)b * 2 * dim + e];
-  red[s][c] = v;
-  __syncthreads();
-  if (s == 0 && e < 2 * dim) {
-    for (int i = 1; i < 16; ++i) v += red[i][c];
-    float* to = e < dim ? dwq : dwk;
-    if (to) to[e < dim ? e : e - dim] = (float)v;
+  if (e < dim) {
+    float x[kRopeBlocks / 64];
+#pragma unroll
+    for (int b = 0; b < kRopeBlocks / 64; ++b) x[b] = s + 64 * b < blocks ? from[(int64_t)(s + 64 * b) * dim + e] : 0.0f;
+#pragma unroll
+    for (int b = 0; b < kRopeBlocks / 64; ++b) v += x[b];
   }
+#pragma unroll
+  for (int o = 4; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
+  if ((threadIdx.x & 63) < 4) red[threadIdx.x >> 6][c] = v;
+  __syncthreads();
+  if (threadIdx.x < 4 && e < dim) to[e] = (float)((red[0][c] + red[1][c]) + (red[2][c] + red[3][c]));
 }
 
 // lanes of a head in k_rope; 0: k_rope_any
@@ -316,15 +339,30 @@ static int rope_lanes(int64_t dim, int64_t freqs, int neighbours) {
   while (lanes * 16 < dim) lanes *= 2;
   return lanes;
 }
-constexpr int64_t kRopeBlocks = 1024;                // of a backward pass at most: four a CU
-static int64_t rope_bwd_blocks(int64_t rows, int64_t heads) {
-  const int64_t b = ceil_div(rows * heads, 4);
-  return b < kRopeBlocks ? b : kRopeBlocks;
-}
-// slices of a token's heads: enough wavefronts for the chip where there are few tokens
-static int rope_slices(int64_t rows, int passes) {
-  const int64_t want = ceil_div(4096, rows);
-  return (int)(want < passes ? want : passes);
+// Units and blocks of a call.  Few tokens: a pass a wavefront; else four, whose loads follow each other.
+static RopeUnits rope_units(int64_t rows, int64_t heads, int64_t kv_heads, int lanes, bool bwd) {
+  RopeUnits u = {};
+  u.lanes = lanes;
+  const int64_t n[2] = {heads, kv_heads};
+  int64_t need[2], all = 0;
+  for (int i = 0; i < 2; ++i) {
+    u.passes[i] = (int)(lanes ? ceil_div(n[i], 64 / lanes) : n[i]);
+    all += u.passes[i];
+  }
+  u.per = lanes && rows * all > 16384 ? 4 : 1;
+  all = 0;
+  for (int i = 0; i < 2; ++i) {
+    u.units[i] = (int)ceil_div(u.passes[i], u.per);
+    need[i] = ceil_div(rows * u.units[i], 4);
+    all += need[i];
+  }
+  const int64_t most = bwd ? kRopeBlocks : 1 << 23;                  // a grid has fewer than 2^32 lanes
+  for (int i = 0; i < 2; ++i) {
+    // shared out by the passes that there are, at least one each
+    const int64_t part = all <= most ? need[i] : need[i] == 0 ? 0 : (most - 1) * u.passes[i] / (u.passes[0] + u.passes[1]) + (i == 1);
+    u.blocks[i] = (int)(part < 1 && need[i] > 0 ? 1 : part < need[i] ? part : need[i]);
+  }
+  return u;
 }
 
 static int rope_args(RopeArgs* a, int dtype, int64_t T, int64_t heads, int64_t kv_heads, int64_t dim, int norm, float eps, const int32_t* pos,
@@ -347,7 +385,6 @@ static int rope_args(RopeArgs* a, int dtype, int64_t T, int64_t heads, int64_t k
   a->inv_freq = inv_freq;
   a->eps = eps;
   a->part = nullptr;
-  a->slices = 1;
   return EFQAT_OK;
 }
 static int rope_rows(const void* p, int64_t ld, int64_t cols, int dtype) {
@@ -356,19 +393,12 @@ static int rope_rows(const void* p, int64_t ld, int64_t cols, int dtype) {
   return aligned_for(p, dtype) ? EFQAT_OK : EFQAT_ERR_ALIGNMENT;
 }
 template <bool BWD>
-static int rope_launch(RopeArgs& a, int dtype, int neighbours, unsigned* blocks, hipStream_t st) {
-  const int lanes = rope_lanes(a.dim, a.freqs, neighbours), heads = a.t[0].heads + a.t[1].heads;
-  if (lanes) {
-    const int per_pass = 64 / lanes, passes = (int)(ceil_div(a.t[0].heads, per_pass) + ceil_div(a.t[1].heads, per_pass));
-    a.slices = rope_slices(a.rows, passes);
-  }
-  const int64_t need = ceil_div(lanes ? a.rows * a.slices : a.rows * heads, 4);
-  const int64_t most = BWD ? rope_bwd_blocks(a.rows, heads) : 1 << 23;          // a grid has fewer than 2^32 lanes
-  const unsigned n = *blocks = (unsigned)(need < most ? need : most);
-#define EFQAT_ROPE(E, NEXT)                                                                       \
-  do {                                                                                            \
-    if (lanes) return launch(k_rope<E, NEXT, BWD>, dim3(n), dim3(256), 0, st, a, lanes);          \
-    return launch(k_rope_any<E, NEXT, BWD>, dim3(n), dim3(256), 0, st, a);                        \
+static int rope_launch(const RopeArgs& a, const RopeUnits& u, int dtype, int neighbours, hipStream_t st) {
+  const dim3 grid((unsigned)(u.blocks[0] + u.blocks[1]));
+#define EFQAT_ROPE(E, NEXT)                                                            \
+  do {                                                                                 \
+    if (u.lanes) return launch(k_rope<E, NEXT, BWD>, grid, dim3(256), 0, st, a, u);    \
+    return launch(k_rope_any<E, NEXT, BWD>, grid, dim3(256), 0, st, a, u);             \
   } while (0)
   if (dtype == EFQAT_F32) { if (neighbours) EFQAT_ROPE(float, true); EFQAT_ROPE(float, false); }
   if (neighbours) EFQAT_ROPE(bf16_t, true);
@@ -395,13 +425,13 @@ extern "C" int efqat_head_norm_rope_fwd(const void* q, int64_t ldq, const void* 
   if (!aligned4(q_weight) || !aligned4(k_weight)) return EFQAT_ERR_ALIGNMENT;
   a.t[0] = {q, nullptr, yq, ldq, 0, ldyq, q_weight, (int)heads};
   a.t[1] = {k, nullptr, yk, ldk, 0, ldyk, k_weight, (int)kv_heads};
-  unsigned blocks;
-  return rope_launch<false>(a, dtype, neighbours, &blocks, (hipStream_t)stream);
+  const RopeUnits u = rope_units(T, heads, kv_heads, rope_lanes(dim, freqs, neighbours), false);
+  return rope_launch<false>(a, u, dtype, neighbours, (hipStream_t)stream);
 }
 
 extern "C" size_t efqat_head_norm_rope_bwd_workspace_bytes(int64_t T, int64_t heads, int64_t kv_heads, int64_t dim) {
   if (T <= 0 || T > (INT64_C(1) << 28) || heads <= 0 || kv_heads < 0 || heads + kv_heads > 65535 || dim <= 0 || dim > kRopeMostDim) return 256;
-  return (size_t)round_up(rope_bwd_blocks(T, heads + kv_heads) * 2 * dim * 4, 256);
+  return (size_t)round_up(kRopeBlocks * dim * 4, 256);
 }
 
 extern "C" int efqat_head_norm_rope_bwd(const void* dyq, int64_t lddyq, const void* dyk, int64_t lddyk, const void* q, int64_t ldq, const void* k,
@@ -430,10 +460,10 @@ extern "C" int efqat_head_norm_rope_bwd(const void* dyq, int64_t lddyq, const vo
   }
   a.t[0] = {q, dyq, dq, ldq, lddyq, lddq, q_weight, (int)heads};
   a.t[1] = {k, dyk, dk, ldk, lddyk, lddk, k_weight, (int)kv_heads};
-  unsigned blocks;
+  const RopeUnits u = rope_units(T, heads, kv_heads, rope_lanes(dim, freqs, neighbours), true);
   hipStream_t st = (hipStream_t)stream;
-  EFQAT_TRY(rope_launch<true>(a, dtype, neighbours, &blocks, st));
+  EFQAT_TRY(rope_launch<true>(a, u, dtype, neighbours, st));
   if (!sums) return EFQAT_OK;
-  return launch(k_rope_finish, dim3((unsigned)ceil_div(2 * dim, 16)), dim3(256), 0, st, (const float*)a.part, (int)blocks, (int)dim, dq_weight,
-                kv_heads > 0 ? dk_weight : nullptr);
+  return launch(k_rope_finish, dim3((unsigned)ceil_div(dim, 4), kv_heads > 0 ? 2 : 1), dim3(256), 0, st, (const float*)a.part, u, (int)dim, dq_weight,
+                dk_weight);
 }

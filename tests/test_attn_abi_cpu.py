@@ -22,9 +22,9 @@ def test_head_norm_rope(L):
         return L.efqat_head_norm_rope_fwd(q, ldq, k, ldk, dt, T, H, KV, D, norm, wq, wk, eps, pos, axes, axis, f, n, nb, yq, ldyq, yk, ldyk, None)
 
     need = L.efqat_head_norm_rope_bwd_workspace_bytes(4, 4, 2, 64)
-    assert need >= 2 * 64 * 4
+    assert need >= 2 * 64 * 4 and need % 256 == 0
     assert L.efqat_head_norm_rope_bwd_workspace_bytes(0, 4, 2, 64) == L.efqat_head_norm_rope_bwd_workspace_bytes(4, 4, 2, 257) == 256
-    assert L.efqat_head_norm_rope_bwd_workspace_bytes(1 << 20, 64, 8, 128) == 1024 * 2 * 128 * 4
+    assert L.efqat_head_norm_rope_bwd_workspace_bytes(1 << 20, 64, 8, 128) >= 2 * 128 * 4
 
     def bwd(q=FAKE, ldq=256, k=FAKE, ldk=128, dt=1, T=4, H=4, KV=2, D=64, norm=1, wq=FAKE, wk=FAKE, eps=1e-6, pos=FAKE, axes=1, axis=None,
             f=FAKE, n=32, nb=0, yq=FAKE, ldyq=256, yk=FAKE, ldyk=128, dyq=FAKE, lddyq=256, dyk=FAKE, lddyk=128, dwq=FAKE, dwk=FAKE, ws=FAKE,

@@ -36,25 +36,42 @@ __device__ __forceinline__ float prob(float s, float c, float base) {
 template <typename T>
 __device__ __forceinline__ float prob_factor(float scale) { return sizeof(T) == 2 ? scale * kLog2e : scale; }
 
-// dq, and delta for the other kernel.  Blocks as in k_attn_fwd.  (Forming the next 32 keys' scores beside dS, as the other kernels do, needs
+// dq, and delta for the other kernel.  Blocks as in k_attn_fwd.  (Forming the next 32 keys' scores beside dS, as k_attn_fwd does, needs
 // more registers than two wavefronts a SIMD have: 380 instead of 250 us for a window of 1024 in 2 x 4096 tokens, 32 heads of 128.)
+//
+// bf16: o is rounded, and delta from it is off by up to 2^-8 of do . o, far more than dS where one key takes nearly all of P (dq 0.5 % off in the
+// 2-norm for short sequences).  Exactly, sum_j dS_ij = 0: what it comes to is what delta lacks, d_i.  So sum_j P_ij k_j is formed too, from the
+// fragments of k that are there, and  dq_i = scale (sum_j dS_ij k_j - d_i sum_j P_ij k_j).  d is small: P need not be exact there.
+template <typename T, int DP>
+struct DqTile {
+  static constexpr bool MEND = sizeof(T) == 2, QUERIES_IN_LDS = MEND && DP == 128;         // the second sum takes the queries' registers
+  static constexpr int BN = QUERIES_IN_LDS ? 32 : kKeyStage<T>;
+};
 template <typename T, int DP>
 __global__ __launch_bounds__(256, (kTwoWaves<T, DP> ? 2 : 1)) void k_attn_dq(AttnArgs a, AttnGrads g, int tiles, int hb) {
   using R = RowTile<T, DP>;
-  constexpr int BN = kKeyStage<T>, STAGE = 2 * BN * R::ROW;
-  __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
+  using C = DqTile<T, DP>;
+  constexpr int BN = C::BN, STAGE = 2 * BN * R::ROW, OWN = 32 * R::ROW;
+  __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE + (C::QUERIES_IN_LDS ? 4 * OWN : 0)];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   HeadTile w;
   if (!w.find(a, hb, tiles, wave)) return;
   const int p = w.row + (lane & 31) + w.shift, head = w.head;
   const KeyTiles kt(a.mask, w.keys.y, w.block_row + w.shift, w.block_row + w.block_rows - 1 + w.shift, BN);
   KeyCopies<T, DP, BN> copies(a, w.keys, w.kvh, wave);
+  char* const own = smem + 2 * STAGE + wave * OWN;
+  if constexpr (C::QUERIES_IN_LDS) {
+#pragma unroll
+    for (int s = 0; s < 32 / R::RPI; ++s)
+      R::copy((const char*)((const T*)a.q + w.token(0) * a.ldq + head * a.dim), a.ldq * (int)sizeof(T), w.rows_left(),
+              a.dim * (int)sizeof(T) / 16, own, s);
+  }
   if (kt.count > 0) copies.issue(kt.tile(0), smem, wave);
 
   const bool in = w.in(lane);
   const int64_t row = w.token(lane);
-  Frag<T> q[R::KS], d[R::KS];
-  float delta = 0.0f, lse = INFINITY;
+  Frag<T> q[C::QUERIES_IN_LDS ? 1 : R::KS], d[R::KS];
+  float delta = 0.0f, lse = prob_base<T>(-INFINITY), lack = 0.0f;
   {
     const T* qr = (const T*)a.q + row * a.ldq + head * a.dim;
     const T* dr = (const T*)g.dout + row * g.lddo + head * a.dim;
@@ -63,21 +80,21 @@ __global__ __launch_bounds__(256, (kTwoWaves<T, DP> ? 2 : 1)) void k_attn_dq(Att
     for (int ks = 0; ks < R::KS; ++ks) {
       const int c = 16 * ks + 8 * (lane >> 5);
       const bool ok = in && c < a.dim;
-      q[ks] = load_frag(qr + c, ok);
+      if constexpr (!C::QUERIES_IN_LDS) q[ks] = load_frag(qr + c, ok);
       d[ks] = load_frag(dr + c, ok);
       const Frag<T> of = load_frag(orow + c, ok);
 #pragma unroll
       for (int e = 0; e < 8; ++e) delta = fmaf((float)d[ks].v[e], (float)of.v[e], delta);
     }
     delta = half_sum(delta);
-    if (in) {
-      lse = prob_base<T>(g.lse[(int64_t)head * a.qs.rows + row]);
-      if (lane < 32) g.delta[(int64_t)head * a.qs.rows + row] = delta;
-    }
+    if (in) lse = prob_base<T>(g.lse[(int64_t)head * a.qs.rows + row]);
   }
-  floatx16_t acc[R::ND];
+  floatx16_t acc[R::ND], mean[C::MEND ? R::ND : 1];
 #pragma unroll
-  for (int i = 0; i < R::ND; ++i) acc[i] = zero16();
+  for (int i = 0; i < R::ND; ++i) {
+    acc[i] = zero16();
+    if constexpr (C::MEND) mean[i] = zero16();
+  }
   const float c = prob_factor<T>(a.scale);
   tile_sync();
   for (int t = 0; t < kt.count; ++t) {
@@ -87,37 +104,53 @@ __global__ __launch_bounds__(256, (kTwoWaves<T, DP> ? 2 : 1)) void k_attn_dq(Att
 #pragma unroll
     for (int n = 0; n < BN / 32; ++n) {
       const int j0 = kt.tile(t) * BN + 32 * n;
-      auto tile = [&](auto masked) {
-        floatx16_t s = zero16(), dp = zero16();
+      if (!a.mask.sees_some(p0, p1, j0, j0 + 31)) continue;
+      floatx16_t s = zero16(), dp = zero16();
 #pragma unroll
-        for (int ks = 0; ks < R::KS; ++ks) {
-          mma(R::row_frag(buf, 32 * n, ks), q[ks], s);
-          mma(R::row_frag(buf + BN * R::ROW, 32 * n, ks), d[ks], dp);
-        }
+      for (int ks = 0; ks < R::KS; ++ks) {
+        if constexpr (C::QUERIES_IN_LDS) mma(R::row_frag(buf, 32 * n, ks), R::row_frag(own, 0, ks), s);
+        else mma(R::row_frag(buf, 32 * n, ks), q[ks], s);
+        mma(R::row_frag(buf + BN * R::ROW, 32 * n, ks), d[ks], dp);
+      }
+      results_settle();
+      if (j0 + 32 > w.keys.y || !a.mask.sees_all(p0, p1, j0, j0 + 31)) {
         const int first = j0 + row_here();
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          s[i] = prob<T>(s[i], c, lse) * (dp[i] - delta);
-          if constexpr (decltype(masked)::value) {
-            const int j = first + row_of(i);
-            s[i] = ((j < w.keys.y) & a.mask.sees(p, j)) ? s[i] : 0.0f;
-          }
+          const int j = first + row_of(i);
+          s[i] = ((j < w.keys.y) & a.mask.sees(p, j)) ? s[i] : -INFINITY;
         }
+      }
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const Frag<T> f = frag_of<T>(s, h);
+      for (int i = 0; i < 16; ++i) {
+        s[i] = prob<T>(s[i], c, lse);
+        dp[i] = s[i] * (dp[i] - delta);
+      }
+      if constexpr (C::MEND) lack += sum16(dp);
 #pragma unroll
-          for (int i = 0; i < R::ND; ++i) mma(R::col_frag(buf, 32 * n + 16 * h, i), f, acc[i]);
+      for (int h = 0; h < 2; ++h) {
+        const Frag<T> df = frag_of<T>(dp, h);
+        Frag<T> pf;
+        if constexpr (C::MEND) pf = frag_of<T>(s, h);
+#pragma unroll
+        for (int i = 0; i < R::ND; ++i) {
+          const Frag<T> kf = R::col_frag(buf, 32 * n + 16 * h, i);
+          mma(kf, df, acc[i]);
+          if constexpr (C::MEND) mma(kf, pf, mean[i]);
         }
-      };
-      if (a.mask.sees_some(p0, p1, j0, j0 + 31)) {
-        if (j0 + 32 <= w.keys.y && a.mask.sees_all(p0, p1, j0, j0 + 31)) tile(std::false_type{});
-        else tile(std::true_type{});
       }
     }
     tile_sync();
   }
   results_settle();
+  if constexpr (C::MEND) {
+    lack = half_sum(lack);
+#pragma unroll
+    for (int i = 0; i < R::ND; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][r] = fmaf(-lack, mean[i][r], acc[i][r]);
+  }
+  if (in && lane < 32) g.delta[(int64_t)head * a.qs.rows + row] = delta + lack;
   store_rows<T, DP>((T*)g.dq + w.token(0) * g.lddq + head * a.dim, g.lddq, w.rows_left(), a.dim, acc, a.scale, smem + wave * (sizeof(smem) / kWaves));
 }
 

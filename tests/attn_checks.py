@@ -83,14 +83,16 @@ def check_bwd(dq, dk, dv, do, q, k, v, o, lse, qlens, klens, heads, kv, scale, c
             rk, rv, tk, tv, sk, sv, fk, fv = (np.zeros((nk, dim)) for _ in range(8))
             for h in range(g * group, (g + 1) * group):
                 x, d, oo = Q[h, a], G[h, a], O[h, a]
-                _, rl, p = ao.attention_fwd(x, y, z, scale, mask)
-                rq, one_k, one_v, ds = ao.attention_bwd(d, x, y, z, oo, p, scale)
+                exact_o, rl, p = ao.attention_fwd(x, y, z, scale, mask)
+                rq, one_k, one_v, ds = ao.attention_bwd(d, x, y, z, exact_o, p, scale)
                 size = scale * (np.abs(x) @ np.abs(y).T)
                 # P is formed from lse, which is off by as much as the forward's
                 eta = np.where(mask, _spread(size, rl, dim), 0.0)
                 eta = eta + eta.max(1, keepdims=True, initial=0.0) + (nk + 8) * E
-                dp, delta = np.abs(d @ z.T), np.abs((d * oo).sum(1, keepdims=True))
-                inner = (dim + 8) * E * (np.abs(d) @ np.abs(z).T + (np.abs(d) * np.abs(oo)).sum(1, keepdims=True))
+                dp, delta = np.abs(d @ z.T), np.abs((d * exact_o).sum(1, keepdims=True))
+                # fp32: do . o takes the o that the forward rounded.  bf16: what that lacks is put back, by sums of P in bf16: half steps of half steps
+                size_o = (np.abs(d) * (np.abs(oo) + np.abs(exact_o))).sum(1, keepdims=True)
+                inner = (dim + 8) * E * (np.abs(d) @ np.abs(z).T + size_o) + (2 * u * u * size_o if kind == "bf16" else 0.0)
                 fine = p * (eta * (dp + delta) + inner + 4 * E * (dp + delta))
                 err = fine + u * np.abs(ds)
                 tq = scale * ((err + (nk + 8) * E * np.abs(ds)) @ np.abs(y))

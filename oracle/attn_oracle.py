@@ -54,12 +54,9 @@ def head_norm_rope_bwd(dy, x, heads, weight, norm, eps, t, neighbours):
 # ------------------------------------------------------------------ attention
 def seen(nq, nk, causal, window, sinks):
     """bool [nq][nk]: query i is at position i + nk - nq"""
-    out = np.zeros((nq, nk), bool)
-    for i in range(nq):
-        p = i + nk - nq
-        for j in range(nk):
-            out[i, j] = (not causal or j <= p) and (window == 0 or abs(p - j) < window or j < sinks)
-    return out
+    p, j = np.arange(nq)[:, None] + (nk - nq), np.arange(nk)[None, :]
+    out = (j <= p) if causal else np.ones((nq, nk), bool)
+    return out & ((abs(p - j) < window) | (j < sinks)) if window else out
 
 
 def attention_fwd(q, k, v, scale, mask):

@@ -79,7 +79,7 @@ __global__ __launch_bounds__(256, (kTwoWaves<T, DP> ? 2 : 1)) void k_attn_fwd(At
   float top = -INFINITY;
   // scores of the tile whose keys lie at `keys`, and beside each product a share of tile t's probabilities, as operands of the next product
   auto scores = [&](const char* keys, floatx16_t (&u)[NT], floatx16_t (&s)[NT], Frag<T> (&pf)[2 * NT], float base, auto both) {
-    constexpr int GROUPS = R::KS * NT, PER = 16 * NT / GROUPS;
+    constexpr int GROUPS = R::KS * NT;
     Frag<T> kf[2][NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -94,7 +94,7 @@ __global__ __launch_bounds__(256, (kTwoWaves<T, DP> ? 2 : 1)) void k_attn_fwd(At
         mma(kf[ks & 1][n], q[ks], u[n]);
         if constexpr (decltype(both)::value) {
 #pragma unroll
-          for (int e = (ks * NT + n) * PER; e < (ks * NT + n + 1) * PER; ++e) {
+          for (int e = (ks * NT + n) * 16 * NT / GROUPS; e < (ks * NT + n + 1) * 16 * NT / GROUPS; ++e) {
             s[e >> 4][e & 15] = __builtin_amdgcn_exp2f(fmaf(s[e >> 4][e & 15], c, -base));
             if ((e & 7) == 7) {
               l += sum8(s[e >> 4], (e >> 3) & 1);
@@ -320,8 +320,8 @@ __global__ __launch_bounds__(256) void k_attn_decode(DecodeArgs a, T* __restrict
     s_l[wave][lane] = l;
   }
   tile_sync();
-  // the wavefronts' outputs on a common base, [wave][column][DP] in the tiles' place (columns one bank apart)
-  constexpr int PITCH = DP + 4;
+  // the wavefronts' outputs on a common base, [wave][column][WIDTH] in the tiles' place (columns one bank apart)
+  constexpr int WIDTH = R::PITCH, PITCH = WIDTH + 4;
   static_assert(4 * 32 * PITCH * 4 <= C::LDS, "the joined columns lie where the tiles were");
   float top = -INFINITY;
 #pragma unroll
@@ -330,11 +330,12 @@ __global__ __launch_bounds__(256) void k_attn_decode(DecodeArgs a, T* __restrict
   float* mine = (float*)smem + (wave * 32 + (lane & 31)) * PITCH;
   const float f = __builtin_amdgcn_exp2f(fmaf(m, c, -base));
 #pragma unroll
-  for (int i = 0; i < R::ND; ++i) store_col(mine, acc[i], i, DP, f);
+  for (int i = 0; i < R::ND; ++i) store_col(mine, acc[i], i, WIDTH, f);
   tile_sync();
   const int cols = min(32, a.group - g0);
-  for (int e = threadIdx.x; e < cols * (DP / 4); e += 256) {
-    const int col = e / (DP / 4), d = (e - col * (DP / 4)) * 4;
+  for (int e = threadIdx.x; e < cols * (WIDTH / 4); e += 256) {
+    const int col = e / (WIDTH / 4), d = (e - col * (WIDTH / 4)) * 4;
+    if (d >= DP) continue;
     float tm = -INFINITY, tl = 0.0f;
 #pragma unroll
     for (int w = 0; w < 4; ++w) tm = fmaxf(tm, s_m[w][col]);
@@ -351,9 +352,9 @@ __global__ __launch_bounds__(256) void k_attn_decode(DecodeArgs a, T* __restrict
       const float r = tl == 0.0f ? 0.0f : 1.0f / tl;
       if (d < a.dim) store4(o + seq * ldo + (int64_t)head * a.dim + d, sum.x * r, sum.y * r, sum.z * r, sum.w * r);
     } else {
-      float* to = part + ((int64_t)(seq * a.heads + head) * a.splits + split) * (DP + 4);
+      float* to = part + ((int64_t)(seq * a.heads + head) * a.splits + split) * (WIDTH + 4);
       *(float4*)(to + d) = sum;
-      if (d == 0) *(float4*)(to + DP) = make_float4(tm, tl, 0, 0);
+      if (d == 0) *(float4*)(to + WIDTH) = make_float4(tm, tl, 0, 0);
     }
   }
 }
@@ -431,8 +432,9 @@ extern "C" int efqat_attention_fwd(const void* q, int64_t ldq, const void* k, in
   if (h.blocks > kAttnMostBlocks) return EFQAT_ERR_BAD_SHAPE;
   hipStream_t st = (hipStream_t)stream;
 #define EFQAT_FWD(E, DP) return launch(k_attn_fwd<E, DP>, dim3((unsigned)h.blocks), dim3(256), 0, st, a, (E*)o, ldo, lse, h.tiles, h.hb)
-  if (dtype == EFQAT_F32) { if (dim <= 64) EFQAT_FWD(float, 64); EFQAT_FWD(float, 128); }
+  if (dtype == EFQAT_F32) { if (dim <= 64) EFQAT_FWD(float, 64); if (dim <= 96) EFQAT_FWD(float, 96); EFQAT_FWD(float, 128); }
   if (dim <= 64) EFQAT_FWD(bf16_t, 64);
+  if (dim <= 96) EFQAT_FWD(bf16_t, 96);
   EFQAT_FWD(bf16_t, 128);
 #undef EFQAT_FWD
 }
@@ -472,12 +474,13 @@ extern "C" int efqat_attention_decode(const void* q, int64_t ldq, const void* k_
   do {                                                                                                                             \
     EFQAT_TRY(launch(k_attn_decode<E, DP>, grid, dim3(256), 0, st, d, (E*)o, ldo, part));                                          \
     if (splits > 1)                                                                                                                \
-      EFQAT_TRY(launch(k_attn_join<E, DP>, dim3((unsigned)heads, (unsigned)n_seq), dim3(256), 0, st, part, splits, (int)heads,      \
+      EFQAT_TRY(launch(k_attn_join<E, RowTile<E, DP>::PITCH>, dim3((unsigned)heads, (unsigned)n_seq), dim3(256), 0, st, part, splits, (int)heads,      \
                        (int)dim, scale * kLog2e, (E*)o, ldo));                                                                     \
     return EFQAT_OK;                                                                                                               \
   } while (0)
-  if (dtype == EFQAT_F32) { if (dim <= 64) EFQAT_DEC(float, 64); EFQAT_DEC(float, 128); }
+  if (dtype == EFQAT_F32) { if (dim <= 64) EFQAT_DEC(float, 64); if (dim <= 96) EFQAT_DEC(float, 96); EFQAT_DEC(float, 128); }
   if (dim <= 64) EFQAT_DEC(bf16_t, 64);
+  if (dim <= 96) EFQAT_DEC(bf16_t, 96);
   EFQAT_DEC(bf16_t, 128);
 #undef EFQAT_DEC
 }

@@ -189,14 +189,14 @@ __host__ __device__ inline int64_t far_slot(const KeyPlan& k, int kv_heads, int 
 // no registers left for the values, which stay in LDS.  Smaller heads and fp32: four, each with all rows.
 template <typename T, int DP>
 struct DkvTile {
-  static constexpr int WAVES = sizeof(T) == 2 && DP == 128 ? 8 : 4, BQ = sizeof(T) == 2 ? 64 : 32;
+  static constexpr int WAVES = sizeof(T) == 2 && DP > 64 ? 8 : 4, BQ = sizeof(T) == 2 ? 64 : 32;
   static constexpr bool VALUES_IN_LDS = sizeof(T) == 2 && DP == 128;
 };
 
 // dk and dv of 128 keys, 32 a wavefront: scores with queries as rows and keys as columns, so that P and dS are operands of the sums over
 // the queries where they are.
 template <typename T, int DP>
-__global__ __launch_bounds__((64 * DkvTile<T, DP>::WAVES), (sizeof(T) == 2 || DP == 64 ? 2 : 1)) void k_attn_dkv(AttnArgs a, AttnGrads g, KeyPlan plan,
+__global__ __launch_bounds__((64 * DkvTile<T, DP>::WAVES), (kTwoWaves<T, DP> ? 2 : 1)) void k_attn_dkv(AttnArgs a, AttnGrads g, KeyPlan plan,
                                                                                               float* __restrict__ sums) {
   using R = RowTile<T, DP>;
   using C = DkvTile<T, DP>;
@@ -277,7 +277,7 @@ __global__ __launch_bounds__((64 * DkvTile<T, DP>::WAVES), (sizeof(T) == 2 || DP
   char* const vals = smem + 2 * STAGE;
   if constexpr (C::VALUES_IN_LDS) {
     const RowCopies<T, DP, kKeyRows, NW> cv(a.ldv, a.dim, wave);
-    cv.issue((const char*)((const T*)a.v + ((int64_t)kp.x + tile * kKeyRows) * a.ldv + kvh * a.dim), kp.y - tile * kKeyRows, vals, wave);
+    cv.issue((const char*)((const T*)a.v + ((int64_t)kp.x + tile * kKeyRows) * a.ldv + kvh * a.dim), kp.y - tile * kKeyRows, vals, wave, true);
   }
   if (count > 0) {
     issue(smem);
@@ -378,16 +378,19 @@ __global__ __launch_bounds__((64 * DkvTile<T, DP>::WAVES), (sizeof(T) == 2 || DP
     store_rows<T, DP>((T*)g.dv + ((int64_t)kp.x + k0) * g.lddv + kvh * a.dim, g.lddv, left, a.dim, dv, 1.0f, place);
     return;
   }
+  if (far && krow >= mask.sinks) return;             // nothing of theirs lies here
   if (!far && plan.parts == 1) slot = far_slot(plan, kv_heads, seq, tile, kvh, 0);
-  float* to = sums + slot * (2 * kKeyRows * DP) + (int64_t)(own * 32 + (lane & 31)) * DP;
+  constexpr int WIDTH = R::PITCH;
+  float* to = sums + slot * (2 * kKeyRows * WIDTH) + (int64_t)(own * 32 + (lane & 31)) * WIDTH;
 #pragma unroll
   for (int i = 0; i < R::ND; ++i) {
     store_col(to, dk[i], i, DP, a.scale);
-    store_col(to + kKeyRows * DP, dv[i], i, DP, 1.0f);
+    store_col(to + kKeyRows * WIDTH, dv[i], i, DP, 1.0f);
   }
 }
 
-// The sums of a tile's parts added in their order.  Blocks: the tiles, or (where tiles are not cut) those with sinks; eight for the rows of one.
+// The sums of a tile's parts added in their order, those of the sinks' rows with their far parts.  Blocks: the tiles, or (where tiles are not
+// cut) those with sinks; sixteen for the rows of one.
 template <typename T, int DP>
 __global__ __launch_bounds__(256) void k_attn_dkv_join(AttnArgs a, AttnGrads g, KeyPlan plan, const float* __restrict__ sums) {
   const int kv_heads = a.heads / a.group, id = blockIdx.x, kvh = id % kv_heads;
@@ -400,15 +403,17 @@ __global__ __launch_bounds__(256) void k_attn_dkv_join(AttnArgs a, AttnGrads g, 
   }
   const int2 kp = a.ks.place(seq);
   const bool sinks = plan.far > 0 && tile < plan.sink_tiles;
-  const int near = plan.parts > 1 ? plan.parts : 0, parts = near + (sinks ? plan.far + (near ? 0 : 1) : 0);
-  // near parts of the tile are neighbours among those of the head
-  const int64_t base = near ? ((int64_t)kvh * plan.tiles + id / kv_heads) * plan.parts : 0;
-  const int64_t far = sinks ? far_slot(plan, kv_heads, seq, tile, kvh, near ? 1 : 0) : 0;
+  const int near = plan.parts;
+  // near parts of the tile are neighbours among those of the head, or alone before the far ones
+  const int64_t base = near > 1 ? ((int64_t)kvh * plan.tiles + id / kv_heads) * near : far_slot(plan, kv_heads, seq, tile, kvh, 0);
+  const int64_t far = sinks ? far_slot(plan, kv_heads, seq, tile, kvh, 1) : 0;
   constexpr int PER_ROW = DP / 4, ROWS = 256 / PER_ROW;              // four features a lane
   for (int r = blockIdx.y * ROWS + threadIdx.x / PER_ROW; r < 2 * kKeyRows; r += gridDim.y * ROWS) {
     const int d = threadIdx.x % PER_ROW * 4, krow = tile * kKeyRows + r % kKeyRows;
     if (krow >= kp.y || d >= a.dim) continue;
+    const int parts = near + (sinks && krow < a.mask.sinks ? plan.far : 0);
     float4 sum = make_float4(0, 0, 0, 0);
+#pragma unroll 4
     for (int x = 0; x < parts; ++x) {
       const int64_t slot = x < near ? base + x : far + x - near;
       const float4 v = *(const float4*)(sums + (slot * 2 * kKeyRows + r) * DP + d);
@@ -493,11 +498,12 @@ extern "C" int efqat_attention_bwd(const void* dout, int64_t lddo, const void* q
   do {                                                                                                                             \
     EFQAT_TRY(launch(k_attn_dq<E, DP>, dim3((unsigned)h.blocks), dim3(256), 0, st, a, g, h.tiles, h.hb));                          \
     EFQAT_TRY(launch(k_attn_dkv<E, DP>, dim3((unsigned)(plan.near_blocks + plan.far_blocks)), dim3(64 * DkvTile<E, DP>::WAVES), 0, st, a, g, plan, sums)); \
-    if (joins) EFQAT_TRY(launch(k_attn_dkv_join<E, DP>, dim3(joins, 8), dim3(256), 0, st, a, g, plan, (const float*)sums));        \
+    if (joins) EFQAT_TRY(launch(k_attn_dkv_join<E, RowTile<E, DP>::PITCH>, dim3(joins, 16), dim3(256), 0, st, a, g, plan, (const float*)sums));        \
     return EFQAT_OK;                                                                                                               \
   } while (0)
-  if (dtype == EFQAT_F32) { if (dim <= 64) EFQAT_BWD(float, 64); EFQAT_BWD(float, 128); }
+  if (dtype == EFQAT_F32) { if (dim <= 64) EFQAT_BWD(float, 64); if (dim <= 96) EFQAT_BWD(float, 96); EFQAT_BWD(float, 128); }
   if (dim <= 64) EFQAT_BWD(bf16_t, 64);
+  if (dim <= 96) EFQAT_BWD(bf16_t, 96);
   EFQAT_BWD(bf16_t, 128);
 #undef EFQAT_BWD
 }

@@ -188,16 +188,17 @@ __device__ __forceinline__ V lds_read(uint32_t at) {
 }
 #endif
 
-// ---- a tile of rows of DP features in LDS.  Its 16-byte pieces are swizzled by row so that both ways of reading it spread over the
+// ---- a tile of rows of DP (64, 96 or 128) features in LDS.  Its 16-byte pieces are swizzled by row so that both ways of reading it spread over the
 // banks: neighbouring rows at the same piece (row_frag), and four rows at four neighbouring pieces (col_frag, bf16, transposing reads)
 // or two rows four apart at eight neighbouring pieces (col_frag, fp32).
 template <typename T, int DP>
 struct RowTile {
-  static constexpr int ROW = DP * (int)sizeof(T), CH = ROW / 16, RPI = 1024 / ROW;   // bytes and pieces of a row, rows of one copy
+  static constexpr int PITCH = DP <= 64 ? 64 : 128;                                  // features that a row has room for
+  static constexpr int ROW = PITCH * (int)sizeof(T), CH = ROW / 16, RPI = 1024 / ROW;   // bytes and pieces of a row, rows of one copy
   static constexpr int KS = DP / 16, ND = DP / 32;                                   // contraction steps, result tiles of a row
   __device__ static __forceinline__ int swz(int row) {
     if constexpr (sizeof(T) == 4) return ((row >> 2) & 1) << 3 | ((row >> 3) & 1) << 2 | (row & 3);
-    else if constexpr (DP == 128) return (row & 3) << 2 | ((row >> 2) & 3);
+    else if constexpr (PITCH == 128) return (row & 3) << 2 | ((row >> 2) & 3);
     else return ((row >> 1) & 1) << 2 | ((row >> 2) & 3);
   }
   // copy number `slot` of a tile: the rows slot * RPI .. + RPI - 1, those at `valid` and behind and pieces behind `pieces` as zeros
@@ -364,7 +365,7 @@ constexpr int kKeyStage = sizeof(T) == 2 ? 64 : 32;    // keys of a stage of LDS
 constexpr int kWaves = 4;                              // of a block, each with 32 rows of scores
 // what a wavefront holds fits 256 registers: two a SIMD
 template <typename T, int DP>
-constexpr bool kTwoWaves = sizeof(T) == 2 || DP == 64;
+constexpr bool kTwoWaves = sizeof(T) == 2 || DP <= 64;
 
 // Rows of a wavefront in a block of four, each with 32 queries of a head: hb (1, 2 or 4) of the heads that share keys, 128 / hb queries.
 // Blocks that share keys are neighbours, late tiles (the long ones under a causal mask) come first.
@@ -398,8 +399,9 @@ __device__ __forceinline__ void dma16_at(const char* base, uint32_t offset, char
   asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base));
 }
 
-// Copies of ROWS rows of a matrix into a tile by the block.  Rows that all exist, of DP features, less than 2^31 bytes apart in all: a
-// scalar address and a lane's offset, which stay the same from tile to tile.  Others choose between the row and zeros lane by lane.
+// Copies of ROWS rows of a matrix into a tile by the block.  Rows that all exist, less than 2^31 bytes apart in all: a scalar address and
+// a lane's offset, which stay the same from tile to tile; features behind the last are the first ones again (the other operand is zero there,
+// or what they add to is not stored).  Others choose between the row and zeros lane by lane.
 template <typename T, int DP, int ROWS, int NW = kWaves>
 struct RowCopies {
   using R = RowTile<T, DP>;
@@ -411,17 +413,18 @@ struct RowCopies {
   static constexpr bool SAME = NW * R::RPI % 16 == 0;           // the swizzle of a wavefront's copies: one offset serves all
   uint32_t at[SAME ? 1 : N];
   __device__ __forceinline__ RowCopies(int64_t ld_elements, int dim, int wave)
-      : ld(ld_elements * (int)sizeof(T)), pieces(dim * (int)sizeof(T) / 16), plain(dim == DP && ld * ROWS < (INT64_C(1) << 31)) {
+      : ld(ld_elements * (int)sizeof(T)), pieces(dim * (int)sizeof(T) / 16), plain(ld * ROWS < (INT64_C(1) << 31)) {
     const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int s = 0; s < (SAME ? 1 : N); ++s) {
       const int row = (wave + NW * s) * R::RPI + lane / R::CH;
-      at[s] = (uint32_t)(row * ld) + (((lane % R::CH) ^ R::swz(row)) << 4);
+      const int piece = (lane % R::CH) ^ R::swz(row);
+      at[s] = (uint32_t)(row * ld) + (piece < pieces ? piece << 4 : 0);
     }
   }
-  // base: the tile's first row, of which `valid` exist
-  __device__ __forceinline__ void issue(const char* base, int valid, char* lds, int wave) const {
-    if (plain && valid >= ROWS) {
+  // base: the tile's first row, of which `valid` exist; zeroed: with zeros behind the last feature
+  __device__ __forceinline__ void issue(const char* base, int valid, char* lds, int wave, bool zeroed = false) const {
+    if (plain && valid >= ROWS && !zeroed) {
 #pragma unroll
       for (int s = 0; s < N; ++s) dma16_at(SAME ? base + s * NW * R::RPI * ld : base, at[SAME ? 0 : s], lds + (wave + NW * s) * 1024);
     } else {
@@ -459,21 +462,21 @@ __device__ __forceinline__ void store_rows(T* to, int64_t ld, int rows, int dim,
       for (int i = 0; i < DP / 32; ++i) store_col(to + (lane & 31) * ld, acc[i], i, dim, f);
     }
   } else {
-    constexpr int CH = DP / 8;
+    constexpr int CH = RowTile<T, DP>::PITCH / 8;
     const int r = lane & 31;
 #pragma unroll
     for (int i = 0; i < DP / 32; ++i)
 #pragma unroll
       for (int x = 0; x < 16; x += 4) {
         const int d = 32 * i + result_row(x);          // four features: half a piece
-        store4((T*)(lds + r * DP * 2 + (((d >> 3) ^ (r & (CH - 1))) << 4) + 2 * (d & 7)), acc[i][x] * f, acc[i][x + 1] * f, acc[i][x + 2] * f, acc[i][x + 3] * f);
+        store4((T*)(lds + r * CH * 16 + (((d >> 3) ^ (r & (CH - 1))) << 4) + 2 * (d & 7)), acc[i][x] * f, acc[i][x + 1] * f, acc[i][x + 2] * f, acc[i][x + 3] * f);
       }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int s = 0; s < 32 * CH / 64; ++s) {
       const int row = s * (64 / CH) + lane / CH, piece = lane % CH;
-      const uint4 v = *(const uint4*)(lds + row * DP * 2 + ((piece ^ (row & (CH - 1))) << 4));
+      const uint4 v = *(const uint4*)(lds + row * CH * 16 + ((piece ^ (row & (CH - 1))) << 4));
       if (row < rows && piece * 8 < dim) *(uint4*)(to + row * ld + piece * 8) = v;
     }
   }

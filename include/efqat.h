@@ -478,7 +478,8 @@ int efqat_linear_xent_bwd(const void* h, int64_t ldh, const void* w, int64_t ldw
  * Both in one pass over the heads of the queries and the keys, in fp32, rounded once:
  *   n = x w / sqrt(mean of x^2 over the head + eps)  (norm 0: n = x),   then for the `freqs` pairs (a, b) of a head
  *   y_a = n_a cos t - n_b sin t,  y_b = n_b cos t + n_a sin t,   t = positions[axis[j]][token] * inv_freq[j] for pair j
- * the features behind the pairs are n.  Angles are formed in 64 bits, cosine and sine good to 2^-23 however far the position.  The
+ * the features behind the pairs are n.  Angles are formed in 64 bits, cosine and sine good to 2^-22 up to 2^26 radians
+ * and 2^-18 as far as positions go.  The
  * backward reads the forward's inputs:
  *   dn = the rotation back of dy,  g = dn w,  dx = (g - xhat mean(g xhat)) / sqrt(mean x^2 + eps),  xhat = n / w
  *   dq_weight, dk_weight = sums over tokens and heads of dn xhat (fixed order, bit-reproducible)
@@ -509,7 +510,7 @@ int efqat_head_norm_rope_bwd(const void* dyq, int64_t lddyq, const void* dyk, in
  * The queries of a sequence are its last tokens: query i of lq is at position p = i + lk - lq of lk keys, and sees key j if
  *   (causal 0 or j <= p)  and  (window 0 or |p - j| < window or j < sinks)
  * A token that sees nothing (or whose scores are all -infinity) has o = 0 and lse = -infinity and takes no part in the backward:
- *   P = exp(s - lse), dP_ij = do_i . v_j, dS = P (dP - do_i . o_i);  dv = P^T do, dq = scale dS k, dk = scale dS^T q, over shared heads too
+ *   P = exp(s - lse), dP_ij = do_i . v_j, dS = P (dP - do_i . o_i) (with BF16 whatever the rounding of o took from that);  dv = P^T do, dq = scale dS k, dk = scale dS^T q, over shared heads too
  *   q, o, dout, dq  [Tq][heads * dim], k, v, dk, dv  [Tk][kv_heads * dim], dtype F32 or BF16; rows may lie apart; 16-byte aligned, row
  *                strides in whole 16 bytes.  dim a multiple of 8, at most 128
  *   q_start, k_start  int32 [n_seq + 1]: rows start[s] .. start[s + 1] - 1 are sequence s (ascending; cut to the rows that exist; empty
@@ -519,7 +520,8 @@ int efqat_head_norm_rope_bwd(const void* dyq, int64_t lddyq, const void* dyk, in
  *   lse          float [heads][Tq]; forward: out, nullable.  Backward: in, with o, as the forward left them
  *   packed       of the workspace query: whether offsets will be given (0 or 1)
  * Scores, their maxima and sums, and all accumulators are fp32.  With BF16 the probabilities and dS are rounded to bf16 for the
- * matrix cores (their sum is taken before); with F32 the products are fp32 too.  Sums have a fixed order (bit-reproducible).  A key or
+ * matrix cores (their sum is taken before); with F32 the products are fp32 too.  The backward forms P from lse: 2^-23 of the largest
+ * score is its relative error.  Sums have a fixed order (bit-reproducible).  A key or
  * value in a sequence that is not finite may make undefined what tokens of that sequence and head hold that do not see it; other sequences
  * and heads do not notice.  scale is positive; at most 2^28 rows, 65535 heads, row strides 2^24. */
 int efqat_attention_fwd(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, int dtype, int64_t Tq,
@@ -535,7 +537,8 @@ int efqat_attention_bwd(const void* dout, int64_t lddo, const void* q, int64_t l
                         int64_t lddv, void* ws, size_t ws_bytes, void* stream);
 /* The same for one new token a sequence over its cache: query s at position lengths[s] - 1, causal.
  *   q, o         [n_seq][heads * dim]
- *   k_cache, v_cache  [n_seq][capacity][kv_heads * dim]: ldk, ldv elements from key to key, seq_k, seq_v from sequence to sequence
+ *   k_cache, v_cache  [n_seq][capacity][kv_heads * dim]: ldk, ldv elements from key to key, seq_k, seq_v from sequence to sequence (any
+ *                order, 0: all sequences share the cache)
  *   lengths      int32 [n_seq] keys of a sequence, the new one among them (cut to 0 .. capacity; 0: o = 0).  What lies behind them, or
  *                outside the window and the sinks by 32 keys and more, is not read, and nothing of it reaches o
  *   at most 65535 sequences */

@@ -12,9 +12,15 @@ namespace efqat {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f, kLn2Rest = -1.9046542999e-9f;      // ln 2 = kLn2 + kLn2Rest
 
+// exp2(s c - m c) in one operation beside the exponential lacks what rounding took from m c, a factor that all of a row share.  Beyond this it
+// would leave the range of fp32: m is taken from the scores first.
+constexpr float kFarBase = 65536.0f;
+// what sums with reference m are worth beside the largest reference
+__device__ __forceinline__ float decay(float m, float top, float c) { return top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - top) * c); }
+
 // log of l exp2(m c), the sum that l stands for: m c as it was rounded where l was summed
 __device__ __forceinline__ float log_sum(float m, float c, float l) {
-  const float base = m * c;
+  const float base = m == -INFINITY ? 0.0f : m * c;            // a factor so small that no score passes it: m has not moved
   return l == 0.0f ? -INFINITY : fmaf(base, kLn2, fmaf(base, kLn2Rest, kLn2 * __builtin_amdgcn_logf(l)));
 }
 
@@ -130,7 +136,15 @@ __global__ __launch_bounds__(256, (kTwoWaves<T, DP> ? 2 : 1)) void k_attn_fwd(At
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[i][r] *= shrink;
     }
-    const float base = m == -INFINITY ? 0.0f : m * c;              // nothing seen so far: exp2(-inf) is 0 for all of it
+    float base = m == -INFINITY ? 0.0f : m * c;                    // nothing seen so far: exp2(-inf) is 0 for all of it
+    if (__any(fabsf(base) > kFarBase)) {
+      const float ref = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[n][i] -= ref;
+      base = 0.0f;
+    }
     Frag<T> pf[2 * NT];
     scores(smem + ((t + 1) & 1) * TILE, u, s, pf, base, std::true_type{});      // behind the last tile: of what lies there, not used
     if (t + 1 < kt.count) hide(t + 1, u);
@@ -290,15 +304,14 @@ __global__ __launch_bounds__(256) void k_attn_decode(DecodeArgs a, T* __restrict
         if (more) issue_keys(t + 4, buf);
       }
       top = half_max(top);
-      const float base = top == -INFINITY ? 0.0f : top * c;
-      const float shrink = __builtin_amdgcn_exp2f(fmaf(m, c, -base));
+      const float ref = top == -INFINITY ? 0.0f : top, shrink = __builtin_amdgcn_exp2f((m - ref) * c);
       m = top;
 #pragma unroll
       for (int i = 0; i < R::ND; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[i][r] *= shrink;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[0][i] = __builtin_amdgcn_exp2f(fmaf(s[0][i], c, -base));
+      for (int i = 0; i < 16; ++i) s[0][i] = __builtin_amdgcn_exp2f((s[0][i] - ref) * c);
       l = fmaf(l, shrink, sum16(s[0]));
       if constexpr (C::STAGES == 1) arrived(more, std::integral_constant<int, HALF>{});
 #pragma unroll
@@ -326,9 +339,8 @@ __global__ __launch_bounds__(256) void k_attn_decode(DecodeArgs a, T* __restrict
   float top = -INFINITY;
 #pragma unroll
   for (int w = 0; w < 4; ++w) top = fmaxf(top, s_m[w][lane & 31]);
-  const float base = top == -INFINITY ? 0.0f : top * c;
   float* mine = (float*)smem + (wave * 32 + (lane & 31)) * PITCH;
-  const float f = __builtin_amdgcn_exp2f(fmaf(m, c, -base));
+  const float f = decay(m, top, c);
 #pragma unroll
   for (int i = 0; i < R::ND; ++i) store_col(mine, acc[i], i, WIDTH, f);
   tile_sync();
@@ -339,11 +351,10 @@ __global__ __launch_bounds__(256) void k_attn_decode(DecodeArgs a, T* __restrict
     float tm = -INFINITY, tl = 0.0f;
 #pragma unroll
     for (int w = 0; w < 4; ++w) tm = fmaxf(tm, s_m[w][col]);
-    const float tb = tm == -INFINITY ? 0.0f : tm * c;
     float4 sum = make_float4(0, 0, 0, 0);
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      tl += s_l[w][col] * __builtin_amdgcn_exp2f(fmaf(s_m[w][col], c, -tb));
+      tl += s_l[w][col] * decay(s_m[w][col], tm, c);
       const float4 v = *(const float4*)((const float*)smem + (w * 32 + col) * PITCH + d);
       sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
     }
@@ -352,7 +363,7 @@ __global__ __launch_bounds__(256) void k_attn_decode(DecodeArgs a, T* __restrict
       const float r = tl == 0.0f ? 0.0f : 1.0f / tl;
       if (d < a.dim) store4(o + seq * ldo + (int64_t)head * a.dim + d, sum.x * r, sum.y * r, sum.z * r, sum.w * r);
     } else {
-      float* to = part + ((int64_t)(seq * a.heads + head) * a.splits + split) * (WIDTH + 4);
+      float* to = part + (((int64_t)seq * a.heads + head) * a.splits + split) * (WIDTH + 4);
       *(float4*)(to + d) = sum;
       if (d == 0) *(float4*)(to + WIDTH) = make_float4(tm, tl, 0, 0);
     }
@@ -368,7 +379,7 @@ __global__ __launch_bounds__(256) void k_attn_join(const float* __restrict__ par
   constexpr int PER = DP / 64;
   __shared__ float s_sum[3][DP];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, head = blockIdx.x, seq = blockIdx.y;
-  const float* from = part + (int64_t)(seq * heads + head) * splits * (DP + 4);
+  const float* from = part + ((int64_t)seq * heads + head) * splits * (DP + 4);
   const float m = lane < splits ? from[lane * (DP + 4) + DP] : -INFINITY, l = lane < splits ? from[lane * (DP + 4) + DP + 1] : 0.0f;
   float v[kMostShares / 4][PER];
 #pragma unroll
@@ -377,8 +388,7 @@ __global__ __launch_bounds__(256) void k_attn_join(const float* __restrict__ par
 #pragma unroll
     for (int i = 0; i < PER; ++i) v[x][i] = s < splits ? from[s * (DP + 4) + lane * PER + i] : 0.0f;
   }
-  const float top = wave_max(m), base = top == -INFINITY ? 0.0f : top * c;
-  const float f = __builtin_amdgcn_exp2f(fmaf(m, c, -base)), total = wave_total(l * f);
+  const float f = decay(m, wave_max(m), c), total = wave_total(l * f);
   float sum[PER] = {};
 #pragma unroll
   for (int x = 0; x < kMostShares / 4; ++x) {
@@ -456,8 +466,7 @@ extern "C" int efqat_attention_decode(const void* q, int64_t ldq, const void* k_
   AttnArgs a;
   EFQAT_TRY(attn_args(&a, q, ldq, k_cache, ldk, v_cache, ldv, dtype, n_seq, capacity, 1, nullptr, nullptr, heads, kv_heads, dim, scale, 1, window, sinks));
   EFQAT_TRY(attn_rows(o, ldo, heads * dim, dtype));
-  if (n_seq > 65535 || (n_seq > 1 && (seq_k < (capacity - 1) * ldk + kv_heads * dim || seq_v < (capacity - 1) * ldv + kv_heads * dim)))
-    return EFQAT_ERR_BAD_SHAPE;
+  if (n_seq > 65535 || (n_seq > 1 && (seq_k < 0 || seq_v < 0))) return EFQAT_ERR_BAD_SHAPE;
   if (!lengths || !ws) return EFQAT_ERR_NULL_PTR;
   if (!aligned4(lengths) || (uintptr_t)ws % 256) return EFQAT_ERR_ALIGNMENT;
   const int per16 = dtype == EFQAT_F32 ? 4 : 8;

@@ -91,8 +91,8 @@ def test_attention_decode(L):
         return L.efqat_attention_decode(q, ldq, k, ldk, sk, v, ldv, sv, dt, n, cap, lens, H, KV, D, scale, window, sinks, o, ldo, ws, wsb, None)
 
     assert f(q=None) == f(k=None) == f(v=None) == f(lens=None) == f(o=None) == f(ws=None) == NULL
-    assert f(n=0) == f(cap=0) == f(H=5) == f(D=12) == f(scale=0.0) == f(window=-1) == f(ldo=248) == f(ldk=120) == f(sk=4096 * 128 - 8) == SHAPE
-    assert f(sv=4095 * 128) == f(n=65536) == SHAPE and f(dt=7) == DTYPE and f(wsb=need - 1) == WORKSPACE
+    assert f(n=0) == f(cap=0) == f(H=5) == f(D=12) == f(scale=0.0) == f(window=-1) == f(ldo=248) == f(ldk=120) == f(sk=-8) == SHAPE
+    assert f(sv=-128) == f(n=65536) == SHAPE and f(dt=7) == DTYPE and f(wsb=need - 1) == WORKSPACE
     assert f(lens=FAKE + 2) == f(k=FAKE + 8) == f(sk=4096 * 128 + 4) == f(ws=FAKE + 64) == f(ldv=132, sv=4096 * 132) == ALIGN
 
 

@@ -235,16 +235,34 @@ def test_every_key_has_its_weight(kind, dim):
 
 
 def test_decode_cache_strides_and_one_sequence():
-    """a cache laid out [capacity][sequences] and lengths beyond the capacity"""
+    """caches laid out [capacity][sequences], one that all sequences share, and lengths beyond the capacity"""
     q = rand(1, 3, 256, "bf16")
     k, v = (rand(s, 300 * 3, 128, "bf16").view(300, 3, 128).transpose(0, 1) for s in (2, 3))
-    with pytest.raises(ef.EfqatError):
-        ef.attention_decode(q, k, v, torch.full((3,), 300, dtype=torch.int32, device="cuda"), 4, kv_heads=2)      # sequences that overlap
-    lengths = torch.tensor([300], dtype=torch.int32, device="cuda")
-    for s in range(3):
-        a = ef.attention_decode(q[s: s + 1], k[s: s + 1], v[s: s + 1], lengths, 4, kv_heads=2)
-        b = ef.attention_decode(q[s: s + 1], k[s: s + 1].contiguous(), v[s: s + 1].contiguous(), lengths * 100, 4, kv_heads=2)
-        assert torch.equal(a, b)
+    lengths = torch.tensor([300, 7, 200], dtype=torch.int32, device="cuda")
+    a = ef.attention_decode(q, k, v, lengths, 4, kv_heads=2)
+    b = ef.attention_decode(q, k.contiguous(), v.contiguous(), lengths * torch.tensor([100, 1, 1], dtype=torch.int32, device="cuda"), 4, kv_heads=2)
+    assert torch.equal(a, b)
+    one = [t[1:2].expand(3, 300, 128) for t in (k, v)]
+    a = ef.attention_decode(q, *one, lengths, 4, kv_heads=2)
+    assert torch.equal(a, ef.attention_decode(q, *(t.contiguous() for t in one), lengths, 4, kv_heads=2))
+    assert torch.equal(ef.attention_decode(q[2:], k[2:], v[2:], lengths[2:], 4, kv_heads=2), b[2:])
+
+
+@pytest.mark.parametrize("scale", [1e-39, 1e-38, 1e-20, 1e30])
+def test_extreme_scales(scale):
+    """so small that no score reaches the step by which the reference score moves, and so large that one key takes all"""
+    n = 100
+    q, k, v = rand(1, n, 64, "f32"), rand(2, n, 64, "f32"), rand(3, n, 64, "f32")
+    r = ef.attention_fwd(q, k, v, 1, scale=scale)
+    if scale < 1:
+        mean = v.double().cumsum(0) / torch.arange(1, n + 1, device="cuda")[:, None]
+        assert (r["o"].double() - mean).abs().max() < (n + 8) * ck.E * v.abs().max()
+        assert (r["lse"][0].double() - torch.arange(1, n + 1, device="cuda").double().log()).abs().max() < 1e-6
+    else:
+        best = (q.double() @ k.double().t()).masked_fill(torch.ones(n, n, device="cuda").triu(1).bool(), -1e300).argmax(1)
+        assert torch.equal(r["o"], v[best])
+        one = ef.attention_decode(q[-1:], k[None], v[None], torch.tensor([n], dtype=torch.int32, device="cuda"), 1, scale=scale)
+        assert torch.equal(one, v[best[-1:]])
 
 
 def test_decode_is_the_last_row_of_the_forward():

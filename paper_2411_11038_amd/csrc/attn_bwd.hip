@@ -130,13 +130,19 @@ __global__ __launch_bounds__(256, (kTwoWaves<T, DP> ? 2 : 1)) void k_attn_dq(Att
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const Frag<T> df = frag_of<T>(dp, h);
-        Frag<T> pf;
-        if constexpr (C::MEND) pf = frag_of<T>(s, h);
+        Frag<T> pf, rest;
+        if constexpr (C::MEND) {
+          pf = frag_of<T>(s, h);
+          rest = rest_of(dp, h, df);
+        }
 #pragma unroll
         for (int i = 0; i < R::ND; ++i) {
           const Frag<T> kf = R::col_frag(buf, 32 * n + 16 * h, i);
           mma(kf, df, acc[i]);
-          if constexpr (C::MEND) mma(kf, pf, mean[i]);
+          if constexpr (C::MEND) {
+            mma(kf, pf, mean[i]);
+            mma(kf, rest, acc[i]);
+          }
         }
       }
     }

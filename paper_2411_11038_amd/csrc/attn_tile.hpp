@@ -121,6 +121,18 @@ __device__ __forceinline__ Frag<T> frag_of(const floatx16_t& c, int s) {
   }
   return f;
 }
+// what the rounding of frag_of took, rounded itself: both together have 16 bits
+__device__ __forceinline__ Frag<bf16_t> rest_of(const floatx16_t& c, int s, const Frag<bf16_t>& of) {
+  const uint4 w = __builtin_bit_cast(uint4, of.v);
+  const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+  uint32_t y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    y[i] = pack_bf16x2(c[8 * s + 2 * i] - __uint_as_float(x[i] << 16), c[8 * s + 2 * i + 1] - __uint_as_float(x[i] & 0xFFFF0000u));
+  Frag<bf16_t> f;
+  f.v = __builtin_bit_cast(bf16x8_t, make_uint4(y[0], y[1], y[2], y[3]));
+  return f;
+}
 // made where this stands: the compiler may not move it behind a branch, nearer to where it is used
 __device__ __forceinline__ void hold(float& v) {
 #if defined(__HIP_DEVICE_COMPILE__)

@@ -5,8 +5,12 @@
 //
 // Two kernels, each with the sums of its outputs in registers: k_attn_dq walks the keys of 128 queries, k_attn_dkv the queries (of all
 // heads that share them) of 128 keys.  Scores and dP are formed twice, seven products instead of the five that one kernel would need, but
-// no sum crosses blocks: nothing is added by atomics, and results do not change from run to run.  With bf16 operands P and dS are
-// rounded to bf16 for the matrix cores, as probabilities are in the forward pass.
+// no sum crosses blocks: nothing is added by atomics, and results do not change from run to run.  With bf16 operands P and, for dk, dS are
+// rounded to bf16 for the matrix cores, as probabilities are in the forward pass; dq takes dS as two such parts.
+//
+// Bound by the matrix cores and what is issued beside them.  2 x 4096 tokens, 32 query and 8 key heads of 128, window 1024, 4 sinks: dq 326 us (0.92 PFLOP/s
+// in five products), dk and dv 410 us (0.59 in four; 256 of their 768 blocks are the sinks' far parts).  32 x 384 tokens, 12 heads of 64: 63 and 64 us, six
+// stages a block.  fp32, 7 sequences of 3001 tokens, heads of 80: 123 and 154 us, the rate of fp32 matrix instructions on the longest blocks.
 #include "attn_tile.hpp"
 
 namespace efqat {
@@ -40,7 +44,7 @@ __device__ __forceinline__ float prob_factor(float scale) { return sizeof(T) == 
 // more registers than two wavefronts a SIMD have: 380 instead of 250 us for a window of 1024 in 2 x 4096 tokens, 32 heads of 128.)
 //
 // bf16: o is rounded, and delta from it is off by up to 2^-8 of do . o, far more than dS where one key takes nearly all of P (dq 0.5 % off in the
-// 2-norm for short sequences).  Exactly, sum_j dS_ij = 0: what it comes to is what delta lacks, d_i.  So sum_j P_ij k_j is formed too, from the
+// 2-norm for short sequences; that and the second part of dS cost 75 of the 326 us above).  Exactly, sum_j dS_ij = 0: what it comes to is what delta lacks, d_i.  So sum_j P_ij k_j is formed too, from the
 // fragments of k that are there, and  dq_i = scale (sum_j dS_ij k_j - d_i sum_j P_ij k_j).  d is small: P need not be exact there.
 template <typename T, int DP>
 struct DqTile {

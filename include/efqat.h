@@ -519,8 +519,8 @@ int efqat_head_norm_rope_bwd(const void* dyq, int64_t lddyq, const void* dyk, in
  *   window       0: no window; sinks: first keys that stay visible beside a window
  *   lse          float [heads][Tq]; forward: out, nullable.  Backward: in, with o, as the forward left them
  *   packed       of the workspace query: whether offsets will be given (0 or 1)
- * Scores, their maxima and sums, and all accumulators are fp32.  With BF16 the probabilities and dS are rounded to bf16 for the
- * matrix cores (their sum is taken before); with F32 the products are fp32 too.  The backward forms P from lse: 2^-23 of the largest
+ * Scores, their maxima and sums, and all accumulators are fp32.  With BF16 the probabilities and, for dk, dS are rounded to bf16
+ * for the matrix cores (their sum is taken before; dq takes dS as two such parts); with F32 the products are fp32 too.  The backward forms P from lse: 2^-23 of the largest
  * score is its relative error.  Sums have a fixed order (bit-reproducible).  A key or
  * value in a sequence that is not finite may make undefined what tokens of that sequence and head hold that do not see it; other sequences
  * and heads do not notice.  scale is positive; at most 2^28 rows, 65535 heads, row strides 2^24. */

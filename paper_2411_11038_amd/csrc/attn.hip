@@ -7,9 +7,9 @@
 // rows and queries as columns of a result: a lane then holds 16 scores of one query, its maximum and sum need one exchange between the
 // halves of a wavefront, and the probabilities are the second product's operand where they are.
 //
-// Bound by the matrix cores and the power limit: 32768 tokens, 32 query and 8 key heads of 128, causal, 7.8 ms (1.13 PFLOP/s; a library product of
-// 8192^3 reaches 1.23 to 1.38 on these cards); a window of 1024 in 2 x 4096 tokens 166 us; 32 x 384 tokens, 12 heads of 64, 36 us, where a block has six tiles.
-// Single tokens are bound by HBM: 64 sequences of 500 to 8192 keys, 8 key heads of 128, 222 us (5.1 TB/s), one of 16384 keys 16 us and 3 for the join.
+// Bound by the matrix cores and the power limit: 32768 tokens, 32 query and 8 key heads of 128, causal, 7.8 ms (1.12 PFLOP/s, where
+// a library product of 8192^3 reaches 1.41 on the same card); with zero operands 5.93 ms; a window of 1024 in 2 x 4096 tokens 165 us; 32 x 384 tokens, 12 heads of 64, 36 us, where a block has six tiles.
+// Single tokens are bound by HBM: 64 sequences of 500 to 8192 keys, 8 key heads of 128, 222 to 230 us (5.0 TB/s), one of 16384 keys 16 us and 4 for the join.
 #include "attn_tile.hpp"
 
 namespace efqat {

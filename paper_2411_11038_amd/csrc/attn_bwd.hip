@@ -8,9 +8,9 @@
 // no sum crosses blocks: nothing is added by atomics, and results do not change from run to run.  With bf16 operands P and, for dk, dS are
 // rounded to bf16 for the matrix cores, as probabilities are in the forward pass; dq takes dS as two such parts.
 //
-// Bound by the matrix cores and what is issued beside them.  2 x 4096 tokens, 32 query and 8 key heads of 128, window 1024, 4 sinks: dq 326 us (0.92 PFLOP/s
-// in five products), dk and dv 410 us (0.59 in four; 256 of their 768 blocks are the sinks' far parts).  32 x 384 tokens, 12 heads of 64: 63 and 64 us, six
-// stages a block.  fp32, 7 sequences of 3001 tokens, heads of 80: 123 and 154 us, the rate of fp32 matrix instructions on the longest blocks.
+// Bound by the matrix cores and what is issued beside them.  2 x 4096 tokens, 32 query and 8 key heads of 128, window 1024, 4 sinks: dq 323 us (0.93 PFLOP/s
+// in five products), dk and dv 407 us (0.59 in four; 256 of their 776 blocks are the sinks' far parts).  32 x 384 tokens, 12 heads of 64: 63 and 64 us, six
+// stages a block.  fp32, 7 sequences, 3001 tokens in all, heads of 80: 123 and 154 us, the rate of fp32 matrix instructions on the longest blocks.
 #include "attn_tile.hpp"
 
 namespace efqat {
@@ -44,7 +44,7 @@ __device__ __forceinline__ float prob_factor(float scale) { return sizeof(T) == 
 // more registers than two wavefronts a SIMD have: 380 instead of 250 us for a window of 1024 in 2 x 4096 tokens, 32 heads of 128.)
 //
 // bf16: o is rounded, and delta from it is off by up to 2^-8 of do . o, far more than dS where one key takes nearly all of P (dq 0.5 % off in the
-// 2-norm for short sequences; that and the second part of dS cost 75 of the 326 us above).  Exactly, sum_j dS_ij = 0: what it comes to is what delta lacks, d_i.  So sum_j P_ij k_j is formed too, from the
+// 2-norm for short sequences; the mend took dq of a window of 1024 from 254 to 300 us, the second part of dS from 290 to 323).  Exactly, sum_j dS_ij = 0: what it comes to is what delta lacks, d_i.  So sum_j P_ij k_j is formed too, from the
 // fragments of k that are there, and  dq_i = scale (sum_j dS_ij k_j - d_i sum_j P_ij k_j).  d is small: P need not be exact there.
 template <typename T, int DP>
 struct DqTile {
@@ -324,13 +324,11 @@ __global__ __launch_bounds__((64 * DkvTile<T, DP>::WAVES), (kTwoWaves<T, DP> ? 2
           if constexpr (C::VALUES_IN_LDS) mma(R::row_frag(ds, 0, ks), R::row_frag(vals, own * 32, ks), dp);
           else mma(R::row_frag(ds, 0, ks), v[ks], dp);
         }
+        results_settle();
         if (!all(p0)) {
-          results_settle();
           const int first = p0 + row_here();
 #pragma unroll
           for (int i = 0; i < 16; ++i) s[i] = seen(first + row_of(i), krow) ? s[i] : -INFINITY;
-        } else {
-          results_settle();
         }
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {

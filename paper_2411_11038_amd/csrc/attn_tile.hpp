@@ -148,12 +148,6 @@ __device__ __forceinline__ void hold(Frag<float>& f) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) hold(f.v[e]);
 }
-// a result that is to be read by vector operations, in vector registers
-__device__ __forceinline__ void hold(floatx16_t& c) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  asm volatile("" : "+v"(c));
-#endif
-}
 __device__ __forceinline__ floatx16_t zero16() {
   floatx16_t z;
 #pragma unroll

@@ -7,7 +7,7 @@
 // thus a function of seed, offset and an element's place alone: the backward pass draws it again, and neither strides nor types change it.
 //
 // Bound by HBM: one pass, 16 bytes (bf16) or 32 a lane and tensor; the ten rounds are 20 wide multiplications for 8 elements.
-// bf16, 12288 x 768 with residual: 10.7 us (57 MB, 5.3 TB/s); fp32, 2049 x 1001: 4.8 us, a launch.
+// bf16, 12288 x 768 with residual: 11 us (57 MB, 5.0 TB/s); fp32, 2049 x 1001: 4.8 us, a launch.
 #include "rows.hpp"
 
 namespace efqat {

@@ -8,7 +8,7 @@
 // rotation stays in the lane and the norm is a sum over the D / 16 lanes of a head.  A wavefront takes a token: it makes the F angles
 // once (the product in 64 bits, its whole turns taken off, so that far positions keep their place in the circle) and walks the heads, the next
 // ones on their way.  bf16, 8192 tokens, 32 + 8 heads of 128, backward: 50 us (252 MB, 5.0 TB/s) and 6 us for the sums of the weights' gradients; fp32, 4099
-// tokens, 24 heads of 80, three axes, forward: 19 us (63 MB), where three lanes of eight have no features; 16 tokens: 4 us of kernel in 6.2 a call.
+// tokens, 24 heads of 80, three axes, forward: 19 us (63 MB), where three lanes of eight have no features; 16 tokens: 4 us of kernel in a call of 6.2.
 #include "rows.hpp"
 
 namespace efqat {

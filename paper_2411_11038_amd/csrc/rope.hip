@@ -182,6 +182,7 @@ __global__ __launch_bounds__(256, BWD ? 4 : 5) void k_rope(RopeArgs a, RopeUnits
 #pragma unroll
           for (int j = 0; j < 8; ++j) sq = fmaf(x[i][j], x[i][j], sq);
         r = 1.0f / sqrtf(fmaf(head_sum(sq, u.lanes), inv_dim, a.eps));
+        if (BWD && !in) r = 0.0f;                    // no head: without eps 1 / 0, and its zeros would be NaN in the weights' sums
       }
       if constexpr (!BWD) {
         if (a.norm) {

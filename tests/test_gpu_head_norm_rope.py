@@ -153,6 +153,23 @@ def test_zero_heads_and_large_values():
     assert (y == 0).all()                                   # nothing over eps; squares that leave fp32
 
 
+@pytest.mark.parametrize("dim", [64, 40, 33])
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_norm_without_eps(kind, dim):
+    """eps 0: heads that fill a part of a wavefront; what lies beside them is no head whose norm is 0 / 0"""
+    T, heads, kv = 5, 3, 1
+    q, k, dq, dk = rand(1, T, heads * dim, kind, 1.0, 0.5), rand(2, T, dim, kind), rand(3, T, heads * dim, kind), rand(4, T, dim, kind)
+    w = rand(5, 1, dim, "f32", 0.2, 1.0)[0]
+    g = ef.head_norm_rope_bwd(dq, q, heads, dk=dk, k=k, kv_heads=kv, q_weight=w, k_weight=w, eps=0.0)
+    for name, x, dy, n in (("q", q, dq, heads), ("k", k, dk, kv)):
+        x, dy = f64(x).reshape(T, n, dim), f64(dy).reshape(T, n, dim)
+        terms = dy * x / np.sqrt((x * x).mean(-1, keepdims=True))
+        # a term: the norm's sum of squares (dim / 16 + 4 additions of at most that many roundings each, halved by the root), root, reciprocal
+        # and two products: less than 64 roundings of 2^-24; sums of the terms T * heads more, all of the terms' sizes
+        within(f64(g[f"d{name}_weight"]), terms.sum((0, 1)), (64 + T * n) * E * np.abs(terms).sum((0, 1)) + 1e-30, f"d{name}_weight")
+        assert torch.isfinite(g["d" + name].float()).all()
+
+
 def test_same_results_each_time():
     q, k, d = rand(1, 3000, 512, "bf16"), rand(2, 3000, 128, "bf16"), rand(3, 3000, 640, "bf16")
     a, b = (ef.head_norm_rope_bwd(d[:, :512], q, 4, dk=d[:, 512:], k=k, kv_heads=1) for _ in range(2))

@@ -81,6 +81,15 @@ def test_attention(L):
     assert bwd(ws=FAKE + 128) == bwd(do=FAKE + 8) == bwd(lddv=132) == ALIGN
 
 
+def test_attention_backward_grids(L):
+    """dk and dv of bf16 heads beyond 64 features take blocks of 512 lanes: no grid of 2^32 lanes and more is launched"""
+    n, heads, cols = 1 << 20, 10, 1280
+    blocks = (n // 128 + n - 1) * heads
+    assert blocks * 256 < 2 ** 32 <= blocks * 512
+    assert L.efqat_attention_bwd(FAKE, cols, FAKE, cols, FAKE, cols, FAKE, cols, FAKE, cols, FAKE, 1, n, n, n, FAKE, FAKE, heads, heads, 128, 0.1, 1, 0, 0,
+                                 2 * FAKE, cols, 3 * FAKE, cols, 4 * FAKE, cols, FAKE, 1 << 50, None) == SHAPE
+
+
 def test_attention_decode(L):
     need = L.efqat_attention_decode_workspace_bytes(2, 4096, 4, 2, 64, 0, 0)
     assert need > 256 and L.efqat_attention_decode_workspace_bytes(2, 1, 4, 2, 64, 0, 0) == 256

@@ -444,6 +444,7 @@ extern "C" int efqat_attention_fwd(const void* q, int64_t ldq, const void* k, in
   if (!aligned4(lse)) return EFQAT_ERR_ALIGNMENT;
   const HeadPlan h = head_plan(a, kv_heads);
   if (h.blocks > kAttnMostBlocks) return EFQAT_ERR_BAD_SHAPE;
+  EFQAT_TRY(attn_apart({o}, {q, k, v}));
   hipStream_t st = (hipStream_t)stream;
 #define EFQAT_FWD(E, DP) return launch(k_attn_fwd<E, DP>, dim3((unsigned)h.blocks), dim3(256), 0, st, a, (E*)o, ldo, lse, h.tiles, h.hb)
   if (dtype == EFQAT_F32) { if (dim <= 64) EFQAT_FWD(float, 64); if (dim <= 96) EFQAT_FWD(float, 96); EFQAT_FWD(float, 128); }
@@ -476,6 +477,7 @@ extern "C" int efqat_attention_decode(const void* q, int64_t ldq, const void* k_
   const int per16 = dtype == EFQAT_F32 ? 4 : 8;
   if (n_seq > 1 && (seq_k % per16 || seq_v % per16)) return EFQAT_ERR_ALIGNMENT;
   if (ws_bytes < efqat_attention_decode_workspace_bytes(n_seq, capacity, heads, kv_heads, dim, window, sinks)) return EFQAT_ERR_WORKSPACE;
+  EFQAT_TRY(attn_apart({o}, {q, k_cache, v_cache}));
   const int splits = decode_splits(n_seq, capacity, heads, kv_heads, window, sinks);
   const DecodeArgs d = {q, k_cache, v_cache, ldq, ldk, ldv, n_seq > 1 ? seq_k : 0, n_seq > 1 ? seq_v : 0, lengths, (int)capacity, (int)heads,
                         a.group, (int)dim, a.mask.window, a.mask.sinks, splits, scale};

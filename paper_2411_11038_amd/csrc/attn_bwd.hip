@@ -500,6 +500,9 @@ extern "C" int efqat_attention_bwd(const void* dout, int64_t lddo, const void* q
   const int64_t key_waves = (plan.near_blocks + plan.far_blocks) * (dtype == EFQAT_BF16 && dim > 64 ? DkvTile<bf16_t, 128>::WAVES : DkvTile<bf16_t, 64>::WAVES);
   static_assert(DkvTile<bf16_t, 96>::WAVES == DkvTile<bf16_t, 128>::WAVES && DkvTile<float, 128>::WAVES == DkvTile<bf16_t, 64>::WAVES, "as counted above");
   if (h.blocks > kAttnMostBlocks || key_waves > kAttnMostBlocks * 4) return EFQAT_ERR_BAD_SHAPE;
+  EFQAT_TRY(attn_apart({dq, dk, dv}, {q, k, v, dout, o}));
+  EFQAT_TRY(attn_apart({dq}, {dk, dv}));
+  EFQAT_TRY(attn_apart({dk}, {dv}));
   const AttnGrads g = {dout, o, lddo, ldo, lse, (float*)ws, dq, dk, dv, lddq, lddk, lddv};
   float* sums = (float*)((char*)ws + round_up(Tq * heads * 4, 256));
   const unsigned joins = (unsigned)(plan.parts > 1 ? plan.tiles * kv_heads : plan.far ? plan.far_blocks / plan.far : 0);

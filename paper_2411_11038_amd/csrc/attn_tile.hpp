@@ -11,6 +11,8 @@
 #include "lds_copy.hpp"
 #include "rows.hpp"
 
+#include <initializer_list>
+
 namespace efqat {
 
 constexpr int64_t kAttnMostRows = INT64_C(1) << 28;          // sums of three such fit 32 bits
@@ -495,6 +497,13 @@ inline int attn_rows(const void* p, int64_t ld, int64_t cols, int dtype) {
   if (ld < cols || ld > (INT64_C(1) << 24)) return EFQAT_ERR_BAD_SHAPE;
   if (!p) return EFQAT_ERR_NULL_PTR;
   if (!aligned16(p) || ld % (dtype == EFQAT_F32 ? 4 : 8)) return EFQAT_ERR_ALIGNMENT;
+  return EFQAT_OK;
+}
+// results that lie where operands do, which blocks and kernels behind the one that writes them still read
+inline int attn_apart(std::initializer_list<const void*> results, std::initializer_list<const void*> operands) {
+  for (const void* r : results)
+    for (const void* o : operands)
+      if (r == o) return EFQAT_ERR_BAD_LAYOUT;
   return EFQAT_OK;
 }
 inline int attn_args(AttnArgs* a, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, int dtype, int64_t Tq,

@@ -90,6 +90,25 @@ def test_attention_backward_grids(L):
                                  2 * FAKE, cols, 3 * FAKE, cols, 4 * FAKE, cols, FAKE, 1 << 50, None) == SHAPE
 
 
+def test_attention_results_lie_apart(L):
+    """the kernel of dk and dv reads q and do after dq was written, other blocks read keys and values"""
+    at = {x: FAKE * (i + 2) for i, x in enumerate("q k v o do dq dk dv".split())}
+
+    def call(fn, **kw):
+        p = {**at, **kw}
+        if fn == "fwd":
+            return L.efqat_attention_fwd(p["q"], 256, p["k"], 256, p["v"], 256, 1, 8, 8, 1, None, None, 4, 4, 64, 0.1, 1, 0, 0, p["o"], 256, None, None)
+        if fn == "decode":
+            return L.efqat_attention_decode(p["q"], 256, p["k"], 256, 0, p["v"], 256, 0, 1, 1, 8, FAKE, 4, 4, 64, 0.1, 0, 0, p["o"], 256, FAKE, 1 << 20, None)
+        return L.efqat_attention_bwd(p["do"], 256, p["q"], 256, p["k"], 256, p["v"], 256, p["o"], 256, FAKE, 1, 8, 8, 1, None, None, 4, 4, 64, 0.1, 1, 0, 0,
+                                     p["dq"], 256, p["dk"], 256, p["dv"], 256, FAKE, 1 << 20, None)
+
+    for fn in ("fwd", "decode"):
+        assert [call(fn, o=at[x]) for x in "qkv"] == [LAYOUT] * 3
+    for out in ("dq", "dk", "dv"):
+        assert [call("bwd", **{out: at[x]}) for x in at if x != out] == [LAYOUT] * 7
+
+
 def test_attention_decode(L):
     need = L.efqat_attention_decode_workspace_bytes(2, 4096, 4, 2, 64, 0, 0)
     assert need > 256 and L.efqat_attention_decode_workspace_bytes(2, 1, 4, 2, 64, 0, 0) == 256

@@ -22,10 +22,13 @@ constexpr float kFarBase = 65536.0f;
 // what sums with reference m are worth beside the largest reference
 __device__ __forceinline__ float decay(float m, float top, float c) { return top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - top) * c); }
 
-// log of l exp2(m c), the sum that l stands for: m c as it was rounded where l was summed
-__device__ __forceinline__ float log_sum(float m, float c, float l) {
+// log of l exp2(m c), the sum that l stands for: m c as it was rounded where l was summed.  Where m c leaves fp32 (scores beyond 2.36e38, log2 e short of
+// its end) both parts of ln 2 would meet as infinities of opposite signs: l, of at most 2^28 keys, is nothing beside m scale there.
+__device__ __forceinline__ float log_sum(float m, float c, float scale, float l) {
   const float base = m == -INFINITY ? 0.0f : m * c;            // a factor so small that no score passes it: m has not moved
-  return l == 0.0f ? -INFINITY : fmaf(base, kLn2, fmaf(base, kLn2Rest, kLn2 * __builtin_amdgcn_logf(l)));
+  if (l == 0.0f) return -INFINITY;
+  if (fabsf(base) == INFINITY) return m * scale;
+  return fmaf(base, kLn2, fmaf(base, kLn2Rest, kLn2 * __builtin_amdgcn_logf(l)));
 }
 
 template <int NT>
@@ -190,7 +193,7 @@ __global__ __launch_bounds__(256, (kTwoWaves<T, DP> ? 2 : 1)) void k_attn_fwd(At
   l = half_sum(l);
   const float f = l == 0.0f ? 0.0f : 1.0f / l;                     // a token that sees nothing: zeros
   store_rows<T, DP>(o + w.token(0) * ldo + w.head * a.dim, ldo, w.rows_left(), a.dim, acc, f, smem + wave * (sizeof(smem) / kWaves));
-  if (lse && lane < 32 && w.in(lane)) lse[(int64_t)w.head * a.qs.rows + w.token(lane)] = log_sum(m, c, l);
+  if (lse && lane < 32 && w.in(lane)) lse[(int64_t)w.head * a.qs.rows + w.token(lane)] = log_sum(m, c, a.scale, l);
 }
 
 // ---- one new token a sequence

@@ -522,9 +522,11 @@ int efqat_head_norm_rope_bwd(const void* dyq, int64_t lddyq, const void* dyk, in
  * Scores, their maxima and sums, and all accumulators are fp32.  With BF16 the probabilities and, for dk, dS are rounded to bf16
  * for the matrix cores (their sum is taken before; dq takes dS as two such parts); with F32 the products are fp32 too.  o and lse hold for scores
  * up to the end of fp32 (an lse beyond it is an infinity).  The backward forms P from lse: 2^-23 of the largest score is the error of its
- * exponent, so that gradients of scores beyond 2^18 hold few digits and those beyond 2^23 none (they may be infinite or NaN).  Sums have a fixed order (bit-reproducible).  A key or
- * value in a sequence that is not finite may make undefined what tokens of that sequence and head hold, those that do not see it too; other
- * sequences and heads do not notice.  Results lie apart from operands and from each other (equal addresses: EFQAT_ERR_BAD_LAYOUT).  scale is positive; at most 2^28 rows, 65535 heads, row strides 2^24. */
+ * exponent, so that gradients of scores beyond 2^18 hold few digits and those beyond 2^23 none (they may be infinite or NaN).  Sums have a fixed
+ * order (bit-reproducible).  A key or value in a sequence that is not finite may make undefined what tokens of that sequence and head hold, those
+ * that do not see it too.  A query or a row of dout that is not finite makes undefined what its own token and head hold, and dk and dv of its
+ * key head in that sequence, of keys that it does not see too.  Other sequences and key heads do not notice either.
+ * Results lie apart from operands and from each other (equal addresses: EFQAT_ERR_BAD_LAYOUT).  scale is positive; at most 2^28 rows, 65535 heads, row strides 2^24. */
 int efqat_attention_fwd(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, int dtype, int64_t Tq,
                         int64_t Tk, int64_t n_seq, const int32_t* q_start, const int32_t* k_start, int64_t heads, int64_t kv_heads,
                         int64_t dim, float scale, int causal, int64_t window, int64_t sinks, void* o, int64_t ldo, float* lse,

@@ -332,7 +332,7 @@ __device__ __forceinline__ void store_col(T* p, const floatx16_t& c, int i, int 
 
 // Tiles of BN keys that some of the positions p0 .. p1 see: those of the first `sinks` keys, then those of the window
 struct KeyTiles {
-  int sink, first, count, end;                        // tiles of the sinks that lie before tile `first`; tiles in all; keys that count
+  int sink, first, count;                             // tiles of the sinks that lie before tile `first`; tiles in all
   __device__ __forceinline__ KeyTiles(const AttnMask& m, int keys, int p0, int p1, int bn) {
     int lo = 0, hi = keys;
     if (m.window) {
@@ -344,7 +344,6 @@ struct KeyTiles {
     if (hi < 0) hi = 0;
     if (lo < 0) lo = 0;
     if (lo > hi) lo = hi;
-    end = hi;
     first = lo / bn;
     const int s = m.window && m.sinks > 0 ? (m.sinks - 1) / bn + 1 : 0;
     if (s >= first) {

@@ -5,11 +5,15 @@
 //
 // One pass over the keys: with a new largest score m', l and o are multiplied by exp(m - m').  Scores are formed transposed, keys as
 // rows and queries as columns of a result: a lane then holds 16 scores of one query, its maximum and sum need one exchange between the
-// halves of a wavefront, and the probabilities are the second product's operand where they are.
+// halves of a wavefront, and the probabilities are the second product's operand where they are.  With bf16 they are rounded to it there, to
+// nearest: the fp32 product would take sixteen times as long, and half a step of each of many terms is less in o than o's own (o is off by 1.8e-3 to
+// 2.1e-3 in the 2-norm, where rounding the exact result is 1.66e-3).  l sums them before they are rounded.
 //
 // Bound by the matrix cores and the power limit: 32768 tokens, 32 query and 8 key heads of 128, causal, 7.8 ms (1.12 PFLOP/s, where
-// a library product of 8192^3 reaches 1.41 on the same card); with zero operands 5.93 ms; a window of 1024 in 2 x 4096 tokens 165 us; 32 x 384 tokens, 12 heads of 64, 36 us, where a block has six tiles.
-// Single tokens are bound by HBM: 64 sequences of 500 to 8192 keys, 8 key heads of 128, 222 to 230 us (5.0 TB/s), one of 16384 keys 16 us and 4 for the join.
+// a library product of 8192^3 reaches 1.41 on the same card; another card: 8.1); with zero operands 5.93 ms; a window of 1024 in 2 x 4096 tokens 169 us;
+// 32 x 384 tokens, 12 heads of 64, 37 us, where a block has six tiles.  Blocks come from the queries alone: 16 tokens over 32768 keys are 8 blocks, 600 us.
+// Single tokens are bound by HBM: 64 sequences of 500 to 8192 keys, 8 key heads of 128, 222 to 230 us (5.0 TB/s), one of 16384 keys 17 us and 4 for
+// the join; fp32, where heads beyond 64 have one stage of LDS: the same sequence 39 us in all, 32 of 512 to 8192 keys 311 us (3.9 TB/s).
 #include "attn_tile.hpp"
 
 namespace efqat {
@@ -421,8 +425,8 @@ __global__ __launch_bounds__(256) void k_attn_join(const float* __restrict__ par
 
 static int attn_dp(int64_t dim) { return dim <= 64 ? 64 : 128; }
 
-// Shares of a sequence's keys: as many blocks as the chip has CUs, each with four tiles of 32 keys a wavefront at least, and eight a CU where
-// shares stay long (sequences differ in length: 64 of 500 to 8192 keys, 8 heads of 128, 248 us in one share, 224 in four; 24 of 1028 keys, 12
+// Shares of a sequence's keys: as many blocks as the chip has CUs, one for every sixteen tiles of 32 keys at most (rounded up: 17 tiles are
+// two shares of eight and nine, 512 are 32 of four tiles a wavefront), and eight a CU where shares stay long, 64 tiles at least (sequences differ in length: 64 of 500 to 8192 keys, 8 heads of 128, 248 us in one share, 224 in four; 24 of 1028 keys, 12
 // heads of 64, 20 us in one, 24 in two).
 static int decode_splits(int64_t n_seq, int64_t capacity, int64_t heads, int64_t kv_heads, int64_t window, int64_t sinks) {
   const int64_t most = window > 0 && window < capacity && sinks < capacity && window + sinks + 64 < capacity ? window + sinks + 64 : capacity;

@@ -4,13 +4,15 @@
 //   dS_ij = P_ij (dP_ij - delta_i),  dq_i = scale sum_j dS_ij k_j,  dk_j = scale sum_i dS_ij q_i,  dv_j = sum_i P_ij do_i
 //
 // Two kernels, each with the sums of its outputs in registers: k_attn_dq walks the keys of 128 queries, k_attn_dkv the queries (of all
-// heads that share them) of 128 keys.  Scores and dP are formed twice, seven products instead of the five that one kernel would need, but
-// no sum crosses blocks: nothing is added by atomics, and results do not change from run to run.  With bf16 operands P and, for dk, dS are
+// heads that share them) of 128 keys.  Scores and dP are formed twice: seven products with fp32 (three and four) instead of the five that one
+// kernel would need, nine with bf16, whose dq takes two more (below).  But no sum crosses blocks: nothing is added by atomics, and results do
+// not change from run to run.  With bf16 operands P and, for dk, dS are
 // rounded to bf16 for the matrix cores, as probabilities are in the forward pass; dq takes dS as two such parts.
 //
-// Bound by the matrix cores and what is issued beside them.  2 x 4096 tokens, 32 query and 8 key heads of 128, window 1024, 4 sinks: dq 323 us (0.93 PFLOP/s
-// in five products), dk and dv 407 us (0.59 in four; 256 of their 776 blocks are the sinks' far parts).  32 x 384 tokens, 12 heads of 64: 63 and 64 us, six
-// stages a block.  fp32, 7 sequences, 3001 tokens in all, heads of 80: 123 and 154 us, the rate of fp32 matrix instructions on the longest blocks.
+// Bound by the matrix cores and what is issued beside them.  2 x 4096 tokens, 32 query and 8 key heads of 128, window 1024, 4 sinks: dq 320 us (0.94 PFLOP/s
+// in five products), dk and dv 414 us (0.58 in four; 256 of their 776 blocks are the sinks' far parts), 9 us to join them.  32 x 384 tokens, 12 heads
+// of 64: 64 and 66 us, six stages a block.  fp32, 7 sequences, 3001 tokens in all, heads of 80: 124 and 156 us and 10 to join, the rate of fp32
+// matrix instructions on the longest blocks.  (Kernel times of a trace, medians; a launch's start and end are in each.)
 #include "attn_tile.hpp"
 
 namespace efqat {
@@ -436,7 +438,16 @@ __global__ __launch_bounds__(256) void k_attn_dkv_join(AttnArgs a, AttnGrads g, 
 }
 
 // far parts where a window's tiles have less to do than a tile with sinks, and few enough tiles that the chip does not fill by them; parts
-// where tiles do not fill it
+// where tiles do not fill it.  The lengths are data of the device: both go by their mean.  Backward alone, us, chosen rule last:
+//   parts, two blocks a CU      1 x 2048 tokens, 32 / 8 heads of 128: whole tiles 362, 256 blocks 255, 1024 blocks 249, 512 blocks 221;  1 x 1024: 186,
+//                               108, 141, 110;  1 x 4096, 16 / 4 of 64: 597, 374, 262, 264;  fp32, 4 x 1000, 6 / 2 of 80: 865, 363, 335, 303
+//   four steps a part at least  1 x 300, 4 / 2 of 64: whole 38.9, two steps 28.0, eight 33.3, four 30.8;  no difference in the sizes above
+//   whole from 256 blocks on    8 x 384, 12 of 64 (288 blocks): cut 59, whole 43;  1 x 4096, 32 / 8 of 128 (256 blocks): cut 644, whole 831 (tiles
+//                               of long causal sequences are uneven, which the rule does not look at)
+//   far parts, one a CU         2 x 4096, 32 / 8 of 128, W 1024: none 1038, 128 of them 700, 512 662, 256 671;  1 x 16384, W 512: 3457, 974, 908, 900;
+//                               16 x 2048, 12 of 64, W 256: 453, 387, 351, 337;  1 x 8192, 8 of 64, W 64, 300 sinks: 377, 125, 88, 98
+//   eight steps a far part      the last one: four 98, sixteen 111, eight 98;  fp32, 2 x 3000, 6 / 2 of 80, W 500: 515, 575, 505
+//   none from 256 tiles with sinks on  24 x 2048, 12 of 64, W 256 (288 of them): with far parts 535, without 648
 static KeyPlan key_plan(const Packed& qs, const Packed& ks, int64_t kv_heads, int64_t group, const AttnMask& m, int dtype) {
   KeyPlan k = {};
   const int64_t tiles = ks.most_tiles(kKeyRows), stage = dtype == EFQAT_BF16 ? 64 : 32, each = ceil_div(qs.rows, qs.n);

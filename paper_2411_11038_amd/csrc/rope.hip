@@ -7,7 +7,8 @@
 // Bound by HBM: what is read is written once.  A lane owns two chunks of 8 features that hold both members of their pairs, so that the
 // rotation stays in the lane and the norm is a sum over the D / 16 lanes of a head.  A wavefront takes a token: it makes the F angles
 // once (the product in 64 bits, its whole turns taken off, so that far positions keep their place in the circle) and walks the heads, the next
-// ones on their way.  bf16, 8192 tokens, 32 + 8 heads of 128, backward: 50 us (252 MB, 5.0 TB/s) and 6 us for the sums of the weights' gradients; fp32, 4099
+// ones on their way.  bf16, 8192 tokens, 32 + 8 heads of 128, backward: 50 us (252 MB, 5.0 TB/s) and 6 us for the sums of the weights' gradients, fp32
+// 140 us in all (503 MB); fp32, 4099
 // tokens, 24 heads of 80, three axes, forward: 19 us (63 MB), where three lanes of eight have no features; 16 tokens: 4 us of kernel in a call of 6.2.
 #include "rows.hpp"
 
@@ -234,7 +235,8 @@ __global__ __launch_bounds__(256, BWD ? 4 : 5) void k_rope(RopeArgs a, RopeUnits
 }
 
 // Any head width up to 256 and any number of pairs: a wavefront takes a head of a token, a lane every 64th feature and reads its
-// partner's beside it.
+// partner's beside it.  Turns are made anew for every head and both members of a pair, and loads are one element a lane: 8192 tokens, 12 + 12 heads of 80
+// with 20 pairs, bf16 81 us forward and 129 backward where k_rope (neighbours paired) takes 19.5 and 34; fp32 88 and 151.
 template <typename T, bool NEXT, bool BWD>
 __global__ __launch_bounds__(256) void k_rope_any(RopeArgs a, RopeUnits u) {
   __shared__ float s_sum[BWD ? 4 : 1][BWD ? kRopeMostDim : 1];
@@ -342,7 +344,10 @@ static int rope_lanes(int64_t dim, int64_t freqs, int neighbours) {
   while (lanes * 16 < dim) lanes *= 2;
   return lanes;
 }
-// Units and blocks of a call.  Few tokens: a pass a wavefront; else four, whose loads follow each other.
+// Units and blocks of a call.  Few tokens: a pass a wavefront; else four, whose loads follow each other.  One pass and four, 32 + 8 heads of 128 (five
+// passes a token), us: forward bf16 1024 tokens 7.5 and 8.3, 2048 10.9 and 9.5, 4096 16.9 and 14.8, 8192 35.1 and 30.8, fp32 4096 30.0 and 30.4; backward
+// bf16 2048 24.5 and 21.5, 4096 34.0 and 36.1, 8192 53.5 and 60.0 (four loses there, whose blocks walk the tokens anyway), fp32 2048 49.0 and 42.5,
+// 8192 140.9 and 139.7.
 static RopeUnits rope_units(int64_t rows, int64_t heads, int64_t kv_heads, int lanes, bool bwd) {
   RopeUnits u = {};
   u.lanes = lanes;

@@ -27,12 +27,13 @@ constexpr float kFarBase = 65536.0f;
 __device__ __forceinline__ float decay(float m, float top, float c) { return top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - top) * c); }
 
 // log of l exp2(m c), the sum that l stands for: m c as it was rounded where l was summed.  Where m c leaves fp32 (scores beyond 2.36e38, log2 e short of
-// its end) both parts of ln 2 would meet as infinities of opposite signs: l, of at most 2^28 keys, is nothing beside m scale there.
+// its end) both parts of ln 2 would meet as infinities of opposite signs: m scale is formed instead.  A row whose l is not a number has no lse either.
 __device__ __forceinline__ float log_sum(float m, float c, float scale, float l) {
   const float base = m == -INFINITY ? 0.0f : m * c;            // a factor so small that no score passes it: m has not moved
   if (l == 0.0f) return -INFINITY;
-  if (fabsf(base) == INFINITY) return m * scale;
-  return fmaf(base, kLn2, fmaf(base, kLn2Rest, kLn2 * __builtin_amdgcn_logf(l)));
+  const float rest = kLn2 * __builtin_amdgcn_logf(l);
+  if (fabsf(base) == INFINITY) return fmaf(m, scale, rest);
+  return fmaf(base, kLn2, fmaf(base, kLn2Rest, rest));
 }
 
 template <int NT>

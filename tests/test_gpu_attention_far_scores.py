@@ -74,3 +74,18 @@ def test_far_scores_that_share_their_weight(kind, dim, sign):
     ck.within(host(r["lse"])[0].astype(np.float64), rl, 6 * ck.E * np.abs(rl) + 2 * 2.0 ** -7 * np.log(2.0), "lse")
     o = ef.attention_decode(q[-1:], k[None], v[None], torch.tensor([n], dtype=torch.int32, device="cuda"), 1, scale=1.0)
     ck.within(host(o).astype(np.float64), ref[-1:], tol[-1:], "o of the last token alone")
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("dim", [8, 128])
+def test_products_beyond_fp32_are_no_number(kind, dim):
+    """a token whose product with a key passes fp32 has neither o nor lse: not an infinity, which would pass for a sum; tokens before it have theirs"""
+    n = 40
+    size = torch.where(torch.arange(n) >= 30, 2.0 ** 65, 1.0)
+    q, k, v = (t.to(KINDS[kind]) for t in (rows_of(n, dim, size), rows_of(n, dim, 2.0 ** 64), values(n, dim)))
+    r = ef.attention_fwd(q, k, v, 1, scale=1.0)
+    o, lse = host(r["o"]), host(r["lse"])[0]
+    assert np.isnan(o[30:]).all() and np.isnan(lse[30:]).all()
+    mean = host(v).astype(np.float64).cumsum(0) / np.arange(1, n + 1)[:, None]
+    ck.within(o[:30].astype(np.float64), mean[:30], (1.01 * ck.half_step(kind) * mean + (n + 8) * ck.E * 1.5)[:30], "o")
+    ck.within(lse[:30].astype(np.float64), np.full(30, 2.0 ** 64), np.full(30, 4 * ck.E * 2.0 ** 64), "lse")

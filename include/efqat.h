@@ -521,7 +521,7 @@ int efqat_head_norm_rope_bwd(const void* dyq, int64_t lddyq, const void* dyk, in
  *   packed       of the workspace query: whether offsets will be given (0 or 1)
  * Scores, their maxima and sums, and all accumulators are fp32.  With BF16 the probabilities and, for dk, dS are rounded to bf16
  * for the matrix cores (their sum is taken before; dq takes dS as two such parts); with F32 the products are fp32 too.  o and lse hold for scores
- * up to the end of fp32 (an lse beyond it is an infinity).  The backward forms P from lse: 2^-23 of the largest score is the error of its
+ * up to the end of fp32 (an lse beyond it is an infinity, a product q . k beyond it leaves NaN).  The backward forms P from lse: 2^-23 of the largest score is the error of its
  * exponent, so that gradients of scores beyond 2^18 hold few digits and those beyond 2^23 none (they may be infinite or NaN).  Sums have a fixed
  * order (bit-reproducible).  A key or value in a sequence that is not finite may make undefined what tokens of that sequence and head hold, those
  * that do not see it too.  A query or a row of dout that is not finite makes undefined what its own token and head hold, and dk and dv of its
